@@ -14,6 +14,9 @@
  * plus two set-up helpers for a dense source loop (Appendix D.2, Eq. 6 with all causal keys):
  *   fl_column_scores, fl_select_columns; the decode step (fl_decode_step), the list pruning for a
  *   shrinking budget (fl_prune_columns) and the recent-token bf16 tail (fl_kv_keep_recent).
+ * and what serving a model needs beside the step, over ragged batches: rotary positions (fl_rope_table,
+ *   fl_rope), a paged key/value cache in 8 bits (fl_paged_append) and dense attention over it
+ *   (fl_paged_attn).
  *
  * Conventions shared by every call
  *   - Every data pointer is a DEVICE pointer (HIP device memory).  The caller allocates and owns all
@@ -475,6 +478,112 @@ int fl_prune_columns(const uint16_t* q, const uint16_t* k_cache, const int32_t* 
  * ---------------------------------------------------------------------------------------------- */
 int fl_kv_keep_recent(const uint16_t* x_cur, const int32_t* idx, int k, int B, int N, int H, int d, int tail,
                       uint16_t* cache, uint16_t* rows, void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * (9) Rotary positions.  Pair i of a head (0 <= i < rot / 2) at position p turns by the angle p * f_i:
+ *     y0 = x0 * cos - x1 * sin,   y1 = x0 * sin + x1 * cos
+ * The step's calls take queries and keys after this rotation; fl_paged_append and fl_paged_attn do it on
+ * the way.
+ *
+ * fl_rope_table writes table[p][i] = (m cos(p f_i), m sin(p f_i)), fp32 [n_pos, rot / 2, 2], the angles
+ * formed and reduced in fp64 (each value within 2 ulp of m, also at far positions).
+ *   f_i = base^(-2 i / rot), m = 1                              FL_ROPE_NONE
+ *   f_i / factor                                                FL_ROPE_LINEAR (positions interpolated)
+ *   base * factor^(rot / (rot - 2)) in place of base            FL_ROPE_NTK (the lowest frequency divided by factor)
+ *   f_i (g_i + (1 - g_i) / factor), m = 1 + 0.1 ln(factor)      FL_ROPE_YARN (Peng et al., "YaRN": g_i = the part of
+ *       [low, high] that the pair's turns within the original context, orig_len f_i / 2 pi, have passed, in [0, 1])
+ *   n_pos >= 1; rot a multiple of 16, 16 <= rot <= 1024; base > 1; factor >= 1 (ignored by NONE);
+ *   orig_len > 0 and low < high for YARN (ignored by the others).  Any other table of this layout serves as well.
+ *
+ * fl_rope rotates the first rot channels of every head and copies the others.
+ *   x, y      : [T, H, d] of `dtype` with x_stride (y_stride) elements from one row to the next (>= H * d), the
+ *               heads of a row dense; y may be x (with the same stride), not overlap it otherwise.
+ *   pos       : int32 [T] positions, or NULL for 0 .. T-1 (then T <= n_pos).  A row whose position is outside
+ *               [0, n_pos) gets NaN in its first rot channels (FL_E_RANGE with the index checks on).
+ *   layout    : FL_ROPE_HALF pairs channel i with i + rot / 2, FL_ROPE_INTERLEAVED 2 i with 2 i + 1.
+ *   inverse   : != 0 turns by -p f_i instead: with m, the gradient of x from that of y.
+ *   d, the strides and rot / 2 are multiples of 8, rot <= d <= 1024; 16-byte aligned tensors.  fp32 arithmetic, one
+ *   rounding to `dtype`.  T = 0 does nothing.
+ * ---------------------------------------------------------------------------------------------- */
+enum fl_dtype { FL_BF16 = 0, FL_F16 = 1 };
+enum fl_rope_scaling { FL_ROPE_NONE = 0, FL_ROPE_LINEAR = 1, FL_ROPE_NTK = 2, FL_ROPE_YARN = 3 };
+enum fl_rope_layout { FL_ROPE_HALF = 0, FL_ROPE_INTERLEAVED = 1 };
+
+int fl_rope_table(int n_pos, int rot, double base, int scaling, double factor, double orig_len, double low,
+                  double high, float* table, void* stream);
+
+int fl_rope(const void* x, int64_t x_stride, const int32_t* pos, const float* table, int n_pos, int rot, int layout,
+            int inverse, int dtype, int T, int H, int d, void* y, int64_t y_stride, void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * (10) A paged key/value cache in 8 bits, appended to for a ragged batch.
+ *
+ * The cache holds num_pages pages of `page` positions: k_cache and v_cache [num_pages, Hkv, page, d] of one-byte
+ * codes, k_scale and v_scale fp32 [num_pages, Hkv].  A stored value is scale * code.
+ *   FL_KV_I8   : code is int8 in [-127, 127]          FL_KV_E4M3 : code is an OCP e4m3 number, the scale a power of two
+ * Sequence b owns the pages block_table[b, 0 ..], int32 [B, max_pages]: position p is row p % page of page
+ * block_table[b, p / page].  Entries outside [0, num_pages) are pages that are not there.
+ *
+ * A batch has T rows of new positions: rows cu[b] .. cu[b+1] - 1 (int32 [B + 1], ascending from 0) are the last
+ * n = cu[b+1] - cu[b] positions of sequence b, whose length with them is lens[b] (int32 [B]): row cu[b] + t is position
+ * lens[b] - n + t.  Rows behind cu[B] belong to no sequence and are not touched; n may be 0.  (cu, lens and block_table are
+ * read by the kernels alone, so a captured graph takes their present contents.)
+ *
+ * fl_paged_append stores keys (rotated by their positions when `table` is given) and values of the new positions:
+ * for each page and head that receives some, over the received values x (keys: the rotated ones, the fp32 rounding of the
+ * exact sum of the two products) with a = max |x|,
+ *     need = fp32(a / 127)   (I8)        the least power of two with a <= 448 need   (E4M3)
+ *     scale <- need                                    when the page holds no earlier position of the sequence,
+ *     scale <- scale * 2^k, least k >= 0 with scale * 2^k >= need, and earlier codes <- round(code / 2^k)   otherwise
+ *     code = round(x / scale)  to nearest, ties to even, of the exact quotient.
+ * Doubling bounds what earlier positions lose to one step of the page's last scale.  a < 2^-100 counts as 0 (need = 0, codes
+ * 0); a scale of 0 grows to need at once.  With an infinity or a NaN among x the scale becomes NaN and the codes 0: the page
+ * reads as NaN until it is begun anew.
+ *   k, v       : [T, Hkv, d] of `dtype`, k_stride / v_stride elements from one row to the next (multiples of 8),
+ *                16-byte aligned.
+ *   table      : fp32 [n_pos, rot / 2, 2] as in (9) with n_pos >= max_pages * page, or NULL (keys stored as they are).
+ *   page       : 16, 32, 64 or 128.  d: 64 or 128.  rot: a multiple of 16, at most d.  B <= 65536, Hkv <= 65535.
+ * Positions that are negative or lie in a page that is not there are dropped.  No two sequences of a call may append to
+ * one page.  With the index checks on, cu, lens and block_table are checked on the host: FL_E_RANGE when cu does not ascend
+ * from 0 to at most T, a length is below its n or above max_pages * page, a page of a new position is not there, or two
+ * sequences append to one page.
+ * ---------------------------------------------------------------------------------------------- */
+enum fl_kv_format { FL_KV_I8 = 0, FL_KV_E4M3 = 1 };
+
+int fl_paged_append(const void* k, int64_t k_stride, const void* v, int64_t v_stride, int dtype, const int32_t* cu,
+                    const int32_t* lens, int B, int T, int Hkv, int d, const float* table, int n_pos, int rot,
+                    int layout, const int32_t* block_table, int max_pages, int num_pages, int page, int format,
+                    void* k_cache, void* v_cache, float* k_scale, float* v_scale, void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * (11) Dense attention of a ragged batch over the paged cache of (10): the loops that run before the sparse ones
+ * (Eq. 2), prompts in whole or in chunks, single positions.  For row t of position i and head h (key/value head
+ * h / (Hq / Hkv)), with q rotated by its position when `table` is given,
+ *     o_t = sum_j p_j v_j,   p_j = exp(sm_scale q . k_j - lse_t),   lse_t = ln sum_j exp(sm_scale q . k_j)
+ * over the stored positions j <= i of its sequence with, when window > 0, j > i - window or j < n_sink.  Positions whose page
+ * is not there are seen by no row.  A row that sees nothing gets o = 0 and lse = -inf.
+ *   q          : [T, Hq, d] of `dtype`, q_stride elements from one row to the next (a multiple of 8), 16-byte aligned.
+ *   cu, lens, B, T, table, block_table, page, format and the caches: as in (10), after the append.
+ *   o          : [T, Hq, d] of `dtype`, o_stride as q_stride.     lse : fp32 [T, Hq], or NULL.
+ *   max_q, max_len : the largest n and the largest length of the batch as far as the caller knows them (max_len = 0:
+ *                max_pages * page).  They choose the kernel and how the keys are split; any values give the result, up to
+ *                rounding.
+ *   ws         : at least fl_paged_attn_ws(...) bytes, for the same B, T, heads, d, page, window, n_sink, max_q and max_len
+ *                (and max_pages); nothing is kept in it between calls.  Calls that overlap need one each.
+ *   Hq a multiple of Hkv; window, n_sink >= 0; other limits as in (10).
+ * Precision: q (rotated in fp32) is multiplied as fp16 relative to the row's largest magnitude, probabilities as fp16
+ * relative to the largest contribution of the row, both against the exact codes; scores, sums and outputs are held in
+ * fp32.  With the index checks on, as in (10) (a page that is not there is no error here, nor is one that two sequences share).
+ * ---------------------------------------------------------------------------------------------- */
+size_t fl_paged_attn_ws(int B, int T, int Hq, int Hkv, int d, int page, int max_pages, int window, int n_sink, int max_q,
+                        int max_len);
+
+int fl_paged_attn(const void* q, int64_t q_stride, int dtype, const int32_t* cu, const int32_t* lens, int B, int T,
+                  int Hq, int Hkv, int d, const float* table, int n_pos, int rot, int layout,
+                  const int32_t* block_table, int max_pages, int num_pages, int page, int format, const void* k_cache,
+                  const void* v_cache, const float* k_scale, const float* v_scale, float sm_scale, int window,
+                  int n_sink, int max_q, int max_len, void* o, int64_t o_stride, float* lse, void* ws, size_t ws_bytes,
+                  void* stream);
 
 #ifdef __cplusplus
 }

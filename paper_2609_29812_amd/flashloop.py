@@ -22,12 +22,15 @@ DQ_COMPACT = 0
 DQ_COMMIT = 1
 ATTN_DENSE = 1
 PASS_ADD, PASS_SUBTRACT, PASS_BOTH = 0, 1, 2
+ROPE_SCALING = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
+ROPE_LAYOUT = {"half": 0, "interleaved": 1}
 
 _c_p = ctypes.c_void_p
 _c_i = ctypes.c_int
 _c_d = ctypes.c_double
 _c_f = ctypes.c_float
 _c_sz = ctypes.c_size_t
+_c_l = ctypes.c_int64
 
 _SIGNATURES = {
     "fl_status_str": (ctypes.c_char_p, [_c_i]),
@@ -76,6 +79,14 @@ _SIGNATURES = {
     "fl_kv_keep_recent": (_c_i, [_c_p, _c_p, _c_i, _c_i, _c_i, _c_i, _c_i, _c_i, _c_p, _c_p, _c_p]),
     "fl_prune_columns": (_c_i, [_c_p, _c_p, _c_p, _c_i, _c_p, _c_i, _c_p, _c_i, _c_i, _c_i, _c_i, _c_d, _c_i, _c_i,
                                 _c_p, _c_p, _c_p, _c_sz, _c_p]),
+    "fl_rope_table": (_c_i, [_c_i, _c_i, _c_d, _c_i, _c_d, _c_d, _c_d, _c_d, _c_p, _c_p]),
+    "fl_rope": (_c_i, [_c_p, _c_l, _c_p, _c_p, _c_i, _c_i, _c_i, _c_i, _c_i, _c_i, _c_i, _c_i, _c_p, _c_l, _c_p]),
+    "fl_paged_append": (_c_i, [_c_p, _c_l, _c_p, _c_l, _c_i, _c_p, _c_p, _c_i, _c_i, _c_i, _c_i, _c_p, _c_i, _c_i, _c_i,
+                               _c_p, _c_i, _c_i, _c_i, _c_i, _c_p, _c_p, _c_p, _c_p, _c_p]),
+    "fl_paged_attn_ws": (_c_sz, [_c_i] * 11),
+    "fl_paged_attn": (_c_i, [_c_p, _c_l, _c_i, _c_p, _c_p, _c_i, _c_i, _c_i, _c_i, _c_i, _c_p, _c_i, _c_i, _c_i, _c_p,
+                             _c_i, _c_i, _c_i, _c_i, _c_p, _c_p, _c_p, _c_p, _c_f, _c_i, _c_i, _c_i, _c_i, _c_p, _c_l,
+                             _c_p, _c_p, _c_sz, _c_p]),
 }
 
 EXPORTS = tuple(_SIGNATURES)
@@ -584,3 +595,181 @@ def kv_keep_recent(x_cur, idx, tail, cache=None, rows=None):
     _dev(rows, torch.bfloat16, "rows", None if rows is None else (B, k, H, d))
     rc = load().fl_kv_keep_recent(_p(x_cur), _p(idx), k, B, N, H, d, tail, _p(cache), _p(rows), _stream())
     _check(rc, "fl_kv_keep_recent")
+
+
+# ---- (9) rotary positions -------------------------------------------------------------------------------
+_DTYPES = {torch.bfloat16: 0, torch.float16: 1}
+_FORMATS = {torch.int8: 0, torch.float8_e4m3fn: 1}
+
+
+def _here(dev):
+    """The calls below launch on the current device's stream: their tensors have to be there."""
+    if dev.type != "cuda":
+        raise FlashLoopError("tensors must be on the device")
+    if dev.index != torch.cuda.current_device():
+        raise FlashLoopError(f"tensors on {dev}, but the current device is cuda:{torch.cuda.current_device()}")
+    return dev
+
+
+def _on(t, dev, dtype, name, shape=None):
+    if t is None or (t.dtype is dtype and t.device == dev and t.is_contiguous() and (shape is None or t.shape == shape)):
+        return
+    _dev(t, dtype, name, shape)
+    raise FlashLoopError(f"{name} is on {t.device}, the call's other tensors on {dev}")
+
+
+def _rows(t, dev, dtype, name, shape=None):
+    """Elements between the rows of [T, H, d], whose heads are dense."""
+    if t.dim() != 3 or (shape is not None and t.shape != shape):
+        raise FlashLoopError(f"{name} must have shape {'[T, H, d]' if shape is None else tuple(shape)}, got {tuple(t.shape)}")
+    if t.dtype is not dtype or dtype not in _DTYPES:
+        raise FlashLoopError(f"{name} must be {dtype if dtype in _DTYPES else 'bfloat16 or float16'}, got {t.dtype}")
+    if t.device != dev:
+        raise FlashLoopError(f"{name} is on {t.device}, the call's other tensors on {dev}")
+    T, H, d = t.shape
+    row, head, one = t.stride()
+    if (one != 1 and d > 1) or (head != d and H > 1):
+        raise FlashLoopError(f"the heads of a row of {name} must be dense, got strides {t.stride()}")
+    return row if T > 1 else H * d
+
+
+def _choice(value, of, name):
+    if value not in of:
+        raise FlashLoopError(f"{name} must be one of {', '.join(of)}, got {value!r}")
+    return of[value]
+
+
+def _turns(table, dev):
+    """(n_pos, rot) of a rotary table, (0, 0) without one."""
+    if table is None:
+        return 0, 0
+    _on(table, dev, torch.float32, "table")
+    if table.dim() != 3 or table.shape[2] != 2:
+        raise FlashLoopError(f"table must have shape [n_pos, rot / 2, 2], got {tuple(table.shape)}")
+    return table.shape[0], 2 * table.shape[1]
+
+
+def rope_table(n_pos, rot, base=10000.0, scaling="none", factor=1.0, orig_len=0, low=1.0, high=32.0, out=None, device=None):
+    """Cosines and sines of positions 0 .. n_pos-1: fp32 [n_pos, rot / 2, 2].  scaling: "none", "linear" (positions divided
+    by factor), "ntk" (a larger base, so that the lowest frequency is divided by factor) or "yarn" (frequencies that turn
+    fewer than low times within orig_len positions divided by factor, those above high kept, and the table multiplied by
+    1 + 0.1 ln(factor)).  On `device` (out's, or the current one)."""
+    how = _choice(scaling, ROPE_SCALING, "scaling")
+    if out is None:
+        dev = _here(torch.device("cuda", torch.cuda.current_device()) if device is None else torch.empty(0, device=device).device)
+        out = torch.empty(n_pos, rot // 2, 2, dtype=torch.float32, device=dev)
+    else:
+        _on(out, _here(out.device), torch.float32, "out", (n_pos, rot // 2, 2))
+    rc = load().fl_rope_table(n_pos, rot, base, how, factor, orig_len, low, high, _p(out), _stream())
+    _check(rc, "fl_rope_table")
+    return out
+
+
+def rope(x, table, pos=None, layout="half", inverse=False, out=None):
+    """The rows of x (bf16 or fp16 [T, H, d], any row stride that is a multiple of 8) with their heads' first rot channels
+    turned by the positions pos (int32 [T]; None: 0 .. T-1).  inverse=True turns back: the gradient of x from that of the
+    result.  out: where to write (x itself: in place).  A dense [B, N, H, d] state is x.view(B * N, H, d)."""
+    dev = _here(x.device)
+    xs = _rows(x, dev, x.dtype, "x")
+    n_pos, rot = _turns(table, dev)
+    if table is None:
+        raise FlashLoopError("rope needs a table")
+    T, H, d = x.shape
+    _on(pos, dev, torch.int32, "pos", (T,))
+    out = torch.empty(T, H, d, dtype=x.dtype, device=dev) if out is None else out
+    ys = _rows(out, dev, x.dtype, "out", x.shape)
+    rc = load().fl_rope(_p(x), xs, _p(pos), _p(table), n_pos, rot, _choice(layout, ROPE_LAYOUT, "layout"), 1 if inverse else 0,
+                        _DTYPES[x.dtype], T, H, d, _p(out), ys, _stream())
+    _check(rc, "fl_rope")
+    return out
+
+
+# ---- (10) the paged 8-bit cache ---------------------------------------------------------------------------
+def _paged(dev, cu, lens, block_table, k_cache, v_cache, k_scale, v_scale, Hkv, d):
+    """(B, max_pages, num_pages, page, format) of a ragged batch over a cache."""
+    if block_table.dim() != 2 or k_cache.dim() != 4:
+        raise FlashLoopError("block_table must be [B, max_pages] and the caches [num_pages, Hkv, page, d]")
+    if k_cache.dtype not in _FORMATS:
+        raise FlashLoopError(f"the caches must be int8 or float8_e4m3fn, got {k_cache.dtype}")
+    B, max_pages = block_table.shape
+    num_pages, page = k_cache.shape[0], k_cache.shape[2]
+    shape = (num_pages, Hkv, page, d)
+    _on(k_cache, dev, k_cache.dtype, "k_cache", shape)
+    _on(v_cache, dev, k_cache.dtype, "v_cache", shape)
+    _on(k_scale, dev, torch.float32, "k_scale", (num_pages, Hkv))
+    _on(v_scale, dev, torch.float32, "v_scale", (num_pages, Hkv))
+    _on(cu, dev, torch.int32, "cu", (B + 1,))
+    _on(lens, dev, torch.int32, "lens", (B,))
+    _on(block_table, dev, torch.int32, "block_table")
+    return B, max_pages, num_pages, page, _FORMATS[k_cache.dtype]
+
+
+def paged_cache(num_pages, Hkv, page, d, dtype=torch.int8, device="cuda"):
+    """An empty cache: (k_cache, v_cache [num_pages, Hkv, page, d] of int8 or float8_e4m3fn codes, k_scale, v_scale fp32
+    [num_pages, Hkv]).  Pages need no clearing, here or when they are given to another sequence."""
+    if dtype not in _FORMATS:
+        raise FlashLoopError(f"the caches must be int8 or float8_e4m3fn, got {dtype}")
+    codes = [torch.empty(num_pages, Hkv, page, d, dtype=dtype, device=device) for _ in range(2)]
+    return (*codes, *(torch.zeros(num_pages, Hkv, dtype=torch.float32, device=device) for _ in range(2)))
+
+
+def paged_append(k, v, cu, lens, block_table, k_cache, v_cache, k_scale, v_scale, table=None, layout="half"):
+    """Store the new positions of a ragged batch.  k, v: bf16 or fp16 [T, Hkv, d], any row stride that is a multiple of 8;
+    rows cu[b] .. cu[b+1]-1 (int32 [B + 1]) are the last positions of sequence b, whose length with them is lens[b] (int32
+    [B]); block_table: int32 [B, max_pages], its pages.  With a rotary table the keys are turned by their positions on the
+    way.  The caches (paged_cache) are updated in place; the scale of a page and head covers what the page holds of the
+    sequence, and doubles (its earlier codes halve) when a new position needs it."""
+    dev = _here(k.device)
+    ks = _rows(k, dev, k.dtype, "k")
+    T, Hkv, d = k.shape
+    vs = _rows(v, dev, k.dtype, "v", k.shape)
+    B, max_pages, num_pages, page, fmt = _paged(dev, cu, lens, block_table, k_cache, v_cache, k_scale, v_scale, Hkv, d)
+    n_pos, rot = _turns(table, dev)
+    rc = load().fl_paged_append(_p(k), ks, _p(v), vs, _DTYPES[k.dtype], _p(cu), _p(lens), B, T, Hkv, d, _p(table), n_pos, rot,
+                                _choice(layout, ROPE_LAYOUT, "layout"), _p(block_table), max_pages, num_pages, page, fmt,
+                                _p(k_cache), _p(v_cache), _p(k_scale), _p(v_scale), _stream())
+    _check(rc, "fl_paged_append")
+
+
+# ---- (11) attention over the paged cache ------------------------------------------------------------------
+def paged_attn(q, cu, lens, block_table, k_cache, v_cache, k_scale, v_scale, table=None, layout="half", sm_scale=None,
+               window=0, n_sink=0, max_q=None, max_len=0, out=None, lse=None, ws=None):
+    """Causal attention of the last positions of every sequence over its cached ones (after paged_append of the same
+    batch): q bf16 or fp16 [T, Hq, d], any row stride that is a multiple of 8, turned by its positions when a rotary table is
+    given; Hq a multiple of the cache's heads.  window > 0: a row at position i sees j > i - window and j < n_sink alone.
+    max_q, max_len: the largest number of new positions and the largest length of a sequence, as far as known (they choose
+    the kernel, not the result; default: an even batch, as long as the block table allows).  lse: optional fp32 [T, Hq] to
+    write the log-normalisers to.  ws: optional uint8 workspace (paged_attn_ws).  Returns out [T, Hq, d]; rows behind cu[B] of
+    a given out are left as they were."""
+    dev = _here(q.device)
+    qs = _rows(q, dev, q.dtype, "q")
+    T, Hq, d = q.shape
+    Hkv = k_cache.shape[1]
+    B, max_pages, num_pages, page, fmt = _paged(dev, cu, lens, block_table, k_cache, v_cache, k_scale, v_scale, Hkv, d)
+    n_pos, rot = _turns(table, dev)
+    out = torch.empty(T, Hq, d, dtype=q.dtype, device=dev) if out is None else out
+    os_ = _rows(out, dev, q.dtype, "out", q.shape)
+    _on(lse, dev, torch.float32, "lse", (T, Hq))
+    max_q = -(-T // B) if max_q is None else max_q
+    lib = load()
+    if ws is None:
+        need = lib.fl_paged_attn_ws(B, T, Hq, Hkv, d, page, max_pages, window, n_sink, max_q, max_len)
+        ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    else:
+        _on(ws, dev, torch.uint8, "ws")
+    rc = lib.fl_paged_attn(_p(q), qs, _DTYPES[q.dtype], _p(cu), _p(lens), B, T, Hq, Hkv, d, _p(table), n_pos, rot,
+                           _choice(layout, ROPE_LAYOUT, "layout"), _p(block_table), max_pages, num_pages, page, fmt,
+                           _p(k_cache), _p(v_cache), _p(k_scale), _p(v_scale),
+                           1.0 / math.sqrt(d) if sm_scale is None else sm_scale, window, n_sink, max_q, max_len, _p(out), os_,
+                           _p(lse), _p(ws), 0 if ws is None else ws.numel(), _stream())
+    _check(rc, "fl_paged_attn")
+    return out
+
+
+def paged_attn_ws(q, block_table, k_cache, window=0, n_sink=0, max_q=None, max_len=0):
+    """A workspace for paged_attn over these shapes and hints (None when it needs none)."""
+    T, Hq, d = q.shape
+    B, max_pages = block_table.shape
+    need = load().fl_paged_attn_ws(B, T, Hq, k_cache.shape[1], d, k_cache.shape[2], max_pages, window, n_sink,
+                                   -(-T // B) if max_q is None else max_q, max_len)
+    return torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
