@@ -532,9 +532,9 @@ int fl_rope(const void* x, int64_t x_stride, const int32_t* pos, const float* ta
  * fl_paged_append stores keys (rotated by their positions when `table` is given) and values of the new positions:
  * for each page and head that receives some, over the received values x (keys: the rotated ones, the fp32 rounding of the
  * exact sum of the two products) with a = max |x|,
- *     need = fp32(a / 127)   (I8)        the least power of two with a <= 448 need   (E4M3)
+ *     need = fp32(a * fp32(1 / 127))   (I8)        the least power of two with a <= 448 need   (E4M3)
  *     scale <- need                                    when the page holds no earlier position of the sequence,
- *     scale <- scale * 2^k, least k >= 0 with scale * 2^k >= need, and earlier codes <- round(code / 2^k)   otherwise
+ *     scale <- scale * 2^k, least k >= 0 with scale * 2^k >= need, and the page's other codes <- round(code / 2^k)   otherwise
  *     code = round(x / scale)  to nearest, ties to even, of the exact quotient.
  * Doubling bounds what earlier positions lose to one step of the page's last scale.  a < 2^-100 counts as 0 (need = 0, codes
  * 0); a scale of 0 grows to need at once.  With an infinity or a NaN among x the scale becomes NaN and the codes 0: the page

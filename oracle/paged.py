@@ -2,7 +2,7 @@
 
 The attention is Eq. 2's softmax attention with the causal row sets of the step, over a cache whose stored values are
 scale * code.  The codes' rounding is the definition's: to nearest, ties to even, of the exact quotient; the scale of a page
-and head is fp32(max / 127) (int8) or the least power of two that keeps the largest value within 448 (e4m3), and grows by
+and head is max * fp32(1 / 127) in fp32 (int8) or the least power of two that keeps the largest value within 448 (e4m3), and grows by
 powers of two while a sequence fills the page.  Nothing here is vectorized over sequences or pages.
 """
 from __future__ import annotations
@@ -92,7 +92,7 @@ def need_of(a, fmt):
     if a < 2.0 ** -100:
         return np.float32(0)
     if fmt == "int8":
-        return np.float32(np.float64(a) / 127.0)
+        return np.float32(a) * np.float32(1 / 127)
     e = math.frexp(a)[1] - 9                 # a < 2^(e + 9) = 512 * 2^e
     while a > math.ldexp(448, e):
         e += 1
@@ -129,9 +129,8 @@ def append(x, cu, lens, block_table, codes, scale, fmt):
                         while float(old) * 2.0 ** k < float(need):
                             k += 1
                         s = np.float32(float(old) * 2.0 ** k)
-                        kept = slice(0, mine[0] % page)
-                        codes[pid, h, kept] = encode(decode(codes[pid, h, kept], fmt) / 2.0 ** k, fmt) if k else \
-                            codes[pid, h, kept]
+                        if k:                # (all of the page: what the call writes is written below)
+                            codes[pid, h] = encode(decode(codes[pid, h], fmt) / 2.0 ** k, fmt)
                 scale[pid, h] = s
                 ok = np.isfinite(s) and s > 0
                 codes[pid, h, mine % page] = encode(v / float(s), fmt) if ok else 0

@@ -78,7 +78,7 @@ __device__ __forceinline__ float scale_for(uint32_t amax_bits) {
   if (amax_bits >= kInfBits) return NAN;
   const float a = __uint_as_float(amax_bits);
   if (a < 0x1p-100f) return 0.0f;
-  if constexpr (I8) return a / 127.0f;
+  if constexpr (I8) return a * (1.0f / 127.0f);
   // 448 = 1.75 * 2^8: a = m 2^e needs 2^(e - 8), or twice that when m > 1.75
   const int e = (int)(amax_bits >> 23) - 127;
   return ldexpf(1.0f, e - 8 + ((amax_bits & 0x7FFFFFu) > 0x600000u ? 1 : 0));
@@ -231,7 +231,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(AppendArgs a) {
 #pragma unroll
     for (int s = 0; s < NP; ++s) {
       const int i = s * PER + i0;
-      if (i >= lo) continue;
+      if (i >= PAGE || (i >= lo && i < hi)) continue;
       uint2* at = reinterpret_cast<uint2*>(codes + i * D + ch * 8);
       *at = shrink8<I8>(*at, f);
     }

@@ -116,7 +116,7 @@ def test_append_edges():
     c, s = put([0.0, 0.0])
     assert s[0, 0] == 0
     c, s = put([3.0], 2, c, s)                          # from zero at once
-    assert s[0, 0] == np.float32(3 / 127)
+    assert s[0, 0] == np.float32(3) * np.float32(1 / 127)
     c, s = put([1.0] * 3, 15)                           # over the border of a page
     assert s[0, 0] == s[1, 0] == np.float32(1 / 127) and c[0, 0, 15, 0] == c[1, 0, 1, 0] == 127
     for a, want in ((448.0, 1.0), (448.5, 2.0), (224.0, 0.5), (1.0, 2.0 ** -8), (1.75, 2.0 ** -8), (1.76, 2.0 ** -7)):
