@@ -522,7 +522,8 @@ int fl_rope(const void* x, int64_t x_stride, const int32_t* pos, const float* ta
  * codes, k_scale and v_scale fp32 [num_pages, Hkv].  A stored value is scale * code.
  *   FL_KV_I8   : code is int8 in [-127, 127]          FL_KV_E4M3 : code is an OCP e4m3 number, the scale a power of two
  * Sequence b owns the pages block_table[b, 0 ..], int32 [B, max_pages]: position p is row p % page of page
- * block_table[b, p / page].  Entries outside [0, num_pages) are pages that are not there.
+ * block_table[b, p / page].  Entries outside [0, num_pages) are pages that are not there.  A page and head whose scale is not
+ * finite reads as NaN.
  *
  * A batch has T rows of new positions: rows cu[b] .. cu[b+1] - 1 (int32 [B + 1], ascending from 0) are the last
  * n = cu[b+1] - cu[b] positions of sequence b, whose length with them is lens[b] (int32 [B]): row cu[b] + t is position

@@ -158,8 +158,8 @@ def attend(q, cu, lens, block_table, k_codes, v_codes, k_scale, v_scale, fmt, sm
             there = np.repeat((ids >= 0) & (ids < n_pages), page)[:max(L, 0)]
             safe = np.clip(ids, 0, n_pages - 1)
             for h in range(Hkv):
-                k = (decode(k_codes[safe, h], fmt) * k_scale[safe, h].astype(np.float64)[:, None, None]).reshape(-1, d)
-                v = (decode(v_codes[safe, h], fmt) * v_scale[safe, h].astype(np.float64)[:, None, None]).reshape(-1, d)
+                k, v = ((decode(c[safe, h], fmt) * np.where(np.isfinite(s[safe, h]), s[safe, h].astype(np.float64), np.nan)
+                         [:, None, None]).reshape(-1, d) for c, s in ((k_codes, k_scale), (v_codes, v_scale)))
                 for t in range(n):
                     r, i = int(cu[b]) + t, int(lens[b]) - n + t
                     j = seen_by(i, L, window, n_sink) if i >= 0 else np.arange(0)

@@ -1,0 +1,131 @@
+// The paged attention's kernels: their arguments, how rows and keys are cut into work, and pieces that both kernels use.
+#pragma once
+
+#include "fl_paged.h"
+
+namespace fl {
+
+struct PagedAttnArgs {
+  const uint16_t* q;
+  uint16_t* o;
+  float* lse;
+  int64_t qs, os;                  // row strides
+  Batch bt;
+  Rotary rt;
+  Pages pg;
+  const uint8_t *kc, *vc;
+  const float *ksc, *vsc;
+  int Hq, G;                       // query heads; of them per key/value head
+  float scale_log2;                // sm_scale * log2(e)
+  int window, n_sink;
+  int n_split, min_tiles;          // at most n_split parts of the keys, each of at least min_tiles tiles (but the last)
+  float *part, *part_ml;           // [T Hq][n_split][d] sums and [T Hq][n_split][2] references and normalisers
+  float pinf;                      // +inf
+};
+
+// What a row tile works on: rows rho0 .. rho0 + rows - 1 of a sequence, a row being (position, head of the group) with the
+// heads fastest, and the tiles of KT keys that some row of it may see, in order: the n_lead tiles of the leading positions,
+// then tiles first .. last.
+struct Span {
+  int b, r0, rho0, rows;           // rows == 0: nothing to do
+  int start;                       // position of the sequence's first row
+  int i_min, i_max;                // positions of the tile's first and last row
+  int n_lead, first, tiles;        // tiles: in all
+  int parts, per;                  // parts that have work, tiles in each but the last
+};
+
+// tiles `slot` of R rows: slots cu[b] G / R + b .. belong to sequence b
+template <int R, int KT>
+__device__ __forceinline__ Span span_of(const PagedAttnArgs& a, int b, int tile) {
+  Span s{};
+  s.b = b;
+  s.r0 = row_of(a.bt, b);
+  const int n = row_of(a.bt, b + 1) - s.r0;
+  s.rho0 = tile * R;
+  s.rows = min(n * a.G - s.rho0, R);
+  if (s.rows <= 0 || tile < 0) {
+    s.rows = 0;
+    return s;
+  }
+  const int cap = a.bt.max_pages * a.pg.size;                // positions that have a block table entry
+  s.start = max(a.bt.lens[b], 0) - n;
+  s.i_min = s.start + s.rho0 / a.G;
+  s.i_max = s.start + (s.rho0 + s.rows - 1) / a.G;
+  const int hi = min(s.i_max, cap - 1);
+  int lo = 0;
+  if (a.window > 0 && s.i_min >= a.window) lo = s.i_min - a.window + 1;
+  s.n_lead = (min(a.n_sink, lo) + KT - 1) / KT;
+  s.first = max(s.n_lead, lo / KT);
+  s.tiles = hi < 0 ? 0 : s.n_lead + max(hi / KT - s.first + 1, 0);
+  s.per = max(a.min_tiles, (s.tiles + a.n_split - 1) / a.n_split);
+  s.parts = max(1, (s.tiles + s.per - 1) / s.per);
+  return s;
+}
+template <int KT>
+__device__ __forceinline__ int key_of(const Span& s, int tile) { return (tile < s.n_lead ? tile : tile - s.n_lead + s.first) * KT; }
+
+// Eight channels 8 ch .. of a query row in fp32, rotated by its position when there is a table (pos within it).
+template <bool F16>
+__device__ __forceinline__ void load_q8(const PagedAttnArgs& a, const uint16_t* row, int pos, int ch, float* x) {
+  unpack8<F16>(*reinterpret_cast<const uint4*>(row + ch * 8), x);
+  if (!a.rt.table || ch * 8 >= a.rt.rot || pos < 0) return;
+  const float* tr = a.rt.table + (int64_t)pos * a.rt.rot;
+  float2 cs[8];
+  if (a.rt.layout == FL_ROPE_HALF) {
+    const int half = a.rt.rot / 16;
+    const bool second = ch >= half;
+    float y[8];
+    unpack8<F16>(*reinterpret_cast<const uint4*>(row + (second ? ch - half : ch + half) * 8), y);
+    load_turn<true>(tr, a.rt.rot, ch, cs);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = fmaf(x[e], cs[e].x, y[e] * (second ? cs[e].y : -cs[e].y));
+  } else {
+    load_turn<false>(tr, a.rt.rot, ch, cs);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float u = x[2 * e], v = x[2 * e + 1];
+      x[2 * e] = u * cs[e].x - v * cs[e].y;
+      x[2 * e + 1] = u * cs[e].y + v * cs[e].x;
+    }
+  }
+}
+
+// 2^-e for the largest magnitude m of a row, e its exponent: the row times it is below 2 and becomes fp16 without losing range
+__device__ __forceinline__ float row_down(float m) {
+  const int e = min(max((int)(__float_as_uint(m) >> 23), 1), 253);
+  return __uint_as_float((uint32_t)(254 - e) << 23);
+}
+
+// Four codes of one word as two fp16 pairs (exact).  Int8: c + 128 under the exponent of 1024, less 1152.
+template <bool I8>
+__device__ __forceinline__ void widen4(uint32_t w, uint32_t* out) {
+  if constexpr (I8) {
+    w ^= 0x80808080u;
+    const f16x2 off = {(_Float16)-1152.0f, (_Float16)-1152.0f};
+    out[0] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, w, 0x04010400u)) + off);
+    out[1] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, w, 0x04030402u)) + off);
+  } else {
+    out[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.0f, false));
+    out[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.0f, true));
+  }
+}
+
+// What the value scale does.  A probability times its page's scale s is exp2(x + log2 s - ref): the running reference follows
+// that contribution, so fp16 holds it whatever the scales are, and its sum over one page divided by s is the page's part of
+// the normaliser.  A scale below 2^-60 counts as 2^-60; one that is not finite as 1 (the normaliser does not depend on it), with
+// a negative reciprocal, and the rows that see the page are made NaN.
+constexpr float kLeastScale = 0x1p-60f;
+__device__ __forceinline__ float key_scale(float s) { return fabsf(s) < INFINITY ? s : NAN; }
+struct ValueScale {
+  float log2, inv;
+};
+__device__ __forceinline__ ValueScale value_scale(float s) {
+  if (!(fabsf(s) < INFINITY)) return {0.0f, -1.0f};
+  s = fmaxf(s, kLeastScale);
+  return {__builtin_amdgcn_logf(s), 1.0f / s};
+}
+
+int launch_paged_merge(const PagedAttnArgs& a, int d, int rows_per_tile, int keys_per_tile, bool f16, hipStream_t st);
+int launch_paged_prompt(const PagedAttnArgs& a, int d, int format, bool f16, hipStream_t st);
+
+}  // namespace fl

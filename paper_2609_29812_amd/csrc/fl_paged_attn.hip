@@ -1,119 +1,438 @@
-// Dense attention of a ragged batch over the paged 8-bit cache.
-#include "fl_paged.h"
+// Dense attention of a ragged batch over the paged 8-bit cache: few rows per sequence (single positions), the joining of
+// split keys, and the entry points.
+#include "fl_paged_attn.h"
+
+#include <algorithm>
 
 namespace fl {
 
-struct PagedAttnArgs {
-  const uint16_t* q;
-  uint16_t* o;
-  float* lse;
-  int64_t qs, os;                  // row strides
-  Batch bt;
-  Rotary rt;
-  Pages pg;
-  const uint8_t *kc, *vc;
-  const float *ksc, *vsc;
-  int Hq, G;                       // query heads; of them per key/value head
-  float scale_log2;                // sm_scale * log2(e)
-  int window, n_sink;
-};
+constexpr int kTokenKeys = 32;     // keys of a wave's tile
 
-template <bool I8>
-__device__ __forceinline__ void decode4(uint32_t w, float* x) {
-  if constexpr (I8) {
+// Few rows: a workgroup has R = 16 NR rows of one key/value head (positions and the head's query heads) and a part of the
+// keys; its four waves take tiles of 32 keys in turn, each by itself.
+//   S^T = K Q^T   v_mfma_f32_16x16x32_f16: a lane loads a quarter of a key's codes as they lie, widened in registers to exact
+//                 fp16; the contraction runs over the channels in the order that this gives.
+//   O^T += V^T P^T  the same product: a lane of S^T holds 2 x 4 keys of one row, which is the P^T operand for keys in that
+//                 order; the lane's V bytes (8 keys x d / 16 channels) are transposed by byte permutes while they are widened.
+// No LDS in the loop: the next tile's codes are in flight while one is multiplied.  Page numbers and scales of 32 tiles are
+// fetched by the lanes at once and handed out by v_readlane.
+template <int D, bool I8, bool F16, int NR>
+__global__ __launch_bounds__(256, 2) void paged_token_kernel(PagedAttnArgs a) {
+  constexpr int R = 16 * NR, KS = D / 32, DT = D / 16;
+  constexpr int KW = D / 64;              // 16-byte loads of a lane per key group
+  constexpr int VW = D / 64;              // words of a lane per key of V
+  constexpr int LD = D + 4;               // row stride of the waves' sums in LDS
+  __shared__ float s_ref[4][R], s_sum[4][R];
+  __shared__ __attribute__((aligned(16))) float s_acc[4][16][LD];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r16 = lane & 15, g4 = lane >> 4;
+  const int kvh = blockIdx.x % a.pg.heads;
+  const int rest = blockIdx.x / a.pg.heads;
+  const int split = rest % a.n_split, slot = rest / a.n_split;
+  const int G = a.G;
+  const int b = __builtin_amdgcn_readfirstlane(find_seq(a.bt, slot, 1, [G](int c) { return c * G / R; }));
+  if (b < 0) return;
+  const Span sp = span_of<R, kTokenKeys>(a, b, slot - (row_of(a.bt, b) * G / R + b));
+  if (sp.rows == 0 || split >= sp.parts) return;
+  const int t0 = split * sp.per, t1 = min(t0 + sp.per, sp.tiles);
+
+  // the lane's rows
+  f16x8 qf[NR][KS];
+  float mul[NR];
+  int jmax[NR], jmin[NR];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = (float)(int8_t)(w >> (8 * e));
-  } else {
-    const auto a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
-    x[0] = a[0]; x[1] = a[1]; x[2] = b[0]; x[3] = b[1];
+  for (int x = 0; x < NR; ++x) {
+    const int rr = x * 16 + r16;
+    const bool ok = rr < sp.rows;
+    const int rho = sp.rho0 + (ok ? rr : 0);
+    const int t = rho / G, pos = sp.start + t;
+    const uint16_t* src = a.q + (int64_t)(sp.r0 + t) * a.qs + (int64_t)(kvh * G + rho % G) * D;
+    const int cap = a.bt.max_pages * a.pg.size;
+    float v[KS][8], top = 0.0f;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      load_q8<F16>(a, src, min(pos, cap - 1), g4 * KS + k, v[k]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[k][e]));
+    }
+    const float down = row_down(row4_max(top));
+    mul[x] = a.scale_log2 / down;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      u32x4 w;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = ok ? pack_f16x2(v[k][2 * e] * down, v[k][2 * e + 1] * down) : 0u;
+      qf[x][k] = __builtin_bit_cast(f16x8, w);
+    }
+    jmax[x] = ok ? min(pos, cap - 1) : -1;
+    jmin[x] = a.window > 0 && pos >= a.window ? pos - a.window + 1 : 0;
+  }
+  // a tile that every row sees in full needs no mask: its keys are at most all_max and at least all_min (or leading)
+  const int all_max = sp.i_min, all_min = a.window > 0 && sp.i_max >= a.window ? sp.i_max - a.window + 1 : 0;
+
+  f32x4 acc[NR][DT];
+  float ref[NR], lsum[NR];
+#pragma unroll
+  for (int x = 0; x < NR; ++x) {
+    ref[x] = -INFINITY;
+    lsum[x] = 0.0f;
+#pragma unroll
+    for (int t = 0; t < DT; ++t) acc[x][t] = f32x4{};
+  }
+
+  // pages and scales of the wave's next 32 tiles: lane l has tile l % 32, key group l / 32
+  int pid_v = -1;
+  float ks_v = 0.0f, lv_v = 0.0f, iv_v = 0.0f;
+  auto fetch_pages = [&](int c0) {
+    const int tile = t0 + wave + 4 * (c0 + (lane & 31));
+    pid_v = -1;
+    ks_v = 0.0f;
+    ValueScale vs{0.0f, 1.0f};
+    if (tile < t1) {
+      const int page = (key_of<kTokenKeys>(sp, tile) + (lane >> 5) * 16) >> a.pg.log2;
+      const int p = page < a.bt.max_pages ? a.bt.table[(int64_t)b * a.bt.max_pages + page] : -1;
+      if ((uint32_t)p < (uint32_t)a.pg.num) {
+        pid_v = p;
+        ks_v = key_scale(a.ksc[(int64_t)p * a.pg.heads + kvh]);
+        vs = value_scale(a.vsc[(int64_t)p * a.pg.heads + kvh]);
+      }
+    }
+    lv_v = vs.log2;
+    iv_v = vs.inv;
+  };
+
+  struct Tile {
+    u32x4 k[2][KW];
+    uint32_t v[8][VW];
+  };
+  auto load = [&](Tile& w, int c) {                          // the wave's tile c
+    const int key0 = key_of<kTokenKeys>(sp, t0 + wave + 4 * c);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int p = max(__builtin_amdgcn_readlane(pid_v, (c & 31) + 32 * h), 0);      // (a page that is not there: masked)
+      const int64_t base = (((int64_t)p * a.pg.heads + kvh) * a.pg.size + ((key0 + 16 * h) & (a.pg.size - 1))) * D;
+      const uint8_t* kb = a.kc + base;
+      const uint8_t* vb = a.vc + base;
+#pragma unroll
+      for (int x = 0; x < KW; ++x) w.k[h][x] = *reinterpret_cast<const u32x4*>(kb + (uint32_t)(r16 * D + g4 * (D / 4) + 16 * x));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t at = (uint32_t)((g4 * 4 + e) * D + r16 * DT);
+        if constexpr (VW == 2) {
+          const u32x2 d2 = *reinterpret_cast<const u32x2*>(vb + at);
+          w.v[4 * h + e][0] = d2[0];
+          w.v[4 * h + e][1] = d2[1];
+        } else {
+          w.v[4 * h + e][0] = *reinterpret_cast<const uint32_t*>(vb + at);
+        }
+      }
+    }
+  };
+  auto compute = [&](Tile& w, int c) {
+    const int key0 = key_of<kTokenKeys>(sp, t0 + wave + 4 * c);
+    const int pid0 = __builtin_amdgcn_readlane(pid_v, c & 31), pid1 = __builtin_amdgcn_readlane(pid_v, (c & 31) + 32);
+    float ks[2], lv[2], iv[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      ks[h] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks_v), (c & 31) + 32 * h));
+      lv[h] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(lv_v), (c & 31) + 32 * h));
+      iv[h] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(iv_v), (c & 31) + 32 * h));
+    }
+    const bool spoilt = iv[0] < 0.0f || iv[1] < 0.0f;
+    const bool masked = key0 + kTokenKeys - 1 > all_max || (key0 < all_min && key0 + kTokenKeys > a.n_sink) || (pid0 | pid1) < 0;
+    f32x4 s[NR][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int x = 0; x < NR; ++x) s[x][h] = f32x4{};
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        u32x4 kw;
+        uint32_t two[2];
+        widen4<I8>(w.k[h][k / 2][2 * (k % 2)], two);
+        kw[0] = two[0]; kw[1] = two[1];
+        widen4<I8>(w.k[h][k / 2][2 * (k % 2) + 1], two);
+        kw[2] = two[0]; kw[3] = two[1];
+#pragma unroll
+        for (int x = 0; x < NR; ++x)
+          s[x][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, kw), qf[x][k], s[x][h], 0, 0, 0);
+      }
+    }
+    if (masked && !I8) {                                     // codes behind the end may be NaN
+      const int hi = sp.i_max;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const bool there = key0 + (e >> 2) * 16 + g4 * 4 + (e & 3) <= hi && (e < 4 ? pid0 : pid1) >= 0;
+#pragma unroll
+        for (int y = 0; y < VW; ++y) w.v[e][y] = there ? w.v[e][y] : 0u;
+      }
+    }
+    f16x8 pf[NR];
+#pragma unroll
+    for (int x = 0; x < NR; ++x) {
+      float y[2][4], top = -INFINITY;
+      bool see[2][4];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float m = ks[h] * mul[x];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[h][i] = s[x][h][i] * m;
+        if (masked) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int j = key0 + 16 * h + 4 * g4 + i;
+            see[h][i] = j <= jmax[x] && (j >= jmin[x] || j < a.n_sink) && (h ? pid1 : pid0) >= 0;
+            y[h][i] = see[h][i] ? y[h][i] : -INFINITY;
+          }
+        }
+        top = fmaxf(top, fmaxf(fmaxf(y[h][0], y[h][1]), fmaxf(y[h][2], y[h][3])) + lv[h]);
+      }
+      top = row4_max(top);
+      const bool raise = top > ref[x] + 8.0f;
+      if (__builtin_amdgcn_ballot_w64(raise) != 0) {
+        const float nm = raise ? top : ref[x];
+        const float alpha = raise ? __builtin_amdgcn_exp2f(ref[x] - nm) : 1.0f;
+        lsum[x] *= alpha;
+#pragma unroll
+        for (int t = 0; t < DT; ++t) acc[x][t] *= alpha;
+        ref[x] = nm;
+      }
+      const float base = ref[x] == -INFINITY ? 0.0f : ref[x];
+      float p[2][4];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float off = lv[h] - base;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          p[h][i] = __builtin_amdgcn_exp2f(y[h][i] + off);
+          if (masked) p[h][i] = see[h][i] ? p[h][i] : 0.0f;  // (a NaN scale times no probability)
+        }
+        const float part = (p[h][0] + p[h][1]) + (p[h][2] + p[h][3]);
+        lsum[x] = fmaf(part, fabsf(iv[h]), lsum[x]);
+      }
+      if (spoilt) {                                          // a value scale that is not finite: the rows that see it
+        bool any = false;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) any |= iv[h] < 0.0f && (!masked || see[h][i]);
+        const float bad = row4_add(any ? 1.0f : 0.0f) > 0.0f ? NAN : 0.0f;
+#pragma unroll
+        for (int t = 0; t < DT; ++t) acc[x][t] += bad;
+      }
+      const u32x4 pw = {pack_f16x2(p[0][0], p[0][1]), pack_f16x2(p[0][2], p[0][3]), pack_f16x2(p[1][0], p[1][1]),
+                        pack_f16x2(p[1][2], p[1][3])};
+      pf[x] = __builtin_bit_cast(f16x8, pw);
+    }
+    if constexpr (I8) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int y = 0; y < VW; ++y) w.v[e][y] ^= 0x80808080u;
+    }
+#pragma unroll
+    for (int y = 0; y < VW; ++y) {
+      if constexpr (I8) {
+        const f16x2 off = {(_Float16)-1152.0f, (_Float16)-1152.0f};
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {                        // channel 4 y + t of the lane: one byte of each of eight keys
+          u32x4 vw;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t two = __builtin_amdgcn_perm(w.v[2 * e + 1][y], w.v[2 * e][y], 0x0c000c00u | ((4 + t) << 16) | t);
+            vw[e] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, two | 0x64006400u) + off);
+          }
+#pragma unroll
+          for (int x = 0; x < NR; ++x)
+            acc[x][4 * y + t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, vw), pf[x], acc[x][4 * y + t], 0, 0, 0);
+        }
+      } else {
+        uint32_t lo[8], hi[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          uint32_t two[2];
+          widen4<false>(w.v[e][y], two);
+          lo[e] = two[0];
+          hi[e] = two[1];
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          u32x4 vw;
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            vw[e] = __builtin_amdgcn_perm(t < 2 ? lo[2 * e + 1] : hi[2 * e + 1], t < 2 ? lo[2 * e] : hi[2 * e],
+                                          t & 1 ? 0x07060302u : 0x05040100u);
+#pragma unroll
+          for (int x = 0; x < NR; ++x)
+            acc[x][4 * y + t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, vw), pf[x], acc[x][4 * y + t], 0, 0, 0);
+        }
+      }
+    }
+  };
+
+  const int mine = t1 - t0 - wave <= 0 ? 0 : (t1 - t0 - wave + 3) / 4;     // tiles of this wave
+  Tile w0, w1;
+  for (int c0 = 0; c0 < mine; c0 += 32) {
+    fetch_pages(c0);
+    const int c1 = min(c0 + 32, mine);
+    load(w0, c0);
+    for (int c = c0; c < c1; c += 2) {
+      if (c + 1 < c1) load(w1, c + 1);
+      compute(w0, c);
+      if (c + 1 < c1) {
+        if (c + 2 < c1) load(w0, c + 2);
+        compute(w1, c + 1);
+      }
+    }
+  }
+
+  // the four waves' states of a row meet in LDS
+#pragma unroll
+  for (int x = 0; x < NR; ++x) {
+    lsum[x] = row4_add(lsum[x]);
+    if (g4 == 0) {
+      s_ref[wave][x * 16 + r16] = ref[x];
+      s_sum[wave][x * 16 + r16] = lsum[x];
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int x = 0; x < NR; ++x) {
+    const int rr = x * 16 + r16;
+    const float m = fmaxf(fmaxf(s_ref[0][rr], s_ref[1][rr]), fmaxf(s_ref[2][rr], s_ref[3][rr]));
+    const float f = ref[x] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ref[x] - m);
+    if (x > 0) __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i)                              // channels (4 g4 + i) DT + t, t < DT
+#pragma unroll
+      for (int t = 0; t < DT; t += 4)
+        *reinterpret_cast<float4*>(&s_acc[wave][r16][(4 * g4 + i) * DT + t]) =
+            make_float4(acc[x][t][i] * f, acc[x][t + 1][i] * f, acc[x][t + 2][i] * f, acc[x][t + 3][i] * f);
+    __syncthreads();
+    constexpr int CPR = D / 4;                               // four channels a thread
+    for (int w = threadIdx.x; w < 16 * CPR; w += 256) {
+      const int row = w / CPR, c = (w % CPR) * 4, rx = x * 16 + row;
+      if (rx >= sp.rows) continue;
+      const float mm = fmaxf(fmaxf(s_ref[0][rx], s_ref[1][rx]), fmaxf(s_ref[2][rx], s_ref[3][rx]));
+      float sum = 0.0f;
+#pragma unroll
+      for (int v = 0; v < 4; ++v) sum += s_ref[v][rx] == -INFINITY ? 0.0f : s_sum[v][rx] * __builtin_amdgcn_exp2f(s_ref[v][rx] - mm);
+      float o[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = (s_acc[0][row][c + e] + s_acc[1][row][c + e]) + (s_acc[2][row][c + e] + s_acc[3][row][c + e]);
+      const int rho = sp.rho0 + rx, t = rho / G, h = kvh * G + rho % G;
+      const int64_t gr = (int64_t)(sp.r0 + t) * a.Hq + h;
+      if (sp.parts > 1) {
+        *reinterpret_cast<float4*>(a.part + (gr * a.n_split + split) * D + c) = make_float4(o[0], o[1], o[2], o[3]);
+        if (c == 0) *reinterpret_cast<float2*>(a.part_ml + (gr * a.n_split + split) * 2) = make_float2(mm, sum);
+      } else {
+        const bool none = mm == -INFINITY && sum == 0.0f;
+        const float inv = none ? 0.0f : 1.0f / sum;
+        const u32x2 two = {F16 ? pack_f16x2(o[0] * inv, o[1] * inv) : pack_bf16x2(o[0] * inv, o[1] * inv),
+                           F16 ? pack_f16x2(o[2] * inv, o[3] * inv) : pack_bf16x2(o[2] * inv, o[3] * inv)};
+        *reinterpret_cast<u32x2*>(a.o + (int64_t)(sp.r0 + t) * a.os + (int64_t)h * D + c) = two;
+        if (c == 0 && a.lse) a.lse[gr] = none ? -INFINITY : (mm + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+      }
+    }
   }
 }
 
-// One wave per row and query head: lanes are keys for the scores, channels for the outputs.
-template <int D, bool I8, bool F16>
-__global__ __launch_bounds__(64) void paged_row_kernel(PagedAttnArgs a) {
-  __shared__ float s_q[D], s_p[64];
-  __shared__ int64_t s_at[64];
-  const int lane = threadIdx.x, h = blockIdx.y, t = blockIdx.x, kvh = h / a.G;
+// The parts of a row's keys joined: one wave a row.
+template <int D, int R, int KT, bool F16>
+__global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t gr = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (gr >= (int64_t)a.bt.T * a.Hq) return;
+  const int t = (int)(gr / a.Hq), h = (int)(gr % a.Hq);
   const int b = __builtin_amdgcn_readfirstlane(find_seq(a.bt, t, 0, [](int c) { return c; }));
-  if (b < 0) return;
-  const int r1 = row_of(a.bt, b + 1);
-  if (t >= r1) return;
-  const int64_t pos = (int64_t)a.bt.lens[b] - (r1 - t);      // the row's position
-  const int last = (int)min(pos, (int64_t)a.bt.max_pages * a.pg.size - 1);
-  for (int c = lane; c < D; c += 64) {
-    const uint16_t* src = a.q + (int64_t)t * a.qs + (int64_t)h * D;
-    float v = to_f32<F16>(src[c]);
-    if (a.rt.table && c < a.rt.rot && pos >= 0 && last == pos) {
-      const int half = a.rt.rot / 2;
-      const bool hl = a.rt.layout == FL_ROPE_HALF;
-      const int i = hl ? c % half : c / 2;
-      const bool second = hl ? c >= half : (c & 1);
-      const float other = to_f32<F16>(src[hl ? (second ? c - half : c + half) : c ^ 1]);
-      const float2 cs = reinterpret_cast<const float2*>(a.rt.table)[pos * half + i];
-      v = second ? other * cs.y + v * cs.x : v * cs.x - other * cs.y;
-    }
-    s_q[c] = v;
+  if (b < 0 || t >= row_of(a.bt, b + 1)) return;
+  const Span sp = span_of<R, KT>(a, b, ((t - row_of(a.bt, b)) * a.G + h % a.G) / R);
+  if (sp.parts <= 1) return;
+  const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + gr * a.n_split;
+  float m = -INFINITY;
+  for (int s = lane; s < sp.parts; s += 64) m = fmaxf(m, ml[s].x);
+  for (int off = 32; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
+  float sum = 0.0f, o[D / 64] = {};
+  for (int s = 0; s < sp.parts; ++s) {
+    const float2 w = ml[s];
+    if (w.x == -INFINITY && w.y == 0.0f) continue;
+    const float f = __builtin_amdgcn_exp2f(w.x - m);
+    sum = fmaf(f, w.y, sum);
+    const float* src = a.part + (gr * a.n_split + s) * D + lane * (D / 64);
+#pragma unroll
+    for (int e = 0; e < D / 64; ++e) o[e] = fmaf(f, src[e], o[e]);
   }
-  __syncthreads();
-  float acc[D / 64] = {}, ref = -INFINITY, sum = 0.0f;
-  for (int j0 = 0; j0 <= last; j0 += 64) {
-    const int j = j0 + lane;
-    bool seen = j <= last && (a.window == 0 || (int64_t)j > pos - a.window || j < a.n_sink);
-    float x = -INFINITY, vs = 0.0f;
-    if (seen) {
-      const int pid = a.bt.table[(int64_t)b * a.bt.max_pages + (j >> a.pg.log2)];
-      seen = (uint32_t)pid < (uint32_t)a.pg.num;
-      if (seen) {
-        const int64_t head = (int64_t)pid * a.pg.heads + kvh;
-        const int64_t at = (head * a.pg.size + (j & (a.pg.size - 1))) * D;
-        float dot = 0.0f;
-        for (int c = 0; c < D; c += 4) {
-          float k[4];
-          decode4<I8>(*reinterpret_cast<const uint32_t*>(a.kc + at + c), k);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) dot = fmaf(s_q[c + e], k[e], dot);
-        }
-        x = dot * (a.ksc[head] * a.scale_log2);
-        vs = a.vsc[head];
-        s_at[lane] = at;
-      }
-    }
-    float top = x;
-    for (int off = 32; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
-    if (__builtin_amdgcn_ballot_w64(seen) == 0) continue;
-    const float nref = fmaxf(ref, top);
-    const float alpha = ref == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ref - nref);
-    const float p = seen ? __builtin_amdgcn_exp2f(x - nref) : 0.0f;
-    ref = nref;
-    sum = sum * alpha + p;
-    s_p[lane] = seen ? p * vs : 0.0f;
-    if (!seen) s_at[lane] = -1;
-    __syncthreads();
-#pragma unroll
-    for (int e = 0; e < D / 64; ++e) acc[e] *= alpha;
-    for (int x2 = 0; x2 < 64; ++x2) {
-      const int64_t at = s_at[x2];
-      if (at < 0) continue;
-#pragma unroll
-      for (int e = 0; e < D / 64; ++e) {
-        const uint32_t c = a.vc[at + e * 64 + lane];
-        float v[4];
-        decode4<I8>(c, v);
-        acc[e] = fmaf(s_p[x2], v[0], acc[e]);
-      }
-    }
-    __syncthreads();
+  const bool none = m == -INFINITY && sum == 0.0f;
+  const float inv = none ? 0.0f : 1.0f / sum;
+  uint16_t* dst = a.o + (int64_t)t * a.os + (int64_t)h * D + lane * (D / 64);
+  if constexpr (D == 128) *reinterpret_cast<uint32_t*>(dst) = F16 ? pack_f16x2(o[0] * inv, o[1] * inv) : pack_bf16x2(o[0] * inv, o[1] * inv);
+  else *dst = (uint16_t)(F16 ? pack_f16x2(o[0] * inv, 0.0f) : pack_bf16x2(o[0] * inv, 0.0f));
+  if (a.lse && lane == 0) a.lse[gr] = none ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+}
+
+template <int R, int KT>
+static int launch_merge(const PagedAttnArgs& a, int d, bool f16, hipStream_t st) {
+  const unsigned grid = (unsigned)(((int64_t)a.bt.T * a.Hq + 3) / 4);
+  if (d == 128) {
+    if (f16) paged_merge_kernel<128, R, KT, true><<<grid, 256, 0, st>>>(a);
+    else paged_merge_kernel<128, R, KT, false><<<grid, 256, 0, st>>>(a);
+  } else {
+    if (f16) paged_merge_kernel<64, R, KT, true><<<grid, 256, 0, st>>>(a);
+    else paged_merge_kernel<64, R, KT, false><<<grid, 256, 0, st>>>(a);
   }
-  for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off, 64);
-  const bool none = ref == -INFINITY && sum == 0.0f;
-#pragma unroll
-  for (int e = 0; e < D / 64; ++e) {
-    const float v = none ? 0.0f : acc[e] / sum;
-    a.o[(int64_t)t * a.os + (int64_t)h * D + e * 64 + lane] =
-        (uint16_t)((F16 ? pack_f16x2(v, 0.0f) : pack_bf16x2(v, 0.0f)) & 0xFFFFu);
-  }
-  if (a.lse && lane == 0) a.lse[(int64_t)t * a.Hq + h] = none ? -INFINITY : (ref + log2f(sum)) * 0.6931471805599453f;
+  return check_launch("paged_merge_kernel");
+}
+
+int launch_paged_merge(const PagedAttnArgs& a, int d, int rows_per_tile, int keys_per_tile, bool f16, hipStream_t st) {
+  if (rows_per_tile == 16) return launch_merge<16, 32>(a, d, f16, st);
+  return launch_merge<32, 32>(a, d, f16, st);
+}
+
+template <int NR>
+static int launch_token(const PagedAttnArgs& a, int d, int format, bool f16, hipStream_t st) {
+  const int64_t slots = (int64_t)a.bt.T * a.G / (16 * NR) + a.bt.B;
+  const int64_t n = slots * a.n_split * a.pg.heads;
+  FL_REQUIRE(n < (1ll << 31), FL_E_SHAPE, "fl_paged_attn: too many rows");
+  const unsigned grid = (unsigned)n;
+#define FL_TOKEN(DD)                                                                        \
+  do {                                                                                      \
+    if (format == FL_KV_I8) {                                                               \
+      if (f16) paged_token_kernel<DD, true, true, NR><<<grid, 256, 0, st>>>(a);             \
+      else paged_token_kernel<DD, true, false, NR><<<grid, 256, 0, st>>>(a);                \
+    } else {                                                                                \
+      if (f16) paged_token_kernel<DD, false, true, NR><<<grid, 256, 0, st>>>(a);            \
+      else paged_token_kernel<DD, false, false, NR><<<grid, 256, 0, st>>>(a);               \
+    }                                                                                       \
+  } while (0)
+  if (d == 128) FL_TOKEN(128);
+  else FL_TOKEN(64);
+#undef FL_TOKEN
+  int rc = check_launch("paged_token_kernel");
+  if (rc != FL_OK || a.n_split == 1) return rc;
+  return launch_paged_merge(a, d, 16 * NR, kTokenKeys, f16, st);
+}
+
+// How a call is cut: rows per tile and parts of the keys.
+struct Plan {
+  int rows, n_split, min_tiles;
+  size_t ws;
+};
+static Plan plan_of(int B, int T, int Hq, int Hkv, int d, int page, int max_pages, int window, int n_sink, int max_q, int max_len) {
+  Plan p{};
+  const int64_t G = Hq / Hkv;
+  const int64_t per_seq = std::max<int64_t>(1, std::min<int64_t>(max_q > 0 ? max_q : 1, T)) * G;
+  p.rows = per_seq <= 16 ? 16 : 32;
+  const int64_t cap = (int64_t)max_pages * page;
+  int64_t len = max_len > 0 ? std::min<int64_t>(max_len, cap) : cap;
+  if (window > 0) len = std::min<int64_t>(len, (int64_t)window + n_sink + std::max(max_q, 1));
+  const int64_t tiles = std::max<int64_t>(1, (len + kTokenKeys - 1) / kTokenKeys);
+  const int64_t units = std::max<int64_t>(1, std::max<int64_t>(B, T * G / p.rows)) * Hkv;
+  int64_t split = std::min<int64_t>(2048 / units, tiles / 8);
+  split = std::min<int64_t>(std::max<int64_t>(split, 1), 256);
+  p.n_split = (int)split;
+  p.min_tiles = (int)((tiles + split - 1) / split);
+  p.ws = split > 1 ? (size_t)T * Hq * split * (d + 2) * sizeof(float) : 0;
+  return p;
 }
 
 }  // namespace fl
@@ -122,7 +441,10 @@ using namespace fl;
 
 extern "C" size_t fl_paged_attn_ws(int B, int T, int Hq, int Hkv, int d, int page, int max_pages, int window, int n_sink,
                                    int max_q, int max_len) {
-  return 0;
+  if (B < 1 || T < 1 || Hkv < 1 || Hq < Hkv || Hq % Hkv || (d != 64 && d != 128) || page < 16 || max_pages < 1 || window < 0 ||
+      n_sink < 0 || max_q < 0 || max_len < 0)
+    return 0;
+  return plan_of(B, T, Hq, Hkv, d, page, max_pages, window, n_sink, max_q, max_len).ws;
 }
 
 extern "C" int fl_paged_attn(const void* q, int64_t q_stride, int dtype, const int32_t* cu, const int32_t* lens, int B, int T,
@@ -138,6 +460,7 @@ extern "C" int fl_paged_attn(const void* q, int64_t q_stride, int dtype, const i
   if (rc != FL_OK) return rc;
   FL_REQUIRE(Hq >= Hkv && Hq % Hkv == 0 && Hq <= 65535, FL_E_SHAPE, "%s: Hq=%d must be a multiple of Hkv=%d, at most 65535", fn,
              Hq, Hkv);
+  FL_REQUIRE((int64_t)T * Hq < (1ll << 31), FL_E_SHAPE, "%s: T * Hq must be below 2^31", fn);
   FL_REQUIRE(sm_scale > 0.0f && sm_scale < INFINITY, FL_E_RANGE, "%s: sm_scale must be positive and finite", fn);
   FL_REQUIRE(window >= 0 && n_sink >= 0, FL_E_RANGE, "%s: window and n_sink must be >= 0", fn);
   FL_REQUIRE(max_q >= 0 && max_len >= 0, FL_E_RANGE, "%s: max_q and max_len must be >= 0", fn);
@@ -148,6 +471,9 @@ extern "C" int fl_paged_attn(const void* q, int64_t q_stride, int dtype, const i
   if (rc != FL_OK) return rc;
   rc = check_apart(fn, "q", q, q_stride, "o", o, o_stride, T, Hq * d);
   if (rc != FL_OK) return rc;
+  const Plan p = plan_of(B, T, Hq, Hkv, d, page, max_pages, window, n_sink, max_q, max_len);
+  FL_REQUIRE(p.ws == 0 || (ws && ws_bytes >= p.ws), FL_E_WORKSPACE, "%s: workspace of %zu bytes required", fn, p.ws);
+  FL_REQUIRE((reinterpret_cast<uintptr_t>(ws) & 15) == 0, FL_E_SHAPE, "%s: ws must be 16-byte aligned", fn);
   hipStream_t st = as_stream(stream);
   PagedAttnArgs a{};
   a.q = static_cast<const uint16_t*>(q); a.o = static_cast<uint16_t*>(o); a.lse = lse; a.qs = q_stride; a.os = o_stride;
@@ -156,22 +482,12 @@ extern "C" int fl_paged_attn(const void* q, int64_t q_stride, int dtype, const i
   a.pg = {num_pages, page, log2_of(page), Hkv};
   a.kc = static_cast<const uint8_t*>(k_cache); a.vc = static_cast<const uint8_t*>(v_cache); a.ksc = k_scale; a.vsc = v_scale;
   a.Hq = Hq; a.G = Hq / Hkv; a.scale_log2 = sm_scale * 1.4426950408889634f; a.window = window; a.n_sink = n_sink;
+  a.n_split = p.n_split; a.min_tiles = p.min_tiles; a.pinf = INFINITY;
+  a.part = static_cast<float*>(ws);
+  a.part_ml = a.part ? a.part + (size_t)T * Hq * p.n_split * d : nullptr;
   rc = check_batch(fn, a.bt, a.pg, false, st);
   if (rc != FL_OK) return rc;
-  const dim3 grid((unsigned)T, (unsigned)Hq);
-#define FL_ROW(DD)                                                                                   \
-  do {                                                                                               \
-    if (format == FL_KV_I8) {                                                                        \
-      if (dtype == FL_F16) paged_row_kernel<DD, true, true><<<grid, 64, 0, st>>>(a);                 \
-      else paged_row_kernel<DD, true, false><<<grid, 64, 0, st>>>(a);                                \
-    } else {                                                                                         \
-      if (dtype == FL_F16) paged_row_kernel<DD, false, true><<<grid, 64, 0, st>>>(a);                \
-      else paged_row_kernel<DD, false, false><<<grid, 64, 0, st>>>(a);                               \
-    }                                                                                                \
-  } while (0)
-  if (d == 128) FL_ROW(128);
-  else FL_ROW(64);
-#undef FL_ROW
-  return check_launch("paged_row_kernel");
+  if (p.rows == 16) return launch_token<1>(a, d, format, dtype == FL_F16, st);
+  return launch_token<2>(a, d, format, dtype == FL_F16, st);
   FL_API_END
 }
