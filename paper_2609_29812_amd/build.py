@@ -23,7 +23,8 @@ BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libflashloop.so")
 
 SOURCES = ["fl_common.hip", "fl_select.hip", "fl_codec.hip", "fl_attn.hip", "fl_dense_attn.hip",
-           "fl_seg_attn.hip", "fl_colscore.hip", "fl_decode.hip", "fl_rope.hip", "fl_paged.hip", "fl_paged_attn.hip"]
+           "fl_seg_attn.hip", "fl_colscore.hip", "fl_decode.hip", "fl_rope.hip", "fl_paged.hip", "fl_paged_attn.hip",
+           "fl_paged_prompt.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 

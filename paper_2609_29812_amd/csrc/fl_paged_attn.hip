@@ -385,7 +385,8 @@ static int launch_merge(const PagedAttnArgs& a, int d, bool f16, hipStream_t st)
 
 int launch_paged_merge(const PagedAttnArgs& a, int d, int rows_per_tile, int keys_per_tile, bool f16, hipStream_t st) {
   if (rows_per_tile == 16) return launch_merge<16, 32>(a, d, f16, st);
-  return launch_merge<32, 32>(a, d, f16, st);
+  if (rows_per_tile == 32) return launch_merge<32, 32>(a, d, f16, st);
+  return launch_merge<128, 64>(a, d, f16, st);
 }
 
 template <int NR>
@@ -421,13 +422,14 @@ static Plan plan_of(int B, int T, int Hq, int Hkv, int d, int page, int max_page
   Plan p{};
   const int64_t G = Hq / Hkv;
   const int64_t per_seq = std::max<int64_t>(1, std::min<int64_t>(max_q > 0 ? max_q : 1, T)) * G;
-  p.rows = per_seq <= 16 ? 16 : 32;
+  p.rows = per_seq <= 16 ? 16 : per_seq <= 32 ? 32 : 128;
   const int64_t cap = (int64_t)max_pages * page;
   int64_t len = max_len > 0 ? std::min<int64_t>(max_len, cap) : cap;
   if (window > 0) len = std::min<int64_t>(len, (int64_t)window + n_sink + std::max(max_q, 1));
-  const int64_t tiles = std::max<int64_t>(1, (len + kTokenKeys - 1) / kTokenKeys);
+  const int keys = p.rows == 128 ? 64 : kTokenKeys;
+  const int64_t tiles = std::max<int64_t>(1, (len + keys - 1) / keys);
   const int64_t units = std::max<int64_t>(1, std::max<int64_t>(B, T * G / p.rows)) * Hkv;
-  int64_t split = std::min<int64_t>(2048 / units, tiles / 8);
+  int64_t split = std::min<int64_t>((p.rows == 128 ? 512 : 2048) / units, tiles / 8);
   split = std::min<int64_t>(std::max<int64_t>(split, 1), 256);
   p.n_split = (int)split;
   p.min_tiles = (int)((tiles + split - 1) / split);
@@ -488,6 +490,7 @@ extern "C" int fl_paged_attn(const void* q, int64_t q_stride, int dtype, const i
   rc = check_batch(fn, a.bt, a.pg, false, st);
   if (rc != FL_OK) return rc;
   if (p.rows == 16) return launch_token<1>(a, d, format, dtype == FL_F16, st);
-  return launch_token<2>(a, d, format, dtype == FL_F16, st);
+  if (p.rows == 32) return launch_token<2>(a, d, format, dtype == FL_F16, st);
+  return launch_paged_prompt(a, d, format, dtype == FL_F16, st);
   FL_API_END
 }

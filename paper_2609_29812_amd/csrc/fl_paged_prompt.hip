@@ -1,0 +1,339 @@
+// Dense attention over the paged 8-bit cache for many rows per sequence: prompts and their chunks.
+//
+// A workgroup of 4 waves takes 128 rows (positions x query heads of one key/value head), 32 per wave, over stages of 64 keys.
+// The codes of the next stage are loaded while this one is multiplied, widened to exact fp16 in registers and written to the
+// other of two LDS buffers: one barrier a stage, each code widened once for 128 rows.
+//   S^T = K Q^T     v_mfma_f32_32x32x16_f16, K rows as the A operand, so a lane holds 16 keys of one row per block;
+//   O^T += V^T P^T  the same product, V read transposed (ds_read_b64_tr_b16), P rounded to fp16.
+// Scales never touch the codes: a key scale multiplies its 16 scores inside the exponent's fma, a value scale enters as its
+// logarithm there and leaves the row sum as its reciprocal, once per 16 keys.
+#include "fl_paged_attn.h"
+
+namespace fl {
+
+constexpr int kPromptRows = 128, kPromptKeys = 64;
+constexpr int kAhead = 32;                 // stages whose pages and scales are in LDS at a time
+
+template <int D>
+struct __attribute__((aligned(16))) PromptSlot {
+  uint16_t k[kPromptKeys * D];             // blocks of 32 rows, 16-byte chunks permuted (swz32_f), fp16
+  uint16_t v[kPromptKeys * D];
+};
+
+template <int D, bool I8, bool F16>
+__global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttnArgs a) {
+  constexpr int R = kPromptRows, COLS = kPromptKeys;
+  constexpr int NBK = COLS / 32;           // 32-key blocks
+  constexpr int KS = D / 16;               // k-steps of QK^T
+  constexpr int DB = D / 32;               // 32-channel output blocks
+  constexpr int LPK = D / 16;              // lanes (16 codes each) per key
+  constexpr int NI = COLS * LPK / 256;     // loads of a thread, tensor and stage
+  __shared__ PromptSlot<D> s0, s1;
+  __shared__ float4 s_page[2][4 * kAhead]; // per 16 keys: key scale, log2 and reciprocal of the value scale, page
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int hw = lane >> 5, r32 = lane & 31;
+  const int kvh = blockIdx.x % a.pg.heads;
+  const int rest = blockIdx.x / a.pg.heads;
+  const int n_slots = gridDim.x / (a.pg.heads * a.n_split);
+  const int split = rest % a.n_split, slot = n_slots - 1 - rest / a.n_split;     // (later rows see more keys: first)
+  const int G = a.G;
+  const int b = __builtin_amdgcn_readfirstlane(find_seq(a.bt, slot, 1, [G](int c) { return c * G / R; }));
+  if (b < 0) return;
+  const Span sp = span_of<R, COLS>(a, b, slot - (row_of(a.bt, b) * G / R + b));
+  if (sp.rows == 0 || split >= sp.parts) return;
+  const int t0 = split * sp.per, n = max(min(sp.per, sp.tiles - t0), 0);         // its stages
+
+  const int cap = a.bt.max_pages * a.pg.size;
+  const int rr = 32 * wave + r32;
+  const bool row_ok = rr < sp.rows;
+  const int rho = sp.rho0 + (row_ok ? rr : 0);
+  const int tok = rho / G, head = kvh * G + rho % G, pos = sp.start + tok;
+  // positions of the wave's first and last row (none: no key is seen)
+  const int last_row = min(32 * wave + 31, sp.rows - 1);
+  const bool wave_ok = 32 * wave < sp.rows;
+  const int w_min = sp.start + (sp.rho0 + 32 * wave) / G;
+  const int w_max = wave_ok ? min(sp.start + (sp.rho0 + last_row) / G, cap - 1) : -1;
+  const int w_lo = a.window > 0 && w_min >= a.window ? w_min - a.window + 1 : 0;         // the first key (but for the leading) of any
+  const int w_all = a.window > 0 && w_max >= a.window ? w_max - a.window + 1 : 0;        // ... of every row
+  const int jmax = row_ok ? min(pos, cap - 1) : -1;
+  const int jmin = a.window > 0 && pos >= a.window ? pos - a.window + 1 : 0;
+
+  f16x8 qf[KS];
+  float mul;
+  {
+    const uint16_t* src = a.q + (int64_t)(sp.r0 + tok) * a.qs + (int64_t)head * D;
+    float v[KS][8], top = 0.0f;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      load_q8<F16>(a, src, min(pos, cap - 1), 2 * k + hw, v[k]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[k][e]));
+    }
+    const float down = row_down(xor32_max(top));
+    mul = a.scale_log2 / down;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      u32x4 w;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = row_ok ? pack_f16x2(v[k][2 * e] * down, v[k][2 * e + 1] * down) : 0u;
+      qf[k] = __builtin_bit_cast(f16x8, w);
+    }
+  }
+
+  // pages and scales of stages [first, first + kAhead): thread x < 128 has 16 keys
+  auto page_of = [&](int first) {
+    const int st = t0 + first + (threadIdx.x >> 2);
+    int p = -1;
+    if (threadIdx.x < 4 * kAhead && st < t0 + n) {
+      const int page = (key_of<COLS>(sp, st) + (threadIdx.x & 3) * 16) >> a.pg.log2;
+      if (page < a.bt.max_pages) p = a.bt.table[(int64_t)b * a.bt.max_pages + page];
+      if ((uint32_t)p >= (uint32_t)a.pg.num) p = -1;
+    }
+    return p;
+  };
+  auto scales_of = [&](int p) {
+    float ks = 0.0f;
+    ValueScale vs{0.0f, 1.0f};
+    if (p >= 0) {
+      ks = key_scale(a.ksc[(int64_t)p * a.pg.heads + kvh]);
+      vs = value_scale(a.vsc[(int64_t)p * a.pg.heads + kvh]);
+    }
+    return make_float4(ks, vs.log2, vs.inv, __int_as_float(p));
+  };
+
+  // loads: x of the wave covers keys of one 16-key group; a lane has 16 channels of a key
+  typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+  v4u kw[NI], vw[NI];
+  const int lane_key = (int)threadIdx.x / LPK, lane_ch = (int)threadIdx.x % LPK;
+  auto fetch = [&](int st) __attribute__((always_inline)) {          // stage st (of the n)
+    const int key0 = key_of<COLS>(sp, t0 + st);
+#pragma unroll
+    for (int x = 0; x < NI; ++x) {
+      const int key = x * (256 / LPK) + lane_key;
+      const int grp = __builtin_amdgcn_readfirstlane(key >> 4);
+      const int p = __builtin_amdgcn_readfirstlane(__float_as_int(s_page[(st / kAhead) & 1][(st % kAhead) * 4 + grp].w));
+      const int64_t base = (((int64_t)max(p, 0) * a.pg.heads + kvh) * a.pg.size + ((key0 + grp * 16) & (a.pg.size - 1))) * D;
+      const uint32_t at = (uint32_t)((key & 15) * D + lane_ch * 16);
+      kw[x] = *reinterpret_cast<const v4u*>(a.kc + base + at);
+      vw[x] = *reinterpret_cast<const v4u*>(a.vc + base + at);
+      if (!I8 && (p < 0 || key0 + key > sp.i_max)) vw[x] = v4u{};    // codes behind the end may be NaN
+    }
+  };
+  auto store = [&](PromptSlot<D>& sl) __attribute__((always_inline)) {
+#pragma unroll
+    for (int x = 0; x < NI; ++x) {
+      const int key = x * (256 / LPK) + lane_key;
+      const int g = swz32_f<D>(key & 31);
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const int at = key * D + ((2 * lane_ch + c) ^ g) * 8;
+        uint32_t w[4];
+        widen4<I8>(kw[x][2 * c], w);
+        widen4<I8>(kw[x][2 * c + 1], w + 2);
+        *reinterpret_cast<u32x4*>(sl.k + at) = u32x4{w[0], w[1], w[2], w[3]};
+        widen4<I8>(vw[x][2 * c], w);
+        widen4<I8>(vw[x][2 * c + 1], w + 2);
+        *reinterpret_cast<u32x4*>(sl.v + at) = u32x4{w[0], w[1], w[2], w[3]};
+      }
+    }
+  };
+  // LDS read offsets (elements), as in the dense kernel: K row r32, chunk 2 ks + hw; V transposed: lane (16 g + 4 t + q) at
+  // V[16 kb + 4 (g >> 1) + t (+ 8)][32 db + 16 (g & 1) + 4 q]
+  int koff[KS], voff[DB], voff8[DB];
+  {
+    const int g16 = lane >> 4, m16 = lane & 15;
+    const int tq = m16 >> 2, q = m16 & 3;
+    const int col0 = 4 * (g16 >> 1) + tq;
+    const int c_lo = 2 * (g16 & 1) + (q >> 1);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) koff[ks] = r32 * D + ((2 * ks + hw) ^ swz32_f<D>(r32)) * 8;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+      voff[db] = col0 * D + ((4 * db + c_lo) ^ swz32_f<D>(col0)) * 8 + 4 * (q & 1);
+      voff8[db] = (col0 + 8) * D + ((4 * db + c_lo) ^ swz32_f<D>(col0 + 8)) * 8 + 4 * (q & 1);
+    }
+  }
+  f32x16 acc[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db) acc[db] = f32x16{};
+  float ref = -INFINITY, lsum = 0.0f;
+
+  auto compute = [&](const PromptSlot<D>& sl, int st) __attribute__((always_inline)) {
+    const int key0 = key_of<COLS>(sp, t0 + st);
+    if (key0 > w_max || (key0 + COLS <= w_lo && key0 >= a.n_sink)) return;     // uniform: no row of the wave sees a key of it
+    const float4* pages = s_page[(st / kAhead) & 1] + (st % kAhead) * 4;
+    f32x16 s[NBK];
+#pragma unroll
+    for (int x = 0; x < NBK; ++x) s[x] = f32x16{};
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int x = 0; x < NBK; ++x) {
+        const u32x4 w = *reinterpret_cast<const u32x4*>(&sl.k[x * 32 * D + koff[ks]]);
+        s[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, w), qf[ks], s[x], 0, 0, 0);
+      }
+    float mg[2 * NBK], lv[2 * NBK], iv[2 * NBK];
+    int gone = 0;
+    bool spoilt = false;
+#pragma unroll
+    for (int g = 0; g < 2 * NBK; ++g) {
+      const float4 w = pages[g];
+      mg[g] = w.x * mul;
+      lv[g] = w.y;
+      iv[g] = w.z;
+      gone |= __float_as_int(w.w);
+      spoilt |= w.z < 0.0f;
+    }
+    const bool holes = __builtin_amdgcn_readfirstlane(gone) < 0;
+    if (key0 + COLS - 1 > w_min || (key0 < w_all && key0 + COLS > a.n_sink) || holes) {    // uniform
+#pragma unroll
+      for (int x = 0; x < NBK; ++x) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const int j = key0 + 32 * x + 8 * (v >> 2) + 4 * hw + (v & 3);
+          const bool see = j <= jmax && (j >= jmin || j < a.n_sink) && (!holes || __float_as_int(pages[2 * x + (v >> 3)].w) >= 0);
+          s[x][v] = see ? s[x][v] * mg[2 * x + (v >> 3)] : -INFINITY;
+        }
+      }
+#pragma unroll
+      for (int g = 0; g < 2 * NBK; ++g) mg[g] = 1.0f;
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int g = 0; g < 2 * NBK; ++g) {
+      const int x = g >> 1, v0 = 8 * (g & 1);
+      float m0 = fmax_nn(s[x][v0], s[x][v0 + 1], a.pinf), m1 = fmax_nn(s[x][v0 + 2], s[x][v0 + 3], a.pinf);
+      m0 = fmax_nn(fmax_nn(m0, s[x][v0 + 4], a.pinf), s[x][v0 + 5], a.pinf);
+      m1 = fmax_nn(fmax_nn(m1, s[x][v0 + 6], a.pinf), s[x][v0 + 7], a.pinf);
+      top = fmaxf(top, fmaf(fmax_nn(m0, m1, a.pinf), mg[g], lv[g]));
+    }
+    top = xor32_max(top);
+    const bool raise = top > ref + 8.0f;
+    if (__builtin_amdgcn_ballot_w64(raise) != 0) {
+      const float nm = raise ? top : ref;
+      const float alpha = raise ? __builtin_amdgcn_exp2f(ref - nm) : 1.0f;
+      lsum *= alpha;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) acc[db] *= alpha;
+      ref = nm;
+    }
+    const float base = ref == -INFINITY ? 0.0f : ref;
+    if (__builtin_amdgcn_ballot_w64(spoilt) != 0) {                   // a value scale that is not finite: the rows that see it
+      bool any = false;
+#pragma unroll
+      for (int x = 0; x < NBK; ++x)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) any |= iv[2 * x + (v >> 3)] < 0.0f && s[x][v] != -INFINITY;
+      const float bad = xor32_add(any ? 1.0f : 0.0f) > 0.0f ? NAN : 0.0f;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) acc[db] += bad;
+    }
+#pragma unroll
+    for (int x = 0; x < NBK; ++x) {
+      float pr[16];
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        const float off = lv[2 * x + g] - base;
+        float ts[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int v = 8 * g; v < 8 * g + 8; ++v) {
+          pr[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][v], mg[2 * x + g], off));
+          ts[v & 1] += pr[v];
+        }
+        lsum = fmaf(ts[0] + ts[1], fabsf(iv[2 * x + g]), lsum);
+      }
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+        const u32x4 pw = {pack_f16x2(pr[8 * kb + 0], pr[8 * kb + 1]), pack_f16x2(pr[8 * kb + 2], pr[8 * kb + 3]),
+                          pack_f16x2(pr[8 * kb + 4], pr[8 * kb + 5]), pack_f16x2(pr[8 * kb + 6], pr[8 * kb + 7])};
+        const f16x8 pf = __builtin_bit_cast(f16x8, pw);
+        const uint16_t* vt = sl.v + x * 32 * D + 16 * kb * D;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          const i16x4 va = __builtin_amdgcn_ds_read_tr16_b64_v4i16(FL_LDS4(vt + voff[db]));
+          const i16x4 vb = __builtin_amdgcn_ds_read_tr16_b64_v4i16(FL_LDS4(vt + voff8[db]));
+          const i16x8 v8 = __builtin_shufflevector(va, vb, 0, 1, 2, 3, 4, 5, 6, 7);
+          acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, v8), pf, acc[db], 0, 0, 0);
+        }
+      }
+    }
+  };
+
+  if (n > 0) {
+    if (threadIdx.x < 4 * kAhead) s_page[0][threadIdx.x] = scales_of(page_of(0));
+    __syncthreads();
+    fetch(0);
+    store(s0);
+    __syncthreads();
+    int ahead = -1;                                                   // page of the next block's 16 keys
+    float4 ahead_s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    auto step = [&](PromptSlot<D>& cur, PromptSlot<D>& nxt, int st) __attribute__((always_inline)) {
+      const int ph = st % kAhead;                                     // uniform; the next block's table in three steps
+      if (ph == 0) ahead = page_of(st + kAhead);
+      if (ph == 8) ahead_s = scales_of(ahead);
+      if (ph == 16 && threadIdx.x < 4 * kAhead) s_page[((st / kAhead) & 1) ^ 1][threadIdx.x] = ahead_s;
+      if (st + 1 < n) fetch(st + 1);
+      compute(cur, st);
+      if (st + 1 < n) store(nxt);
+      __syncthreads();
+    };
+    for (int st = 0; st < n; st += 2) {
+      step(s0, s1, st);
+      if (st + 1 < n) step(s1, s0, st + 1);
+    }
+  }
+  lsum = xor32_add(lsum);
+  if (!row_ok) return;
+  const int64_t gr = (int64_t)(sp.r0 + tok) * a.Hq + head;
+  const bool none = ref == -INFINITY && lsum == 0.0f;
+  if (sp.parts > 1) {
+    float* out = a.part + (gr * a.n_split + split) * D + 4 * hw;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<float4*>(out + db * 32 + 8 * j) =
+            make_float4(acc[db][4 * j], acc[db][4 * j + 1], acc[db][4 * j + 2], acc[db][4 * j + 3]);
+    if (hw == 0) *reinterpret_cast<float2*>(a.part_ml + (gr * a.n_split + split) * 2) = make_float2(ref, lsum);
+    return;
+  }
+  const float inv = none ? 0.0f : 1.0f / lsum;
+  uint16_t* out = a.o + (int64_t)(sp.r0 + tok) * a.os + (int64_t)head * D + 4 * hw;
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float o[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = acc[db][4 * j + e] * inv;
+      *reinterpret_cast<u32x2*>(out + db * 32 + 8 * j) = u32x2{F16 ? pack_f16x2(o[0], o[1]) : pack_bf16x2(o[0], o[1]),
+                                                               F16 ? pack_f16x2(o[2], o[3]) : pack_bf16x2(o[2], o[3])};
+    }
+  if (hw == 0 && a.lse) a.lse[gr] = none ? -INFINITY : (ref + __builtin_amdgcn_logf(lsum)) * 0.6931471805599453f;
+}
+
+int launch_paged_prompt(const PagedAttnArgs& a, int d, int format, bool f16, hipStream_t st) {
+  const int64_t slots = (int64_t)a.bt.T * a.G / kPromptRows + a.bt.B;
+  const int64_t n = slots * a.n_split * a.pg.heads;
+  FL_REQUIRE(n < (1ll << 31), FL_E_SHAPE, "fl_paged_attn: too many rows");
+  const unsigned grid = (unsigned)n;
+#define FL_PROMPT(DD)                                                                  \
+  do {                                                                                 \
+    if (format == FL_KV_I8) {                                                          \
+      if (f16) paged_prompt_kernel<DD, true, true><<<grid, 256, 0, st>>>(a);           \
+      else paged_prompt_kernel<DD, true, false><<<grid, 256, 0, st>>>(a);              \
+    } else {                                                                           \
+      if (f16) paged_prompt_kernel<DD, false, true><<<grid, 256, 0, st>>>(a);          \
+      else paged_prompt_kernel<DD, false, false><<<grid, 256, 0, st>>>(a);             \
+    }                                                                                  \
+  } while (0)
+  if (d == 128) FL_PROMPT(128);
+  else FL_PROMPT(64);
+#undef FL_PROMPT
+  const int rc = check_launch("paged_prompt_kernel");
+  if (rc != FL_OK || a.n_split == 1) return rc;
+  return launch_paged_merge(a, d, kPromptRows, kPromptKeys, f16, st);
+}
+
+}  // namespace fl
