@@ -205,7 +205,6 @@ __global__ __launch_bounds__(256, 2) void paged_token_kernel(PagedAttnArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           p[h][i] = __builtin_amdgcn_exp2f(y[h][i] + off);
-          if (masked) p[h][i] = see[h][i] ? p[h][i] : 0.0f;  // (a NaN scale times no probability)
         }
         const float part = (p[h][0] + p[h][1]) + (p[h][2] + p[h][3]);
         lsum[x] = fmaf(part, fabsf(iv[h]), lsum[x]);
@@ -337,42 +336,68 @@ __global__ __launch_bounds__(256, 2) void paged_token_kernel(PagedAttnArgs a) {
   }
 }
 
-// The parts of a row's keys joined: one wave a row.
+// The parts of a row's keys joined: a workgroup a row, d / 4 threads across its channels and 1024 / d groups that take the
+// parts in turn, so that the loads of one part are never waited for before those of the next.
+constexpr int kMaxSplit = 256;
 template <int D, int R, int KT, bool F16>
 __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t gr = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (gr >= (int64_t)a.bt.T * a.Hq) return;
-  const int t = (int)(gr / a.Hq), h = (int)(gr % a.Hq);
+  constexpr int LN = D / 4, NG = 256 / LN;
+  __shared__ float s_f[kMaxSplit], s_w[2][4];
+  __shared__ float4 s_o[NG][LN];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int t = blockIdx.x / a.Hq, h = blockIdx.x % a.Hq;
   const int b = __builtin_amdgcn_readfirstlane(find_seq(a.bt, t, 0, [](int c) { return c; }));
   if (b < 0 || t >= row_of(a.bt, b + 1)) return;
   const Span sp = span_of<R, KT>(a, b, ((t - row_of(a.bt, b)) * a.G + h % a.G) / R);
   if (sp.parts <= 1) return;
-  const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + gr * a.n_split;
-  float m = -INFINITY;
-  for (int s = lane; s < sp.parts; s += 64) m = fmaxf(m, ml[s].x);
-  for (int off = 32; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
-  float sum = 0.0f, o[D / 64] = {};
-  for (int s = 0; s < sp.parts; ++s) {
-    const float2 w = ml[s];
-    if (w.x == -INFINITY && w.y == 0.0f) continue;
-    const float f = __builtin_amdgcn_exp2f(w.x - m);
-    sum = fmaf(f, w.y, sum);
-    const float* src = a.part + (gr * a.n_split + s) * D + lane * (D / 64);
+  const int64_t gr = blockIdx.x;
+  float2 w = make_float2(-INFINITY, 0.0f);
+  if ((int)threadIdx.x < sp.parts) w = reinterpret_cast<const float2*>(a.part_ml)[gr * a.n_split + threadIdx.x];
+  float m = w.x;
 #pragma unroll
-    for (int e = 0; e < D / 64; ++e) o[e] = fmaf(f, src[e], o[e]);
+  for (int off = 32; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
+  if (lane == 0) s_w[0][wave] = m;
+  __syncthreads();
+  m = fmaxf(fmaxf(s_w[0][0], s_w[0][1]), fmaxf(s_w[0][2], s_w[0][3]));
+  const float f = w.x == -INFINITY && w.y == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(w.x - m);
+  float sum = f * w.y;
+  s_f[threadIdx.x] = f;
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off, 64);
+  if (lane == 0) s_w[1][wave] = sum;
+  __syncthreads();
+  sum = (s_w[1][0] + s_w[1][1]) + (s_w[1][2] + s_w[1][3]);
+  const int c = threadIdx.x % LN, grp = threadIdx.x / LN;
+  const float4* src = reinterpret_cast<const float4*>(a.part + gr * a.n_split * D) + c;
+  float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+  for (int s = grp; s < sp.parts; s += NG) {
+    const float4 x = src[(int64_t)s * LN];
+    const float g = s_f[s];
+    o.x = fmaf(g, x.x, o.x);
+    o.y = fmaf(g, x.y, o.y);
+    o.z = fmaf(g, x.z, o.z);
+    o.w = fmaf(g, x.w, o.w);
+  }
+  s_o[grp][c] = o;
+  __syncthreads();
+  if (grp != 0) return;
+#pragma unroll
+  for (int s = 1; s < NG; ++s) {
+    const float4 x = s_o[s][c];
+    o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
   }
   const bool none = m == -INFINITY && sum == 0.0f;
   const float inv = none ? 0.0f : 1.0f / sum;
-  uint16_t* dst = a.o + (int64_t)t * a.os + (int64_t)h * D + lane * (D / 64);
-  if constexpr (D == 128) *reinterpret_cast<uint32_t*>(dst) = F16 ? pack_f16x2(o[0] * inv, o[1] * inv) : pack_bf16x2(o[0] * inv, o[1] * inv);
-  else *dst = (uint16_t)(F16 ? pack_f16x2(o[0] * inv, 0.0f) : pack_bf16x2(o[0] * inv, 0.0f));
-  if (a.lse && lane == 0) a.lse[gr] = none ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+  *reinterpret_cast<u32x2*>(a.o + (int64_t)t * a.os + (int64_t)h * D + 4 * c) =
+      u32x2{F16 ? pack_f16x2(o.x * inv, o.y * inv) : pack_bf16x2(o.x * inv, o.y * inv),
+            F16 ? pack_f16x2(o.z * inv, o.w * inv) : pack_bf16x2(o.z * inv, o.w * inv)};
+  if (a.lse && c == 0) a.lse[gr] = none ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
 }
 
 template <int R, int KT>
 static int launch_merge(const PagedAttnArgs& a, int d, bool f16, hipStream_t st) {
-  const unsigned grid = (unsigned)(((int64_t)a.bt.T * a.Hq + 3) / 4);
+  const unsigned grid = (unsigned)((int64_t)a.bt.T * a.Hq);
   if (d == 128) {
     if (f16) paged_merge_kernel<128, R, KT, true><<<grid, 256, 0, st>>>(a);
     else paged_merge_kernel<128, R, KT, false><<<grid, 256, 0, st>>>(a);
@@ -430,7 +455,7 @@ static Plan plan_of(int B, int T, int Hq, int Hkv, int d, int page, int max_page
   const int64_t tiles = std::max<int64_t>(1, (len + keys - 1) / keys);
   const int64_t units = std::max<int64_t>(1, std::max<int64_t>(B, T * G / p.rows)) * Hkv;
   int64_t split = std::min<int64_t>((p.rows == 128 ? 512 : 2048) / units, tiles / 8);
-  split = std::min<int64_t>(std::max<int64_t>(split, 1), 256);
+  split = std::min<int64_t>(std::max<int64_t>(split, 1), kMaxSplit);
   p.n_split = (int)split;
   p.min_tiles = (int)((tiles + split - 1) / split);
   p.ws = split > 1 ? (size_t)T * Hq * split * (d + 2) * sizeof(float) : 0;
