@@ -23,20 +23,26 @@ struct Pages {
 // cu[b] as a row number in [0, T], whatever it holds
 __device__ __forceinline__ int row_of(const Batch& bt, int b) { return min(max(bt.cu[b], 0), bt.T); }
 
-// The last sequence b whose first slot, f(cu[b]) + extra * b, is at most `slot`; -1 if there is none.  f ascends, so with
-// extra >= 1 a sequence's slots are slot numbers of its own.  The wave looks at 64 sequences at a time.
+// The last sequence b whose first slot, f(cu[b]) + extra * b, is at most `slot` (b = -1: there is none), its rows and its
+// length.  f ascends, so with extra >= 1 a sequence's slots are slot numbers of its own.  The wave looks at 64 sequences at a
+// time, rows and lengths in one round of loads: these stand before everything else that a workgroup reads.
+struct Seq {
+  int b, r0, r1, len;
+};
 template <class F>
-__device__ __forceinline__ int find_seq(const Batch& bt, int slot, int extra, F f) {
+__device__ __forceinline__ Seq find_seq(const Batch& bt, int slot, int extra, F f) {
   const int lane = threadIdx.x & 63;
-  int n = 0;
+  Seq s{-1, 0, 0, 0};
   for (int b0 = 0; b0 < bt.B; b0 += 64) {
-    const int b = b0 + lane;
-    const bool in = b < bt.B && f(row_of(bt, min(b, bt.B - 1))) + extra * b <= slot;
-    const uint64_t m = __builtin_amdgcn_ballot_w64(in);
-    n += __popcll(m);
-    if (m != ~0ull) break;
+    const int b = b0 + lane, bc = min(b, bt.B - 1);
+    const int r0 = row_of(bt, bc), r1 = row_of(bt, bc + 1), len = bt.lens[bc];
+    const uint64_t m = __builtin_amdgcn_ballot_w64(b < bt.B && f(r0) + extra * b <= slot);
+    const int n = __popcll(m);
+    if (n > 0) s = {b0 + n - 1, __builtin_amdgcn_readlane(r0, n - 1), __builtin_amdgcn_readlane(r1, n - 1),
+                    __builtin_amdgcn_readlane(len, n - 1)};
+    if (n < 64) break;
   }
-  return n - 1;
+  return s;
 }
 
 // 16-bit value to fp32 (exact)

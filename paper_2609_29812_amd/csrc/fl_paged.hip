@@ -150,9 +150,9 @@ __global__ __launch_bounds__(256) void paged_append_kernel(AppendArgs a) {
   __shared__ uint32_t s_max[4];
   const int slot = blockIdx.x, h = blockIdx.y;
   const bool is_k = blockIdx.z == 0;
-  const int b = __builtin_amdgcn_readfirstlane(find_seq(a.bt, slot, 2, [](int c) { return c >> LOG2; }));
+  const Seq sq = find_seq(a.bt, slot, 2, [](int c) { return c >> LOG2; });
+  const int b = sq.b, r0 = sq.r0, n = sq.r1 - sq.r0, len = sq.len;
   if (b < 0) return;
-  const int r0 = row_of(a.bt, b), n = row_of(a.bt, b + 1) - r0, len = a.bt.lens[b];
   if (n <= 0 || len <= 0) return;
   const int start = max(len - n, 0);                         // first stored position; (len - n < 0: the first are dropped)
   const int64_t pi = (int64_t)(start >> LOG2) + (slot - ((r0 >> LOG2) + 2 * b));

@@ -36,11 +36,11 @@ struct Span {
 
 // tiles `slot` of R rows: slots cu[b] G / R + b .. belong to sequence b
 template <int R, int KT>
-__device__ __forceinline__ Span span_of(const PagedAttnArgs& a, int b, int tile) {
+__device__ __forceinline__ Span span_of(const PagedAttnArgs& a, const Seq& q, int tile) {
   Span s{};
-  s.b = b;
-  s.r0 = row_of(a.bt, b);
-  const int n = row_of(a.bt, b + 1) - s.r0;
+  s.b = q.b;
+  s.r0 = q.r0;
+  const int n = q.r1 - q.r0;
   s.rho0 = tile * R;
   s.rows = min(n * a.G - s.rho0, R);
   if (s.rows <= 0 || tile < 0) {
@@ -48,7 +48,7 @@ __device__ __forceinline__ Span span_of(const PagedAttnArgs& a, int b, int tile)
     return s;
   }
   const int cap = a.bt.max_pages * a.pg.size;                // positions that have a block table entry
-  s.start = max(a.bt.lens[b], 0) - n;
+  s.start = max(q.len, 0) - n;
   s.i_min = s.start + s.rho0 / a.G;
   s.i_max = s.start + (s.rho0 + s.rows - 1) / a.G;
   const int hi = min(s.i_max, cap - 1);

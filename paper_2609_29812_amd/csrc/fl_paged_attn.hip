@@ -14,10 +14,11 @@ constexpr int kTokenKeys = 32;     // keys of a wave's tile
 //                 fp16; the contraction runs over the channels in the order that this gives.
 //   O^T += V^T P^T  the same product: a lane of S^T holds 2 x 4 keys of one row, which is the P^T operand for keys in that
 //                 order; the lane's V bytes (8 keys x d / 16 channels) are transposed by byte permutes while they are widened.
-// No LDS in the loop: the next tile's codes are in flight while one is multiplied.  Page numbers and scales of 32 tiles are
+// No LDS in the loop: the next tile's keys are fetched into the registers that the scores leave, its values into those that the
+// outputs leave.  Page numbers and scales of 32 tiles are
 // fetched by the lanes at once and handed out by v_readlane.
 template <int D, bool I8, bool F16, int NR>
-__global__ __launch_bounds__(256, 2) void paged_token_kernel(PagedAttnArgs a) {
+__global__ __launch_bounds__(256, NR == 1 ? 4 : 2) void paged_token_kernel(PagedAttnArgs a) {
   constexpr int R = 16 * NR, KS = D / 32, DT = D / 16;
   constexpr int KW = D / 64;              // 16-byte loads of a lane per key group
   constexpr int VW = D / 64;              // words of a lane per key of V
@@ -30,11 +31,39 @@ __global__ __launch_bounds__(256, 2) void paged_token_kernel(PagedAttnArgs a) {
   const int rest = blockIdx.x / a.pg.heads;
   const int split = rest % a.n_split, slot = rest / a.n_split;
   const int G = a.G;
-  const int b = __builtin_amdgcn_readfirstlane(find_seq(a.bt, slot, 1, [G](int c) { return c * G / R; }));
+  const Seq sq = find_seq(a.bt, slot, 1, [G](int c) { return c * G / R; });
+  const int b = sq.b;
   if (b < 0) return;
-  const Span sp = span_of<R, kTokenKeys>(a, b, slot - (row_of(a.bt, b) * G / R + b));
+  const Span sp = span_of<R, kTokenKeys>(a, sq, slot - (sq.r0 * G / R + b));
   if (sp.rows == 0 || split >= sp.parts) return;
   const int t0 = split * sp.per, t1 = min(t0 + sp.per, sp.tiles);
+
+  // pages and scales of the wave's next 32 tiles: lane l has tile l % 32, key group l / 32.  The pages are asked for before the
+  // queries, and their scales before the first codes but waited for after them.
+  int pid_v = -1;
+  float ks_v = 0.0f, lv_v = 1.0f, iv_v = 0.0f;
+  auto fetch_pages = [&](int c0) {
+    const int tile = t0 + wave + 4 * (c0 + (lane & 31));
+    pid_v = -1;
+    if (tile < t1) {
+      const int page = (key_of<kTokenKeys>(sp, tile) + (lane >> 5) * 16) >> a.pg.log2;
+      if (page < a.bt.max_pages) pid_v = a.bt.table[(int64_t)b * a.bt.max_pages + page];
+    }
+  };
+  auto fetch_scales = [&] {
+    const bool there = (uint32_t)pid_v < (uint32_t)a.pg.num;
+    pid_v = there ? pid_v : -1;
+    const int64_t at = (int64_t)max(pid_v, 0) * a.pg.heads + kvh;
+    ks_v = a.ksc[at];
+    lv_v = a.vsc[at];
+  };
+  auto use_scales = [&] {
+    const ValueScale vs = value_scale(pid_v < 0 ? 1.0f : lv_v);
+    ks_v = pid_v < 0 ? 0.0f : key_scale(ks_v);
+    lv_v = vs.log2;
+    iv_v = vs.inv;
+  };
+  fetch_pages(0);
 
   // the lane's rows
   f16x8 qf[NR][KS];
@@ -51,7 +80,7 @@ __global__ __launch_bounds__(256, 2) void paged_token_kernel(PagedAttnArgs a) {
     float v[KS][8], top = 0.0f;
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
-      load_q8<F16>(a, src, min(pos, cap - 1), g4 * KS + k, v[k]);
+      load_q8<F16>(a, src, min(pos, cap - 1), 8 * (k / 2) + 2 * g4 + k % 2, v[k]);   // (the order in which keys lie in the lanes)
 #pragma unroll
       for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[k][e]));
     }
@@ -80,55 +109,39 @@ __global__ __launch_bounds__(256, 2) void paged_token_kernel(PagedAttnArgs a) {
     for (int t = 0; t < DT; ++t) acc[x][t] = f32x4{};
   }
 
-  // pages and scales of the wave's next 32 tiles: lane l has tile l % 32, key group l / 32
-  int pid_v = -1;
-  float ks_v = 0.0f, lv_v = 0.0f, iv_v = 0.0f;
-  auto fetch_pages = [&](int c0) {
-    const int tile = t0 + wave + 4 * (c0 + (lane & 31));
-    pid_v = -1;
-    ks_v = 0.0f;
-    ValueScale vs{0.0f, 1.0f};
-    if (tile < t1) {
-      const int page = (key_of<kTokenKeys>(sp, tile) + (lane >> 5) * 16) >> a.pg.log2;
-      const int p = page < a.bt.max_pages ? a.bt.table[(int64_t)b * a.bt.max_pages + page] : -1;
-      if ((uint32_t)p < (uint32_t)a.pg.num) {
-        pid_v = p;
-        ks_v = key_scale(a.ksc[(int64_t)p * a.pg.heads + kvh]);
-        vs = value_scale(a.vsc[(int64_t)p * a.pg.heads + kvh]);
-      }
-    }
-    lv_v = vs.log2;
-    iv_v = vs.inv;
-  };
-
-  struct Tile {
-    u32x4 k[2][KW];
-    uint32_t v[8][VW];
-  };
-  auto load = [&](Tile& w, int c) {                          // the wave's tile c
+  u32x4 wk[2][KW];                                           // the tile's codes of the lane
+  uint32_t wv[8][VW];
+  auto base_of = [&](int c, int h) {                         // first code of key group h of the wave's tile c
     const int key0 = key_of<kTokenKeys>(sp, t0 + wave + 4 * c);
+    const int p = max(__builtin_amdgcn_readlane(pid_v, (c & 31) + 32 * h), 0);        // (a page that is not there: masked)
+    return (((int64_t)p * a.pg.heads + kvh) * a.pg.size + ((key0 + 16 * h) & (a.pg.size - 1))) * D;
+  };
+  auto load_k = [&](int c) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int p = max(__builtin_amdgcn_readlane(pid_v, (c & 31) + 32 * h), 0);      // (a page that is not there: masked)
-      const int64_t base = (((int64_t)p * a.pg.heads + kvh) * a.pg.size + ((key0 + 16 * h) & (a.pg.size - 1))) * D;
-      const uint8_t* kb = a.kc + base;
-      const uint8_t* vb = a.vc + base;
+      const uint8_t* kb = a.kc + base_of(c, h);
 #pragma unroll
-      for (int x = 0; x < KW; ++x) w.k[h][x] = *reinterpret_cast<const u32x4*>(kb + (uint32_t)(r16 * D + g4 * (D / 4) + 16 * x));
+      for (int x = 0; x < KW; ++x) wk[h][x] = *reinterpret_cast<const u32x4*>(kb + (uint32_t)(r16 * D + 64 * x + 16 * g4));
+    }
+  };
+  auto load_v = [&](int c) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint8_t* vb = a.vc + base_of(c, h);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const uint32_t at = (uint32_t)((g4 * 4 + e) * D + r16 * DT);
         if constexpr (VW == 2) {
           const u32x2 d2 = *reinterpret_cast<const u32x2*>(vb + at);
-          w.v[4 * h + e][0] = d2[0];
-          w.v[4 * h + e][1] = d2[1];
+          wv[4 * h + e][0] = d2[0];
+          wv[4 * h + e][1] = d2[1];
         } else {
-          w.v[4 * h + e][0] = *reinterpret_cast<const uint32_t*>(vb + at);
+          wv[4 * h + e][0] = *reinterpret_cast<const uint32_t*>(vb + at);
         }
       }
     }
   };
-  auto compute = [&](Tile& w, int c) {
+  auto compute = [&](int c, bool more) {
     const int key0 = key_of<kTokenKeys>(sp, t0 + wave + 4 * c);
     const int pid0 = __builtin_amdgcn_readlane(pid_v, c & 31), pid1 = __builtin_amdgcn_readlane(pid_v, (c & 31) + 32);
     float ks[2], lv[2], iv[2];
@@ -149,22 +162,23 @@ __global__ __launch_bounds__(256, 2) void paged_token_kernel(PagedAttnArgs a) {
       for (int k = 0; k < KS; ++k) {
         u32x4 kw;
         uint32_t two[2];
-        widen4<I8>(w.k[h][k / 2][2 * (k % 2)], two);
+        widen4<I8>(wk[h][k / 2][2 * (k % 2)], two);
         kw[0] = two[0]; kw[1] = two[1];
-        widen4<I8>(w.k[h][k / 2][2 * (k % 2) + 1], two);
+        widen4<I8>(wk[h][k / 2][2 * (k % 2) + 1], two);
         kw[2] = two[0]; kw[3] = two[1];
 #pragma unroll
         for (int x = 0; x < NR; ++x)
           s[x][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, kw), qf[x][k], s[x][h], 0, 0, 0);
       }
     }
+    if (more) load_k(c + 1);
     if (masked && !I8) {                                     // codes behind the end may be NaN
       const int hi = sp.i_max;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const bool there = key0 + (e >> 2) * 16 + g4 * 4 + (e & 3) <= hi && (e < 4 ? pid0 : pid1) >= 0;
 #pragma unroll
-        for (int y = 0; y < VW; ++y) w.v[e][y] = there ? w.v[e][y] : 0u;
+        for (int y = 0; y < VW; ++y) wv[e][y] = there ? wv[e][y] : 0u;
       }
     }
     f16x8 pf[NR];
@@ -223,65 +237,38 @@ __global__ __launch_bounds__(256, 2) void paged_token_kernel(PagedAttnArgs a) {
                         pack_f16x2(p[1][2], p[1][3])};
       pf[x] = __builtin_bit_cast(f16x8, pw);
     }
-    if constexpr (I8) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
+    for (int y = 0; y < VW; ++y)
 #pragma unroll
-        for (int y = 0; y < VW; ++y) w.v[e][y] ^= 0x80808080u;
-    }
+      for (int u = 0; u < 2; ++u) {                          // channels 4 y + 2 u and the next of the lane, eight keys
+        u32x4 va, vb;
 #pragma unroll
-    for (int y = 0; y < VW; ++y) {
-      if constexpr (I8) {
-        const f16x2 off = {(_Float16)-1152.0f, (_Float16)-1152.0f};
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {                        // channel 4 y + t of the lane: one byte of each of eight keys
-          u32x4 vw;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const uint32_t two = __builtin_amdgcn_perm(w.v[2 * e + 1][y], w.v[2 * e][y], 0x0c000c00u | ((4 + t) << 16) | t);
-            vw[e] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, two | 0x64006400u) + off);
-          }
-#pragma unroll
-          for (int x = 0; x < NR; ++x)
-            acc[x][4 * y + t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, vw), pf[x], acc[x][4 * y + t], 0, 0, 0);
-        }
-      } else {
-        uint32_t lo[8], hi[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int e = 0; e < 4; ++e) {
           uint32_t two[2];
-          widen4<false>(w.v[e][y], two);
-          lo[e] = two[0];
-          hi[e] = two[1];
+          widen4<I8>(__builtin_amdgcn_perm(wv[2 * e + 1][y], wv[2 * e][y], u ? 0x07030602u : 0x05010400u), two);
+          va[e] = two[0];
+          vb[e] = two[1];
         }
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          u32x4 vw;
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            vw[e] = __builtin_amdgcn_perm(t < 2 ? lo[2 * e + 1] : hi[2 * e + 1], t < 2 ? lo[2 * e] : hi[2 * e],
-                                          t & 1 ? 0x07060302u : 0x05040100u);
-#pragma unroll
-          for (int x = 0; x < NR; ++x)
-            acc[x][4 * y + t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, vw), pf[x], acc[x][4 * y + t], 0, 0, 0);
+        for (int x = 0; x < NR; ++x) {
+          const int t = 4 * y + 2 * u;
+          acc[x][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, va), pf[x], acc[x][t], 0, 0, 0);
+          acc[x][t + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, vb), pf[x], acc[x][t + 1], 0, 0, 0);
         }
       }
-    }
   };
 
   const int mine = t1 - t0 - wave <= 0 ? 0 : (t1 - t0 - wave + 3) / 4;     // tiles of this wave
-  Tile w0, w1;
   for (int c0 = 0; c0 < mine; c0 += 32) {
-    fetch_pages(c0);
+    if (c0 > 0) fetch_pages(c0);
+    fetch_scales();
     const int c1 = min(c0 + 32, mine);
-    load(w0, c0);
-    for (int c = c0; c < c1; c += 2) {
-      if (c + 1 < c1) load(w1, c + 1);
-      compute(w0, c);
-      if (c + 1 < c1) {
-        if (c + 2 < c1) load(w0, c + 2);
-        compute(w1, c + 1);
-      }
+    load_k(c0);
+    load_v(c0);
+    use_scales();
+    for (int c = c0; c < c1; ++c) {
+      compute(c, c + 1 < c1);
+      if (c + 1 < c1) load_v(c + 1);
     }
   }
 
@@ -346,9 +333,9 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
   __shared__ float4 s_o[NG][LN];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int t = blockIdx.x / a.Hq, h = blockIdx.x % a.Hq;
-  const int b = __builtin_amdgcn_readfirstlane(find_seq(a.bt, t, 0, [](int c) { return c; }));
-  if (b < 0 || t >= row_of(a.bt, b + 1)) return;
-  const Span sp = span_of<R, KT>(a, b, ((t - row_of(a.bt, b)) * a.G + h % a.G) / R);
+  const Seq sq = find_seq(a.bt, t, 0, [](int c) { return c; });
+  if (sq.b < 0 || t >= sq.r1) return;
+  const Span sp = span_of<R, KT>(a, sq, ((t - sq.r0) * a.G + h % a.G) / R);
   if (sp.parts <= 1) return;
   const int64_t gr = blockIdx.x;
   float2 w = make_float2(-INFINITY, 0.0f);

@@ -38,9 +38,10 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttnArgs a) {
   const int n_slots = gridDim.x / (a.pg.heads * a.n_split);
   const int split = rest % a.n_split, slot = n_slots - 1 - rest / a.n_split;     // (later rows see more keys: first)
   const int G = a.G;
-  const int b = __builtin_amdgcn_readfirstlane(find_seq(a.bt, slot, 1, [G](int c) { return c * G / R; }));
+  const Seq sq = find_seq(a.bt, slot, 1, [G](int c) { return c * G / R; });
+  const int b = sq.b;
   if (b < 0) return;
-  const Span sp = span_of<R, COLS>(a, b, slot - (row_of(a.bt, b) * G / R + b));
+  const Span sp = span_of<R, COLS>(a, sq, slot - (sq.r0 * G / R + b));
   if (sp.rows == 0 || split >= sp.parts) return;
   const int t0 = split * sp.per, n = max(min(sp.per, sp.tiles - t0), 0);         // its stages
 
