@@ -18,7 +18,8 @@ struct PagedAttnArgs {
   int Hq, G;                       // query heads; of them per key/value head
   float scale_log2;                // sm_scale * log2(e)
   int window, n_sink;
-  int n_split, min_tiles;          // at most n_split parts of the keys, each of at least min_tiles tiles (but the last)
+  int n_split, min_tiles;          // at most n_split parts of the keys, each of about min_tiles tiles or more
+  int share;                       // workgroups that the tiles of a batch of few rows are shared out to
   float *part, *part_ml;           // [T Hq][n_split][d] sums and [T Hq][n_split][2] references and normalisers
   float pinf;                      // +inf
 };
@@ -60,6 +61,83 @@ __device__ __forceinline__ Span span_of(const PagedAttnArgs& a, const Seq& q, in
   s.per = max(a.min_tiles, (s.tiles + a.n_split - 1) / a.n_split);
   s.parts = max(1, (s.tiles + s.per - 1) / s.per);
   return s;
+}
+
+// Split keys of few rows: the tiles of all sequences are shared out evenly, whatever the lengths are.  With `per` = all
+// (sequence, row tile, key/value head, tile)s / share, a sequence of t tiles gets ceil(t / per) parts (at most n_split), and
+// work item u of a head goes to sequences in order: rt_b * parts_b items each.  t is the number of tiles that a row tile sees at
+// most; span_of then cuts what it does see into that many parts.
+template <int R, int KT>
+struct Shares {
+  int per;
+  int r0, r1, len;                                           // the lane's sequence of the first 64
+  const PagedAttnArgs& a;
+  __device__ __forceinline__ Shares(const PagedAttnArgs& args) : a(args) {
+    float total = 0.0f;                                      // (a share: exactness is of no matter, and every wave has the same)
+    const int lane = threadIdx.x & 63;
+    load(lane, r0, r1, len);
+    if (lane < a.bt.B) total = (float)row_tiles(r1 - r0) * (float)tiles(r1 - r0, len);
+    for (int b = lane + 64; b - lane < a.bt.B; b += 64) {
+      int x0, x1, l;
+      load(b, x0, x1, l);
+      if (b < a.bt.B) total += (float)row_tiles(x1 - x0) * (float)tiles(x1 - x0, l);
+    }
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) total += __shfl_xor(total, off, 64);
+    const float share = ceilf(total * (float)a.pg.heads / (float)a.share);
+    per = __builtin_amdgcn_readfirstlane(max(a.min_tiles, (int)fminf(share, 1073741824.0f)));
+  }
+  __device__ __forceinline__ void load(int b, int& x0, int& x1, int& l) const {
+    const int bc = min(b, a.bt.B - 1);
+    x0 = row_of(a.bt, bc);
+    x1 = row_of(a.bt, bc + 1);
+    l = a.bt.lens[bc];
+  }
+  __device__ __forceinline__ int row_tiles(int n) const { return n <= 0 ? 0 : (n * a.G + R - 1) / R; }
+  __device__ __forceinline__ int tiles(int n, int len) const {
+    int64_t l = min(max(len, 0), a.bt.max_pages * a.pg.size);
+    if (a.window > 0) l = min(l, (int64_t)a.window + a.n_sink + n);
+    return (int)((l + KT - 1) / KT);
+  }
+  __device__ __forceinline__ int parts(int n, int len) const {
+    return min(max((tiles(n, len) + per - 1) / per, 1), a.n_split);
+  }
+  // the sequence of item u, the row tile and the part; seq.b = -1 behind the last
+  __device__ __forceinline__ Seq find(int u, int& tile, int& part) const {
+    const int lane = threadIdx.x & 63;
+    Seq s{-1, 0, 0, 0};
+    tile = part = 0;
+    int before = 0;                                          // items of the sequences looked at
+    for (int b0 = 0; b0 < a.bt.B; b0 += 64) {
+      int x0 = r0, x1 = r1, xl = len;
+      if (b0 > 0) load(b0 + lane, x0, x1, xl);
+      const int p = parts(x1 - x0, xl);
+      const int items = b0 + lane < a.bt.B ? row_tiles(x1 - x0) * p : 0;
+      int end = items;                                       // items up to and with the lane's
+#pragma unroll
+      for (int off = 1; off < 64; off <<= 1) {
+        const int x = __shfl_up(end, off, 64);
+        end += lane >= off ? x : 0;
+      }
+      const uint64_t m = __builtin_amdgcn_ballot_w64(before + end > u);
+      if (m != 0) {
+        const int l = __builtin_ctzll(m);
+        s = {b0 + l, __builtin_amdgcn_readlane(x0, l), __builtin_amdgcn_readlane(x1, l), __builtin_amdgcn_readlane(xl, l)};
+        const int at = u - before - (__builtin_amdgcn_readlane(end, l) - __builtin_amdgcn_readlane(items, l));
+        const int ps = __builtin_amdgcn_readlane(p, l);
+        tile = at / ps;
+        part = at % ps;
+        break;
+      }
+      before += __builtin_amdgcn_readlane(end, 63);
+    }
+    return s;
+  }
+};
+// cuts a span into the parts that its sequence has (some may have no tile)
+__device__ __forceinline__ void cut(Span& s, int parts) {
+  s.parts = parts;
+  s.per = (s.tiles + parts - 1) / parts;
 }
 template <int KT>
 __device__ __forceinline__ int key_of(const Span& s, int tile) { return (tile < s.n_lead ? tile : tile - s.n_lead + s.first) * KT; }

@@ -28,14 +28,26 @@ __global__ __launch_bounds__(256, NR == 1 ? 4 : 2) void paged_token_kernel(Paged
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r16 = lane & 15, g4 = lane >> 4;
   const int kvh = blockIdx.x % a.pg.heads;
-  const int rest = blockIdx.x / a.pg.heads;
-  const int split = rest % a.n_split, slot = rest / a.n_split;
+  const int slot = blockIdx.x / a.pg.heads;
   const int G = a.G;
-  const Seq sq = find_seq(a.bt, slot, 1, [G](int c) { return c * G / R; });
+  Seq sq;
+  Span sp;
+  int split = 0;
+  if (a.n_split == 1) {
+    sq = find_seq(a.bt, slot, 1, [G](int c) { return c * G / R; });
+    if (sq.b < 0) return;
+    sp = span_of<R, kTokenKeys>(a, sq, slot - (sq.r0 * G / R + sq.b));
+    cut(sp, 1);
+  } else {
+    const Shares<R, kTokenKeys> shares(a);
+    int tile;
+    sq = shares.find(slot, tile, split);
+    if (sq.b < 0) return;
+    sp = span_of<R, kTokenKeys>(a, sq, tile);
+    cut(sp, shares.parts(sq.r1 - sq.r0, sq.len));
+  }
+  if (sp.rows == 0) return;
   const int b = sq.b;
-  if (b < 0) return;
-  const Span sp = span_of<R, kTokenKeys>(a, sq, slot - (sq.r0 * G / R + b));
-  if (sp.rows == 0 || split >= sp.parts) return;
   const int t0 = split * sp.per, t1 = min(t0 + sp.per, sp.tiles);
 
   // pages and scales of the wave's next 32 tiles: lane l has tile l % 32, key group l / 32.  The pages are asked for before the
@@ -121,7 +133,7 @@ __global__ __launch_bounds__(256, NR == 1 ? 4 : 2) void paged_token_kernel(Paged
     for (int h = 0; h < 2; ++h) {
       const uint8_t* kb = a.kc + base_of(c, h);
 #pragma unroll
-      for (int x = 0; x < KW; ++x) wk[h][x] = *reinterpret_cast<const u32x4*>(kb + (uint32_t)(r16 * D + 64 * x + 16 * g4));
+      for (int x = 0; x < KW; ++x) wk[h][x] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(kb + (uint32_t)(r16 * D + 64 * x + 16 * g4)));
     }
   };
   auto load_v = [&](int c) {
@@ -132,11 +144,11 @@ __global__ __launch_bounds__(256, NR == 1 ? 4 : 2) void paged_token_kernel(Paged
       for (int e = 0; e < 4; ++e) {
         const uint32_t at = (uint32_t)((g4 * 4 + e) * D + r16 * DT);
         if constexpr (VW == 2) {
-          const u32x2 d2 = *reinterpret_cast<const u32x2*>(vb + at);
+          const u32x2 d2 = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(vb + at));
           wv[4 * h + e][0] = d2[0];
           wv[4 * h + e][1] = d2[1];
         } else {
-          wv[4 * h + e][0] = *reinterpret_cast<const uint32_t*>(vb + at);
+          wv[4 * h + e][0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(vb + at));
         }
       }
     }
@@ -335,7 +347,8 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
   const int t = blockIdx.x / a.Hq, h = blockIdx.x % a.Hq;
   const Seq sq = find_seq(a.bt, t, 0, [](int c) { return c; });
   if (sq.b < 0 || t >= sq.r1) return;
-  const Span sp = span_of<R, KT>(a, sq, ((t - sq.r0) * a.G + h % a.G) / R);
+  Span sp = span_of<R, KT>(a, sq, ((t - sq.r0) * a.G + h % a.G) / R);
+  if constexpr (KT == kTokenKeys) cut(sp, Shares<R, KT>(a).parts(sq.r1 - sq.r0, sq.len));
   if (sp.parts <= 1) return;
   const int64_t gr = blockIdx.x;
   float2 w = make_float2(-INFINITY, 0.0f);
@@ -403,8 +416,9 @@ int launch_paged_merge(const PagedAttnArgs& a, int d, int rows_per_tile, int key
 
 template <int NR>
 static int launch_token(const PagedAttnArgs& a, int d, int format, bool f16, hipStream_t st) {
+  // row tiles, and with split keys as many parts more as the tiles are shared out to
   const int64_t slots = (int64_t)a.bt.T * a.G / (16 * NR) + a.bt.B;
-  const int64_t n = slots * a.n_split * a.pg.heads;
+  const int64_t n = (slots + (a.n_split > 1 ? a.share / a.pg.heads + 1 : 0)) * a.pg.heads;
   FL_REQUIRE(n < (1ll << 31), FL_E_SHAPE, "fl_paged_attn: too many rows");
   const unsigned grid = (unsigned)n;
 #define FL_TOKEN(DD)                                                                        \
@@ -426,8 +440,9 @@ static int launch_token(const PagedAttnArgs& a, int d, int format, bool f16, hip
 }
 
 // How a call is cut: rows per tile and parts of the keys.
+constexpr int kShare = 768, kLeastTiles = 8;
 struct Plan {
-  int rows, n_split, min_tiles;
+  int rows, n_split, min_tiles, share;
   size_t ws;
 };
 static Plan plan_of(int B, int T, int Hq, int Hkv, int d, int page, int max_pages, int window, int n_sink, int max_q, int max_len) {
@@ -441,10 +456,17 @@ static Plan plan_of(int B, int T, int Hq, int Hkv, int d, int page, int max_page
   const int keys = p.rows == 128 ? 64 : kTokenKeys;
   const int64_t tiles = std::max<int64_t>(1, (len + keys - 1) / keys);
   const int64_t units = std::max<int64_t>(1, std::max<int64_t>(B, T * G / p.rows)) * Hkv;
-  int64_t split = std::min<int64_t>((p.rows == 128 ? 512 : 2048) / units, tiles / 8);
-  split = std::min<int64_t>(std::max<int64_t>(split, 1), kMaxSplit);
+  int64_t split;
+  if (p.rows == 128) {
+    split = std::min<int64_t>(512 / units, tiles / 8);
+    split = std::min<int64_t>(std::max<int64_t>(split, 1), kMaxSplit);
+    p.min_tiles = (int)((tiles + split - 1) / split);
+  } else {
+    p.share = kShare;
+    p.min_tiles = kLeastTiles;
+    split = units < kShare ? std::min<int64_t>(std::max<int64_t>(tiles / kLeastTiles, 1), kMaxSplit) : 1;
+  }
   p.n_split = (int)split;
-  p.min_tiles = (int)((tiles + split - 1) / split);
   p.ws = split > 1 ? (size_t)T * Hq * split * (d + 2) * sizeof(float) : 0;
   return p;
 }
@@ -496,7 +518,7 @@ extern "C" int fl_paged_attn(const void* q, int64_t q_stride, int dtype, const i
   a.pg = {num_pages, page, log2_of(page), Hkv};
   a.kc = static_cast<const uint8_t*>(k_cache); a.vc = static_cast<const uint8_t*>(v_cache); a.ksc = k_scale; a.vsc = v_scale;
   a.Hq = Hq; a.G = Hq / Hkv; a.scale_log2 = sm_scale * 1.4426950408889634f; a.window = window; a.n_sink = n_sink;
-  a.n_split = p.n_split; a.min_tiles = p.min_tiles; a.pinf = INFINITY;
+  a.n_split = p.n_split; a.min_tiles = p.min_tiles; a.share = p.share; a.pinf = INFINITY;
   a.part = static_cast<float*>(ws);
   a.part_ml = a.part ? a.part + (size_t)T * Hq * p.n_split * d : nullptr;
   rc = check_batch(fn, a.bt, a.pg, false, st);
