@@ -149,6 +149,8 @@ APPENDS = [
     ([200, 5], [1, 127], 128, 2, 128, 128),
     ([130, 64, 65], [0, 0, 63], 64, 5, 64, 48),
     ([1] * 70, list(range(70)), 64, 1, 128, 128),
+    ([1, 0, 2, 0, 0, 0, 0, 50, 1], [5, 3, 31, 0, 1, 2, 3, 9, 100], 64, 2, 64, 32),    # few on average, many for one
+    ([23, 1, 1, 1], [8, 127, 128, 1], 128, 3, 128, 64),
 ]
 
 
