@@ -19,7 +19,9 @@ struct PagedAttnArgs {
   float scale_log2;                // sm_scale * log2(e)
   int window, n_sink;
   int n_split, min_tiles;          // at most n_split parts of the keys, each of about min_tiles tiles or more
-  int share;                       // workgroups that the tiles of a batch of few rows are shared out to
+  int share;                       // workgroups that the tiles of a batch are shared out to (many rows: per key/value head)
+  int* ends;                       // many rows, shared out: units up to and with each row tile's
+  int slots;                       // ... and how many row tiles there are at most
   float *part, *part_ml;           // [T Hq][n_split][d] sums and [T Hq][n_split][2] references and normalisers
   float pinf;                      // +inf
 };
@@ -58,8 +60,8 @@ __device__ __forceinline__ Span span_of(const PagedAttnArgs& a, const Seq& q, in
   s.n_lead = (min(a.n_sink, lo) + KT - 1) / KT;
   s.first = max(s.n_lead, lo / KT);
   s.tiles = hi < 0 ? 0 : s.n_lead + max(hi / KT - s.first + 1, 0);
-  s.per = max(a.min_tiles, (s.tiles + a.n_split - 1) / a.n_split);
-  s.parts = max(1, (s.tiles + s.per - 1) / s.per);
+  s.parts = 1;
+  s.per = s.tiles;
   return s;
 }
 
@@ -142,36 +144,85 @@ __device__ __forceinline__ void cut(Span& s, int parts) {
 template <int KT>
 __device__ __forceinline__ int key_of(const Span& s, int tile) { return (tile < s.n_lead ? tile : tile - s.n_lead + s.first) * KT; }
 
-// Eight channels 8 ch .. of a query row in fp32, rotated by its position when there is a table (pos within it).
-template <bool F16>
-__device__ __forceinline__ void load_q8(const PagedAttnArgs& a, const uint16_t* row, int pos, int ch, float* x) {
-  unpack8<F16>(*reinterpret_cast<const uint4*>(row + ch * 8), x);
-  if (!a.rt.table || ch * 8 >= a.rt.rot || pos < 0) return;
-  const float* tr = a.rt.table + (int64_t)pos * a.rt.rot;
-  float2 cs[8];
-  if (a.rt.layout == FL_ROPE_HALF) {
-    const int half = a.rt.rot / 16;
-    const bool second = ch >= half;
-    float y[8];
-    unpack8<F16>(*reinterpret_cast<const uint4*>(row + (second ? ch - half : ch + half) * 8), y);
-    load_turn<true>(tr, a.rt.rot, ch, cs);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = fmaf(x[e], cs[e].x, y[e] * (second ? cs[e].y : -cs[e].y));
-  } else {
-    load_turn<false>(tr, a.rt.rot, ch, cs);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float u = x[2 * e], v = x[2 * e + 1];
-      x[2 * e] = u * cs[e].x - v * cs[e].y;
-      x[2 * e + 1] = u * cs[e].y + v * cs[e].x;
-    }
-  }
-}
-
-// 2^-e for the largest magnitude m of a row, e its exponent: the row times it is below 2 and becomes fp16 without losing range
+// The chunks of eight channels ch(0) .. ch(N - 1) of a query row as fp16 relative to the row's largest magnitude (2^-e, e its
+// exponent, so that no range is lost), rotated by its position `pos` in fp32 when there is a table (a position outside it,
+// which sees nothing, as if at its border).  `most` takes the largest magnitude of the lane to that of the row.  The row's
+// factor comes back.  Loads stand in front and under no branch that lanes could take apart: a row costs two rounds of them.
 __device__ __forceinline__ float row_down(float m) {
   const int e = min(max((int)(__float_as_uint(m) >> 23), 1), 253);
   return __uint_as_float((uint32_t)(254 - e) << 23);
+}
+template <int N, bool F16, class Ch, class Most>
+__device__ __forceinline__ float load_query(const PagedAttnArgs& a, const uint16_t* row, bool ok, int pos, int cap, f16x8* q, Ch ch,
+                                            Most most) {
+  uint4 raw[N], par[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) raw[k] = reinterpret_cast<const uint4*>(row)[ch(k)];
+  float v[N][8];
+  if (!a.rt.table) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) unpack8<F16>(raw[k], v[k]);
+  } else {
+    const float* tr = a.rt.table + (int64_t)min(max(pos, 0), cap - 1) * a.rt.rot;
+    const int half = a.rt.rot / 16;                          // chunks of half the rotated part
+    if (a.rt.layout == FL_ROPE_HALF) {
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        const int c = ch(k);
+        par[k] = reinterpret_cast<const uint4*>(row)[c < half ? c + half : c < 2 * half ? c - half : c];
+      }
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        const int c = ch(k);
+        const bool turn = c < 2 * half;
+        const float sign = c < half ? -1.0f : 1.0f;
+        const float4* p = reinterpret_cast<const float4*>(tr + 16 * (turn ? (c < half ? c : c - half) : 0));
+        float y[8];
+        unpack8<F16>(raw[k], v[k]);
+        unpack8<F16>(par[k], y);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float4 w = p[e];
+          const float r0 = fmaf(v[k][2 * e], w.x, y[2 * e] * (sign * w.y)), r1 = fmaf(v[k][2 * e + 1], w.z, y[2 * e + 1] * (sign * w.w));
+          v[k][2 * e] = turn ? r0 : v[k][2 * e];
+          v[k][2 * e + 1] = turn ? r1 : v[k][2 * e + 1];
+        }
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        const int c = ch(k);
+        const bool turn = c < 2 * half;
+        const float4* p = reinterpret_cast<const float4*>(tr + 8 * (turn ? c : 0));
+        unpack8<F16>(raw[k], v[k]);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float4 w = p[e];
+          float* x = v[k] + 4 * e;
+          const float r0 = x[0] * w.x - x[1] * w.y, r1 = x[0] * w.y + x[1] * w.x;
+          const float r2 = x[2] * w.z - x[3] * w.w, r3 = x[2] * w.w + x[3] * w.z;
+          x[0] = turn ? r0 : x[0];
+          x[1] = turn ? r1 : x[1];
+          x[2] = turn ? r2 : x[2];
+          x[3] = turn ? r3 : x[3];
+        }
+      }
+    }
+  }
+  float top = 0.0f;
+#pragma unroll
+  for (int k = 0; k < N; ++k)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[k][e]));
+  const float down = row_down(most(top));
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    u32x4 w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = ok ? pack_f16x2(v[k][2 * e] * down, v[k][2 * e + 1] * down) : 0u;
+    q[k] = __builtin_bit_cast(f16x8, w);
+  }
+  return a.scale_log2 / down;
 }
 
 // Four codes of one word as two fp16 pairs (exact).  Int8: c + 128 under the exponent of 1024, less 1152.
@@ -203,7 +254,25 @@ __device__ __forceinline__ ValueScale value_scale(float s) {
   return {__builtin_amdgcn_logf(s), 1.0f / s};
 }
 
-int launch_paged_merge(const PagedAttnArgs& a, int d, int rows_per_tile, int keys_per_tile, bool f16, hipStream_t st);
-int launch_paged_prompt(const PagedAttnArgs& a, int d, int format, bool f16, hipStream_t st);
+// The work of a head, row tile after row tile, cut into shares of `per`: unit x belongs to workgroup owner(x).  A row tile is
+// kTileUnits for its queries and what stands before its first product, then one unit a stage (at least one, so that the rows of a
+// tile that sees no key are written).
+constexpr int kTileUnits = 6;
+struct Cut {
+  int total, per;
+  __device__ __forceinline__ int begin(int p) const { return (int)min((int64_t)total, (int64_t)per * p); }
+  __device__ __forceinline__ int owner(int x) const { return x / per; }
+};
+constexpr int kLeastUnits = 24;    // of a share
+__device__ __forceinline__ Cut cut_of(const PagedAttnArgs& a) {
+  const int total = __builtin_amdgcn_readfirstlane(a.ends[a.slots - 1]);
+  return {total, __builtin_amdgcn_readfirstlane(max(kLeastUnits, (total + a.share - 1) / a.share))};
+}
+
+// many rows
+constexpr int kPromptRows = 128, kPromptKeys = 64;
+constexpr int kPromptShares = 512;         // two workgroups per CU
+size_t paged_prompt_ws(int64_t slots, int Hkv, int d, int64_t cap, int64_t keys);
+int launch_paged_prompt(const PagedAttnArgs& a, int d, int format, bool f16, int64_t keys, hipStream_t st);
 
 }  // namespace fl

@@ -89,22 +89,9 @@ __global__ __launch_bounds__(256, NR == 1 ? 4 : 2) void paged_token_kernel(Paged
     const int t = rho / G, pos = sp.start + t;
     const uint16_t* src = a.q + (int64_t)(sp.r0 + t) * a.qs + (int64_t)(kvh * G + rho % G) * D;
     const int cap = a.bt.max_pages * a.pg.size;
-    float v[KS][8], top = 0.0f;
-#pragma unroll
-    for (int k = 0; k < KS; ++k) {
-      load_q8<F16>(a, src, min(pos, cap - 1), 8 * (k / 2) + 2 * g4 + k % 2, v[k]);   // (the order in which keys lie in the lanes)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[k][e]));
-    }
-    const float down = row_down(row4_max(top));
-    mul[x] = a.scale_log2 / down;
-#pragma unroll
-    for (int k = 0; k < KS; ++k) {
-      u32x4 w;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) w[e] = ok ? pack_f16x2(v[k][2 * e] * down, v[k][2 * e + 1] * down) : 0u;
-      qf[x][k] = __builtin_bit_cast(f16x8, w);
-    }
+    // (the order in which keys lie in the lanes)
+    mul[x] = load_query<KS, F16>(a, src, ok, pos, cap, qf[x], [g4](int k) { return 8 * (k / 2) + 2 * g4 + k % 2; },
+                                 [](float m) { return row4_max(m); });
     jmax[x] = ok ? min(pos, cap - 1) : -1;
     jmin[x] = a.window > 0 && pos >= a.window ? pos - a.window + 1 : 0;
   }
@@ -207,7 +194,7 @@ __global__ __launch_bounds__(256, NR == 1 ? 4 : 2) void paged_token_kernel(Paged
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int j = key0 + 16 * h + 4 * g4 + i;
-            see[h][i] = j <= jmax[x] && (j >= jmin[x] || j < a.n_sink) && (h ? pid1 : pid0) >= 0;
+            see[h][i] = (j <= jmax[x]) & ((j >= jmin[x]) | (j < a.n_sink)) & ((h ? pid1 : pid0) >= 0);
             y[h][i] = see[h][i] ? y[h][i] : -INFINITY;
           }
         }
@@ -348,7 +335,7 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
   const Seq sq = find_seq(a.bt, t, 0, [](int c) { return c; });
   if (sq.b < 0 || t >= sq.r1) return;
   Span sp = span_of<R, KT>(a, sq, ((t - sq.r0) * a.G + h % a.G) / R);
-  if constexpr (KT == kTokenKeys) cut(sp, Shares<R, KT>(a).parts(sq.r1 - sq.r0, sq.len));
+  cut(sp, Shares<R, KT>(a).parts(sq.r1 - sq.r0, sq.len));
   if (sp.parts <= 1) return;
   const int64_t gr = blockIdx.x;
   float2 w = make_float2(-INFINITY, 0.0f);
@@ -408,12 +395,6 @@ static int launch_merge(const PagedAttnArgs& a, int d, bool f16, hipStream_t st)
   return check_launch("paged_merge_kernel");
 }
 
-int launch_paged_merge(const PagedAttnArgs& a, int d, int rows_per_tile, int keys_per_tile, bool f16, hipStream_t st) {
-  if (rows_per_tile == 16) return launch_merge<16, 32>(a, d, f16, st);
-  if (rows_per_tile == 32) return launch_merge<32, 32>(a, d, f16, st);
-  return launch_merge<128, 64>(a, d, f16, st);
-}
-
 template <int NR>
 static int launch_token(const PagedAttnArgs& a, int d, int format, bool f16, hipStream_t st) {
   // row tiles, and with split keys as many parts more as the tiles are shared out to
@@ -436,13 +417,14 @@ static int launch_token(const PagedAttnArgs& a, int d, int format, bool f16, hip
 #undef FL_TOKEN
   int rc = check_launch("paged_token_kernel");
   if (rc != FL_OK || a.n_split == 1) return rc;
-  return launch_paged_merge(a, d, 16 * NR, kTokenKeys, f16, st);
+  return launch_merge<16 * NR, kTokenKeys>(a, d, f16, st);
 }
 
 // How a call is cut: rows per tile and parts of the keys.
 constexpr int kShare = 768, kLeastTiles = 8;
 struct Plan {
   int rows, n_split, min_tiles, share;
+  int64_t keys;                   // that a row sees at most, as far as the caller knows
   size_t ws;
 };
 static Plan plan_of(int B, int T, int Hq, int Hkv, int d, int page, int max_pages, int window, int n_sink, int max_q, int max_len) {
@@ -453,19 +435,17 @@ static Plan plan_of(int B, int T, int Hq, int Hkv, int d, int page, int max_page
   const int64_t cap = (int64_t)max_pages * page;
   int64_t len = max_len > 0 ? std::min<int64_t>(max_len, cap) : cap;
   if (window > 0) len = std::min<int64_t>(len, (int64_t)window + n_sink + std::max(max_q, 1));
-  const int keys = p.rows == 128 ? 64 : kTokenKeys;
-  const int64_t tiles = std::max<int64_t>(1, (len + keys - 1) / keys);
-  const int64_t units = std::max<int64_t>(1, std::max<int64_t>(B, T * G / p.rows)) * Hkv;
-  int64_t split;
+  p.n_split = p.min_tiles = 1;
+  p.keys = len;
   if (p.rows == 128) {
-    split = std::min<int64_t>(512 / units, tiles / 8);
-    split = std::min<int64_t>(std::max<int64_t>(split, 1), kMaxSplit);
-    p.min_tiles = (int)((tiles + split - 1) / split);
-  } else {
-    p.share = kShare;
-    p.min_tiles = kLeastTiles;
-    split = units < kShare ? std::min<int64_t>(std::max<int64_t>(tiles / kLeastTiles, 1), kMaxSplit) : 1;
+    p.ws = paged_prompt_ws((int64_t)T * G / kPromptRows + B, Hkv, d, cap, len);
+    return p;
   }
+  const int64_t tiles = std::max<int64_t>(1, (len + kTokenKeys - 1) / kTokenKeys);
+  const int64_t units = std::max<int64_t>(1, std::max<int64_t>(B, T * G / p.rows)) * Hkv;
+  p.share = kShare;
+  p.min_tiles = kLeastTiles;
+  const int64_t split = units < kShare ? std::min<int64_t>(std::max<int64_t>(tiles / kLeastTiles, 1), kMaxSplit) : 1;
   p.n_split = (int)split;
   p.ws = split > 1 ? (size_t)T * Hq * split * (d + 2) * sizeof(float) : 0;
   return p;
@@ -525,6 +505,6 @@ extern "C" int fl_paged_attn(const void* q, int64_t q_stride, int dtype, const i
   if (rc != FL_OK) return rc;
   if (p.rows == 16) return launch_token<1>(a, d, format, dtype == FL_F16, st);
   if (p.rows == 32) return launch_token<2>(a, d, format, dtype == FL_F16, st);
-  return launch_paged_prompt(a, d, format, dtype == FL_F16, st);
+  return launch_paged_prompt(a, d, format, dtype == FL_F16, p.keys, st);
   FL_API_END
 }

@@ -7,11 +7,72 @@
 //   O^T += V^T P^T  the same product, V read transposed (ds_read_b64_tr_b16), P rounded to fp16.
 // Scales never touch the codes: a key scale multiplies its 16 scores inside the exponent's fma, a value scale enters as its
 // logarithm there and leaves the row sum as its reciprocal, once per 16 keys.
+//
+// One workgroup for each row tile and head, the longest first, from two rounds of them on.  Fewer leave the chip idle, so there
+// workgroups have equal shares of the work, whatever the lengths are: a first small kernel adds up the units of all row tiles,
+// each of the 512 / Hkv workgroups of a key/value head takes an equal run of them, and row tiles that a border cuts are joined at
+// the end from the sides' sums.  (1024 positions after 16000, 16 heads: 523 us without shares, 233 with; a whole prompt of 8192,
+// 1040 workgroups: 446 without, 491 with.)
 #include "fl_paged_attn.h"
+
+#include <algorithm>
 
 namespace fl {
 
-constexpr int kPromptRows = 128, kPromptKeys = 64;
+// ends[s]: units of row tiles 0 .. s
+__global__ __launch_bounds__(1024) void paged_plan_kernel(PagedAttnArgs a) {
+  __shared__ int s_sum[16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int before = 0;
+  for (int s0 = 0; s0 < a.slots; s0 += 1024) {
+    const int slot = s0 + threadIdx.x;
+    int n = 0;
+    if (slot < a.slots) {
+      int lo = 0, hi = a.bt.B;                                // the last sequence whose first slot is at most this one
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (row_of(a.bt, mid) * a.G / kPromptRows + mid <= slot) lo = mid;
+        else hi = mid;
+      }
+      const Seq q{lo, row_of(a.bt, lo), row_of(a.bt, lo + 1), a.bt.lens[lo]};
+      const Span sp = span_of<kPromptRows, kPromptKeys>(a, q, slot - (q.r0 * a.G / kPromptRows + lo));
+      n = sp.rows > 0 ? kTileUnits + max(sp.tiles, 1) : 0;
+    }
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const int x = __shfl_up(n, off, 64);
+      n += lane >= off ? x : 0;
+    }
+    if (lane == 63) s_sum[wave] = n;
+    __syncthreads();
+    int all = 0;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) {
+      if (w < wave) n += s_sum[w];
+      all += s_sum[w];
+    }
+    if (slot < a.slots) a.ends[slot] = before + n;
+    before += all;
+    __syncthreads();
+  }
+}
+
+// first row tile whose end is beyond unit x (the wave looks at 64 places at a time)
+__device__ __forceinline__ int tile_of_unit(const int* ends, int slots, int x) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, n = slots;
+  while (n > 1) {
+    const int step = (n + 63) / 64;
+    const int at = min(lo + (lane + 1) * step, lo + n) - 1;
+    const uint64_t m = __builtin_amdgcn_ballot_w64(ends[at] > x);
+    const int l = m ? __builtin_ctzll(m) : 63;
+    const int next = min(lo + l * step, lo + n - 1);
+    n = min(step, lo + n - next);
+    lo = next;
+  }
+  return lo;
+}
+
 constexpr int kAhead = 32;                 // stages whose pages and scales are in LDS at a time
 
 template <int D>
@@ -20,7 +81,7 @@ struct __attribute__((aligned(16))) PromptSlot {
   uint16_t v[kPromptKeys * D];
 };
 
-template <int D, bool I8, bool F16>
+template <int D, bool I8, bool F16, bool SHARED>
 __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttnArgs a) {
   constexpr int R = kPromptRows, COLS = kPromptKeys;
   constexpr int NBK = COLS / 32;           // 32-key blocks
@@ -33,17 +94,43 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttnArgs a) {
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int hw = lane >> 5, r32 = lane & 31;
-  const int kvh = blockIdx.x % a.pg.heads;
-  const int rest = blockIdx.x / a.pg.heads;
-  const int n_slots = gridDim.x / (a.pg.heads * a.n_split);
-  const int split = rest % a.n_split, slot = n_slots - 1 - rest / a.n_split;     // (later rows see more keys: first)
+  const int kvh = blockIdx.x % a.pg.heads, wg = blockIdx.x / a.pg.heads;
   const int G = a.G;
+  // the workgroup's run of units at .. end - 1 of its head, from row tile `slot` on; or all of one row tile
+  int at = 0, end = 1, slot = gridDim.x / a.pg.heads - 1 - wg;          // (later rows see more keys: first)
+  if constexpr (SHARED) {
+    const Cut cut = cut_of(a);
+    at = cut.begin(wg);
+    end = cut.begin(wg + 1);
+    if (at >= end) return;
+    slot = tile_of_unit(a.ends, a.slots, at);
+  }
+  const int first = at;
+  for (; at < end; ++slot) {
   const Seq sq = find_seq(a.bt, slot, 1, [G](int c) { return c * G / R; });
   const int b = sq.b;
   if (b < 0) return;
   const Span sp = span_of<R, COLS>(a, sq, slot - (sq.r0 * G / R + b));
-  if (sp.rows == 0 || split >= sp.parts) return;
-  const int t0 = split * sp.per, n = max(min(sp.per, sp.tiles - t0), 0);         // its stages
+  if (sp.rows == 0) {
+    if constexpr (SHARED) continue;
+    return;
+  }
+  // its stages t0 .. t0 + n - 1 of the row tile; `whole`: these are all
+  int t0 = 0, n = sp.tiles;
+  bool whole = true;
+  int place = 0;
+  if constexpr (SHARED) {
+    const int tile_end = __builtin_amdgcn_readfirstlane(a.ends[slot]), units = max(sp.tiles, 1), unit0 = tile_end - units;
+    t0 = max(at - unit0, 0);
+    const int t1 = min(end - unit0, units);
+    place = unit0 + t0 == first ? 0 : 1;                     // of the two row tiles that a share may cut
+    at = min(tile_end, end);
+    if (t0 >= t1) continue;                                  // (the tile's stages are the next share's)
+    whole = t0 == 0 && t1 == units;
+    n = min(t1, sp.tiles) - t0;
+  } else {
+    at = end;
+  }
 
   const int cap = a.bt.max_pages * a.pg.size;
   const int rr = 32 * wave + r32;
@@ -60,31 +147,9 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttnArgs a) {
   const int jmax = row_ok ? min(pos, cap - 1) : -1;
   const int jmin = a.window > 0 && pos >= a.window ? pos - a.window + 1 : 0;
 
-  f16x8 qf[KS];
-  float mul;
-  {
-    const uint16_t* src = a.q + (int64_t)(sp.r0 + tok) * a.qs + (int64_t)head * D;
-    float v[KS][8], top = 0.0f;
-#pragma unroll
-    for (int k = 0; k < KS; ++k) {
-      load_q8<F16>(a, src, min(pos, cap - 1), 2 * k + hw, v[k]);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[k][e]));
-    }
-    const float down = row_down(xor32_max(top));
-    mul = a.scale_log2 / down;
-#pragma unroll
-    for (int k = 0; k < KS; ++k) {
-      u32x4 w;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) w[e] = row_ok ? pack_f16x2(v[k][2 * e] * down, v[k][2 * e + 1] * down) : 0u;
-      qf[k] = __builtin_bit_cast(f16x8, w);
-    }
-  }
-
-  // pages and scales of stages [first, first + kAhead): thread x < 128 has 16 keys
-  auto page_of = [&](int first) {
-    const int st = t0 + first + (threadIdx.x >> 2);
+  // pages and scales of stages [from, from + kAhead): thread x < 128 has 16 keys
+  auto page_of = [&](int from) {
+    const int st = t0 + from + (threadIdx.x >> 2);
     int p = -1;
     if (threadIdx.x < 4 * kAhead && st < t0 + n) {
       const int page = (key_of<COLS>(sp, st) + (threadIdx.x & 3) * 16) >> a.pg.log2;
@@ -103,6 +168,15 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttnArgs a) {
     return make_float4(ks, vs.log2, vs.inv, __int_as_float(p));
   };
 
+  const int page0 = page_of(0);                                       // (asked for before the queries)
+  f16x8 qf[KS];
+  float mul;
+  {
+    const uint16_t* src = a.q + (int64_t)(sp.r0 + tok) * a.qs + (int64_t)head * D;
+    mul = load_query<KS, F16>(a, src, row_ok, pos, cap, qf, [hw](int k) { return 2 * k + hw; },
+                              [](float m) { return xor32_max(m); });
+  }
+
   // loads: x of the wave covers keys of one 16-key group; a lane has 16 channels of a key
   typedef uint32_t v4u __attribute__((ext_vector_type(4)));
   v4u kw[NI], vw[NI];
@@ -118,13 +192,18 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttnArgs a) {
       const uint32_t at = (uint32_t)((key & 15) * D + lane_ch * 16);
       kw[x] = *reinterpret_cast<const v4u*>(a.kc + base + at);
       vw[x] = *reinterpret_cast<const v4u*>(a.vc + base + at);
-      if (!I8 && (p < 0 || key0 + key > sp.i_max)) vw[x] = v4u{};    // codes behind the end may be NaN
     }
   };
-  auto store = [&](PromptSlot<D>& sl) __attribute__((always_inline)) {
+  auto store = [&](PromptSlot<D>& sl, int st) __attribute__((always_inline)) {
 #pragma unroll
     for (int x = 0; x < NI; ++x) {
       const int key = x * (256 / LPK) + lane_key;
+      if constexpr (!I8) {                                            // codes behind the end may be NaN
+        const float gone = s_page[(st / kAhead) & 1][(st % kAhead) * 4 + (key >> 4)].w;
+        const bool there = (__float_as_int(gone) >= 0) & (key_of<COLS>(sp, t0 + st) + key <= sp.i_max);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) vw[x][e] = there ? vw[x][e] : 0u;
+      }
       const int g = swz32_f<D>(key & 31);
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
@@ -189,16 +268,16 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttnArgs a) {
     const bool holes = __builtin_amdgcn_readfirstlane(gone) < 0;
     if (key0 + COLS - 1 > w_min || (key0 < w_all && key0 + COLS > a.n_sink) || holes) {    // uniform
 #pragma unroll
-      for (int x = 0; x < NBK; ++x) {
+      for (int g = 0; g < 2 * NBK; ++g) {
+        const int most = __float_as_int(pages[g].w) < 0 ? -1 : jmax;
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          const int j = key0 + 32 * x + 8 * (v >> 2) + 4 * hw + (v & 3);
-          const bool see = j <= jmax && (j >= jmin || j < a.n_sink) && (!holes || __float_as_int(pages[2 * x + (v >> 3)].w) >= 0);
-          s[x][v] = see ? s[x][v] * mg[2 * x + (v >> 3)] : -INFINITY;
+        for (int v = 8 * (g & 1); v < 8 * (g & 1) + 8; ++v) {
+          const int j = key0 + 32 * (g >> 1) + 8 * (v >> 2) + 4 * hw + (v & 3);
+          const bool see = (j <= most) & ((j >= jmin) | (j < a.n_sink));
+          s[g >> 1][v] = see ? s[g >> 1][v] * mg[g] : -INFINITY;
         }
+        mg[g] = 1.0f;
       }
-#pragma unroll
-      for (int g = 0; g < 2 * NBK; ++g) mg[g] = 1.0f;
     }
     float top = -INFINITY;
 #pragma unroll
@@ -262,10 +341,11 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttnArgs a) {
   };
 
   if (n > 0) {
-    if (threadIdx.x < 4 * kAhead) s_page[0][threadIdx.x] = scales_of(page_of(0));
+    if constexpr (SHARED) __syncthreads();                                      // (the last row tile's stages are read)
+    if (threadIdx.x < 4 * kAhead) s_page[0][threadIdx.x] = scales_of(page0);
     __syncthreads();
     fetch(0);
-    store(s0);
+    store(s0, 0);
     __syncthreads();
     int ahead = -1;                                                   // page of the next block's 16 keys
     float4 ahead_s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -276,7 +356,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttnArgs a) {
       if (ph == 16 && threadIdx.x < 4 * kAhead) s_page[((st / kAhead) & 1) ^ 1][threadIdx.x] = ahead_s;
       if (st + 1 < n) fetch(st + 1);
       compute(cur, st);
-      if (st + 1 < n) store(nxt);
+      if (st + 1 < n) store(nxt, st + 1);
       __syncthreads();
     };
     for (int st = 0; st < n; st += 2) {
@@ -285,20 +365,21 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttnArgs a) {
     }
   }
   lsum = xor32_add(lsum);
-  if (!row_ok) return;
   const int64_t gr = (int64_t)(sp.r0 + tok) * a.Hq + head;
   const bool none = ref == -INFINITY && lsum == 0.0f;
-  if (sp.parts > 1) {
-    float* out = a.part + (gr * a.n_split + split) * D + 4 * hw;
+  if (SHARED && row_ok && !whole) {
+    // a share cuts at most two row tiles: the one it begins with and the one it ends with
+    const int64_t row = ((int64_t)(kvh * a.share + wg) * 2 + place) * R + rr;
+    float* out = a.part + row * D + 4 * hw;
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
       for (int j = 0; j < 4; ++j)
         *reinterpret_cast<float4*>(out + db * 32 + 8 * j) =
             make_float4(acc[db][4 * j], acc[db][4 * j + 1], acc[db][4 * j + 2], acc[db][4 * j + 3]);
-    if (hw == 0) *reinterpret_cast<float2*>(a.part_ml + (gr * a.n_split + split) * 2) = make_float2(ref, lsum);
-    return;
+    if (hw == 0) *reinterpret_cast<float2*>(a.part_ml + row * 2) = make_float2(ref, lsum);
   }
+  if (row_ok && whole) {
   const float inv = none ? 0.0f : 1.0f / lsum;
   uint16_t* out = a.o + (int64_t)(sp.r0 + tok) * a.os + (int64_t)head * D + 4 * hw;
 #pragma unroll
@@ -312,29 +393,111 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttnArgs a) {
                                                                F16 ? pack_f16x2(o[2], o[3]) : pack_bf16x2(o[2], o[3])};
     }
   if (hw == 0 && a.lse) a.lse[gr] = none ? -INFINITY : (ref + __builtin_amdgcn_logf(lsum)) * 0.6931471805599453f;
+ }
+  }
 }
 
-int launch_paged_prompt(const PagedAttnArgs& a, int d, int format, bool f16, hipStream_t st) {
+// Row tiles that shares cut: a workgroup has 32 rows of one, d / 4 threads a row.
+template <int D, bool F16>
+__global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a) {
+  constexpr int R = kPromptRows, LN = D / 4;
+  const int kvh = blockIdx.x % a.pg.heads, rest = blockIdx.x / a.pg.heads;
+  const int slot = rest / 4, r0 = (rest % 4) * 32;
+  const Cut cut = cut_of(a);
+  const int before = slot > 0 ? a.ends[slot - 1] : 0, end = a.ends[slot];
+  if (before >= end) return;
+  const int begin = before + kTileUnits;                     // its first stage
+  const int p0 = cut.owner(begin), p1 = cut.owner(end - 1);
+  if (p0 == p1) return;
+  const int G = a.G;
+  const Seq sq = find_seq(a.bt, slot, 1, [G](int c) { return c * G / R; });
+  if (sq.b < 0) return;
+  const Span sp = span_of<R, kPromptKeys>(a, sq, slot - (sq.r0 * G / R + sq.b));
+  const int c = threadIdx.x % LN;
+  for (int rr = r0 + threadIdx.x / LN; rr < min(r0 + 32, sp.rows); rr += 256 / LN) {
+    auto place = [&](int p) { return ((int64_t)(kvh * a.share + p) * 2 + (max(begin, cut.begin(p)) == cut.begin(p) ? 0 : 1)) * R + rr; };
+    float m = -INFINITY;
+    for (int p = p0; p <= p1; ++p) m = fmaxf(m, a.part_ml[place(p) * 2]);
+    float sum = 0.0f;
+    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int p = p0; p <= p1; ++p) {
+      const int64_t at = place(p);
+      const float2 w = *reinterpret_cast<const float2*>(a.part_ml + at * 2);
+      const float4 x = *reinterpret_cast<const float4*>(a.part + at * D + 4 * c);
+      const float f = w.x == -INFINITY && w.y == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(w.x - m);
+      sum = fmaf(f, w.y, sum);
+      o.x = fmaf(f, x.x, o.x);
+      o.y = fmaf(f, x.y, o.y);
+      o.z = fmaf(f, x.z, o.z);
+      o.w = fmaf(f, x.w, o.w);
+    }
+    const bool none = m == -INFINITY && sum == 0.0f;
+    const float inv = none ? 0.0f : 1.0f / sum;
+    const int rho = sp.rho0 + rr, tok = rho / G, head = kvh * G + rho % G;
+    *reinterpret_cast<u32x2*>(a.o + (int64_t)(sp.r0 + tok) * a.os + (int64_t)head * D + 4 * c) =
+        u32x2{F16 ? pack_f16x2(o.x * inv, o.y * inv) : pack_bf16x2(o.x * inv, o.y * inv),
+              F16 ? pack_f16x2(o.z * inv, o.w * inv) : pack_bf16x2(o.z * inv, o.w * inv)};
+    if (a.lse && c == 0)
+      a.lse[(int64_t)(sp.r0 + tok) * a.Hq + head] = none ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+  }
+}
+
+// Sums of cut row tiles, two for each share, and the ends of the row tiles.  No key is split where every row tile has a workgroup
+// of its own.
+static int shares_of(int Hkv) { return std::max(1, kPromptShares / Hkv); }
+// (keys: that a row sees at most; below 1024 the two kernels more cost more than idle CUs.  cap: positions of a block table's row;
+// all units of a head count below 2^31)
+static bool is_shared(int64_t slots, int Hkv, int64_t cap, int64_t keys) {
+  return slots * Hkv < 2 * kPromptShares && keys >= 1024 && slots * (cap / kPromptKeys + 16) < (1ll << 31) - 65536;
+}
+size_t paged_prompt_ws(int64_t slots, int Hkv, int d, int64_t cap, int64_t keys) {
+  if (!is_shared(slots, Hkv, cap, keys)) return 0;
+  return (size_t)shares_of(Hkv) * Hkv * 2 * kPromptRows * (d + 2) * sizeof(float) + (size_t)slots * sizeof(int);
+}
+
+int launch_paged_prompt(const PagedAttnArgs& args, int d, int format, bool f16, int64_t keys, hipStream_t st) {
+  PagedAttnArgs a = args;
   const int64_t slots = (int64_t)a.bt.T * a.G / kPromptRows + a.bt.B;
-  const int64_t n = slots * a.n_split * a.pg.heads;
-  FL_REQUIRE(n < (1ll << 31), FL_E_SHAPE, "fl_paged_attn: too many rows");
-  const unsigned grid = (unsigned)n;
-#define FL_PROMPT(DD)                                                                  \
+  const bool shared = is_shared(slots, a.pg.heads, (int64_t)a.bt.max_pages * a.pg.size, keys);
+  FL_REQUIRE(slots * a.pg.heads * 4 < (1ll << 31), FL_E_SHAPE, "fl_paged_attn: too many rows");
+  a.slots = (int)slots;
+  a.share = shares_of(a.pg.heads);
+  int rc;
+  if (shared) {
+    const size_t places = (size_t)a.share * a.pg.heads * 2 * kPromptRows;
+    a.part_ml = a.part + places * d;
+    a.ends = reinterpret_cast<int*>(a.part_ml + places * 2);
+    paged_plan_kernel<<<1, 1024, 0, st>>>(a);
+    rc = check_launch("paged_plan_kernel");
+    if (rc != FL_OK) return rc;
+  }
+  const unsigned grid = (unsigned)((shared ? a.share : slots) * a.pg.heads);
+#define FL_PROMPT(DD, SS)                                                              \
   do {                                                                                 \
     if (format == FL_KV_I8) {                                                          \
-      if (f16) paged_prompt_kernel<DD, true, true><<<grid, 256, 0, st>>>(a);           \
-      else paged_prompt_kernel<DD, true, false><<<grid, 256, 0, st>>>(a);              \
+      if (f16) paged_prompt_kernel<DD, true, true, SS><<<grid, 256, 0, st>>>(a);       \
+      else paged_prompt_kernel<DD, true, false, SS><<<grid, 256, 0, st>>>(a);          \
     } else {                                                                           \
-      if (f16) paged_prompt_kernel<DD, false, true><<<grid, 256, 0, st>>>(a);          \
-      else paged_prompt_kernel<DD, false, false><<<grid, 256, 0, st>>>(a);             \
+      if (f16) paged_prompt_kernel<DD, false, true, SS><<<grid, 256, 0, st>>>(a);      \
+      else paged_prompt_kernel<DD, false, false, SS><<<grid, 256, 0, st>>>(a);         \
     }                                                                                  \
   } while (0)
-  if (d == 128) FL_PROMPT(128);
-  else FL_PROMPT(64);
+  if (d == 128 && shared) FL_PROMPT(128, true);
+  else if (d == 128) FL_PROMPT(128, false);
+  else if (shared) FL_PROMPT(64, true);
+  else FL_PROMPT(64, false);
 #undef FL_PROMPT
-  const int rc = check_launch("paged_prompt_kernel");
-  if (rc != FL_OK || a.n_split == 1) return rc;
-  return launch_paged_merge(a, d, kPromptRows, kPromptKeys, f16, st);
+  rc = check_launch("paged_prompt_kernel");
+  if (rc != FL_OK || !shared) return rc;
+  const unsigned join = (unsigned)(slots * 4 * a.pg.heads);
+  if (d == 128) {
+    if (f16) paged_join_kernel<128, true><<<join, 256, 0, st>>>(a);
+    else paged_join_kernel<128, false><<<join, 256, 0, st>>>(a);
+  } else {
+    if (f16) paged_join_kernel<64, true><<<join, 256, 0, st>>>(a);
+    else paged_join_kernel<64, false><<<join, 256, 0, st>>>(a);
+  }
+  return check_launch("paged_join_kernel");
 }
 
 }  // namespace fl
