@@ -602,30 +602,38 @@ _DTYPES = {torch.bfloat16: 0, torch.float16: 1}
 _FORMATS = {torch.int8: 0, torch.float8_e4m3fn: 1}
 
 
-def _here(dev):
-    """The calls below launch on the current device's stream: their tensors have to be there."""
-    if dev.type != "cuda":
-        raise FlashLoopError("tensors must be on the device")
-    if dev.index != torch.cuda.current_device():
-        raise FlashLoopError(f"tensors on {dev}, but the current device is cuda:{torch.cuda.current_device()}")
-    return dev
+# (As above, a tensor that passes its checks passes them in one expression: a call's host time is that of its launch.)
+if hasattr(torch._C, "_cuda_getDevice"):
+    _current = torch._C._cuda_getDevice
+else:
+    _current = torch.cuda.current_device
 
 
-def _on(t, dev, dtype, name, shape=None):
-    if t is None or (t.dtype is dtype and t.device == dev and t.is_contiguous() and (shape is None or t.shape == shape)):
+def _here(t, name):
+    """The device number of t: the calls below launch on the current device's stream, so their tensors have to be there."""
+    if not t.is_cuda:
+        raise FlashLoopError(f"{name} must be a device tensor")
+    at = t.get_device()
+    if at != _current():
+        raise FlashLoopError(f"{name} is on cuda:{at}, but the current device is cuda:{_current()}")
+    return at
+
+
+def _on(t, at, dtype, name, shape=None):
+    if t is None or (t.dtype is dtype and t.get_device() == at and t.is_contiguous() and (shape is None or t.shape == shape)):
         return
     _dev(t, dtype, name, shape)
-    raise FlashLoopError(f"{name} is on {t.device}, the call's other tensors on {dev}")
+    raise FlashLoopError(f"{name} is on {t.device}, the call's other tensors on cuda:{at}")
 
 
-def _rows(t, dev, dtype, name, shape=None):
+def _rows(t, at, dtype, name, shape=None):
     """Elements between the rows of [T, H, d], whose heads are dense."""
     if t.dim() != 3 or (shape is not None and t.shape != shape):
         raise FlashLoopError(f"{name} must have shape {'[T, H, d]' if shape is None else tuple(shape)}, got {tuple(t.shape)}")
     if t.dtype is not dtype or dtype not in _DTYPES:
         raise FlashLoopError(f"{name} must be {dtype if dtype in _DTYPES else 'bfloat16 or float16'}, got {t.dtype}")
-    if t.device != dev:
-        raise FlashLoopError(f"{name} is on {t.device}, the call's other tensors on {dev}")
+    if t.get_device() != at:
+        raise FlashLoopError(f"{name} is on {t.device}, the call's other tensors on cuda:{at}")
     T, H, d = t.shape
     row, head, one = t.stride()
     if (one != 1 and d > 1) or (head != d and H > 1):
@@ -639,14 +647,15 @@ def _choice(value, of, name):
     return of[value]
 
 
-def _turns(table, dev):
+def _turns(table, at):
     """(n_pos, rot) of a rotary table, (0, 0) without one."""
     if table is None:
         return 0, 0
-    _on(table, dev, torch.float32, "table")
+    _on(table, at, torch.float32, "table")
     if table.dim() != 3 or table.shape[2] != 2:
         raise FlashLoopError(f"table must have shape [n_pos, rot / 2, 2], got {tuple(table.shape)}")
-    return table.shape[0], 2 * table.shape[1]
+    n_pos, half, _ = table.shape
+    return n_pos, 2 * half
 
 
 def rope_table(n_pos, rot, base=10000.0, scaling="none", factor=1.0, orig_len=0, low=1.0, high=32.0, out=None, device=None):
@@ -656,10 +665,10 @@ def rope_table(n_pos, rot, base=10000.0, scaling="none", factor=1.0, orig_len=0,
     1 + 0.1 ln(factor)).  On `device` (out's, or the current one)."""
     how = _choice(scaling, ROPE_SCALING, "scaling")
     if out is None:
-        dev = _here(torch.device("cuda", torch.cuda.current_device()) if device is None else torch.empty(0, device=device).device)
-        out = torch.empty(n_pos, rot // 2, 2, dtype=torch.float32, device=dev)
+        out = torch.empty(n_pos, rot // 2, 2, dtype=torch.float32, device="cuda" if device is None else device)
+        _here(out, "device")
     else:
-        _on(out, _here(out.device), torch.float32, "out", (n_pos, rot // 2, 2))
+        _on(out, _here(out, "out"), torch.float32, "out", (n_pos, rot // 2, 2))
     rc = load().fl_rope_table(n_pos, rot, base, how, factor, orig_len, low, high, _p(out), _stream())
     _check(rc, "fl_rope_table")
     return out
@@ -669,39 +678,43 @@ def rope(x, table, pos=None, layout="half", inverse=False, out=None):
     """The rows of x (bf16 or fp16 [T, H, d], any row stride that is a multiple of 8) with their heads' first rot channels
     turned by the positions pos (int32 [T]; None: 0 .. T-1).  inverse=True turns back: the gradient of x from that of the
     result.  out: where to write (x itself: in place).  A dense [B, N, H, d] state is x.view(B * N, H, d)."""
-    dev = _here(x.device)
-    xs = _rows(x, dev, x.dtype, "x")
-    n_pos, rot = _turns(table, dev)
+    at, dtype = _here(x, "x"), x.dtype
+    xs = _rows(x, at, dtype, "x")
+    n_pos, rot = _turns(table, at)
     if table is None:
         raise FlashLoopError("rope needs a table")
     T, H, d = x.shape
-    _on(pos, dev, torch.int32, "pos", (T,))
-    out = torch.empty(T, H, d, dtype=x.dtype, device=dev) if out is None else out
-    ys = _rows(out, dev, x.dtype, "out", x.shape)
+    _on(pos, at, torch.int32, "pos", (T,))
+    if out is None:
+        out, ys = x.new_empty((T, H, d)), H * d
+    else:
+        ys = _rows(out, at, dtype, "out", x.shape)
     rc = load().fl_rope(_p(x), xs, _p(pos), _p(table), n_pos, rot, _choice(layout, ROPE_LAYOUT, "layout"), 1 if inverse else 0,
-                        _DTYPES[x.dtype], T, H, d, _p(out), ys, _stream())
+                        _DTYPES[dtype], T, H, d, _p(out), ys, _stream())
     _check(rc, "fl_rope")
     return out
 
 
 # ---- (10) the paged 8-bit cache ---------------------------------------------------------------------------
-def _paged(dev, cu, lens, block_table, k_cache, v_cache, k_scale, v_scale, Hkv, d):
+def _paged(at, cu, lens, block_table, k_cache, v_cache, k_scale, v_scale, Hkv, d):
     """(B, max_pages, num_pages, page, format) of a ragged batch over a cache."""
     if block_table.dim() != 2 or k_cache.dim() != 4:
         raise FlashLoopError("block_table must be [B, max_pages] and the caches [num_pages, Hkv, page, d]")
-    if k_cache.dtype not in _FORMATS:
-        raise FlashLoopError(f"the caches must be int8 or float8_e4m3fn, got {k_cache.dtype}")
+    code = k_cache.dtype
+    if code not in _FORMATS:
+        raise FlashLoopError(f"the caches must be int8 or float8_e4m3fn, got {code}")
     B, max_pages = block_table.shape
-    num_pages, page = k_cache.shape[0], k_cache.shape[2]
-    shape = (num_pages, Hkv, page, d)
-    _on(k_cache, dev, k_cache.dtype, "k_cache", shape)
-    _on(v_cache, dev, k_cache.dtype, "v_cache", shape)
-    _on(k_scale, dev, torch.float32, "k_scale", (num_pages, Hkv))
-    _on(v_scale, dev, torch.float32, "v_scale", (num_pages, Hkv))
-    _on(cu, dev, torch.int32, "cu", (B + 1,))
-    _on(lens, dev, torch.int32, "lens", (B,))
-    _on(block_table, dev, torch.int32, "block_table")
-    return B, max_pages, num_pages, page, _FORMATS[k_cache.dtype]
+    shape = num_pages, _, page, _ = k_cache.shape
+    if (shape[1] != Hkv or shape[3] != d or v_cache.dtype is not code or v_cache.shape != shape
+            or not (k_cache.is_contiguous() and v_cache.is_contiguous() and k_cache.get_device() == v_cache.get_device() == at)):
+        for name, c in (("k_cache", k_cache), ("v_cache", v_cache)):
+            _on(c, at, code, name, (num_pages, Hkv, page, d))
+    _on(k_scale, at, torch.float32, "k_scale", (num_pages, Hkv))
+    _on(v_scale, at, torch.float32, "v_scale", (num_pages, Hkv))
+    _on(cu, at, torch.int32, "cu", (B + 1,))
+    _on(lens, at, torch.int32, "lens", (B,))
+    _on(block_table, at, torch.int32, "block_table")
+    return B, max_pages, num_pages, page, _FORMATS[code]
 
 
 def paged_cache(num_pages, Hkv, page, d, dtype=torch.int8, device="cuda"):
@@ -719,13 +732,13 @@ def paged_append(k, v, cu, lens, block_table, k_cache, v_cache, k_scale, v_scale
     [B]); block_table: int32 [B, max_pages], its pages.  With a rotary table the keys are turned by their positions on the
     way.  The caches (paged_cache) are updated in place; the scale of a page and head covers what the page holds of the
     sequence, and doubles (its earlier codes halve) when a new position needs it."""
-    dev = _here(k.device)
-    ks = _rows(k, dev, k.dtype, "k")
+    at, dtype = _here(k, "k"), k.dtype
+    ks = _rows(k, at, dtype, "k")
     T, Hkv, d = k.shape
-    vs = _rows(v, dev, k.dtype, "v", k.shape)
-    B, max_pages, num_pages, page, fmt = _paged(dev, cu, lens, block_table, k_cache, v_cache, k_scale, v_scale, Hkv, d)
-    n_pos, rot = _turns(table, dev)
-    rc = load().fl_paged_append(_p(k), ks, _p(v), vs, _DTYPES[k.dtype], _p(cu), _p(lens), B, T, Hkv, d, _p(table), n_pos, rot,
+    vs = _rows(v, at, dtype, "v", k.shape)
+    B, max_pages, num_pages, page, fmt = _paged(at, cu, lens, block_table, k_cache, v_cache, k_scale, v_scale, Hkv, d)
+    n_pos, rot = _turns(table, at)
+    rc = load().fl_paged_append(_p(k), ks, _p(v), vs, _DTYPES[dtype], _p(cu), _p(lens), B, T, Hkv, d, _p(table), n_pos, rot,
                                 _choice(layout, ROPE_LAYOUT, "layout"), _p(block_table), max_pages, num_pages, page, fmt,
                                 _p(k_cache), _p(v_cache), _p(k_scale), _p(v_scale), _stream())
     _check(rc, "fl_paged_append")
@@ -741,23 +754,25 @@ def paged_attn(q, cu, lens, block_table, k_cache, v_cache, k_scale, v_scale, tab
     the kernel, not the result; default: an even batch, as long as the block table allows).  lse: optional fp32 [T, Hq] to
     write the log-normalisers to.  ws: optional uint8 workspace (paged_attn_ws).  Returns out [T, Hq, d]; rows behind cu[B] of
     a given out are left as they were."""
-    dev = _here(q.device)
-    qs = _rows(q, dev, q.dtype, "q")
+    at, dtype = _here(q, "q"), q.dtype
+    qs = _rows(q, at, dtype, "q")
     T, Hq, d = q.shape
-    Hkv = k_cache.shape[1]
-    B, max_pages, num_pages, page, fmt = _paged(dev, cu, lens, block_table, k_cache, v_cache, k_scale, v_scale, Hkv, d)
-    n_pos, rot = _turns(table, dev)
-    out = torch.empty(T, Hq, d, dtype=q.dtype, device=dev) if out is None else out
-    os_ = _rows(out, dev, q.dtype, "out", q.shape)
-    _on(lse, dev, torch.float32, "lse", (T, Hq))
+    Hkv = k_cache.shape[1] if k_cache.dim() == 4 else 0
+    B, max_pages, num_pages, page, fmt = _paged(at, cu, lens, block_table, k_cache, v_cache, k_scale, v_scale, Hkv, d)
+    n_pos, rot = _turns(table, at)
+    if out is None:
+        out, os_ = q.new_empty((T, Hq, d)), Hq * d
+    else:
+        os_ = _rows(out, at, dtype, "out", q.shape)
+    _on(lse, at, torch.float32, "lse", (T, Hq))
     max_q = -(-T // B) if max_q is None else max_q
     lib = load()
     if ws is None:
         need = lib.fl_paged_attn_ws(B, T, Hq, Hkv, d, page, max_pages, window, n_sink, max_q, max_len)
-        ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+        ws = lens.new_empty(need, dtype=torch.uint8) if need else None
     else:
-        _on(ws, dev, torch.uint8, "ws")
-    rc = lib.fl_paged_attn(_p(q), qs, _DTYPES[q.dtype], _p(cu), _p(lens), B, T, Hq, Hkv, d, _p(table), n_pos, rot,
+        _on(ws, at, torch.uint8, "ws")
+    rc = lib.fl_paged_attn(_p(q), qs, _DTYPES[dtype], _p(cu), _p(lens), B, T, Hq, Hkv, d, _p(table), n_pos, rot,
                            _choice(layout, ROPE_LAYOUT, "layout"), _p(block_table), max_pages, num_pages, page, fmt,
                            _p(k_cache), _p(v_cache), _p(k_scale), _p(v_scale),
                            1.0 / math.sqrt(d) if sm_scale is None else sm_scale, window, n_sink, max_q, max_len, _p(out), os_,

@@ -117,11 +117,19 @@ def test_binding_refuses_tensors_of_another_place(monkeypatch):
         fl.paged_append(x, x, None, None, None, None, None, None, None)
     with pytest.raises(fl.FlashLoopError, match="device"):
         fl.paged_attn(x, None, None, None, None, None, None, None)
-    # a tensor of another GPU than the current one
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    # a tensor of another GPU than the current one, or than the call's first tensor
+    class Elsewhere:
+        is_cuda, dtype, device, shape = True, torch.float32, torch.device("cuda", 1), (4,)
+        def get_device(self): return 1
+        def is_contiguous(self): return True
+    monkeypatch.setattr(fl, "_current", lambda: 0)
     with pytest.raises(fl.FlashLoopError, match="current device"):
-        fl._here(torch.device("cuda", 1))
-    assert fl._here(torch.device("cuda", 0)).index == 0
+        fl._here(Elsewhere(), "x")
+    monkeypatch.setattr(fl, "_current", lambda: 1)
+    assert fl._here(Elsewhere(), "x") == 1
+    with pytest.raises(fl.FlashLoopError, match="other tensors"):
+        fl._on(Elsewhere(), 0, torch.float32, "table", (4,))
+    fl._on(Elsewhere(), 1, torch.float32, "table", (4,))
     with pytest.raises(fl.FlashLoopError, match="scaling must be one of"):
         fl.rope_table(4, 64, scaling="other")
     with pytest.raises(fl.FlashLoopError, match="int8 or float8"):
@@ -129,7 +137,7 @@ def test_binding_refuses_tensors_of_another_place(monkeypatch):
 
 
 def test_rows_of_the_binding():
-    cpu = torch.device("cpu")
+    cpu = torch.zeros(1).get_device()
     x = torch.zeros(6, 3 * 128, dtype=torch.float16)[:, 128:256].view(6, 2, 64)
     assert fl._rows(x, cpu, torch.float16, "x") == 384
     assert fl._rows(x[:1], cpu, torch.float16, "x") == 128           # one row has no stride
