@@ -152,9 +152,11 @@ __device__ __forceinline__ float row_down(float m) {
   const int e = min(max((int)(__float_as_uint(m) >> 23), 1), 253);
   return __uint_as_float((uint32_t)(254 - e) << 23);
 }
+// fp16 queries get a second part, what the rounding of the rotated values to fp16 left (`low`; bf16 ones do not: their outputs are
+// rounded eight times as coarsely).
 template <int N, bool F16, class Ch, class Most>
-__device__ __forceinline__ float load_query(const PagedAttnArgs& a, const uint16_t* row, bool ok, int pos, int cap, f16x8* q, Ch ch,
-                                            Most most) {
+__device__ __forceinline__ float load_query(const PagedAttnArgs& a, const uint16_t* row, bool ok, int pos, int cap, f16x8* q,
+                                            f16x8* low, Ch ch, Most most) {
   uint4 raw[N], par[N];
 #pragma unroll
   for (int k = 0; k < N; ++k) raw[k] = reinterpret_cast<const uint4*>(row)[ch(k)];
@@ -221,6 +223,12 @@ __device__ __forceinline__ float load_query(const PagedAttnArgs& a, const uint16
 #pragma unroll
     for (int e = 0; e < 4; ++e) w[e] = ok ? pack_f16x2(v[k][2 * e] * down, v[k][2 * e + 1] * down) : 0u;
     q[k] = __builtin_bit_cast(f16x8, w);
+    if constexpr (F16) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        w[e] = ok ? pack_f16x2(v[k][2 * e] * down - (float)q[k][2 * e], v[k][2 * e + 1] * down - (float)q[k][2 * e + 1]) : 0u;
+      low[k] = __builtin_bit_cast(f16x8, w);
+    }
   }
   return a.scale_log2 / down;
 }

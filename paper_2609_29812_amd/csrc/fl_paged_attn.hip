@@ -18,7 +18,7 @@ constexpr int kTokenKeys = 32;     // keys of a wave's tile
 // outputs leave.  Page numbers and scales of 32 tiles are
 // fetched by the lanes at once and handed out by v_readlane.
 template <int D, bool I8, bool F16, int NR>
-__global__ __launch_bounds__(256, NR == 1 ? 4 : 2) void paged_token_kernel(PagedAttnArgs a) {
+__global__ __launch_bounds__(256, NR == 1 ? (F16 ? 3 : 4) : 2) void paged_token_kernel(PagedAttnArgs a) {
   constexpr int R = 16 * NR, KS = D / 32, DT = D / 16;
   constexpr int KW = D / 64;              // 16-byte loads of a lane per key group
   constexpr int VW = D / 64;              // words of a lane per key of V
@@ -78,7 +78,7 @@ __global__ __launch_bounds__(256, NR == 1 ? 4 : 2) void paged_token_kernel(Paged
   fetch_pages(0);
 
   // the lane's rows
-  f16x8 qf[NR][KS];
+  f16x8 qf[NR][KS], ql[NR][F16 ? KS : 1];
   float mul[NR];
   int jmax[NR], jmin[NR];
 #pragma unroll
@@ -90,7 +90,7 @@ __global__ __launch_bounds__(256, NR == 1 ? 4 : 2) void paged_token_kernel(Paged
     const uint16_t* src = a.q + (int64_t)(sp.r0 + t) * a.qs + (int64_t)(kvh * G + rho % G) * D;
     const int cap = a.bt.max_pages * a.pg.size;
     // (the order in which keys lie in the lanes)
-    mul[x] = load_query<KS, F16>(a, src, ok, pos, cap, qf[x], [g4](int k) { return 8 * (k / 2) + 2 * g4 + k % 2; },
+    mul[x] = load_query<KS, F16>(a, src, ok, pos, cap, qf[x], ql[x], [g4](int k) { return 8 * (k / 2) + 2 * g4 + k % 2; },
                                  [](float m) { return row4_max(m); });
     jmax[x] = ok ? min(pos, cap - 1) : -1;
     jmin[x] = a.window > 0 && pos >= a.window ? pos - a.window + 1 : 0;
@@ -168,6 +168,12 @@ __global__ __launch_bounds__(256, NR == 1 ? 4 : 2) void paged_token_kernel(Paged
 #pragma unroll
         for (int x = 0; x < NR; ++x)
           s[x][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, kw), qf[x][k], s[x][h], 0, 0, 0);
+        if constexpr (F16)
+          if (a.rt.table) {
+#pragma unroll
+            for (int x = 0; x < NR; ++x)
+              s[x][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, kw), ql[x][k], s[x][h], 0, 0, 0);
+          }
       }
     }
     if (more) load_k(c + 1);

@@ -92,8 +92,6 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttnArgs a) {
   __shared__ PromptSlot<D> s0, s1;
   __shared__ float4 s_page[2][4 * kAhead]; // per 16 keys: key scale, log2 and reciprocal of the value scale, page
 
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int hw = lane >> 5, r32 = lane & 31;
   const int kvh = blockIdx.x % a.pg.heads, wg = blockIdx.x / a.pg.heads;
   const int G = a.G;
   // the workgroup's run of units at .. end - 1 of its head, from row tile `slot` on; or all of one row tile
@@ -107,6 +105,11 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttnArgs a) {
   }
   const int first = at;
   for (; at < end; ++slot) {
+  int tid = threadIdx.x;
+  // what a row tile derives from the lane is formed anew: kept over the stages, it spilled
+  if constexpr (SHARED) asm volatile("" : "+v"(tid));
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int hw = lane >> 5, r32 = lane & 31;
   const Seq sq = find_seq(a.bt, slot, 1, [G](int c) { return c * G / R; });
   const int b = sq.b;
   if (b < 0) return;
@@ -149,10 +152,10 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttnArgs a) {
 
   // pages and scales of stages [from, from + kAhead): thread x < 128 has 16 keys
   auto page_of = [&](int from) {
-    const int st = t0 + from + (threadIdx.x >> 2);
+    const int st = t0 + from + (tid >> 2);
     int p = -1;
-    if (threadIdx.x < 4 * kAhead && st < t0 + n) {
-      const int page = (key_of<COLS>(sp, st) + (threadIdx.x & 3) * 16) >> a.pg.log2;
+    if (tid < 4 * kAhead && st < t0 + n) {
+      const int page = (key_of<COLS>(sp, st) + (tid & 3) * 16) >> a.pg.log2;
       if (page < a.bt.max_pages) p = a.bt.table[(int64_t)b * a.bt.max_pages + page];
       if ((uint32_t)p >= (uint32_t)a.pg.num) p = -1;
     }
@@ -169,18 +172,18 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttnArgs a) {
   };
 
   const int page0 = page_of(0);                                       // (asked for before the queries)
-  f16x8 qf[KS];
+  f16x8 qf[KS], ql[F16 ? KS : 1];
   float mul;
   {
     const uint16_t* src = a.q + (int64_t)(sp.r0 + tok) * a.qs + (int64_t)head * D;
-    mul = load_query<KS, F16>(a, src, row_ok, pos, cap, qf, [hw](int k) { return 2 * k + hw; },
+    mul = load_query<KS, F16>(a, src, row_ok, pos, cap, qf, ql, [hw](int k) { return 2 * k + hw; },
                               [](float m) { return xor32_max(m); });
   }
 
   // loads: x of the wave covers keys of one 16-key group; a lane has 16 channels of a key
   typedef uint32_t v4u __attribute__((ext_vector_type(4)));
   v4u kw[NI], vw[NI];
-  const int lane_key = (int)threadIdx.x / LPK, lane_ch = (int)threadIdx.x % LPK;
+  const int lane_key = tid / LPK, lane_ch = tid % LPK;
   auto fetch = [&](int st) __attribute__((always_inline)) {          // stage st (of the n)
     const int key0 = key_of<COLS>(sp, t0 + st);
 #pragma unroll
@@ -252,6 +255,8 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttnArgs a) {
       for (int x = 0; x < NBK; ++x) {
         const u32x4 w = *reinterpret_cast<const u32x4*>(&sl.k[x * 32 * D + koff[ks]]);
         s[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, w), qf[ks], s[x], 0, 0, 0);
+        if constexpr (F16)
+          if (a.rt.table) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, w), ql[ks], s[x], 0, 0, 0);
       }
     float mg[2 * NBK], lv[2 * NBK], iv[2 * NBK];
     int gone = 0;
@@ -342,7 +347,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttnArgs a) {
 
   if (n > 0) {
     if constexpr (SHARED) __syncthreads();                                      // (the last row tile's stages are read)
-    if (threadIdx.x < 4 * kAhead) s_page[0][threadIdx.x] = scales_of(page0);
+    if (tid < 4 * kAhead) s_page[0][tid] = scales_of(page0);
     __syncthreads();
     fetch(0);
     store(s0, 0);
@@ -353,7 +358,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttnArgs a) {
       const int ph = st % kAhead;                                     // uniform; the next block's table in three steps
       if (ph == 0) ahead = page_of(st + kAhead);
       if (ph == 8) ahead_s = scales_of(ahead);
-      if (ph == 16 && threadIdx.x < 4 * kAhead) s_page[((st / kAhead) & 1) ^ 1][threadIdx.x] = ahead_s;
+      if (ph == 16 && tid < 4 * kAhead) s_page[((st / kAhead) & 1) ^ 1][tid] = ahead_s;
       if (st + 1 < n) fetch(st + 1);
       compute(cur, st);
       if (st + 1 < n) store(nxt, st + 1);

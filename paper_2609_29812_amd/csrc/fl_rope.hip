@@ -25,18 +25,24 @@ __device__ __forceinline__ double frequency(const TableArgs& a, int i) {
   return f;
 }
 
-// A thread has one pair and `per` positions, so that the fp64 power is paid once for all of them.
+// A thread has one pair and `per` positions, so that the fp64 power is paid once for all of them.  The angle is reduced in turns,
+// in fp64 (p f / 2 pi less its nearest integer: exact but for the product's rounding, 2^-53 of it); the remainder's sine and
+// cosine are fp32 ones of its high part, corrected to first order by its low part.  The bound is the 8 bytes written per pair:
+// 131072 positions x 64 pairs in 15 us, 4.5 TB/s (28 us with fp64 sines and cosines).
 __global__ __launch_bounds__(256) void rope_table_kernel(TableArgs a) {
   const int64_t g = (int64_t)blockIdx.x * 256 + threadIdx.x;
   const int i = (int)(g % a.half);
   const int64_t p0 = g / a.half * a.per;
   if (p0 >= a.n_pos) return;
-  const double f = frequency(a, i);
+  const double turns = frequency(a, i) * 0.15915494309189533577;    // of a position: f / 2 pi
+  const float m = (float)a.m;
   const int n = (int)min((int64_t)a.per, (int64_t)a.n_pos - p0);
   for (int x = 0; x < n; ++x) {
-    double s, c;
-    sincos((double)(p0 + x) * f, &s, &c);
-    a.out[(p0 + x) * a.half + i] = make_float2((float)(a.m * c), (float)(a.m * s));
+    const double t = (double)(p0 + x) * turns, r = 2.0 * (t - rint(t));     // half turns, in [-1, 1]
+    const float hi = (float)r, lo = (float)(r - (double)hi) * 3.14159265358979f;
+    float s, c;
+    sincospif(hi, &s, &c);
+    a.out[(p0 + x) * a.half + i] = make_float2(m * fmaf(-s, lo, c), m * fmaf(c, lo, s));
   }
 }
 
@@ -156,7 +162,7 @@ extern "C" int fl_rope_table(int n_pos, int rot, double base, int scaling, doubl
   a.factor = factor; a.orig_len = orig_len; a.low = low; a.high = high;
   a.m = scaling == FL_ROPE_YARN ? 1.0 + 0.1 * std::log(factor) : 1.0;
   a.out = reinterpret_cast<float2*>(table);
-  a.per = n_pos >= 65536 ? 16 : n_pos >= 8192 ? 4 : 1;
+  a.per = n_pos >= 65536 ? 32 : n_pos >= 8192 ? 4 : 1;
   const int64_t threads = (int64_t)((n_pos + a.per - 1) / a.per) * a.half;
   rope_table_kernel<<<(unsigned)((threads + 255) / 256), 256, 0, as_stream(stream)>>>(a);
   return check_launch("rope_table_kernel");
