@@ -27,12 +27,14 @@ _POS = E4M3[:127]                       # 0 .. 448, ascending with the code
 
 
 def e4m3_encode(x):
-    """Codes of x (|x| <= 448), to nearest, ties to the even code."""
+    """Codes of x (|x| <= 448, or NaN), to nearest, ties to the even code."""
     a = np.abs(np.asarray(x, np.float64))
+    bad, a = np.isnan(a), np.nan_to_num(a)
     hi = np.clip(np.searchsorted(_POS, a), 0, 126)
     lo = np.maximum(hi - 1, 0)
     dl, dh = a - _POS[lo], _POS[hi] - a
     code = np.where((dl < dh) | ((dl == dh) & (lo % 2 == 0)), lo, hi)
+    code = np.where(bad, 127, code)
     return np.where(np.signbit(x), code | 128, code).astype(np.uint8)
 
 
@@ -144,12 +146,13 @@ def seen_by(i, n, window, n_sink):
 
 def attend(q, cu, lens, block_table, k_codes, v_codes, k_scale, v_scale, fmt, sm_scale, window=0, n_sink=0):
     """q [T, Hq, d] fp64, already rotated.  Returns o [T, Hq, d], lse [T, Hq] (NaN at rows of no sequence), and what bounds
-    rounding errors: sum_j p_j |v_j| [T, Hq, d] and max_j sm_scale sum_e |q_e k_je| [T, Hq]."""
+    rounding errors: sum_j p_j |v_j| [T, Hq, d], max_j sm_scale sum_e |q_e k_je| [T, Hq], and with the values' scales s_j and
+    codes c_j max_j (p_j s_j) sum_j |c_j| [T, Hq, d]."""
     T, Hq, d = q.shape
     n_pages, Hkv, page, _ = k_codes.shape
     G = Hq // Hkv
     o, lse = np.full((T, Hq, d), np.nan), np.full((T, Hq), np.nan)
-    av, aq = np.zeros((T, Hq, d)), np.zeros((T, Hq))
+    av, aq, aw = np.zeros((T, Hq, d)), np.zeros((T, Hq)), np.zeros((T, Hq, d))
     with np.errstate(invalid="ignore"):
         for b in range(len(lens)):
             n = int(cu[b + 1] - cu[b])
@@ -160,6 +163,8 @@ def attend(q, cu, lens, block_table, k_codes, v_codes, k_scale, v_scale, fmt, sm
             for h in range(Hkv):
                 k, v = ((decode(c[safe, h], fmt) * np.where(np.isfinite(s[safe, h]), s[safe, h].astype(np.float64), np.nan)
                          [:, None, None]).reshape(-1, d) for c, s in ((k_codes, k_scale), (v_codes, v_scale)))
+                vc = np.abs(decode(v_codes[safe, h], fmt)).reshape(-1, d)
+                vs = np.repeat(v_scale[safe, h].astype(np.float64), page)
                 for t in range(n):
                     r, i = int(cu[b]) + t, int(lens[b]) - n + t
                     j = seen_by(i, L, window, n_sink) if i >= 0 else np.arange(0)
@@ -176,5 +181,6 @@ def attend(q, cu, lens, block_table, k_codes, v_codes, k_scale, v_scale, fmt, sm
                         p = p / p.sum()
                         o[r, hq] = p @ v[j]
                         av[r, hq] = p @ np.abs(v[j])
+                        aw[r, hq] = (p * vs[j]).max() * vc[j].sum(axis=0)
                         aq[r, hq] = sm_scale * (np.abs(k[j]) @ np.abs(q[r, hq])).max()
-    return o, lse, av, aq
+    return o, lse, av, aq, aw

@@ -17,6 +17,8 @@ sparse_step() one sparse loop r >= 2: select the active rows among the previous 
 The layer also keeps an fp16 copy of the value cache (v16): the quantizers write it with the committed rows,
 and the attention's segment kernels load value tiles from it instead of converting bf16 tiles in LDS
 (bitwise the same results).
+paged_step()  a dense loop (a prompt, a chunk of one, the newest positions) of a ragged batch whose contexts lie in a
+              paged 8-bit cache: new keys rotated and stored with the values, then attention over the cache.
 prune_list()  a smaller column budget for the next loop (Section 4.2): keep the sinks and the entries the
               last loop's updated rows gave the most probability mass.  The next loop then runs both passes
               (its subtract pass recomputes the kept columns' share with the same lse_ref).
@@ -132,6 +134,16 @@ def sparse_step(st: LayerState, qr, qp, kr, kp, vr, vp, k_r, bits, keep=False):
         return dict(idx=idx, slot=slot, key=key, codes_k=ck, scale_k=sk, zero_k=zk, codes_v=cv,
                     scale_v=sv, zero_v=zv, k_new=k_new, v_new=v_new)
     return None
+
+
+def paged_step(cache, q, k, v, cu, lens, block_table, table=None, layout="half", window=0, n_sink=0, max_q=None, max_len=0,
+               out=None, lse=None, ws=None):
+    """One dense loop of one layer for the new positions of a ragged batch: cache (fl.paged_cache) holds what the sequences
+    had, cu, lens and block_table say which rows of q [T, Hq, d] and k, v [T, Hkv, d] are whose newest positions, table turns
+    queries and keys by them.  Returns the output [T, Hq, d]; a looped model has a cache for each of its loops."""
+    fl.paged_append(k, v, cu, lens, block_table, *cache, table=table, layout=layout)
+    return fl.paged_attn(q, cu, lens, block_table, *cache, table=table, layout=layout, window=window, n_sink=n_sink,
+                         max_q=max_q, max_len=max_len, out=out, lse=lse, ws=ws)
 
 
 def prune_list(st: LayerState, qr, t_next, n_sink):

@@ -3,8 +3,11 @@
 Tolerances.  Rotations are rounded once to their type from fp32 sums of two rounded products: half a step of the type plus
 2^-22 (|x0 c| + |x1 s|).  Codes and scales are equal.  Attention: with fp16 queries each |q_e| is off by at most 2^-11 of
 itself (2^-25 of the row's largest below its normal range), so a score by e = 2^-11 A, A = max_j sm_scale sum |q_e k_je|, a
-probability by 2 e of itself, and it is rounded to fp16 (2^-11; 2^-24 absolute against the largest contribution); the
-output's own rounding adds half a step.  fp32 sums add at most (n + d) 2^-23 to either."""
+probability by 2 e of itself, and it is rounded to fp16: 2^-11 of itself, or 2^-25 of the unit below fp16's normal range.  The unit
+is at most the row's largest contribution w = max_j p_j s_j (s_j the value's scale: the kernels round p_j s_j over a running
+maximum of it), so those roundings add up to 2^-25 w sum_j |c_j| over the value's codes c_j; where the keys that carry a row have
+the code 0 in a channel, that is what remains of it.  The output's own rounding adds half a step.  fp32 sums add at most
+(n + d) 2^-23 to either."""
 import numpy as np
 import pytest
 import torch
@@ -305,7 +308,7 @@ def check_attn(F, rng, new, past, page, Hq, Hkv, d, dtype, fmt, layout=None, rot
         cs = paged.table(tab.shape[1] * page, rot).astype(np.float32)
         pos = np.concatenate([np.arange(lens[b] - new[b], lens[b]) for b in range(len(new))] + [np.zeros(2, int)]).astype(int)
         qx = paged.rotate(qx, cs[pos], layout)
-    want, wlse, av, aq = paged.attend(qx, cu, lens, tab, *codes, *scale, fmt, d ** -0.5, window, n_sink)
+    want, wlse, av, aq, aw = paged.attend(qx, cu, lens, tab, *codes, *scale, fmt, d ** -0.5, window, n_sink)
     args = (i32(cu), i32(lens), i32(tab), dev_codes(codes[0], fmt), dev_codes(codes[1], fmt),
             torch.from_numpy(scale[0]).cuda(), torch.from_numpy(scale[1]).cuda())
     n = int(cu[-1])
@@ -323,7 +326,7 @@ def check_attn(F, rng, new, past, page, Hq, Hkv, d, dtype, fmt, layout=None, rot
         keys = int(max(lens))
         e = 2.0 ** -11 * aq[:n]
         acc = (keys + d) * 2.0 ** -23
-        tol = (2 * e[..., None] + 2.0 ** -10 + acc) * av[:n] + half_step(dt) * np.abs(want[:n]) + 2.0 ** -24
+        tol = (2 * e[..., None] + 2.0 ** -10 + acc) * av[:n] + 2.0 ** -25 * aw[:n] + half_step(dt) * np.abs(want[:n]) + 2.0 ** -24
         err = np.abs(got[:n] - want[:n])[fin]
         den = np.linalg.norm(want[:n][fin])
         rel = np.linalg.norm(err) / den if den else 0.0
@@ -356,6 +359,7 @@ ATTN = [
     ([257, 30], [130, 5], 64, 4, 1, 96, 17),
     ([300], [20], 16, 2, 1, 33, 70),
     ([70, 90, 0], [513, 0, 12], 128, 5, 5, 0, 0),
+    ([1] * 100 + [0] * 20 + [3] * 10, [7 * i % 211 for i in range(129)] + [1500], 16, 2, 1, 0, 0),     # more than 64 sequences
 ]
 
 
@@ -368,6 +372,47 @@ def test_attention(F, case, dtype, fmt, d):
     layout, rot = [(None, 0), ("half", d), ("interleaved", d // 2), ("half", 16)][(case + d // 64) % 4]
     check_attn(F, rng, new, past, page, Hq, Hkv, d, dtype, fmt, layout, rot, window, n_sink,
                hints=((None, 0), (1, 5000), (1000, 1), (1000, 5000)), spoil=True)
+
+
+@pytest.mark.parametrize("dtype,fmt,d,page,window,n_sink", [("bf16", "int8", 128, 64, 0, 0), ("f16", "e4m3", 64, 32, 700, 40),
+                                                            ("bf16", "e4m3", 128, 16, 1500, 4), ("f16", "int8", 64, 128, 0, 0)])
+def test_attention_of_long_chunks(F, dtype, fmt, d, page, window, n_sink):
+    """Many row tiles over long contexts: shares of the work that begin and end inside row tiles, of one sequence and between
+    sequences; also with a hint that leaves each tile to a workgroup, and with the kernel for few rows."""
+    rng = np.random.default_rng(12)
+    check_attn(F, rng, [300, 0, 1, 170], [1200, 50, 2000, 3], page, 4, 2, d, dtype, fmt, "half", d, window, n_sink,
+               hints=((300, 2001), (300, 500), (300, 0), (1, 2001)), spoil=True)
+
+
+def test_attention_beyond_4_gib(F):
+    """Pages whose offsets in the cache pass 32 bits, written and read."""
+    page, Hkv, d = 128, 8, 128
+    n_pages = (1 << 32) // (Hkv * page * d) + 600
+    cache = F.paged_cache(n_pages, Hkv, page, d)
+    assert cache[0].numel() > 1 << 32
+    rng = np.random.default_rng(13)
+    far = np.sort(rng.choice(np.arange(n_pages - 500, n_pages), 6, replace=False))[::-1].copy()
+    tab = np.stack([far[:3], far[3:]]).astype(np.int32)
+    for new, lens, max_q in (([300, 257], [300, 257], 300), ([1, 1], [301, 258], 1), ([40, 30], [341, 288], 40)):
+        cu = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+        T = int(cu[-1])
+        q, k, v = (torch.from_numpy(rng.normal(size=(T, h, d))).to(torch.bfloat16) for h in (16, Hkv, Hkv))
+        keep = [c[torch.from_numpy(far).long().cuda()].clone() for c in cache]
+        F.paged_append(k.cuda(), v.cuda(), i32(cu), i32(lens), i32(tab), *cache)
+        o = F.paged_attn(q.cuda(), i32(cu), i32(lens), i32(tab), *cache, max_q=max_q)
+        torch.cuda.synchronize()
+        near = np.arange(6, dtype=np.int32).reshape(2, 3)           # the same pages, six of them on the host
+        codes = [raw(c) if i < 2 else c.cpu().numpy() for i, c in enumerate(keep)]
+        for x, c, s in ((f64(k), codes[0], codes[2]), (f64(v), codes[1], codes[3])):
+            paged.append(x, cu, lens, near, c, s, "int8")
+        got = [c[torch.from_numpy(far).long().cuda()] for c in cache]
+        held = [[p for b in range(2) for p in range(3 * b, 3 * b - (-lens[b] // page))]]
+        for i in range(4):
+            g = raw(got[i]) if i < 2 else got[i].cpu().numpy()
+            assert np.array_equal(g[held[0]], codes[i][held[0]])
+        want, _, av, aq, aw = paged.attend(f64(q), cu, lens, near, *codes, "int8", d ** -0.5)
+        tol = (2 * 2.0 ** -11 * aq[..., None] + 2.0 ** -10 + 500 * 2.0 ** -23) * av + 2.0 ** -25 * aw + 2.0 ** -8 * np.abs(want) + 2.0 ** -24
+        assert np.all(np.abs(f64(o) - want) <= tol)
 
 
 def test_attention_holes_and_empty_rows(F):

@@ -146,7 +146,7 @@ def test_attention_against_sdpa(fmt, window, n_sink):
         codes = [np.where((c & 127) == 127, 5, c).astype(np.uint8) for c in codes]
     scale = [rng.uniform(0.001, 0.02, (n_pages, Hkv)).astype(np.float32) for _ in range(2)]
     q = rng.normal(size=(T, Hq, d))
-    o, lse, av, aq = paged.attend(q, cu, lens, tab, *codes, *scale, fmt, d ** -0.5, window, n_sink)
+    o, lse, av, aq, aw = paged.attend(q, cu, lens, tab, *codes, *scale, fmt, d ** -0.5, window, n_sink)
     assert np.isnan(o[cu[-1]:]).all()
     for b in range(4):
         n, L = new[b], lens[b]
@@ -163,5 +163,5 @@ def test_attention_against_sdpa(fmt, window, n_sink):
     # a page that is not there: its positions are seen by no row; a row that sees nothing is 0
     gone = tab.copy()
     gone[0] = -1
-    o2, lse2, _, _ = paged.attend(q, cu, lens, gone, *codes, *scale, fmt, d ** -0.5, window, n_sink)
+    o2, lse2, *_ = paged.attend(q, cu, lens, gone, *codes, *scale, fmt, d ** -0.5, window, n_sink)
     assert np.all(o2[:5] == 0) and np.all(lse2[:5] == -np.inf) and np.array_equal(o2[5:], o[5:], equal_nan=True)
