@@ -24,25 +24,29 @@ struct Pages {
 __device__ __forceinline__ int row_of(const Batch& bt, int b) { return min(max(bt.cu[b], 0), bt.T); }
 
 // The last sequence b whose first slot, f(cu[b]) + extra * b, is at most `slot` (b = -1: there is none), its rows and its
-// length.  f ascends, so with extra >= 1 a sequence's slots are slot numbers of its own.  The wave looks at 64 sequences at a
-// time, rows and lengths in one round of loads: these stand before everything else that a workgroup reads.
+// length.  f ascends, so with extra >= 1 a sequence's slots are slot numbers of its own.  The wave looks at 64 places at a time
+// until 64 sequences are left; their rows and lengths are one round of loads, which stands before everything else that a workgroup
+// reads.
 struct Seq {
   int b, r0, r1, len;
 };
 template <class F>
 __device__ __forceinline__ Seq find_seq(const Batch& bt, int slot, int extra, F f) {
   const int lane = threadIdx.x & 63;
-  Seq s{-1, 0, 0, 0};
-  for (int b0 = 0; b0 < bt.B; b0 += 64) {
-    const int b = b0 + lane, bc = min(b, bt.B - 1);
-    const int r0 = row_of(bt, bc), r1 = row_of(bt, bc + 1), len = bt.lens[bc];
-    const uint64_t m = __builtin_amdgcn_ballot_w64(b < bt.B && f(r0) + extra * b <= slot);
-    const int n = __popcll(m);
-    if (n > 0) s = {b0 + n - 1, __builtin_amdgcn_readlane(r0, n - 1), __builtin_amdgcn_readlane(r1, n - 1),
-                    __builtin_amdgcn_readlane(len, n - 1)};
-    if (n < 64) break;
+  int lo = 0, left = bt.B;                                   // the sequence is one of lo .. lo + left - 1, if there is one
+  while (left > 64) {
+    const int step = (left + 63) / 64;
+    const int b = lo + lane * step;
+    const uint64_t m = __builtin_amdgcn_ballot_w64(lane * step < left && f(row_of(bt, min(b, bt.B - 1))) + extra * b <= slot);
+    const int n = max((int)__popcll(m), 1);
+    left = min(step, left - (n - 1) * step);
+    lo += (n - 1) * step;
   }
-  return s;
+  const int b = lo + lane, bc = min(b, bt.B - 1);
+  const int r0 = row_of(bt, bc), r1 = row_of(bt, bc + 1), len = bt.lens[bc];
+  const int n = __popcll(__builtin_amdgcn_ballot_w64(lane < left && f(r0) + extra * b <= slot));
+  if (n == 0) return {-1, 0, 0, 0};
+  return {lo + n - 1, __builtin_amdgcn_readlane(r0, n - 1), __builtin_amdgcn_readlane(r1, n - 1), __builtin_amdgcn_readlane(len, n - 1)};
 }
 
 // 16-bit value to fp32 (exact)

@@ -704,6 +704,8 @@ def _paged(at, cu, lens, block_table, k_cache, v_cache, k_scale, v_scale, Hkv, d
     if code not in _FORMATS:
         raise FlashLoopError(f"the caches must be int8 or float8_e4m3fn, got {code}")
     B, max_pages = block_table.shape
+    if B == 0:
+        raise FlashLoopError("a batch has at least one sequence")
     shape = num_pages, _, page, _ = k_cache.shape
     if (shape[1] != Hkv or shape[3] != d or v_cache.dtype is not code or v_cache.shape != shape
             or not (k_cache.is_contiguous() and v_cache.is_contiguous() and k_cache.get_device() == v_cache.get_device() == at)):
@@ -784,7 +786,7 @@ def paged_attn(q, cu, lens, block_table, k_cache, v_cache, k_scale, v_scale, tab
 def paged_attn_ws(q, block_table, k_cache, window=0, n_sink=0, max_q=None, max_len=0):
     """A workspace for paged_attn over these shapes and hints (None when it needs none)."""
     T, Hq, d = q.shape
-    B, max_pages = block_table.shape
+    B, max_pages = max(1, block_table.shape[0]), block_table.shape[1]
     need = load().fl_paged_attn_ws(B, T, Hq, k_cache.shape[1], d, k_cache.shape[2], max_pages, window, n_sink,
                                    -(-T // B) if max_q is None else max_q, max_len)
     return torch.empty(need, dtype=torch.uint8, device=q.device) if need else None

@@ -384,6 +384,29 @@ def test_attention_of_long_chunks(F, dtype, fmt, d, page, window, n_sink):
                hints=((300, 2001), (300, 500), (300, 0), (1, 2001)), spoil=True)
 
 
+def test_thousands_of_sequences(F):
+    """More sequences than a search looks at in one or two rounds, many of them without a row."""
+    rng = np.random.default_rng(14)
+    B, page, d = 5000, 16, 64
+    new = (np.arange(B) % 3 > 0).astype(int)
+    new[[0, 17, 4097, B - 1]] = [0, 20, 33, 0]
+    past = rng.integers(0, 40, B)
+    check_attn(F, rng, list(new), list(past), page, 1, 1, d, "bf16", "int8", hints=((1, 0), (33, 0), (33, 2000)))
+    cu, lens, tab, n_pages = batch(rng, list(new), list(past), page)
+    x = torch.from_numpy(rng.normal(size=(int(cu[-1]), 1, d))).to(torch.float16)
+    for few in (True, False):                               # an average of up to eight rows takes the kernel for few
+        if not few:
+            new = new * 13
+            cu, lens, tab, n_pages = batch(rng, list(new), list(past), page)
+            x = torch.from_numpy(rng.normal(size=(int(cu[-1]), 1, d))).to(torch.float16)
+        codes, scale = make_cache(rng, n_pages, 1, page, d, "int8")
+        gc, gs = [dev_codes(c, "int8") for c in codes], [torch.from_numpy(s.copy()).cuda() for s in scale]
+        F.paged_append(x.cuda(), (-x).cuda(), i32(cu), i32(lens), i32(tab), *gc, *gs)
+        for y, c, s, g, h in ((f64(x), codes[0], scale[0], gc[0], gs[0]), (-f64(x), codes[1], scale[1], gc[1], gs[1])):
+            paged.append(y, cu, lens, tab, c, s, "int8")
+            assert np.array_equal(h.cpu().numpy(), s) and np.array_equal(raw(g), c)
+
+
 def test_attention_beyond_4_gib(F):
     """Pages whose offsets in the cache pass 32 bits, written and read."""
     page, Hkv, d = 128, 8, 128
