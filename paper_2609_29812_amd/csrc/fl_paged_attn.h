@@ -23,7 +23,6 @@ struct PagedAttnArgs {
   int* ends;                       // many rows, shared out: units up to and with each row tile's
   int slots;                       // ... and how many row tiles there are at most
   float *part, *part_ml;           // [T Hq][n_split][d] sums and [T Hq][n_split][2] references and normalisers
-  float pinf;                      // +inf
 };
 
 // What a row tile works on: rows rho0 .. rho0 + rows - 1 of a sequence, a row being (position, head of the group) with the
@@ -245,6 +244,11 @@ __device__ __forceinline__ void widen4(uint32_t w, uint32_t* out) {
     out[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.0f, false));
     out[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)w, 1.0f, true));
   }
+}
+
+// The largest of three in one instruction (v_maximum3_f32; a NaN comes through, where a maximum would first quiet its operands).
+__device__ __forceinline__ float max3(float x, float y, float z) {
+  return __builtin_elementwise_maximum(__builtin_elementwise_maximum(x, y), z);
 }
 
 // What the value scale does.  A probability times its page's scale s is exp2(x + log2 s - ref): the running reference follows

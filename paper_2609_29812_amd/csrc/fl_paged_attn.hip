@@ -204,7 +204,7 @@ __global__ __launch_bounds__(256, NR == 1 ? (F16 ? 3 : 4) : 2) void paged_token_
             y[h][i] = see[h][i] ? y[h][i] : -INFINITY;
           }
         }
-        top = fmaxf(top, fmaxf(fmaxf(y[h][0], y[h][1]), fmaxf(y[h][2], y[h][3])) + lv[h]);
+        top = fmaxf(top, max3(max3(y[h][0], y[h][1], y[h][2]), y[h][3], y[h][3]) + lv[h]);
       }
       top = row4_max(top);
       const bool raise = top > ref[x] + 8.0f;
@@ -504,7 +504,7 @@ extern "C" int fl_paged_attn(const void* q, int64_t q_stride, int dtype, const i
   a.pg = {num_pages, page, log2_of(page), Hkv};
   a.kc = static_cast<const uint8_t*>(k_cache); a.vc = static_cast<const uint8_t*>(v_cache); a.ksc = k_scale; a.vsc = v_scale;
   a.Hq = Hq; a.G = Hq / Hkv; a.scale_log2 = sm_scale * 1.4426950408889634f; a.window = window; a.n_sink = n_sink;
-  a.n_split = p.n_split; a.min_tiles = p.min_tiles; a.share = p.share; a.pinf = INFINITY;
+  a.n_split = p.n_split; a.min_tiles = p.min_tiles; a.share = p.share;
   a.part = static_cast<float*>(ws);
   a.part_ml = a.part ? a.part + (size_t)T * Hq * p.n_split * d : nullptr;
   rc = check_batch(fn, a.bt, a.pg, false, st);

@@ -288,10 +288,8 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttnArgs a) {
 #pragma unroll
     for (int g = 0; g < 2 * NBK; ++g) {
       const int x = g >> 1, v0 = 8 * (g & 1);
-      float m0 = fmax_nn(s[x][v0], s[x][v0 + 1], a.pinf), m1 = fmax_nn(s[x][v0 + 2], s[x][v0 + 3], a.pinf);
-      m0 = fmax_nn(fmax_nn(m0, s[x][v0 + 4], a.pinf), s[x][v0 + 5], a.pinf);
-      m1 = fmax_nn(fmax_nn(m1, s[x][v0 + 6], a.pinf), s[x][v0 + 7], a.pinf);
-      top = fmaxf(top, fmaf(fmax_nn(m0, m1, a.pinf), mg[g], lv[g]));
+      const float m0 = max3(s[x][v0], s[x][v0 + 1], s[x][v0 + 2]), m1 = max3(s[x][v0 + 3], s[x][v0 + 4], s[x][v0 + 5]);
+      top = fmaxf(top, fmaf(max3(max3(m0, s[x][v0 + 6], s[x][v0 + 7]), m1, m1), mg[g], lv[g]));
     }
     top = xor32_max(top);
     const bool raise = top > ref + 8.0f;
