@@ -569,12 +569,12 @@ int fl_paged_append(const void* k, int64_t k_stride, const void* v, int64_t v_st
  *   max_q, max_len : the largest n and the largest length of the batch as far as the caller knows them (max_len = 0:
  *                max_pages * page).  They choose the kernel and how the keys are split; any values give the result, up to
  *                rounding.
- *   ws         : at least fl_paged_attn_ws(...) bytes, for the same B, T, heads, d, page, window, n_sink, max_q and max_len
+ *   ws         : 16-byte aligned, at least fl_paged_attn_ws(...) bytes, for the same B, T, heads, d, page, window, n_sink, max_q and max_len
  *                (and max_pages); nothing is kept in it between calls.  Calls that overlap need one each.
  *   Hq a multiple of Hkv; window, n_sink >= 0; other limits as in (10).
- * Precision: q (rotated in fp32) is multiplied as fp16 relative to the row's largest magnitude, probabilities as fp16
- * relative to the largest contribution of the row, both against the exact codes; scores, sums and outputs are held in
- * fp32.  With the index checks on, as in (10) (a page that is not there is no error here, nor is one that two sequences share).
+ * Precision: q (rotated in fp32) is multiplied as fp16 relative to the row's largest magnitude, for FL_F16 with what that
+ * rounding leaves as a second part; probabilities times their value's scale as fp16 relative to the largest such product of the
+ * row; both against the exact codes.  Scores, sums and outputs are held in fp32.  With the index checks on, as in (10) (a page that is not there is no error here, nor is one that two sequences share).
  * ---------------------------------------------------------------------------------------------- */
 size_t fl_paged_attn_ws(int B, int T, int Hq, int Hkv, int d, int page, int max_pages, int window, int n_sink, int max_q,
                         int max_len);

