@@ -295,7 +295,7 @@ __global__ __launch_bounds__(256, NR == 1 ? (F16 ? 3 : 4) : 2) void paged_token_
   for (int x = 0; x < NR; ++x) {
     const int rr = x * 16 + r16;
     const float m = fmaxf(fmaxf(s_ref[0][rr], s_ref[1][rr]), fmaxf(s_ref[2][rr], s_ref[3][rr]));
-    const float f = ref[x] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ref[x] - m);
+    const float f = ref[x] == -INFINITY && lsum[x] == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(ref[x] - m);
     if (x > 0) __syncthreads();
 #pragma unroll
     for (int i = 0; i < 4; ++i)                              // channels (4 g4 + i) DT + t, t < DT
@@ -311,7 +311,8 @@ __global__ __launch_bounds__(256, NR == 1 ? (F16 ? 3 : 4) : 2) void paged_token_
       const float mm = fmaxf(fmaxf(s_ref[0][rx], s_ref[1][rx]), fmaxf(s_ref[2][rx], s_ref[3][rx]));
       float sum = 0.0f;
 #pragma unroll
-      for (int v = 0; v < 4; ++v) sum += s_ref[v][rx] == -INFINITY ? 0.0f : s_sum[v][rx] * __builtin_amdgcn_exp2f(s_ref[v][rx] - mm);
+      for (int v = 0; v < 4; ++v)                            // (a sum of NaN scores has no reference, but counts)
+        sum += s_ref[v][rx] == -INFINITY && s_sum[v][rx] == 0.0f ? 0.0f : s_sum[v][rx] * __builtin_amdgcn_exp2f(s_ref[v][rx] - mm);
       float o[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[e] = (s_acc[0][row][c + e] + s_acc[1][row][c + e]) + (s_acc[2][row][c + e] + s_acc[3][row][c + e]);

@@ -486,6 +486,17 @@ def test_attention_scales(F, new, past, fmt):
                scale_edit=poison)
 
 
+@pytest.mark.parametrize("new,past", [([1, 1], [400, 20]), ([80, 25], [300, 0])])
+def test_attention_key_scales_that_are_not_finite(F, new, past):
+    """The row's normaliser is NaN with its output, also where a wave, a part or the whole row has no other key."""
+    rng = np.random.default_rng(15)
+
+    def poison(scale, tab):
+        scale[0][tab[0, 5], 0] = np.nan           # one head of keys 160 .. 191
+        scale[0][tab[1, 0], 1] = np.inf           # the only page of sequence 1
+    check_attn(F, rng, new, past, 32, 4, 2, 64, "bf16", "int8", hints=((None, 0), (1, 3000), (400, 3000)), scale_edit=poison)
+
+
 def test_attention_peaked_rows(F):
     """Scores of hundreds: the softmax reference moves far and often; one key carries a row."""
     rng = np.random.default_rng(9)
