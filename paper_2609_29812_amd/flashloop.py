@@ -628,23 +628,23 @@ def _on(t, at, dtype, name, shape=None):
 
 def _rows(t, at, dtype, name, shape=None):
     """Elements between the rows of [T, H, d], whose heads are dense."""
-    if t.dim() != 3 or (shape is not None and t.shape != shape):
+    if (shape is None and t.dim() != 3) or (shape is not None and t.shape != shape):
         raise FlashLoopError(f"{name} must have shape {'[T, H, d]' if shape is None else tuple(shape)}, got {tuple(t.shape)}")
     if t.dtype is not dtype or dtype not in _DTYPES:
         raise FlashLoopError(f"{name} must be {dtype if dtype in _DTYPES else 'bfloat16 or float16'}, got {t.dtype}")
     if t.get_device() != at:
         raise FlashLoopError(f"{name} is on {t.device}, the call's other tensors on cuda:{at}")
-    T, H, d = t.shape
-    row, head, one = t.stride()
+    (T, H, d), (row, head, one) = t.shape, t.stride()
     if (one != 1 and d > 1) or (head != d and H > 1):
         raise FlashLoopError(f"the heads of a row of {name} must be dense, got strides {t.stride()}")
     return row if T > 1 else H * d
 
 
 def _choice(value, of, name):
-    if value not in of:
+    number = of.get(value)
+    if number is None:
         raise FlashLoopError(f"{name} must be one of {', '.join(of)}, got {value!r}")
-    return of[value]
+    return number
 
 
 def _turns(table, at):
@@ -689,9 +689,10 @@ def rope(x, table, pos=None, layout="half", inverse=False, out=None):
         out, ys = x.new_empty((T, H, d)), H * d
     else:
         ys = _rows(out, at, dtype, "out", x.shape)
-    rc = load().fl_rope(_p(x), xs, _p(pos), _p(table), n_pos, rot, _choice(layout, ROPE_LAYOUT, "layout"), 1 if inverse else 0,
-                        _DTYPES[dtype], T, H, d, _p(out), ys, _stream())
-    _check(rc, "fl_rope")
+    rc = (_lib or load()).fl_rope(x.data_ptr(), xs, _p(pos), table.data_ptr(), n_pos, rot, _choice(layout, ROPE_LAYOUT, "layout"),
+                                  1 if inverse else 0, _DTYPES[dtype], T, H, d, out.data_ptr(), ys, _stream())
+    if rc:
+        _check(rc, "fl_rope")
     return out
 
 
@@ -711,11 +712,16 @@ def _paged(at, cu, lens, block_table, k_cache, v_cache, k_scale, v_scale, Hkv, d
             or not (k_cache.is_contiguous() and v_cache.is_contiguous() and k_cache.get_device() == v_cache.get_device() == at)):
         for name, c in (("k_cache", k_cache), ("v_cache", v_cache)):
             _on(c, at, code, name, (num_pages, Hkv, page, d))
-    _on(k_scale, at, torch.float32, "k_scale", (num_pages, Hkv))
-    _on(v_scale, at, torch.float32, "v_scale", (num_pages, Hkv))
-    _on(cu, at, torch.int32, "cu", (B + 1,))
-    _on(lens, at, torch.int32, "lens", (B,))
-    _on(block_table, at, torch.int32, "block_table")
+    if not (k_scale.dtype is v_scale.dtype is torch.float32 and cu.dtype is lens.dtype is block_table.dtype is torch.int32
+            and k_scale.get_device() == v_scale.get_device() == cu.get_device() == lens.get_device() == block_table.get_device() == at
+            and k_scale.shape == v_scale.shape == (num_pages, Hkv) and cu.shape == (B + 1,) and lens.shape == (B,)
+            and k_scale.is_contiguous() and v_scale.is_contiguous() and cu.is_contiguous() and lens.is_contiguous()
+            and block_table.is_contiguous()):
+        _on(k_scale, at, torch.float32, "k_scale", (num_pages, Hkv))
+        _on(v_scale, at, torch.float32, "v_scale", (num_pages, Hkv))
+        _on(cu, at, torch.int32, "cu", (B + 1,))
+        _on(lens, at, torch.int32, "lens", (B,))
+        _on(block_table, at, torch.int32, "block_table")
     return B, max_pages, num_pages, page, _FORMATS[code]
 
 
@@ -740,10 +746,12 @@ def paged_append(k, v, cu, lens, block_table, k_cache, v_cache, k_scale, v_scale
     vs = _rows(v, at, dtype, "v", k.shape)
     B, max_pages, num_pages, page, fmt = _paged(at, cu, lens, block_table, k_cache, v_cache, k_scale, v_scale, Hkv, d)
     n_pos, rot = _turns(table, at)
-    rc = load().fl_paged_append(_p(k), ks, _p(v), vs, _DTYPES[dtype], _p(cu), _p(lens), B, T, Hkv, d, _p(table), n_pos, rot,
-                                _choice(layout, ROPE_LAYOUT, "layout"), _p(block_table), max_pages, num_pages, page, fmt,
-                                _p(k_cache), _p(v_cache), _p(k_scale), _p(v_scale), _stream())
-    _check(rc, "fl_paged_append")
+    rc = (_lib or load()).fl_paged_append(
+        k.data_ptr(), ks, v.data_ptr(), vs, _DTYPES[dtype], cu.data_ptr(), lens.data_ptr(), B, T, Hkv, d, _p(table), n_pos, rot,
+        _choice(layout, ROPE_LAYOUT, "layout"), block_table.data_ptr(), max_pages, num_pages, page, fmt, k_cache.data_ptr(),
+        v_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), _stream())
+    if rc:
+        _check(rc, "fl_paged_append")
 
 
 # ---- (11) attention over the paged cache ------------------------------------------------------------------
@@ -768,18 +776,19 @@ def paged_attn(q, cu, lens, block_table, k_cache, v_cache, k_scale, v_scale, tab
         os_ = _rows(out, at, dtype, "out", q.shape)
     _on(lse, at, torch.float32, "lse", (T, Hq))
     max_q = -(-T // B) if max_q is None else max_q
-    lib = load()
+    lib = _lib or load()
     if ws is None:
         need = lib.fl_paged_attn_ws(B, T, Hq, Hkv, d, page, max_pages, window, n_sink, max_q, max_len)
         ws = lens.new_empty(need, dtype=torch.uint8) if need else None
     else:
         _on(ws, at, torch.uint8, "ws")
-    rc = lib.fl_paged_attn(_p(q), qs, _DTYPES[dtype], _p(cu), _p(lens), B, T, Hq, Hkv, d, _p(table), n_pos, rot,
-                           _choice(layout, ROPE_LAYOUT, "layout"), _p(block_table), max_pages, num_pages, page, fmt,
-                           _p(k_cache), _p(v_cache), _p(k_scale), _p(v_scale),
-                           1.0 / math.sqrt(d) if sm_scale is None else sm_scale, window, n_sink, max_q, max_len, _p(out), os_,
-                           _p(lse), _p(ws), 0 if ws is None else ws.numel(), _stream())
-    _check(rc, "fl_paged_attn")
+    rc = lib.fl_paged_attn(
+        q.data_ptr(), qs, _DTYPES[dtype], cu.data_ptr(), lens.data_ptr(), B, T, Hq, Hkv, d, _p(table), n_pos, rot,
+        _choice(layout, ROPE_LAYOUT, "layout"), block_table.data_ptr(), max_pages, num_pages, page, fmt, k_cache.data_ptr(),
+        v_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), 1.0 / math.sqrt(d) if sm_scale is None else sm_scale, window,
+        n_sink, max_q, max_len, out.data_ptr(), os_, _p(lse), _p(ws), 0 if ws is None else ws.numel(), _stream())
+    if rc:
+        _check(rc, "fl_paged_attn")
     return out
 
 
