@@ -73,25 +73,6 @@ __device__ __forceinline__ uint4 pack8(const float* x) {
   return make_uint4(u[0], u[1], u[2], u[3]);
 }
 
-// Cosines and sines of the pairs that the eight channels 8 ch .. 8 ch + 7 of a rotated head belong to: for FL_ROPE_HALF
-// channel e has cs[e], for FL_ROPE_INTERLEAVED channels 2e and 2e + 1 have cs[e], e < 4.
-template <bool HALF>
-__device__ __forceinline__ void load_turn(const float* __restrict__ row, int rot, int ch, float2* cs) {
-  const float4* p;
-  if constexpr (HALF) {
-    const int i = 8 * ch < rot / 2 ? 8 * ch : 8 * ch - rot / 2;
-    p = reinterpret_cast<const float4*>(row + 2 * i);
-  } else {
-    p = reinterpret_cast<const float4*>(row + 8 * ch);
-  }
-#pragma unroll
-  for (int e = 0; e < (HALF ? 4 : 2); ++e) {
-    const float4 w = p[e];
-    cs[2 * e] = make_float2(w.x, w.y);
-    cs[2 * e + 1] = make_float2(w.z, w.w);
-  }
-}
-
 // host: the checks that the calls of a paged cache have in common
 int check_paged(const char* fn, int dtype, const int32_t* cu, const int32_t* lens, int B, int T, int Hkv, int d,
                 const float* table, int n_pos, int rot, int layout, const int32_t* block_table, int max_pages,

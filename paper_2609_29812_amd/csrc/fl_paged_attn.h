@@ -29,7 +29,7 @@ struct PagedAttnArgs {
 // heads fastest, and the tiles of KT keys that some row of it may see, in order: the n_lead tiles of the leading positions,
 // then tiles first .. last.
 struct Span {
-  int b, r0, rho0, rows;           // rows == 0: nothing to do
+  int r0, rho0, rows;              // rows == 0: nothing to do
   int start;                       // position of the sequence's first row
   int i_min, i_max;                // positions of the tile's first and last row
   int n_lead, first, tiles;        // tiles: in all
@@ -40,7 +40,6 @@ struct Span {
 template <int R, int KT>
 __device__ __forceinline__ Span span_of(const PagedAttnArgs& a, const Seq& q, int tile) {
   Span s{};
-  s.b = q.b;
   s.r0 = q.r0;
   const int n = q.r1 - q.r0;
   s.rho0 = tile * R;
@@ -275,7 +274,10 @@ struct Cut {
   __device__ __forceinline__ int begin(int p) const { return (int)min((int64_t)total, (int64_t)per * p); }
   __device__ __forceinline__ int owner(int x) const { return x / per; }
 };
-constexpr int kLeastUnits = 24;    // of a share
+// Units of a share at least: its queries, its sums and their join cost about ten.  Where few row tiles stand against many CUs
+// (100 rows of 8 heads over 5000 positions, 320 units a head) 8, 12, 16 and 24 took 44, 48, 55 and 70 us; 64 rows over 32000
+// positions 124, 112, 94 and 98 us, being joined from more parts then.
+constexpr int kLeastUnits = 12;
 __device__ __forceinline__ Cut cut_of(const PagedAttnArgs& a) {
   const int total = __builtin_amdgcn_readfirstlane(a.ends[a.slots - 1]);
   return {total, __builtin_amdgcn_readfirstlane(max(kLeastUnits, (total + a.share - 1) / a.share))};

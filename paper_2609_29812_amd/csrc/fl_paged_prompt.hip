@@ -424,9 +424,11 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a) {
   for (int rr = r0 + threadIdx.x / LN; rr < min(r0 + 32, sp.rows); rr += 256 / LN) {
     auto place = [&](int p) { return ((int64_t)(kvh * a.share + p) * 2 + (max(begin, cut.begin(p)) == cut.begin(p) ? 0 : 1)) * R + rr; };
     float m = -INFINITY;
+#pragma unroll 4
     for (int p = p0; p <= p1; ++p) m = fmaxf(m, a.part_ml[place(p) * 2]);
     float sum = 0.0f;
     float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
     for (int p = p0; p <= p1; ++p) {
       const int64_t at = place(p);
       const float2 w = *reinterpret_cast<const float2*>(a.part_ml + at * 2);

@@ -384,6 +384,14 @@ def test_attention_of_long_chunks(F, dtype, fmt, d, page, window, n_sink):
                hints=((300, 2001), (300, 500), (300, 0), (1, 2001)), spoil=True)
 
 
+@pytest.mark.parametrize("dtype,fmt,d,window,n_sink", [("bf16", "int8", 128, 0, 0), ("f16", "e4m3", 64, 900, 20)])
+def test_attention_of_few_row_tiles(F, dtype, fmt, d, window, n_sink):
+    """Few row tiles against many workgroups: shares of the least length, a row tile joined from many of them."""
+    rng = np.random.default_rng(22)
+    check_attn(F, rng, [33, 0, 64, 1], [2500, 0, 1100, 3], 64, 2, 1, d, dtype, fmt, "half", d, window, n_sink,
+               hints=((64, 2533),), spoil=True)
+
+
 def test_thousands_of_sequences(F):
     """More sequences than a search looks at in one or two rounds, many of them without a row."""
     rng = np.random.default_rng(14)
