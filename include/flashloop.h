@@ -522,8 +522,8 @@ int fl_rope(const void* x, int64_t x_stride, const int32_t* pos, const float* ta
  * codes, k_scale and v_scale fp32 [num_pages, Hkv].  A stored value is scale * code.
  *   FL_KV_I8   : code is int8 in [-127, 127]          FL_KV_E4M3 : code is an OCP e4m3 number, the scale a power of two
  * Sequence b owns the pages block_table[b, 0 ..], int32 [B, max_pages]: position p is row p % page of page
- * block_table[b, p / page].  Entries outside [0, num_pages) are pages that are not there.  A page and head whose scale is not
- * finite reads as NaN.
+ * block_table[b, p / page].  Entries outside [0, num_pages) are pages that are not there.  A page and head whose scale is
+ * negative or not finite reads as NaN.
  *
  * A batch has T rows of new positions: rows cu[b] .. cu[b+1] - 1 (int32 [B + 1], ascending from 0) are the last
  * n = cu[b+1] - cu[b] positions of sequence b, whose length with them is lens[b] (int32 [B]): row cu[b] + t is position
@@ -574,7 +574,8 @@ int fl_paged_append(const void* k, int64_t k_stride, const void* v, int64_t v_st
  *   Hq a multiple of Hkv; window, n_sink >= 0; other limits as in (10).
  * Precision: q (rotated in fp32) is multiplied as fp16 relative to the row's largest magnitude, for FL_F16 with what that
  * rounding leaves as a second part; probabilities times their value's scale as fp16 relative to the largest such product of the
- * row; both against the exact codes.  Scores, sums and outputs are held in fp32.  With the index checks on, as in (10) (a page that is not there is no error here, nor is one that two sequences share).
+ * row; both against the exact codes.  Scores, sums and outputs are held in fp32.  Value scales may lie anywhere from 2^-112 (below:
+ * as 0; the append writes none between 0 and 2^-109) up, side by side: every key counts in the normaliser.  With the index checks on, as in (10) (a page that is not there is no error here, nor is one that two sequences share).
  * ---------------------------------------------------------------------------------------------- */
 size_t fl_paged_attn_ws(int B, int T, int Hq, int Hkv, int d, int page, int max_pages, int window, int n_sink, int max_q,
                         int max_len);

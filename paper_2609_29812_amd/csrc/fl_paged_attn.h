@@ -22,7 +22,7 @@ struct PagedAttnArgs {
   int share;                       // workgroups that the tiles of a batch are shared out to (many rows: per key/value head)
   int* ends;                       // many rows, shared out: units up to and with each row tile's
   int slots;                       // ... and how many row tiles there are at most
-  float *part, *part_ml;           // [T Hq][n_split][d] sums and [T Hq][n_split][2] references and normalisers
+  float *part, *part_ml;           // [T Hq][n_split][d] sums and [T Hq][n_split][4]: ref, top and normaliser (below), unused
 };
 
 // What a row tile works on: rows rho0 .. rho0 + rows - 1 of a sequence, a row being (position, head of the group) with the
@@ -250,19 +250,28 @@ __device__ __forceinline__ float max3(float x, float y, float z) {
   return __builtin_elementwise_maximum(__builtin_elementwise_maximum(x, y), z);
 }
 
-// What the value scale does.  A probability times its page's scale s is exp2(x + log2 s - ref): the running reference follows
-// that contribution, so fp16 holds it whatever the scales are, and its sum over one page divided by s is the page's part of
-// the normaliser.  A scale below 2^-60 counts as 2^-60; one that is not finite as 1 (the normaliser does not depend on it), with
-// a negative reciprocal, and the rows that see the page are made NaN.
-constexpr float kLeastScale = 0x1p-60f;
-__device__ __forceinline__ float key_scale(float s) { return fabsf(s) < INFINITY ? s : NAN; }
+// What the value scale does.  A row has two references.  `ref` follows the contributions x + log2 s of its keys (x: a score in
+// octaves, s: its page's scale), so exp2(x + log2 s - ref), a probability times its page's scale, stays within fp16's range whatever
+// the scales are; `top` follows the scores, and the normaliser is held in units of 2^top.  A page's part of it is the
+// sum of its contributions, times 2^(ref - top) / s.  That sum has room for 2^-126, so where ref - top - log2 s stays below kRoom
+// octaves, what it loses is below 2^-62 of the normaliser.  Above (a page of values far smaller than those that carry the row) the
+// page's exponentials are taken once more, relative to `top`.  The output is sums * 2^(ref - top) / normaliser.
+// A scale below 2^-112 (the append writes none between 0 and 2^-109) counts as 0: it has kNoScale, and its products are 0.
+// One that is negative or not finite counts as 1 with a negative reciprocal (the normaliser does not depend on it), and the rows
+// that see the page are made NaN.
+constexpr float kRoom = 64.0f, kNoScale = -112.0f;
+__device__ __forceinline__ float key_scale(float s) { return s >= 0.0f && s < INFINITY ? s : NAN; }
 struct ValueScale {
   float log2, inv;
 };
 __device__ __forceinline__ ValueScale value_scale(float s) {
-  if (!(fabsf(s) < INFINITY)) return {0.0f, -1.0f};
-  s = fmaxf(s, kLeastScale);
+  if (!(s >= 0.0f && s < INFINITY)) return {0.0f, -1.0f};
+  if (s < 0x1p-112f) return {kNoScale, 0x1p112f};
   return {__builtin_amdgcn_logf(s), 1.0f / s};
+}
+// 2^(ref - top); 1 for a row that has seen nothing, or nothing but NaN
+__device__ __forceinline__ float ref_to_top(float ref, float top) {
+  return ref == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ref - top);
 }
 
 // The work of a head, row tile after row tile, cut into shares of `per`: unit x belongs to workgroup owner(x).  A row tile is

@@ -27,10 +27,10 @@ __global__ __launch_bounds__(256, NR == 1 ? (F16 ? 3 : 4) : 2) void paged_token_
   constexpr int KW = D / 64;              // 16-byte loads of a lane per key group
   constexpr int VW = D / 64;              // words of a lane per key of V
   constexpr int LD = D + 4;               // row stride of the waves' sums in LDS
-  __shared__ float s_ref[4][R], s_sum[4][R];
+  __shared__ float s_ref[4][R], s_top[4][R], s_sum[4][R];
   __shared__ __attribute__((aligned(16))) float s_acc[4][16][LD];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int r16 = lane & 15, g4 = lane >> 4;
+  int r16 = lane & 15, g4 = lane >> 4;
   const int kvh = blockIdx.x % a.pg.heads;
   const int slot = blockIdx.x / a.pg.heads;
   const int G = a.G;
@@ -103,10 +103,10 @@ __global__ __launch_bounds__(256, NR == 1 ? (F16 ? 3 : 4) : 2) void paged_token_
   const int all_max = sp.i_min, all_min = a.window > 0 && sp.i_max >= a.window ? sp.i_max - a.window + 1 : 0;
 
   f32x4 acc[NR][DT];
-  float ref[NR], lsum[NR];
+  float ref[NR], top[NR], lsum[NR];
 #pragma unroll
   for (int x = 0; x < NR; ++x) {
-    ref[x] = -INFINITY;
+    ref[x] = top[x] = -INFINITY;
     lsum[x] = 0.0f;
 #pragma unroll
     for (int t = 0; t < DT; ++t) acc[x][t] = f32x4{};
@@ -155,6 +155,7 @@ __global__ __launch_bounds__(256, NR == 1 ? (F16 ? 3 : 4) : 2) void paged_token_
       iv[h] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(iv_v), (c & 31) + 32 * h));
     }
     const bool spoilt = iv[0] < 0.0f || iv[1] < 0.0f;
+    const float least = fminf(lv[0], lv[1]);
     const bool masked = key0 + kTokenKeys - 1 > all_max || (key0 < all_min && key0 + kTokenKeys > a.n_sink) || (pid0 | pid1) < 0;
     f32x4 s[NR][2];
 #pragma unroll
@@ -181,11 +182,11 @@ __global__ __launch_bounds__(256, NR == 1 ? (F16 ? 3 : 4) : 2) void paged_token_
       }
     }
     if (more) load_k(c + 1);
-    if (masked && !I8) {                                     // codes behind the end may be NaN
+    if ((masked && !I8) || least <= kNoScale) {              // codes behind the end may be NaN; those of a scale of 0 count as 0
       const int hi = sp.i_max;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const bool there = key0 + (e >> 2) * 16 + g4 * 4 + (e & 3) <= hi && (e < 4 ? pid0 : pid1) >= 0;
+        const bool there = key0 + (e >> 2) * 16 + g4 * 4 + (e & 3) <= hi && (e < 4 ? pid0 : pid1) >= 0 && lv[e >> 2] > kNoScale;
 #pragma unroll
         for (int y = 0; y < VW; ++y) wv[e][y] = there ? wv[e][y] : 0u;
       }
@@ -193,7 +194,7 @@ __global__ __launch_bounds__(256, NR == 1 ? (F16 ? 3 : 4) : 2) void paged_token_
     f16x8 pf[NR];
 #pragma unroll
     for (int x = 0; x < NR; ++x) {
-      float y[2][4], top = -INFINITY;
+      float y[2][4], most = -INFINITY;                       // scores; the largest contribution
       bool see[2][4];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -208,20 +209,38 @@ __global__ __launch_bounds__(256, NR == 1 ? (F16 ? 3 : 4) : 2) void paged_token_
             y[h][i] = see[h][i] ? y[h][i] : -INFINITY;
           }
         }
-        top = fmaxf(top, max3(max3(y[h][0], y[h][1], y[h][2]), y[h][3], y[h][3]) + lv[h]);
+        most = fmaxf(most, max3(max3(y[h][0], y[h][1], y[h][2]), y[h][3], y[h][3]) + lv[h]);
       }
-      top = row4_max(top);
-      const bool raise = top > ref[x] + 8.0f;
+      most = row4_max(most);
+      auto best = [&] {                                      // the largest score
+        return row4_max(max3(max3(y[0][0], y[0][1], y[0][2]), max3(y[0][3], y[1][0], y[1][1]), max3(y[1][2], y[1][3], y[1][3])));
+      };
+      auto lift = [&](float to) {                            // the normaliser in units of a larger 2^top
+        if (to > top[x]) {
+          lsum[x] *= __builtin_amdgcn_exp2f(top[x] - to);
+          top[x] = to;
+        }
+      };
+      const bool raise = most > ref[x] + 8.0f;
       if (__builtin_amdgcn_ballot_w64(raise) != 0) {
-        const float nm = raise ? top : ref[x];
+        const float nm = raise ? most : ref[x];
         const float alpha = raise ? __builtin_amdgcn_exp2f(ref[x] - nm) : 1.0f;
-        lsum[x] *= alpha;
 #pragma unroll
         for (int t = 0; t < DT; ++t) acc[x][t] *= alpha;
         ref[x] = nm;
+        lift(best());
       }
       const float base = ref[x] == -INFINITY ? 0.0f : ref[x];
-      float p[2][4];
+      const bool apart = __builtin_amdgcn_ballot_w64(ref[x] - top[x] - least > kRoom) != 0;
+      if (apart) {
+        lift(best());
+        const float from = top[x] == -INFINITY ? 0.0f : top[x];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) lsum[x] += __builtin_amdgcn_exp2f(y[h][i] - from);
+      }
+      float p[2][4], sum = 0.0f;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const float off = lv[h] - base;
@@ -230,8 +249,9 @@ __global__ __launch_bounds__(256, NR == 1 ? (F16 ? 3 : 4) : 2) void paged_token_
           p[h][i] = __builtin_amdgcn_exp2f(y[h][i] + off);
         }
         const float part = (p[h][0] + p[h][1]) + (p[h][2] + p[h][3]);
-        lsum[x] = fmaf(part, fabsf(iv[h]), lsum[x]);
+        sum = fmaf(part, fabsf(iv[h]), sum);
       }
+      lsum[x] = fmaf(sum, apart ? 0.0f : ref_to_top(ref[x], top[x]), lsum[x]);
       if (spoilt) {                                          // a value scale that is not finite: the rows that see it
         bool any = false;
 #pragma unroll
@@ -281,12 +301,17 @@ __global__ __launch_bounds__(256, NR == 1 ? (F16 ? 3 : 4) : 2) void paged_token_
     }
   }
 
-  // the four waves' states of a row meet in LDS
+  // the four waves' states of a row meet in LDS (the lane's place is formed anew: kept over the loop, it spilled)
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));
+  r16 = tid & 15;
+  g4 = (tid & 63) >> 4;
 #pragma unroll
   for (int x = 0; x < NR; ++x) {
     lsum[x] = row4_add(lsum[x]);
     if (g4 == 0) {
       s_ref[wave][x * 16 + r16] = ref[x];
+      s_top[wave][x * 16 + r16] = top[x];
       s_sum[wave][x * 16 + r16] = lsum[x];
     }
   }
@@ -305,14 +330,15 @@ __global__ __launch_bounds__(256, NR == 1 ? (F16 ? 3 : 4) : 2) void paged_token_
             make_float4(acc[x][t][i] * f, acc[x][t + 1][i] * f, acc[x][t + 2][i] * f, acc[x][t + 3][i] * f);
     __syncthreads();
     constexpr int CPR = D / 4;                               // four channels a thread
-    for (int w = threadIdx.x; w < 16 * CPR; w += 256) {
+    for (int w = tid; w < 16 * CPR; w += 256) {
       const int row = w / CPR, c = (w % CPR) * 4, rx = x * 16 + row;
       if (rx >= sp.rows) continue;
       const float mm = fmaxf(fmaxf(s_ref[0][rx], s_ref[1][rx]), fmaxf(s_ref[2][rx], s_ref[3][rx]));
+      const float mt = fmaxf(fmaxf(s_top[0][rx], s_top[1][rx]), fmaxf(s_top[2][rx], s_top[3][rx]));
       float sum = 0.0f;
 #pragma unroll
       for (int v = 0; v < 4; ++v)                            // (a sum of NaN scores has no reference, but counts)
-        sum += s_ref[v][rx] == -INFINITY && s_sum[v][rx] == 0.0f ? 0.0f : s_sum[v][rx] * __builtin_amdgcn_exp2f(s_ref[v][rx] - mm);
+        sum += s_top[v][rx] == -INFINITY && s_sum[v][rx] == 0.0f ? 0.0f : s_sum[v][rx] * __builtin_amdgcn_exp2f(s_top[v][rx] - mt);
       float o[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[e] = (s_acc[0][row][c + e] + s_acc[1][row][c + e]) + (s_acc[2][row][c + e] + s_acc[3][row][c + e]);
@@ -320,14 +346,14 @@ __global__ __launch_bounds__(256, NR == 1 ? (F16 ? 3 : 4) : 2) void paged_token_
       const int64_t gr = (int64_t)(sp.r0 + t) * a.Hq + h;
       if (sp.parts > 1) {
         *reinterpret_cast<float4*>(a.part + (gr * a.n_split + split) * D + c) = make_float4(o[0], o[1], o[2], o[3]);
-        if (c == 0) *reinterpret_cast<float2*>(a.part_ml + (gr * a.n_split + split) * 2) = make_float2(mm, sum);
+        if (c == 0) *reinterpret_cast<float4*>(a.part_ml + (gr * a.n_split + split) * 4) = make_float4(mm, mt, sum, 0.0f);
       } else {
-        const bool none = mm == -INFINITY && sum == 0.0f;
-        const float inv = none ? 0.0f : 1.0f / sum;
+        const bool none = mt == -INFINITY && sum == 0.0f;
+        const float inv = none ? 0.0f : ref_to_top(mm, mt) / sum;
         const u32x2 two = {F16 ? pack_f16x2(o[0] * inv, o[1] * inv) : pack_bf16x2(o[0] * inv, o[1] * inv),
                            F16 ? pack_f16x2(o[2] * inv, o[3] * inv) : pack_bf16x2(o[2] * inv, o[3] * inv)};
         *reinterpret_cast<u32x2*>(a.o + (int64_t)(sp.r0 + t) * a.os + (int64_t)h * D + c) = two;
-        if (c == 0 && a.lse) a.lse[gr] = none ? -INFINITY : (mm + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+        if (c == 0 && a.lse) a.lse[gr] = none ? -INFINITY : (mt + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
       }
     }
   }
@@ -339,7 +365,7 @@ constexpr int kMaxSplit = 256;
 template <int D, int R, int KT, bool F16>
 __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
   constexpr int LN = D / 4, NG = 256 / LN;
-  __shared__ float s_f[kMaxSplit], s_w[2][4];
+  __shared__ float s_f[kMaxSplit], s_w[3][4];
   __shared__ float4 s_o[NG][LN];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int t = blockIdx.x / a.Hq, h = blockIdx.x % a.Hq;
@@ -349,17 +375,24 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
   cut(sp, Shares<R, KT>(a).parts(sq.r1 - sq.r0, sq.len));
   if (sp.parts <= 1) return;
   const int64_t gr = blockIdx.x;
-  float2 w = make_float2(-INFINITY, 0.0f);
-  if ((int)threadIdx.x < sp.parts) w = reinterpret_cast<const float2*>(a.part_ml)[gr * a.n_split + threadIdx.x];
-  float m = w.x;
+  float4 w = make_float4(-INFINITY, -INFINITY, 0.0f, 0.0f);  // ref, top, normaliser
+  if ((int)threadIdx.x < sp.parts) w = reinterpret_cast<const float4*>(a.part_ml)[gr * a.n_split + threadIdx.x];
+  float m = w.x, top = w.y;
 #pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
-  if (lane == 0) s_w[0][wave] = m;
+  for (int off = 32; off >= 1; off >>= 1) {
+    m = fmaxf(m, __shfl_xor(m, off, 64));
+    top = fmaxf(top, __shfl_xor(top, off, 64));
+  }
+  if (lane == 0) {
+    s_w[0][wave] = m;
+    s_w[2][wave] = top;
+  }
   __syncthreads();
   m = fmaxf(fmaxf(s_w[0][0], s_w[0][1]), fmaxf(s_w[0][2], s_w[0][3]));
-  const float f = w.x == -INFINITY && w.y == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(w.x - m);
-  float sum = f * w.y;
-  s_f[threadIdx.x] = f;
+  top = fmaxf(fmaxf(s_w[2][0], s_w[2][1]), fmaxf(s_w[2][2], s_w[2][3]));
+  const bool idle = w.y == -INFINITY && w.z == 0.0f;
+  float sum = idle ? 0.0f : w.z * __builtin_amdgcn_exp2f(w.y - top);
+  s_f[threadIdx.x] = idle ? 0.0f : __builtin_amdgcn_exp2f(w.x - m);
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off, 64);
   if (lane == 0) s_w[1][wave] = sum;
@@ -385,12 +418,12 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
     const float4 x = s_o[s][c];
     o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
   }
-  const bool none = m == -INFINITY && sum == 0.0f;
-  const float inv = none ? 0.0f : 1.0f / sum;
+  const bool none = top == -INFINITY && sum == 0.0f;
+  const float inv = none ? 0.0f : ref_to_top(m, top) / sum;
   *reinterpret_cast<u32x2*>(a.o + (int64_t)t * a.os + (int64_t)h * D + 4 * c) =
       u32x2{F16 ? pack_f16x2(o.x * inv, o.y * inv) : pack_bf16x2(o.x * inv, o.y * inv),
             F16 ? pack_f16x2(o.z * inv, o.w * inv) : pack_bf16x2(o.z * inv, o.w * inv)};
-  if (a.lse && c == 0) a.lse[gr] = none ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+  if (a.lse && c == 0) a.lse[gr] = none ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
 }
 
 template <int R, int KT>
@@ -461,7 +494,7 @@ static Plan plan_of(int B, int T, int Hq, int Hkv, int d, int page, int max_page
   p.min_tiles = kLeastTiles;
   const int64_t split = units < kShare ? std::min<int64_t>(std::max<int64_t>(tiles / kLeastTiles, 1), kMaxSplit) : 1;
   p.n_split = (int)split;
-  p.ws = split > 1 ? (size_t)T * Hq * split * (d + 2) * sizeof(float) : 0;
+  p.ws = split > 1 ? (size_t)T * Hq * split * (d + 4) * sizeof(float) : 0;
   return p;
 }
 

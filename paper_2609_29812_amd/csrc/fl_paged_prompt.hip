@@ -244,7 +244,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttnArgs a) {
   f32x16 acc[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) acc[db] = f32x16{};
-  float ref = -INFINITY, lsum = 0.0f;
+  float ref = -INFINITY, top = -INFINITY, lsum = 0.0f;
 
   auto compute = [&](const PromptSlot<D>& sl, int st) __attribute__((always_inline)) {
     const int key0 = key_of<COLS>(sp, t0 + st);
@@ -262,7 +262,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttnArgs a) {
         if constexpr (F16)
           if (a.rt.table) s[x] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, w), ql[ks], s[x], 0, 0, 0);
       }
-    float mg[2 * NBK], lv[2 * NBK], iv[2 * NBK];
+    float mg[2 * NBK], lv[2 * NBK], iv[2 * NBK], least = INFINITY;
     int gone = 0;
     bool spoilt = false;
 #pragma unroll
@@ -273,6 +273,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttnArgs a) {
       iv[g] = w.z;
       gone |= __float_as_int(w.w);
       spoilt |= w.z < 0.0f;
+      least = fminf(least, w.y);
     }
     const bool holes = __builtin_amdgcn_readfirstlane(gone) < 0;
     if (key0 + COLS - 1 > w_min || (key0 < w_all && key0 + COLS > a.n_sink) || holes) {    // uniform
@@ -288,24 +289,48 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttnArgs a) {
         mg[g] = 1.0f;
       }
     }
-    float top = -INFINITY;
-#pragma unroll
-    for (int g = 0; g < 2 * NBK; ++g) {
+    auto largest = [&](int g) {                                       // of a group's products
       const int x = g >> 1, v0 = 8 * (g & 1);
       const float m0 = max3(s[x][v0], s[x][v0 + 1], s[x][v0 + 2]), m1 = max3(s[x][v0 + 3], s[x][v0 + 4], s[x][v0 + 5]);
-      top = fmaxf(top, fmaf(max3(max3(m0, s[x][v0 + 6], s[x][v0 + 7]), m1, m1), mg[g], lv[g]));
-    }
-    top = xor32_max(top);
-    const bool raise = top > ref + 8.0f;
+      return max3(max3(m0, s[x][v0 + 6], s[x][v0 + 7]), m1, m1);
+    };
+    float most = -INFINITY;                                           // contribution
+#pragma unroll
+    for (int g = 0; g < 2 * NBK; ++g) most = fmaxf(most, fmaf(largest(g), mg[g], lv[g]));
+    most = xor32_max(most);
+    auto lift = [&] {                                                 // the normaliser in units of the largest score
+      float to = -INFINITY;
+#pragma unroll
+      for (int g = 0; g < 2 * NBK; ++g) to = fmaxf(to, largest(g) * mg[g]);
+      to = xor32_max(to);
+      if (to > top) {
+        lsum *= __builtin_amdgcn_exp2f(top - to);
+        top = to;
+      }
+    };
+    const bool raise = most > ref + 8.0f;
     if (__builtin_amdgcn_ballot_w64(raise) != 0) {
-      const float nm = raise ? top : ref;
+      const float nm = raise ? most : ref;
       const float alpha = raise ? __builtin_amdgcn_exp2f(ref - nm) : 1.0f;
-      lsum *= alpha;
 #pragma unroll
       for (int db = 0; db < DB; ++db) acc[db] *= alpha;
       ref = nm;
+      lift();
     }
     const float base = ref == -INFINITY ? 0.0f : ref;
+    float share = ref_to_top(ref, top);
+    if (__builtin_amdgcn_ballot_w64((least <= kNoScale) | (ref - top - least > kRoom)) != 0) {
+      lift();
+      const float from = top == -INFINITY ? 0.0f : top;
+      share = 0.0f;
+#pragma unroll
+      for (int g = 0; g < 2 * NBK; ++g) {
+#pragma unroll
+        for (int v = 8 * (g & 1); v < 8 * (g & 1) + 8; ++v)
+          lsum += __builtin_amdgcn_exp2f(__builtin_fmaf(s[g >> 1][v], mg[g], -from));
+        lv[g] = lv[g] <= kNoScale ? -INFINITY : lv[g];
+      }
+    }
     if (__builtin_amdgcn_ballot_w64(spoilt) != 0) {                   // a value scale that is not finite: the rows that see it
       bool any = false;
 #pragma unroll
@@ -316,6 +341,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttnArgs a) {
 #pragma unroll
       for (int db = 0; db < DB; ++db) acc[db] += bad;
     }
+    float sum = 0.0f;                                                 // the stage's part of the normaliser, in units of 2^ref
 #pragma unroll
     for (int x = 0; x < NBK; ++x) {
       float pr[16];
@@ -328,7 +354,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttnArgs a) {
           pr[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][v], mg[2 * x + g], off));
           ts[v & 1] += pr[v];
         }
-        lsum = fmaf(ts[0] + ts[1], fabsf(iv[2 * x + g]), lsum);
+        sum = fmaf(ts[0] + ts[1], fabsf(iv[2 * x + g]), sum);
       }
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) {
@@ -345,6 +371,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttnArgs a) {
         }
       }
     }
+    lsum = fmaf(sum, share, lsum);
   };
 
   if (n > 0) {
@@ -373,7 +400,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttnArgs a) {
   }
   lsum = xor32_add(lsum);
   const int64_t gr = (int64_t)(sp.r0 + tok) * a.Hq + head;
-  const bool none = ref == -INFINITY && lsum == 0.0f;
+  const bool none = top == -INFINITY && lsum == 0.0f;
   if (SHARED && row_ok && !whole) {
     // a share cuts at most two row tiles: the one it begins with and the one it ends with
     const int64_t row = ((int64_t)(kvh * a.share + wg) * 2 + place) * R + rr;
@@ -384,10 +411,10 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttnArgs a) {
       for (int j = 0; j < 4; ++j)
         *reinterpret_cast<float4*>(out + db * 32 + 8 * j) =
             make_float4(acc[db][4 * j], acc[db][4 * j + 1], acc[db][4 * j + 2], acc[db][4 * j + 3]);
-    if (hw == 0) *reinterpret_cast<float2*>(a.part_ml + row * 2) = make_float2(ref, lsum);
+    if (hw == 0) *reinterpret_cast<float4*>(a.part_ml + row * 4) = make_float4(ref, top, lsum, 0.0f);
   }
   if (row_ok && whole) {
-  const float inv = none ? 0.0f : 1.0f / lsum;
+  const float inv = none ? 0.0f : ref_to_top(ref, top) / lsum;
   uint16_t* out = a.o + (int64_t)(sp.r0 + tok) * a.os + (int64_t)head * D + 4 * hw;
 #pragma unroll
   for (int db = 0; db < DB; ++db)
@@ -399,7 +426,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttnArgs a) {
       *reinterpret_cast<u32x2*>(out + db * 32 + 8 * j) = u32x2{F16 ? pack_f16x2(o[0], o[1]) : pack_bf16x2(o[0], o[1]),
                                                                F16 ? pack_f16x2(o[2], o[3]) : pack_bf16x2(o[2], o[3])};
     }
-  if (hw == 0 && a.lse) a.lse[gr] = none ? -INFINITY : (ref + __builtin_amdgcn_logf(lsum)) * 0.6931471805599453f;
+  if (hw == 0 && a.lse) a.lse[gr] = none ? -INFINITY : (top + __builtin_amdgcn_logf(lsum)) * 0.6931471805599453f;
  }
   }
 }
@@ -423,31 +450,37 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a) {
   const int c = threadIdx.x % LN;
   for (int rr = r0 + threadIdx.x / LN; rr < min(r0 + 32, sp.rows); rr += 256 / LN) {
     auto place = [&](int p) { return ((int64_t)(kvh * a.share + p) * 2 + (max(begin, cut.begin(p)) == cut.begin(p) ? 0 : 1)) * R + rr; };
-    float m = -INFINITY;
+    const float4* ml = reinterpret_cast<const float4*>(a.part_ml);
+    float m = -INFINITY, top = -INFINITY;
 #pragma unroll 4
-    for (int p = p0; p <= p1; ++p) m = fmaxf(m, a.part_ml[place(p) * 2]);
+    for (int p = p0; p <= p1; ++p) {
+      const float4 w = ml[place(p)];
+      m = fmaxf(m, w.x);
+      top = fmaxf(top, w.y);
+    }
     float sum = 0.0f;
     float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 4
     for (int p = p0; p <= p1; ++p) {
       const int64_t at = place(p);
-      const float2 w = *reinterpret_cast<const float2*>(a.part_ml + at * 2);
+      const float4 w = ml[at];
       const float4 x = *reinterpret_cast<const float4*>(a.part + at * D + 4 * c);
-      const float f = w.x == -INFINITY && w.y == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(w.x - m);
-      sum = fmaf(f, w.y, sum);
+      const bool idle = w.y == -INFINITY && w.z == 0.0f;
+      const float f = idle ? 0.0f : __builtin_amdgcn_exp2f(w.x - m);
+      sum = fmaf(idle ? 0.0f : __builtin_amdgcn_exp2f(w.y - top), w.z, sum);
       o.x = fmaf(f, x.x, o.x);
       o.y = fmaf(f, x.y, o.y);
       o.z = fmaf(f, x.z, o.z);
       o.w = fmaf(f, x.w, o.w);
     }
-    const bool none = m == -INFINITY && sum == 0.0f;
-    const float inv = none ? 0.0f : 1.0f / sum;
+    const bool none = top == -INFINITY && sum == 0.0f;
+    const float inv = none ? 0.0f : ref_to_top(m, top) / sum;
     const int rho = sp.rho0 + rr, tok = rho / G, head = kvh * G + rho % G;
     *reinterpret_cast<u32x2*>(a.o + (int64_t)(sp.r0 + tok) * a.os + (int64_t)head * D + 4 * c) =
         u32x2{F16 ? pack_f16x2(o.x * inv, o.y * inv) : pack_bf16x2(o.x * inv, o.y * inv),
               F16 ? pack_f16x2(o.z * inv, o.w * inv) : pack_bf16x2(o.z * inv, o.w * inv)};
     if (a.lse && c == 0)
-      a.lse[(int64_t)(sp.r0 + tok) * a.Hq + head] = none ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+      a.lse[(int64_t)(sp.r0 + tok) * a.Hq + head] = none ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
   }
 }
 
@@ -461,7 +494,7 @@ static bool is_shared(int64_t slots, int Hkv, int64_t cap, int64_t keys) {
 }
 size_t paged_prompt_ws(int64_t slots, int Hkv, int d, int64_t cap, int64_t keys) {
   if (!is_shared(slots, Hkv, cap, keys)) return 0;
-  return (size_t)shares_of(Hkv) * Hkv * 2 * kPromptRows * (d + 2) * sizeof(float) + (size_t)slots * sizeof(int);
+  return (size_t)shares_of(Hkv) * Hkv * 2 * kPromptRows * (d + 4) * sizeof(float) + (size_t)slots * sizeof(int);
 }
 
 int launch_paged_prompt(const PagedAttnArgs& args, int d, int format, bool f16, int64_t keys, hipStream_t st) {
@@ -475,7 +508,7 @@ int launch_paged_prompt(const PagedAttnArgs& args, int d, int format, bool f16, 
   if (shared) {
     const size_t places = (size_t)a.share * a.pg.heads * 2 * kPromptRows;
     a.part_ml = a.part + places * d;
-    a.ends = reinterpret_cast<int*>(a.part_ml + places * 2);
+    a.ends = reinterpret_cast<int*>(a.part_ml + places * 4);
     paged_plan_kernel<<<1, 1024, 0, st>>>(a);
     rc = check_launch("paged_plan_kernel");
     if (rc != FL_OK) return rc;
