@@ -62,6 +62,11 @@ __device__ __forceinline__ Span span_of(const PagedAttnArgs& a, const Seq& q, in
   s.per = s.tiles;
   return s;
 }
+// whether some row of the tile sees key j (when its page is there)
+__device__ __forceinline__ bool seen_by_any(const PagedAttnArgs& a, const Span& s, int j) {
+  const int lo = a.window > 0 && s.i_min >= a.window ? s.i_min - a.window + 1 : 0;
+  return (j <= s.i_max) & ((j >= lo) | (j < a.n_sink));
+}
 
 // Split keys of few rows: the tiles of all sequences are shared out evenly, whatever the lengths are.  With `per` = all
 // (sequence, row tile, key/value head, tile)s / share, a sequence of t tiles gets ceil(t / per) parts (at most n_split), and

@@ -182,11 +182,11 @@ __global__ __launch_bounds__(256, NR == 1 ? (F16 ? 3 : 4) : 2) void paged_token_
       }
     }
     if (more) load_k(c + 1);
-    if ((masked && !I8) || least <= kNoScale) {              // codes behind the end may be NaN; those of a scale of 0 count as 0
-      const int hi = sp.i_max;
+    if ((masked && !I8) || least <= kNoScale) {              // codes that no row sees may be NaN; those of a scale of 0 count as 0
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const bool there = key0 + (e >> 2) * 16 + g4 * 4 + (e & 3) <= hi && (e < 4 ? pid0 : pid1) >= 0 && lv[e >> 2] > kNoScale;
+        const bool there = seen_by_any(a, sp, key0 + (e >> 2) * 16 + g4 * 4 + (e & 3)) && (e < 4 ? pid0 : pid1) >= 0 &&
+                           lv[e >> 2] > kNoScale;
 #pragma unroll
         for (int y = 0; y < VW; ++y) wv[e][y] = there ? wv[e][y] : 0u;
       }

@@ -205,9 +205,9 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttnArgs a) {
 #pragma unroll
     for (int x = 0; x < NI; ++x) {
       const int key = x * (256 / LPK) + lane_key;
-      if constexpr (!I8) {                                            // codes behind the end may be NaN
+      if constexpr (!I8) {                                            // codes that no row sees may be NaN
         const float gone = s_page[(st / kAhead) & 1][(st % kAhead) * 4 + (key >> 4)].w;
-        const bool there = (__float_as_int(gone) >= 0) & (key_of<COLS>(sp, t0 + st) + key <= sp.i_max);
+        const bool there = (__float_as_int(gone) >= 0) & seen_by_any(a, sp, key_of<COLS>(sp, t0 + st) + key);
 #pragma unroll
         for (int e = 0; e < 4; ++e) vw[x][e] = there ? vw[x][e] : 0u;
       }

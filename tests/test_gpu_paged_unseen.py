@@ -1,0 +1,47 @@
+"""Attention over the paged cache beside what no row sees: freed pages between the leading positions and the window that still
+have an entry in the block table, whatever they hold."""
+import numpy as np
+import pytest
+import torch
+
+from gpu_util import say
+from test_gpu_paged import DT, batch, check_attn, dev_codes, i32, make_cache
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("fmt,dtype", [("e4m3", "bf16"), ("e4m3", "f16"), ("int8", "bf16")])
+@pytest.mark.parametrize("new,past,page,window,n_sink,d", [([1, 1, 1], [1000, 200, 40], 16, 50, 5, 64),
+                                                           ([3, 2], [2100, 130], 16, 70, 17, 128),
+                                                           ([6, 1], [500, 300], 32, 33, 0, 64),
+                                                           ([150, 40], [1300, 90], 16, 60, 20, 128),
+                                                           ([70, 200], [400, 0], 32, 37, 3, 64),
+                                                           ([300], [1500], 128, 200, 1, 128)])
+def test_freed_pages_that_hold_anything(F, new, past, page, window, n_sink, d, fmt, dtype):
+    """Entries of freed pages name a spare page of NaN codes and scales that are not finite: the bits of a table without them."""
+    rng = np.random.default_rng(len(new) + page)
+    cu, lens, tab, n_pages = batch(rng, new, past, page)
+    codes, scale = make_cache(rng, n_pages + 2, 2, page, d, fmt)
+    gone = tab.copy()
+    for b, n in enumerate(new):
+        first = max(0, lens[b] - n - window + 1) // page
+        gone[b, -(-n_sink // page):first] = -1
+    spare = np.where((gone < 0) & (tab >= 0), n_pages + np.arange(tab.shape[1]) % 2, tab)
+    assert (spare != tab).any()
+    codes[0][n_pages:], codes[1][n_pages:] = 255, 127
+    scale[0][n_pages:], scale[1][n_pages], scale[1][n_pages + 1] = np.nan, np.inf, 1.0
+    args = (dev_codes(codes[0], fmt), dev_codes(codes[1], fmt), torch.from_numpy(scale[0]).cuda(), torch.from_numpy(scale[1]).cuda())
+    q = torch.from_numpy(rng.normal(size=(int(cu[-1]), 6, d))).to(DT[dtype]).cuda()
+    for max_q, max_len in ((None, 0), (1, 0), (max(new), 4000), (200, 500)):
+        say(f"  new={new} past={past} page={page} {fmt} {dtype} w={window}+{n_sink} hint={max_q},{max_len}")
+        one, two = (F.paged_attn(q, i32(cu), i32(lens), i32(t), *args, window=window, n_sink=n_sink, max_q=max_q, max_len=max_len)
+                    for t in (gone, spare))
+        assert torch.isfinite(one).all() and torch.equal(one, two)
+
+
+def test_the_same_against_the_oracle(F):
+    """Pages of nobody and positions behind the end hold NaN; the block table is whole."""
+    rng = np.random.default_rng(3)
+    for new, past in (([1, 2], [300, 70]), ([90, 40], [250, 0])):
+        check_attn(F, rng, new, past, 16, 4, 2, 64, "bf16", "e4m3", window=45, n_sink=6, hints=((None, 0), (1, 1000), (90, 2000)),
+                   spoil=True)
