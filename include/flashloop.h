@@ -562,7 +562,9 @@ int fl_paged_append(const void* k, int64_t k_stride, const void* v, int64_t v_st
  * h / (Hq / Hkv)), with q rotated by its position when `table` is given,
  *     o_t = sum_j p_j v_j,   p_j = exp(sm_scale q . k_j - lse_t),   lse_t = ln sum_j exp(sm_scale q . k_j)
  * over the stored positions j <= i of its sequence with, when window > 0, j > i - window or j < n_sink.  Positions whose page
- * is not there are seen by no row.  A row that sees nothing gets o = 0 and lse = -inf.  What no row sees is of no effect, whatever
+ * is not there are seen by no row.  A row that sees nothing gets o = 0 and lse = -inf.  A position at or
+ * behind max_pages * page (the index checks refuse it) sees the stored keys that its window leaves, its query turned by the last
+ * position of the block table.  What no row sees is of no effect, whatever
  * its codes and scales are: pages outside the window may belong to another sequence, or hold nothing yet.
  *   q          : [T, Hq, d] of `dtype`, q_stride elements from one row to the next (a multiple of 8), 16-byte aligned.
  *   cu, lens, B, T, table, block_table, page, format and the caches: as in (10), after the append.

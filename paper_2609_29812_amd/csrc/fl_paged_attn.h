@@ -54,7 +54,7 @@ __device__ __forceinline__ Span span_of(const PagedAttnArgs& a, const Seq& q, in
   s.i_max = s.start + (s.rho0 + s.rows - 1) / a.G;
   const int hi = min(s.i_max, cap - 1);
   int lo = 0;
-  if (a.window > 0 && s.i_min >= a.window) lo = s.i_min - a.window + 1;
+  if (a.window > 0 && s.i_min >= a.window) lo = min(s.i_min - a.window + 1, cap);    // (a length beyond the block table)
   s.n_lead = (min(a.n_sink, lo) + KT - 1) / KT;
   s.first = max(s.n_lead, lo / KT);
   s.tiles = hi < 0 ? 0 : s.n_lead + max(hi / KT - s.first + 1, 0);
@@ -148,8 +148,8 @@ template <int KT>
 __device__ __forceinline__ int key_of(const Span& s, int tile) { return (tile < s.n_lead ? tile : tile - s.n_lead + s.first) * KT; }
 
 // The chunks of eight channels ch(0) .. ch(N - 1) of a query row as fp16 relative to the row's largest magnitude (2^-e, e its
-// exponent, so that no range is lost), rotated by its position `pos` in fp32 when there is a table (a position outside it,
-// which sees nothing, as if at its border).  `most` takes the largest magnitude of the lane to that of the row.  The row's
+// exponent, so that no range is lost), rotated by its position `pos` in fp32 when there is a table (a position outside the block
+// table as if at its border).  `most` takes the largest magnitude of the lane to that of the row.  The row's
 // factor comes back.  Loads stand in front and under no branch that lanes could take apart: a row costs two rounds of them.
 __device__ __forceinline__ float row_down(float m) {
   const int e = min(max((int)(__float_as_uint(m) >> 23), 1), 253);

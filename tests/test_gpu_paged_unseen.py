@@ -1,11 +1,12 @@
 """Attention over the paged cache beside what no row sees: freed pages between the leading positions and the window that still
-have an entry in the block table, whatever they hold."""
+have an entry in the block table, whatever they hold; lengths beyond the block table."""
 import numpy as np
 import pytest
 import torch
 
 from gpu_util import say
-from test_gpu_paged import DT, batch, check_attn, dev_codes, i32, make_cache
+from oracle import paged
+from test_gpu_paged import DT, batch, check_attn, dev_codes, f64, i32, make_cache
 
 pytestmark = pytest.mark.gpu
 
@@ -45,3 +46,25 @@ def test_the_same_against_the_oracle(F):
     for new, past in (([1, 2], [300, 70]), ([90, 40], [250, 0])):
         check_attn(F, rng, new, past, 16, 4, 2, 64, "bf16", "e4m3", window=45, n_sink=6, hints=((None, 0), (1, 1000), (90, 2000)),
                    spoil=True)
+
+
+@pytest.mark.parametrize("window,n_sink", [(30, 20), (30, 2 ** 31 - 1), (1500, 2 ** 30), (2 ** 31 - 1, 0), (0, 7)])
+def test_lengths_beyond_the_block_table(F, window, n_sink):
+    """Positions behind the last page see what the window and the leading positions leave of the stored ones."""
+    rng = np.random.default_rng(4)
+    for new, lens in (([1, 2], [2 ** 31 - 1, 100000]), ([300, 40], [2 ** 31 - 1, 1700])):
+        max_pages, page = 100, 16
+        cu = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+        tab = rng.permutation(2 * max_pages).reshape(2, max_pages).astype(np.int32)
+        codes, scale = make_cache(rng, 2 * max_pages, 1, page, 64, "int8")
+        q = torch.from_numpy(rng.normal(size=(int(cu[-1]), 2, 64))).to(torch.bfloat16)
+        want, wlse, av, aq, aw = paged.attend(f64(q), cu, np.array(lens), tab, *codes, *scale, "int8", 0.125, window, n_sink)
+        args = (i32(cu), i32(lens), i32(tab), dev_codes(codes[0], "int8"), dev_codes(codes[1], "int8"),
+                torch.from_numpy(scale[0]).cuda(), torch.from_numpy(scale[1]).cuda())
+        tol = (2 * 2.0 ** -11 * aq[..., None] + 2.0 ** -10 + 1700 * 2.0 ** -23) * av + 2.0 ** -25 * aw + 2.0 ** -8 * np.abs(want)
+        for max_q, max_len in ((1, 0), (300, 0), (300, 100)):
+            say(f"  new={new} w={window}+{n_sink} hint={max_q},{max_len}")
+            lse = torch.empty(q.shape[:2], device="cuda")
+            got = F.paged_attn(q.cuda(), *args, window=window, n_sink=n_sink, max_q=max_q, max_len=max_len, lse=lse)
+            assert np.all(np.abs(f64(got) - want) <= tol)
+            assert np.array_equal(np.isneginf(f64(lse)), np.isneginf(wlse))
