@@ -21,8 +21,8 @@ struct PagedAttnArgs {
   int n_split, min_tiles;          // at most n_split parts of the keys, each of about min_tiles tiles or more
   int share;                       // workgroups that the tiles of a batch are shared out to (many rows: per key/value head)
   int* ends;                       // many rows, shared out: units up to and with each row tile's
-  int slots;                       // ... and how many row tiles there are at most
-  float *part, *part_ml;           // [T Hq][n_split][d] sums and [T Hq][n_split][4]: ref, top and normaliser (below), unused
+  int slots;                       // work items of a head at most: row tiles, with split keys of few rows their parts too
+  float *part, *part_ml;           // rows of a split work item: [..][d] sums and [..][4]: ref, top and normaliser (below), unused
 };
 
 // What a row tile works on: rows rho0 .. rho0 + rows - 1 of a sequence, a row being (position, head of the group) with the
@@ -106,6 +106,19 @@ struct Shares {
   }
   __device__ __forceinline__ int parts(int n, int len) const {
     return min(max((tiles(n, len) + per - 1) / per, 1), a.n_split);
+  }
+  // items of the sequences before sequence `seq`
+  __device__ __forceinline__ int before(int seq) const {
+    const int lane = threadIdx.x & 63;
+    int sum = 0;
+    for (int b0 = 0; b0 < seq; b0 += 64) {
+      int x0 = r0, x1 = r1, xl = len;
+      if (b0 > 0) load(b0 + lane, x0, x1, xl);
+      sum += b0 + lane < seq ? row_tiles(x1 - x0) * parts(x1 - x0, xl) : 0;
+    }
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off, 64);
+    return sum;
   }
   // the sequence of item u, the row tile and the part; seq.b = -1 behind the last
   __device__ __forceinline__ Seq find(int u, int& tile, int& part) const {

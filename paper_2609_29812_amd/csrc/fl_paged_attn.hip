@@ -345,8 +345,9 @@ __global__ __launch_bounds__(256, NR == 1 ? (F16 ? 3 : 4) : 2) void paged_token_
       const int rho = sp.rho0 + rx, t = rho / G, h = kvh * G + rho % G;
       const int64_t gr = (int64_t)(sp.r0 + t) * a.Hq + h;
       if (sp.parts > 1) {
-        *reinterpret_cast<float4*>(a.part + (gr * a.n_split + split) * D + c) = make_float4(o[0], o[1], o[2], o[3]);
-        if (c == 0) *reinterpret_cast<float4*>(a.part_ml + (gr * a.n_split + split) * 4) = make_float4(mm, mt, sum, 0.0f);
+        const int64_t at = (int64_t)blockIdx.x * R + rx;
+        *reinterpret_cast<float4*>(a.part + at * D + c) = make_float4(o[0], o[1], o[2], o[3]);
+        if (c == 0) *reinterpret_cast<float4*>(a.part_ml + at * 4) = make_float4(mm, mt, sum, 0.0f);
       } else {
         const bool none = mt == -INFINITY && sum == 0.0f;
         const float inv = none ? 0.0f : ref_to_top(mm, mt) / sum;
@@ -371,12 +372,16 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
   const int t = blockIdx.x / a.Hq, h = blockIdx.x % a.Hq;
   const Seq sq = find_seq(a.bt, t, 0, [](int c) { return c; });
   if (sq.b < 0 || t >= sq.r1) return;
-  Span sp = span_of<R, KT>(a, sq, ((t - sq.r0) * a.G + h % a.G) / R);
-  cut(sp, Shares<R, KT>(a).parts(sq.r1 - sq.r0, sq.len));
-  if (sp.parts <= 1) return;
+  const Shares<R, KT> shares(a);
+  const int parts = shares.parts(sq.r1 - sq.r0, sq.len);
+  if (parts <= 1) return;
+  const int rho = (t - sq.r0) * a.G + h % a.G;
+  const int item = shares.before(sq.b) + rho / R * parts;    // the row tile's first; the parts follow
+  if (item < 0 || item + parts > a.slots) return;            // (offsets that do not ascend: nothing was written)
   const int64_t gr = blockIdx.x;
+  const int64_t first = ((int64_t)item * a.pg.heads + h / a.G) * R + rho % R, step = (int64_t)a.pg.heads * R;
   float4 w = make_float4(-INFINITY, -INFINITY, 0.0f, 0.0f);  // ref, top, normaliser
-  if ((int)threadIdx.x < sp.parts) w = reinterpret_cast<const float4*>(a.part_ml)[gr * a.n_split + threadIdx.x];
+  if ((int)threadIdx.x < parts) w = reinterpret_cast<const float4*>(a.part_ml)[first + threadIdx.x * step];
   float m = w.x, top = w.y;
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1) {
@@ -399,11 +404,11 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
   __syncthreads();
   sum = (s_w[1][0] + s_w[1][1]) + (s_w[1][2] + s_w[1][3]);
   const int c = threadIdx.x % LN, grp = threadIdx.x / LN;
-  const float4* src = reinterpret_cast<const float4*>(a.part + gr * a.n_split * D) + c;
+  const float4* src = reinterpret_cast<const float4*>(a.part + first * D) + c;
   float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 4
-  for (int s = grp; s < sp.parts; s += NG) {
-    const float4 x = src[(int64_t)s * LN];
+  for (int s = grp; s < parts; s += NG) {
+    const float4 x = src[s * step * LN];
     const float g = s_f[s];
     o.x = fmaf(g, x.x, o.x);
     o.y = fmaf(g, x.y, o.y);
@@ -439,12 +444,18 @@ static int launch_merge(const PagedAttnArgs& a, int d, bool f16, hipStream_t st)
   return check_launch("paged_merge_kernel");
 }
 
+// Work items of a head: row tiles, and with split keys as many parts more as the tiles are shared out to.
+static int64_t items_of(int T, int G, int B, int Hkv, int rows, int n_split, int share) {
+  return (int64_t)T * G / rows + B + (n_split > 1 ? share / Hkv + 1 : 0);
+}
+
 template <int NR>
-static int launch_token(const PagedAttnArgs& a, int d, int format, bool f16, hipStream_t st) {
-  // row tiles, and with split keys as many parts more as the tiles are shared out to
-  const int64_t slots = (int64_t)a.bt.T * a.G / (16 * NR) + a.bt.B;
-  const int64_t n = (slots + (a.n_split > 1 ? a.share / a.pg.heads + 1 : 0)) * a.pg.heads;
+static int launch_token(const PagedAttnArgs& args, int d, int format, bool f16, hipStream_t st) {
+  PagedAttnArgs a = args;
+  const int64_t items = items_of(a.bt.T, a.G, a.bt.B, a.pg.heads, 16 * NR, a.n_split, a.share), n = items * a.pg.heads;
   FL_REQUIRE(n < (1ll << 31), FL_E_SHAPE, "fl_paged_attn: too many rows");
+  a.slots = (int)items;
+  a.part_ml = a.part ? a.part + n * 16 * NR * d : nullptr;
   const unsigned grid = (unsigned)n;
 #define FL_TOKEN(DD)                                                                        \
   do {                                                                                      \
@@ -494,7 +505,8 @@ static Plan plan_of(int B, int T, int Hq, int Hkv, int d, int page, int max_page
   p.min_tiles = kLeastTiles;
   const int64_t split = units < kShare ? std::min<int64_t>(std::max<int64_t>(tiles / kLeastTiles, 1), kMaxSplit) : 1;
   p.n_split = (int)split;
-  p.ws = split > 1 ? (size_t)T * Hq * split * (d + 4) * sizeof(float) : 0;
+  // (a place for each row of each work item, however long the contexts are)
+  p.ws = split > 1 ? (size_t)items_of(T, (int)G, B, Hkv, p.rows, p.n_split, p.share) * Hkv * p.rows * (d + 4) * sizeof(float) : 0;
   return p;
 }
 
@@ -547,7 +559,6 @@ extern "C" int fl_paged_attn(const void* q, int64_t q_stride, int dtype, const i
   a.Hq = Hq; a.G = Hq / Hkv; a.scale_log2 = sm_scale * 1.4426950408889634f; a.window = window; a.n_sink = n_sink;
   a.n_split = p.n_split; a.min_tiles = p.min_tiles; a.share = p.share;
   a.part = static_cast<float*>(ws);
-  a.part_ml = a.part ? a.part + (size_t)T * Hq * p.n_split * d : nullptr;
   rc = check_batch(fn, a.bt, a.pg, false, st);
   if (rc != FL_OK) return rc;
   if (p.rows == 16) return launch_token<1>(a, d, format, dtype == FL_F16, st);

@@ -68,3 +68,23 @@ def test_lengths_beyond_the_block_table(F, window, n_sink):
             got = F.paged_attn(q.cuda(), *args, window=window, n_sink=n_sink, max_q=max_q, max_len=max_len, lse=lse)
             assert np.all(np.abs(f64(got) - want) <= tol)
             assert np.array_equal(np.isneginf(f64(lse)), np.isneginf(wlse))
+
+
+@pytest.mark.parametrize("new,past,Hq,Hkv,max_q", [([1] * 7, [3000, 1, 900, 40, 5000, 64, 0], 8, 2, 1), ([2, 0, 1], [9000, 10, 700], 12, 1, 2),
+                                                   ([1] * 150, [37 * i % 1500 for i in range(150)], 4, 2, 1),
+                                                   ([200, 0, 30], [1300, 5, 10], 4, 2, 200), ([3, 5], [2000, 4000], 16, 4, 1)])
+def test_the_workspace_is_enough(F, new, past, Hq, Hkv, max_q):
+    """A workspace of exactly the size asked for, between guards that stay as they are, whatever it held before."""
+    rng = np.random.default_rng(6)
+    cu, lens, tab, n_pages = batch(rng, new, past, 64)
+    codes, scale = make_cache(rng, n_pages, Hkv, 64, 64, "int8")
+    args = (i32(cu), i32(lens), i32(tab), dev_codes(codes[0], "int8"), dev_codes(codes[1], "int8"),
+            torch.from_numpy(scale[0]).cuda(), torch.from_numpy(scale[1]).cuda())
+    q = torch.from_numpy(rng.normal(size=(int(cu[-1]), Hq, 64))).to(torch.bfloat16).cuda()
+    one = F.paged_attn(q, *args, max_q=max_q)
+    need = F.paged_attn_ws(q, args[2], args[3], max_q=max_q).numel()
+    for fill in (0, 255):
+        room = torch.full((need + 2048,), fill, dtype=torch.uint8, device="cuda")
+        room[:1024], room[1024 + need:] = 85, 85
+        assert torch.equal(F.paged_attn(q, *args, max_q=max_q, ws=room[1024:1024 + need]), one)
+        assert torch.all(room[:1024] == 85) and torch.all(room[1024 + need:] == 85)

@@ -109,6 +109,20 @@ def test_attn_refusals(lib):
     assert b"fl_paged_attn" in lib.fl_last_error()
 
 
+def test_workspace_of_few_rows(lib):
+    """It holds a place for each row of the work items, which the chip's size bounds: not one for every part of every row, nor
+    more of them for longer contexts."""
+    def ws(B, T, Hq, Hkv, d=128, page=64, max_pages=2048, max_q=1, max_len=0):
+        return lib.fl_paged_attn_ws(B, T, Hq, Hkv, d, page, max_pages, 0, 0, max_q, max_len)
+    for B, T, Hq, Hkv, max_q in ((48, 48, 64, 8, 1), (32, 32, 32, 8, 1), (48, 192, 32, 8, 4), (95, 95, 128, 8, 1), (1, 1, 8, 1, 1)):
+        rows = 16 if max_q * Hq // Hkv <= 16 else 32
+        items = (T * (Hq // Hkv) // rows + B + 768 // Hkv + 1) * Hkv
+        need = ws(B, T, Hq, Hkv, max_q=max_q)
+        assert 0 < need <= items * rows * (128 + 4) * 4
+        assert ws(B, T, Hq, Hkv, max_q=max_q, max_pages=1 << 17) == need
+    assert ws(1, 1, 16, 16, max_len=300) == 0                    # one part: nothing to join
+
+
 def test_binding_refuses_tensors_of_another_place(monkeypatch):
     x = torch.zeros(4, 2, 64, dtype=torch.bfloat16)
     with pytest.raises(fl.FlashLoopError, match="device"):
