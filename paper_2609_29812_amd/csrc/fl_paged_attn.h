@@ -232,7 +232,8 @@ __device__ __forceinline__ float load_query(const PagedAttnArgs& a, const uint16
   for (int k = 0; k < N; ++k)
 #pragma unroll
     for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[k][e]));
-  const float down = row_down(most(top));
+  top = most(top);
+  const float down = row_down(top);
 #pragma unroll
   for (int k = 0; k < N; ++k) {
     u32x4 w;
@@ -246,7 +247,7 @@ __device__ __forceinline__ float load_query(const PagedAttnArgs& a, const uint16
       low[k] = __builtin_bit_cast(f16x8, w);
     }
   }
-  return a.scale_log2 / down;
+  return top < INFINITY ? a.scale_log2 / down : NAN;         // (scores of an infinite query may all be -inf: NaN, not unseen)
 }
 
 // Four codes of one word as two fp16 pairs (exact).  Int8: c + 128 under the exponent of 1024, less 1152.

@@ -140,3 +140,31 @@ def test_a_negative_scale_reads_nan(F):
         for max_q in (1, 40):
             bad = torch.isnan(F.paged_attn(q, *args, max_q=max_q)).flatten(1).all(dim=1).cpu().numpy()
             assert np.array_equal(bad, np.arange(43) >= 3 + 16)
+
+
+@pytest.mark.parametrize("dtype,layout", [("bf16", None), ("f16", None), ("bf16", "half"), ("f16", "interleaved")])
+def test_a_query_that_is_not_finite(F, dtype, layout):
+    """NaN in the output and the normaliser of the rows that see a key, also where every score is -inf; other rows as they were."""
+    rng = np.random.default_rng(6)
+    new, past = [2, 40, 1], [30, 0, 0]
+    cu, lens, tab, n_pages = batch(rng, new, past, 16)
+    tab[2] = -1                                             # a row that sees nothing
+    codes, scale = make_cache(rng, n_pages, 1, 16, 64, "int8")
+    codes[0][..., :2] = 256 - 5
+    q = torch.from_numpy(rng.normal(size=(43, 2, 64))).to(DT[dtype])
+    table = None if layout is None else F.rope_table(100 * 16, 16)
+    args = (i32(cu), i32(lens), i32(tab), *(dev_codes(c, "int8") for c in codes), *(torch.from_numpy(s).cuda() for s in scale))
+    bad = np.zeros((43, 2), bool)
+    for r, h, c, x in ((0, 0, 0, np.inf), (5, 1, 0, np.inf), (6, 0, 1, -np.inf), (20, 1, 63, np.nan), (42, 0, 0, np.inf)):
+        bad[r, h] = r != 42
+        p = q.clone() if r == 0 else p
+        p[r, h, c] = x
+    for max_q, max_len in ((1, 0), (40, 0), (40, 3000)):
+        lse, was = torch.empty(43, 2, device="cuda"), torch.empty(43, 2, device="cuda")
+        kw = dict(table=table, layout=layout or "half", max_q=max_q, max_len=max_len)
+        want = F.paged_attn(q.cuda(), *args, **kw, lse=was).cpu()
+        got = F.paged_attn(p.cuda(), *args, **kw, lse=lse).cpu()
+        nan = torch.from_numpy(bad)
+        assert torch.isnan(got[nan]).all() and torch.isnan(lse.cpu()[nan]).all()
+        assert torch.equal(got[~nan], want[~nan]) and torch.equal(lse.cpu()[~nan], was.cpu()[~nan])
+        assert torch.all(got[42] == 0) and torch.isneginf(lse[42]).all()
