@@ -486,7 +486,8 @@ int fl_kv_keep_recent(const uint16_t* x_cur, const int32_t* idx, int k, int B, i
  * the way.
  *
  * fl_rope_table writes table[p][i] = (m cos(p f_i), m sin(p f_i)), fp32 [n_pos, rot / 2, 2], the angles
- * formed and reduced in fp64 (each value within 2 ulp of m, also at far positions).
+ * formed and reduced in fp64: each value within 2 ulp of m, and m p f_i 2^-51, the frequency's own rounding, which shows from
+ * positions of 2^28 on.
  *   f_i = base^(-2 i / rot), m = 1                              FL_ROPE_NONE
  *   f_i / factor                                                FL_ROPE_LINEAR (positions interpolated)
  *   base * factor^(rot / (rot - 2)) in place of base            FL_ROPE_NTK (the lowest frequency divided by factor)

@@ -161,7 +161,7 @@ extern "C" int fl_rope_table(int n_pos, int rot, double base, int scaling, doubl
   a.m = scaling == FL_ROPE_YARN ? 1.0 + 0.1 * std::log(factor) : 1.0;
   a.out = reinterpret_cast<float2*>(table);
   a.per = n_pos >= 65536 ? 32 : n_pos >= 8192 ? 4 : 1;
-  const int64_t threads = (int64_t)((n_pos + a.per - 1) / a.per) * a.half;
+  const int64_t threads = ((int64_t)n_pos + a.per - 1) / a.per * a.half;
   rope_table_kernel<<<(unsigned)((threads + 255) / 256), 256, 0, as_stream(stream)>>>(a);
   return check_launch("rope_table_kernel");
   FL_API_END
