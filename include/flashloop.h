@@ -538,8 +538,8 @@ int fl_rope(const void* x, int64_t x_stride, const int32_t* pos, const float* ta
  *     scale <- need                                    when the page holds no earlier position of the sequence,
  *     scale <- scale * 2^k, least k >= 0 with scale * 2^k >= need, and the page's other codes <- round(code / 2^k)   otherwise
  *     code = round(x / scale)  to nearest, ties to even, of the exact quotient.
- * Doubling bounds what earlier positions lose to one step of the page's last scale.  a < 2^-100 counts as 0 (need = 0, codes
- * 0); a scale of 0 grows to need at once.  With an infinity or a NaN among x the scale becomes NaN and the codes 0: the page
+ * Doubling bounds what earlier positions lose to one step of the page's last scale.  a < 2^-100 counts as 0 (need = 0, and
+ * codes 0 where the page's scale is below what 2^-100 needs); a scale of 0 grows to need at once.  With an infinity or a NaN among x the scale becomes NaN and the codes 0: the page
  * reads as NaN until it is begun anew.
  *   k, v       : [T, Hkv, d] of `dtype`, k_stride / v_stride elements from one row to the next (multiples of 8),
  *                16-byte aligned.

@@ -237,10 +237,17 @@ __device__ __forceinline__ float grow(float held, uint32_t most, bool went_on, i
   k = doublings(held, need);
   return ldexpf(held, k);
 }
+// The factor of the codes; 0, for codes of 0, where the scale is NaN or below that of 2^-100: then every value counts as 0 (a held
+// scale that a caller formed may be so small that its reciprocal, or a value over it, leaves its range).
+template <bool I8>
+__device__ __forceinline__ float inverse(float sc) {
+  constexpr float kLeast = I8 ? 0x1p-100f * (1.0f / 127.0f) : 0x1p-108f;
+  return sc >= kLeast ? 1.0f / sc : 0.0f;
+}
 template <bool I8>
 __device__ __forceinline__ void put(const Unit& un, uint8_t* row, const float* x, float sc, float inv) {
   uint2 y0 = make_uint2(0, 0), y1 = y0;
-  if (sc > 0.0f) {                                           // (0 or NaN: codes 0)
+  if (inv > 0.0f) {
     y0 = encode8<I8>(x, sc, inv);
     y1 = encode8<I8>(x + 8, sc, inv);
   }
@@ -334,7 +341,7 @@ __global__ __launch_bounds__(PAGE * D / 16 < 256 ? PAGE * D / 16 : 256) void pag
         if (i < w.lo || i >= w.hi) halve<I8>(un, codes + i * D, f);
       }
     }
-    const float inv = sc > 0.0f ? 1.0f / sc : 0.0f;
+    const float inv = inverse<I8>(sc);
 #pragma unroll
     for (int s = 0; s < NP; ++s) {
       const int i = s * PER + i0;
@@ -395,7 +402,7 @@ __global__ __launch_bounds__(256) void paged_append_few_kernel(AppendArgs a, int
     for (int i = i0; i < a.pg.size; i += PER)
       if (i < w.lo || i >= w.hi) halve<I8>(un, codes + i * D, f);
   }
-  const float inv = sc > 0.0f ? 1.0f / sc : 0.0f;
+  const float inv = inverse<I8>(sc);
   for (int i = last; i >= w.lo; i -= PER) {
     if (i < last) read(i + i0);
     if (i + i0 < w.hi) put<I8>(un, codes + (i + i0) * D, x, sc, inv);
