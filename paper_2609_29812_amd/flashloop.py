@@ -647,6 +647,13 @@ def _choice(value, of, name):
     return number
 
 
+def _counts(**counts):
+    """Refuses what a C int does not hold (it would be passed modulo 2^32).  Callers test that first, in one expression."""
+    for name, n in counts.items():
+        if n >> 31:
+            raise FlashLoopError(f"{name} must be in [0, 2^31), got {n}")
+
+
 def _turns(table, at):
     """(n_pos, rot) of a rotary table, (0, 0) without one."""
     if table is None:
@@ -664,6 +671,7 @@ def rope_table(n_pos, rot, base=10000.0, scaling="none", factor=1.0, orig_len=0,
     fewer than low times within orig_len positions divided by factor, those above high kept, and the table multiplied by
     1 + 0.1 ln(factor)).  On `device` (out's, or the current one)."""
     how = _choice(scaling, ROPE_SCALING, "scaling")
+    _counts(n_pos=n_pos, rot=rot)
     if out is None:
         out = torch.empty(n_pos, rot // 2, 2, dtype=torch.float32, device="cuda" if device is None else device)
         _here(out, "device")
@@ -684,6 +692,8 @@ def rope(x, table, pos=None, layout="half", inverse=False, out=None):
     if table is None:
         raise FlashLoopError("rope needs a table")
     T, H, d = x.shape
+    if (T | n_pos) >> 31:
+        _counts(T=T, n_pos=n_pos)
     _on(pos, at, torch.int32, "pos", (T,))
     if out is None:
         out, ys = x.new_empty((T, H, d)), H * d
@@ -697,7 +707,7 @@ def rope(x, table, pos=None, layout="half", inverse=False, out=None):
 
 
 # ---- (10) the paged 8-bit cache ---------------------------------------------------------------------------
-def _paged(at, cu, lens, block_table, k_cache, v_cache, k_scale, v_scale, Hkv, d):
+def _paged(at, T, cu, lens, block_table, k_cache, v_cache, k_scale, v_scale, Hkv, d):
     """(B, max_pages, num_pages, page, format) of a ragged batch over a cache."""
     if block_table.dim() != 2 or k_cache.dim() != 4:
         raise FlashLoopError("block_table must be [B, max_pages] and the caches [num_pages, Hkv, page, d]")
@@ -708,6 +718,8 @@ def _paged(at, cu, lens, block_table, k_cache, v_cache, k_scale, v_scale, Hkv, d
     if B == 0:
         raise FlashLoopError("a batch has at least one sequence")
     shape = num_pages, _, page, _ = k_cache.shape
+    if (T | B | max_pages | num_pages) >> 31:
+        _counts(T=T, B=B, max_pages=max_pages, num_pages=num_pages)
     if (shape[1] != Hkv or shape[3] != d or v_cache.dtype is not code or v_cache.shape != shape
             or not (k_cache.is_contiguous() and v_cache.is_contiguous() and k_cache.get_device() == v_cache.get_device() == at)):
         for name, c in (("k_cache", k_cache), ("v_cache", v_cache)):
@@ -744,8 +756,10 @@ def paged_append(k, v, cu, lens, block_table, k_cache, v_cache, k_scale, v_scale
     ks = _rows(k, at, dtype, "k")
     T, Hkv, d = k.shape
     vs = _rows(v, at, dtype, "v", k.shape)
-    B, max_pages, num_pages, page, fmt = _paged(at, cu, lens, block_table, k_cache, v_cache, k_scale, v_scale, Hkv, d)
+    B, max_pages, num_pages, page, fmt = _paged(at, T, cu, lens, block_table, k_cache, v_cache, k_scale, v_scale, Hkv, d)
     n_pos, rot = _turns(table, at)
+    if n_pos >> 31:
+        _counts(n_pos=n_pos)
     rc = (_lib or load()).fl_paged_append(
         k.data_ptr(), ks, v.data_ptr(), vs, _DTYPES[dtype], cu.data_ptr(), lens.data_ptr(), B, T, Hkv, d, _p(table), n_pos, rot,
         _choice(layout, ROPE_LAYOUT, "layout"), block_table.data_ptr(), max_pages, num_pages, page, fmt, k_cache.data_ptr(),
@@ -768,7 +782,7 @@ def paged_attn(q, cu, lens, block_table, k_cache, v_cache, k_scale, v_scale, tab
     qs = _rows(q, at, dtype, "q")
     T, Hq, d = q.shape
     Hkv = k_cache.shape[1] if k_cache.dim() == 4 else 0
-    B, max_pages, num_pages, page, fmt = _paged(at, cu, lens, block_table, k_cache, v_cache, k_scale, v_scale, Hkv, d)
+    B, max_pages, num_pages, page, fmt = _paged(at, T, cu, lens, block_table, k_cache, v_cache, k_scale, v_scale, Hkv, d)
     n_pos, rot = _turns(table, at)
     if out is None:
         out, os_ = q.new_empty((T, Hq, d)), Hq * d
@@ -776,6 +790,8 @@ def paged_attn(q, cu, lens, block_table, k_cache, v_cache, k_scale, v_scale, tab
         os_ = _rows(out, at, dtype, "out", q.shape)
     _on(lse, at, torch.float32, "lse", (T, Hq))
     max_q = -(-T // B) if max_q is None else max_q
+    if (window | n_sink | max_q | max_len | n_pos) >> 31:
+        _counts(window=window, n_sink=n_sink, max_q=max_q, max_len=max_len, n_pos=n_pos)
     lib = _lib or load()
     if ws is None:
         need = lib.fl_paged_attn_ws(B, T, Hq, Hkv, d, page, max_pages, window, n_sink, max_q, max_len)
@@ -796,6 +812,7 @@ def paged_attn_ws(q, block_table, k_cache, window=0, n_sink=0, max_q=None, max_l
     """A workspace for paged_attn over these shapes and hints (None when it needs none)."""
     T, Hq, d = q.shape
     B, max_pages = max(1, block_table.shape[0]), block_table.shape[1]
-    need = load().fl_paged_attn_ws(B, T, Hq, k_cache.shape[1], d, k_cache.shape[2], max_pages, window, n_sink,
-                                   -(-T // B) if max_q is None else max_q, max_len)
+    max_q = -(-T // B) if max_q is None else max_q
+    _counts(T=T, B=B, max_pages=max_pages, window=window, n_sink=n_sink, max_q=max_q, max_len=max_len)
+    need = load().fl_paged_attn_ws(B, T, Hq, k_cache.shape[1], d, k_cache.shape[2], max_pages, window, n_sink, max_q, max_len)
     return torch.empty(need, dtype=torch.uint8, device=q.device) if need else None

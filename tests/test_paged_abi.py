@@ -150,6 +150,34 @@ def test_binding_refuses_tensors_of_another_place(monkeypatch):
         fl.paged_cache(4, 1, 16, 64, dtype=torch.uint8, device="cpu")
 
 
+def test_counts_beyond_an_int(lib, monkeypatch):
+    """Sizes, windows and hints that a C int does not hold are refused, and not passed modulo 2^32."""
+    class Fake(torch.Tensor):                                     # a CPU tensor that says it is on the current device
+        is_cuda = True
+        def get_device(self): return 0
+    monkeypatch.setattr(fl, "_current", lambda: 0)
+    monkeypatch.setattr(fl, "_stream", lambda: 0)
+    def fake(*shape, dtype): return torch.zeros(*shape, dtype=dtype).as_subclass(Fake)
+    q = fake(4, 4, 64, dtype=torch.bfloat16)
+    cu, lens, tab = (fake(*s, dtype=torch.int32) for s in ((3,), (2,), (2, 8)))
+    cache = [fake(4, 2, 16, 64, dtype=torch.int8) for _ in range(2)] + [fake(4, 2, dtype=torch.float32) for _ in range(2)]
+    for name in ("window", "n_sink", "max_q", "max_len"):
+        for n in (2 ** 32 + 5, 2 ** 31, -1):
+            with pytest.raises(fl.FlashLoopError, match=name):
+                fl.paged_attn(q, cu, lens, tab, *cache, **{name: n})
+            with pytest.raises(fl.FlashLoopError, match=name):
+                fl.paged_attn_ws(q, tab, cache[0], **{name: n})
+    for kw in (dict(n_pos=2 ** 32 + 8, rot=64), dict(n_pos=8, rot=2 ** 32 + 64), dict(n_pos=-1, rot=64)):
+        with pytest.raises(fl.FlashLoopError, match="must be in"):
+            fl.rope_table(**kw, device="meta")
+    # views of one row, as many as a C int does not hold: the strides are refused only afterwards
+    many = torch.zeros(1, 1, 64, dtype=torch.bfloat16).expand(2 ** 32 + 5, 1, 64).as_subclass(Fake)
+    with pytest.raises(fl.FlashLoopError, match="T must be in"):
+        fl.rope(many, fake(8, 8, 2, dtype=torch.float32))
+    with pytest.raises(fl.FlashLoopError, match="T must be in"):
+        fl.paged_append(many, many, cu, lens, tab, *(fake(4, 1, 16, 64, dtype=torch.int8) for _ in range(2)), *cache[2:])
+
+
 def test_rows_of_the_binding():
     cpu = torch.zeros(1).get_device()
     x = torch.zeros(6, 3 * 128, dtype=torch.float16)[:, 128:256].view(6, 2, 64)
