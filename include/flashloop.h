@@ -578,8 +578,8 @@ int fl_paged_append(const void* k, int64_t k_stride, const void* v, int64_t v_st
  *   Hq a multiple of Hkv; window, n_sink >= 0; other limits as in (10).
  * Precision: q (rotated in fp32) is multiplied as fp16 relative to the row's largest magnitude, for FL_F16 with what that
  * rounding leaves as a second part; probabilities times their value's scale as fp16 relative to the largest such product of the
- * row; both against the exact codes.  Scores, sums and outputs are held in fp32.  Value scales may lie anywhere from 2^-112 (below:
- * as 0; the append writes none between 0 and 2^-109) up, side by side: every key counts in the normaliser.  With the index checks on, as in (10) (a page that is not there is no error here, nor is one that two sequences share).
+ * row; both against the exact codes.  Scores, sums and outputs are held in fp32.  Value scales may lie anywhere from 2^-112 to
+ * 2^121, all that an append writes, side by side: every key counts in the normaliser.  Below 2^-112 one counts as 0.  With the index checks on, as in (10) (a page that is not there is no error here, nor is one that two sequences share).
  * ---------------------------------------------------------------------------------------------- */
 size_t fl_paged_attn_ws(int B, int T, int Hq, int Hkv, int d, int page, int max_pages, int window, int n_sink, int max_q,
                         int max_len);

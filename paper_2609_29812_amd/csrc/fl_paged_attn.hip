@@ -182,7 +182,7 @@ __global__ __launch_bounds__(256, NR == 1 ? (F16 ? 3 : 4) : 2) void paged_token_
       }
     }
     if (more) load_k(c + 1);
-    if ((masked && !I8) || least <= kNoScale) {              // codes that no row sees may be NaN; those of a scale of 0 count as 0
+    if (__builtin_expect((masked && !I8) || least <= kNoScale, 0)) {              // codes that no row sees may be NaN; those of a scale of 0 count as 0
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const bool there = seen_by_any(a, sp, key0 + (e >> 2) * 16 + g4 * 4 + (e & 3)) && (e < 4 ? pid0 : pid1) >= 0 &&
@@ -232,7 +232,7 @@ __global__ __launch_bounds__(256, NR == 1 ? (F16 ? 3 : 4) : 2) void paged_token_
       }
       const float base = ref[x] == -INFINITY ? 0.0f : ref[x];
       const bool apart = __builtin_amdgcn_ballot_w64(ref[x] - top[x] - least > kRoom) != 0;
-      if (apart) {
+      if (__builtin_expect(apart, 0)) {                      // (out of the way of the loop's code)
         lift(best());
         const float from = top[x] == -INFINITY ? 0.0f : top[x];
 #pragma unroll
@@ -252,7 +252,7 @@ __global__ __launch_bounds__(256, NR == 1 ? (F16 ? 3 : 4) : 2) void paged_token_
         sum = fmaf(part, fabsf(iv[h]), sum);
       }
       lsum[x] = fmaf(sum, apart ? 0.0f : ref_to_top(ref[x], top[x]), lsum[x]);
-      if (spoilt) {                                          // a value scale that is not finite: the rows that see it
+      if (__builtin_expect(spoilt, 0)) {                                          // a value scale that is not finite: the rows that see it
         bool any = false;
 #pragma unroll
         for (int h = 0; h < 2; ++h)

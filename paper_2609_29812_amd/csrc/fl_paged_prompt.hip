@@ -319,7 +319,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttnArgs a) {
     }
     const float base = ref == -INFINITY ? 0.0f : ref;
     float share = ref_to_top(ref, top);
-    if (__builtin_amdgcn_ballot_w64((least <= kNoScale) | (ref - top - least > kRoom)) != 0) {
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64((least <= kNoScale) | (ref - top - least > kRoom)) != 0, 0)) {
       lift();
       const float from = top == -INFINITY ? 0.0f : top;
       share = 0.0f;
@@ -331,7 +331,7 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttnArgs a) {
         lv[g] = lv[g] <= kNoScale ? -INFINITY : lv[g];
       }
     }
-    if (__builtin_amdgcn_ballot_w64(spoilt) != 0) {                   // a value scale that is not finite: the rows that see it
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(spoilt) != 0, 0)) {                   // a value scale that is not finite: the rows that see it
       bool any = false;
 #pragma unroll
       for (int x = 0; x < NBK; ++x)
