@@ -492,7 +492,8 @@ int fl_kv_keep_recent(const uint16_t* x_cur, const int32_t* idx, int k, int B, i
  *   f_i / factor                                                FL_ROPE_LINEAR (positions interpolated)
  *   base * factor^(rot / (rot - 2)) in place of base            FL_ROPE_NTK (the lowest frequency divided by factor)
  *   f_i (g_i + (1 - g_i) / factor), m = 1 + 0.1 ln(factor)      FL_ROPE_YARN (Peng et al., "YaRN": g_i = the part of
- *       [low, high] that the pair's turns within the original context, orig_len f_i / 2 pi, have passed, in [0, 1])
+ *       [low, high] that the pair's turns within the original context, orig_len f_i / 2 pi, have passed, in [0, 1]; model code
+ *       that ramps over the pair's index between rounded bounds instead has other tables)
  *   n_pos >= 1; rot a multiple of 16, 16 <= rot <= 1024; base > 1; factor >= 1 (ignored by NONE);
  *   orig_len > 0 and low < high for YARN (ignored by the others).  Any other table of this layout serves as well.
  *

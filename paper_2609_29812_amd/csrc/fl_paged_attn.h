@@ -303,8 +303,8 @@ struct Cut {
   __device__ __forceinline__ int owner(int x) const { return x / per; }
 };
 // Units of a share at least: its queries, its sums and their join cost about ten.  Where few row tiles stand against many CUs
-// (100 rows of 8 heads over 5000 positions, 320 units a head) 8, 12, 16 and 24 took 44, 48, 55 and 70 us; 64 rows over 32000
-// positions 124, 112, 94 and 98 us, being joined from more parts then.
+// (100 rows of 8 heads over 5000 positions, 320 units a head) 8, 12, 16 and 24 took 44, 48, 55 and 67 us; 64 rows over 32000
+// positions 132, 116, 96 and 99 us, being joined from more parts then.
 constexpr int kLeastUnits = 12;
 __device__ __forceinline__ Cut cut_of(const PagedAttnArgs& a) {
   const int total = __builtin_amdgcn_readfirstlane(a.ends[a.slots - 1]);

@@ -19,7 +19,7 @@ constexpr int kTokenKeys = 32;     // keys of a wave's tile
 // read once, non-temporally (131072 positions: 53 us against 60 under the default policy).
 //
 // Bound by HBM for long contexts, by the chain of loads before the first product (sequences; pages and queries; scales and codes)
-// for short ones.  8 heads x 128: 131072 positions of one sequence 50 us, 5.3 TB/s; 32 sequences of 1 to 8191 positions 53 us, 4.5
+// for short ones.  8 heads x 128: 131072 positions of one sequence 50 us, 5.4 TB/s; 32 sequences of 1 to 8191 positions 53 us, 4.5
 // TB/s (64 us with the same number of parts for every sequence); 16 heads, 299 positions 9.5 us.
 template <int D, bool I8, bool F16, int NR>
 __global__ __launch_bounds__(256, NR == 1 ? (F16 ? 3 : 4) : 2) void paged_token_kernel(PagedAttnArgs a) {

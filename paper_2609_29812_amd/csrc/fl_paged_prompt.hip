@@ -8,9 +8,10 @@
 // Scales never touch the codes: a key scale multiplies its 16 scores inside the exponent's fma, a value scale enters as its
 // logarithm there and leaves the row sum as its reciprocal, once per 16 keys.
 //
-// Bound by the vector ALU beside the matrix cores, at the clock that both allow: per wave and stage 32 products (1024 matrix cycles)
-// against about 350 vector instructions and 32 exponentials; 16 heads x 128, 16384 positions 1.24 ms (885 TFLOP/s), where the
-// dense loop over bf16 states, which widens no codes, takes 1.15.
+// Bound by neither unit alone: vector instructions are issued in 56 % of the cycles and the matrix cores are busy in 41 %, one after
+// the other, for a stage multiplies and then takes its scores through the exponent.  Per wave and stage 32 products (1024 matrix
+// cycles; 48 with fp16 queries that are rotated) against about 360 vector instructions and 33 exponentials; 16 heads x 128, 16384
+// positions 1.29 ms (850 TFLOP/s), where the dense loop over bf16 states, which widens no codes, takes 1.16.
 //
 // One workgroup for each row tile and head, the longest first, from two rounds of them on.  Fewer leave the chip idle, so there
 // workgroups have equal shares of the work, whatever the lengths are: a first small kernel adds up the units of all row tiles,
@@ -110,7 +111,8 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttnArgs a) {
   const int first = at;
   for (; at < end; ++slot) {
   int tid = threadIdx.x;
-  // what a row tile derives from the lane is formed anew: kept over the stages, it spilled
+  // what a row tile derives from the lane is formed anew: kept over the stages, it spilled (128 channels with fp16 queries still
+  // hold 3 to 9 registers of a lane in scratch, all but one of them read outside the stages)
   if constexpr (SHARED) asm volatile("" : "+v"(tid));
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hw = lane >> 5, r32 = lane & 31;

@@ -27,8 +27,8 @@ __device__ __forceinline__ double frequency(const TableArgs& a, int i) {
 
 // A thread has one pair and `per` positions, so that the fp64 power is paid once for all of them.  The angle is reduced in turns,
 // in fp64 (p f / 2 pi less its nearest integer: exact but for the product's rounding, 2^-53 of it); the remainder's sine and
-// cosine are fp32 ones of its high part, corrected to first order by its low part.  The bound is the 8 bytes written per pair:
-// 131072 positions x 64 pairs in 15 us, 4.5 TB/s (28 us with fp64 sines and cosines).
+// cosine are fp32 ones of its high part, corrected to first order by its low part.  Bound by the vector ALU (busy in all of the
+// compute units' cycles): 131072 positions x 64 pairs, 67 MB, in 19 us, 3.6 TB/s (28 us with fp64 sines and cosines).
 __global__ __launch_bounds__(256) void rope_table_kernel(TableArgs a) {
   const int64_t g = (int64_t)blockIdx.x * 256 + threadIdx.x;
   const int i = (int)(g % a.half);
@@ -58,8 +58,8 @@ struct RopeArgs {
 
 // A unit is 16 channels of a head: chunks i and i + rot / 16 of its rotated part (FL_ROPE_HALF) or two neighbouring chunks
 // of eight, so that a thread holds both values of every pair and the rotation may be in place.  A thread has one unit; the heads of a
-// row find its cosines and sines in the caches (two heads a thread: 48 us against 50 for 32768 rows, 5.0 against 4.6 for 2000).
-// Bound by HBM: 32768 rows of 16 heads x 128 in 47 us, 285 MB at 6.1 TB/s; eight rows 2.8 us.
+// row find its cosines and sines in the caches.  Bound by HBM: 32768 rows of 16 heads x 128 in 47 us, 285 MB at 6.1 TB/s; eight
+// rows 2.9 us.
 template <bool HALF, bool F16>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
   const int64_t g = (int64_t)blockIdx.x * 256 + threadIdx.x;

@@ -140,7 +140,8 @@ def paged_step(cache, q, k, v, cu, lens, block_table, table=None, layout="half",
                out=None, lse=None, ws=None):
     """One dense loop of one layer for the new positions of a ragged batch: cache (fl.paged_cache) holds what the sequences
     had, cu, lens and block_table say which rows of q [T, Hq, d] and k, v [T, Hkv, d] are whose newest positions, table turns
-    queries and keys by them.  Returns the output [T, Hq, d]; a looped model has a cache for each of its loops."""
+    queries and keys by them.  Returns the output [T, Hq, d]; a looped model has a cache for each of its loops.  The sparse loops
+    (sparse_step, fl.decode_step) read bf16 [B, N, H, d] states and not this cache."""
     fl.paged_append(k, v, cu, lens, block_table, *cache, table=table, layout=layout)
     return fl.paged_attn(q, cu, lens, block_table, *cache, table=table, layout=layout, window=window, n_sink=n_sink,
                          max_q=max_q, max_len=max_len, out=out, lse=lse, ws=ws)
