@@ -275,17 +275,18 @@ __device__ __forceinline__ float max3(float x, float y, float z) {
 // sum of its contributions, times 2^(ref - top) / s.  That sum has room for 2^-126, so where ref - top - log2 s stays below kRoom
 // octaves, what it loses is below 2^-62 of the normaliser.  Above (a page of values far smaller than those that carry the row) the
 // page's exponentials are taken once more, relative to `top`.  The output is sums * 2^(ref - top) / normaliser.
-// A scale below 2^-112 (the append writes none between 0 and 2^-109) counts as 0: it has kNoScale, and its products are 0.
+// A scale below 2^-112 (the append writes none between 0 and 2^-109) counts as 0: it has kNoScale, one octave below any other, and
+// its products are 0.
 // One that is negative or not finite counts as 1 with a negative reciprocal (the normaliser does not depend on it), and the rows
 // that see the page are made NaN.
-constexpr float kRoom = 64.0f, kNoScale = -112.0f;
+constexpr float kRoom = 64.0f, kNoScale = -113.0f;
 __device__ __forceinline__ float key_scale(float s) { return s >= 0.0f && s < INFINITY ? s : NAN; }
 struct ValueScale {
   float log2, inv;
 };
 __device__ __forceinline__ ValueScale value_scale(float s) {
   if (!(s >= 0.0f && s < INFINITY)) return {0.0f, -1.0f};
-  if (s < 0x1p-112f) return {kNoScale, 0x1p112f};
+  if (s < 0x1p-112f) return {kNoScale, 0x1p113f};
   return {__builtin_amdgcn_logf(s), 1.0f / s};
 }
 // 2^(ref - top); 1 for a row that has seen nothing, or nothing but NaN

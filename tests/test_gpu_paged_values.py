@@ -60,6 +60,28 @@ def test_values_of_any_magnitude(F, octave, shape, fmt):
         assert np.linalg.norm(got - want) <= 2.0 ** -7 * np.linalg.norm(want)
 
 
+@pytest.mark.parametrize("shape", range(len(SHAPES)))
+def test_the_least_scale(F, shape):
+    """2^-112 itself, and the next number, beside scales that count as 0."""
+    new, past, page, Hq, Hkv, d, hints = SHAPES[shape]
+    rng = np.random.default_rng(shape)
+    least = np.float32(2.0 ** -112)
+
+    def edit(scale, tab, codes):
+        scale[1][:] = rng.choice([least, np.nextafter(least, np.float32(1)), np.nextafter(least, np.float32(0)), 0], scale[1].shape)
+    reads = []
+    for got, _, _, _, _ in attend(F, rng, new, past, page, Hq, Hkv, d, "int8", edit, hints):
+        reads.append(got)
+    # (the oracle knows of no least scale: the same with those below it as 0)
+    rng = np.random.default_rng(shape)
+
+    def cut(scale, tab, codes):
+        edit(scale, tab, codes)
+        scale[1][scale[1] < least] = 0
+    for was, (got, _, want, _, tol) in zip(reads, attend(F, rng, new, past, page, Hq, Hkv, d, "int8", cut, hints)):
+        assert np.array_equal(got, was) and np.all(np.abs(got - want) <= tol) and np.abs(got).max() > 0
+
+
 @pytest.mark.parametrize("fmt", ["int8", "e4m3"])
 @pytest.mark.parametrize("amp", [0.3, 12.0])
 @pytest.mark.parametrize("shape", range(len(SHAPES)))
