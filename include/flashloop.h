@@ -16,7 +16,8 @@
  *   shrinking budget (fl_prune_columns) and the recent-token bf16 tail (fl_kv_keep_recent).
  * and what serving a model needs beside the step, over ragged batches: rotary positions (fl_rope_table,
  *   fl_rope), a paged key/value cache in 8 bits (fl_paged_append) and dense attention over it
- *   (fl_paged_attn).
+ *   (fl_paged_attn); attention over packed prompts (fl_packed_attn); and such a cache in 4 bits, written,
+ *   read back and attended over (fl_paged4_append, fl_paged4_read, fl_paged4_attn).
  *
  * Conventions shared by every call
  *   - Every data pointer is a DEVICE pointer (HIP device memory).  The caller allocates and owns all
@@ -591,6 +592,99 @@ int fl_paged_attn(const void* q, int64_t q_stride, int dtype, const int32_t* cu,
                   const void* v_cache, const float* k_scale, const float* v_scale, float sm_scale, int window,
                   int n_sink, int max_q, int max_len, void* o, int64_t o_stride, float* lse, void* ws, size_t ws_bytes,
                   void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * (12) Dense attention of packed prompts (Eq. 2 over a ragged batch): the rows of all sequences lie one after the other.
+ * Sequence b has the query rows cu_q[b] .. cu_q[b+1] - 1, n_q of them, and the key and value rows cu_k[b] .. cu_k[b+1] - 1,
+ * n_k; its queries are the last n_q of its n_k positions, so row t of them has position i = n_k - n_q + t.  With grouped heads
+ * (key/value head h / (Hq / Hkv) of query head h)
+ *     o_t = sum_j p_j v_j,   p_j = exp(sm_scale q . k_j - lse_t),   lse_t = ln sum_j exp(sm_scale q . k_j)
+ * over the sequence's positions j <= i with, when window > 0, j > i - window or j < n_sink.  A row that sees nothing (i < 0)
+ * gets o = 0 and lse = -inf.  What a row does not see is of no effect on it, whatever it holds.
+ *   q, o       : [Tq, Hq, d] of `dtype`, k and v: [Tk, Hkv, d], with q_stride .. elements from one row to the next (multiples of
+ *                8, at most 2^24), the heads of a row dense, 16-byte aligned; o overlaps none of the others.
+ *   cu_q, cu_k : int32 [B + 1], ascending from 0 to at most Tq and Tk (cu_k may be cu_q: whole prompts).  Read by the kernels alone,
+ *                so a captured graph takes their present contents.  Rows behind cu_q[B] belong to no sequence and are not touched.
+ *   table      : fp32 [n_pos, rot / 2, 2] as in (9), or NULL.  With it the queries are turned by their positions and rounded to
+ *                `dtype`, as fl_rope leaves them (a position outside [0, n_pos): NaN).  Keys are taken as they are.
+ *   lse        : fp32 [Tq, Hq], or NULL.
+ *   max_k      : the largest n_k as far as the caller knows it (0: Tk).  It chooses how the work is cut; any value gives the
+ *                result, up to rounding.
+ *   ws         : 16-byte aligned, at least fl_packed_attn_ws(...) bytes, for the same arguments; nothing is kept in it between calls.
+ *                Calls that overlap need one each.
+ *   d: 64 or 128.  Hq a multiple of Hkv, at most 65535.  B <= 65536.  With the index checks on, cu_q and cu_k are checked on the
+ *   host: FL_E_RANGE when one does not ascend from 0 to at most Tq (Tk).
+ * Precision: products in `dtype`, probabilities rounded to it relative to a running reference of the row; scores, sums and outputs
+ * are held in fp32.  A value that is not finite leaves what sees it, in its channel, not finite; a row whose scores are all -inf
+ * counts as one that sees nothing.
+ * ---------------------------------------------------------------------------------------------- */
+size_t fl_packed_attn_ws(int B, int Tq, int Tk, int Hq, int Hkv, int d, int window, int n_sink, int max_k);
+
+int fl_packed_attn(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                   int dtype, const int32_t* cu_q, const int32_t* cu_k, int B, int Tq, int Tk, int Hq, int Hkv, int d,
+                   const float* table, int n_pos, int rot, int layout, float sm_scale, int window, int n_sink, int max_k,
+                   void* o, int64_t o_stride, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * (13) A paged key/value cache in 4 bits, appended to for a ragged batch.
+ *
+ * Batch, pages and block tables are those of (10).  k_cache and v_cache: uint8 [num_pages, Hkv, page, d / 2], channel 2 j in the
+ * low four bits of byte j (as the codes of (2)).  The 32 channels 32 g .. 32 g + 31 of a position and head are a group, with numbers
+ * of its own in k_meta and v_meta:
+ *   FL_KV4_INT  : fp16 [num_pages, Hkv, page, d / 32, 2], (scale s, zero z); a code c in 0 .. 15 stands for z + s c
+ *   FL_KV4_E2M1 : uint8 [num_pages, Hkv, page, d / 32], e + 127; a code is an OCP e2m1 number c (0, 0.5, 1, 1.5, 2, 3, 4, 6 and
+ *                 their negatives) and stands for c 2^e
+ * A group with numbers that an append does not write (|z| > 2^15, s < 0, s > 4372 or NaN; e outside [-23, 13]) reads as NaN.
+ * Every position stands by itself: nothing that a page holds changes when another position is written.
+ *
+ * fl_paged4_append stores the new positions; x: the values, or the keys rotated by their positions when `table` is given (the
+ * fp32 rounding of the exact sum of the two products), magnitudes above 2^15 counted as 2^15:
+ *   FL_KV4_INT  : z = largest fp16 <= min x, s = smallest fp16 with 15 s >= fp64(max x - z),
+ *                 c = rint((x - z) / s) of fp64 arithmetic, ties to even, within 0 .. 15; 0 where s = 0.  No zero is -0.
+ *   FL_KV4_E2M1 : e = the least e >= -23 with max |x| <= 6 2^e; c = the e2m1 number nearest to x 2^-e, ties to the even code.
+ *   A group with an infinity or a NaN: s = z = NaN, or e + 127 = 255, and codes 0.
+ *   k, v       : [T, Hkv, d] of `dtype`, k_stride / v_stride elements from one row to the next (multiples of 8), 16-byte aligned.
+ *   k_rows, v_rows : NULL, or [T, Hkv, d] of `dtype` with strides of their own: the rows that the codes stand for, rounded to
+ *                `dtype`, as fl_paged4_read gives them.  k_rows may be k and v_rows v (with the same stride); otherwise they overlap
+ *                nothing.
+ *   Limits, dropped positions (which leave k_rows and v_rows as they were) and the index checks are those of (10).
+ * ---------------------------------------------------------------------------------------------- */
+enum fl_kv4_format { FL_KV4_INT = 0, FL_KV4_E2M1 = 1 };
+
+int fl_paged4_append(const void* k, int64_t k_stride, const void* v, int64_t v_stride, int dtype, const int32_t* cu,
+                     const int32_t* lens, int B, int T, int Hkv, int d, const float* table, int n_pos, int rot, int layout,
+                     const int32_t* block_table, int max_pages, int num_pages, int page, int format, void* k_cache,
+                     void* v_cache, void* k_meta, void* v_meta, void* k_rows, int64_t k_rows_stride, void* v_rows,
+                     int64_t v_rows_stride, void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * (14) Positions of a ragged batch back out of the cache of (13), as rows: row cu[b] + t of k_out and v_out is position
+ * lens[b] - n + t of sequence b (n = cu[b+1] - cu[b]; with n = lens[b] all of it), z + s c or c 2^e rounded to `dtype`.
+ *   k_out, v_out : [T, Hkv, d] of `dtype`, strides as in (13); either may be NULL, not both.  They do not overlap.
+ * Rows of positions that are negative, or whose page is not there, become 0; rows behind cu[B] are not touched.
+ * Limits and index checks: as in (10), a page that is not there being no error.
+ * ---------------------------------------------------------------------------------------------- */
+int fl_paged4_read(const int32_t* cu, const int32_t* lens, int B, int T, int Hkv, int d, const int32_t* block_table,
+                   int max_pages, int num_pages, int page, int format, const void* k_cache, const void* v_cache,
+                   const void* k_meta, const void* v_meta, int dtype, void* k_out, int64_t k_out_stride, void* v_out,
+                   int64_t v_out_stride, void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * (15) Dense attention of a ragged batch over the paged 4-bit cache of (13): fl_paged_attn of (11) with this cache.  Arguments,
+ * masks, rows that see nothing, positions behind the block table, hints and workspace (fl_paged4_attn_ws) are those of (11).
+ * A row that sees a position of which a key's or a value's group reads as NaN is NaN.
+ * Precision: codes are widened to fp16 (one rounding of z + s c; e2m1 exactly); q (rotated in fp32) is multiplied as fp16 relative
+ * to the row's largest magnitude, for FL_F16 with what that rounding leaves as a second part where it is rotated; probabilities
+ * are fp16 relative to a running reference of the row.  Scores, sums and outputs are held in fp32.
+ * ---------------------------------------------------------------------------------------------- */
+size_t fl_paged4_attn_ws(int B, int T, int Hq, int Hkv, int d, int page, int max_pages, int window, int n_sink, int max_q,
+                         int max_len);
+
+int fl_paged4_attn(const void* q, int64_t q_stride, int dtype, const int32_t* cu, const int32_t* lens, int B, int T,
+                   int Hq, int Hkv, int d, const float* table, int n_pos, int rot, int layout,
+                   const int32_t* block_table, int max_pages, int num_pages, int page, int format, const void* k_cache,
+                   const void* v_cache, const void* k_meta, const void* v_meta, float sm_scale, int window, int n_sink,
+                   int max_q, int max_len, void* o, int64_t o_stride, float* lse, void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

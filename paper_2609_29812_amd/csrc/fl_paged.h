@@ -73,7 +73,10 @@ __device__ __forceinline__ uint4 pack8(const float* x) {
   return make_uint4(u[0], u[1], u[2], u[3]);
 }
 
-// host: the checks that the calls of a paged cache have in common
+// host: the checks that the calls of a paged cache have in common (check_ragged: all but its codes and scales)
+int check_ragged(const char* fn, int dtype, const int32_t* cu, const int32_t* lens, int B, int T, int Hkv, int d,
+                 const float* table, int n_pos, int rot, int layout, const int32_t* block_table, int max_pages,
+                 int num_pages, int page);
 int check_paged(const char* fn, int dtype, const int32_t* cu, const int32_t* lens, int B, int T, int Hkv, int d,
                 const float* table, int n_pos, int rot, int layout, const int32_t* block_table, int max_pages,
                 int num_pages, int page, int format, const void* kc, const void* vc, const float* ks, const float* vs);
@@ -82,6 +85,9 @@ int check_rows(const char* fn, const char* name, const void* x, int64_t stride, 
 int check_apart(const char* fn, const char* xn, const void* x, int64_t xs, const char* yn, const void* y, int64_t ys, int T,
                 int width);
 int check_rotary(const char* fn, const float* table, int rot, int layout, int d);
+// the same for rows of their own number and width each
+int check_disjoint(const char* fn, const char* xn, const void* x, int64_t xs, int tx, int wx, const char* yn, const void* y,
+                   int64_t ys, int ty, int wy);
 // with the index checks on: cu, lens and block_table on the host (`append`: the pages of the new positions too)
 int check_batch(const char* fn, const Batch& bt, const Pages& pg, bool append, hipStream_t st);
 

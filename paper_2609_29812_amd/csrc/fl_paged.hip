@@ -7,11 +7,10 @@
 
 namespace fl {
 
-int check_paged(const char* fn, int dtype, const int32_t* cu, const int32_t* lens, int B, int T, int Hkv, int d,
-                const float* table, int n_pos, int rot, int layout, const int32_t* block_table, int max_pages,
-                int num_pages, int page, int format, const void* kc, const void* vc, const float* ks, const float* vs) {
+int check_ragged(const char* fn, int dtype, const int32_t* cu, const int32_t* lens, int B, int T, int Hkv, int d,
+                 const float* table, int n_pos, int rot, int layout, const int32_t* block_table, int max_pages,
+                 int num_pages, int page) {
   FL_REQUIRE(dtype == FL_BF16 || dtype == FL_F16, FL_E_UNSUPPORTED, "%s: unknown dtype %d", fn, dtype);
-  FL_REQUIRE(format == FL_KV_I8 || format == FL_KV_E4M3, FL_E_UNSUPPORTED, "%s: unknown cache format %d", fn, format);
   FL_REQUIRE(d == 64 || d == 128, FL_E_SHAPE, "%s: d=%d must be 64 or 128", fn, d);
   FL_REQUIRE(page == 16 || page == 32 || page == 64 || page == 128, FL_E_SHAPE, "%s: page=%d must be 16, 32, 64 or 128", fn,
              page);
@@ -21,16 +20,25 @@ int check_paged(const char* fn, int dtype, const int32_t* cu, const int32_t* len
              "%s: max_pages=%d pages of %d positions: between 1 page and 2^31 - 4097 positions", fn, max_pages, page);
   FL_REQUIRE(num_pages >= 1, FL_E_SHAPE, "%s: num_pages=%d must be positive", fn, num_pages);
   FL_REQUIRE(cu && lens && block_table, FL_E_NULL, "%s: cu, lens and block_table are required", fn);
-  FL_REQUIRE(kc && vc && ks && vs, FL_E_NULL, "%s: k_cache, v_cache, k_scale and v_scale are required", fn);
-  FL_REQUIRE(kc != vc && ks != vs, FL_E_SHAPE, "%s: keys and values need a cache and scales each", fn);
-  FL_REQUIRE(((reinterpret_cast<uintptr_t>(kc) | reinterpret_cast<uintptr_t>(vc)) & 15) == 0, FL_E_SHAPE,
-             "%s: the caches must be 16-byte aligned", fn);
   if (table) {
     const int rc = check_rotary(fn, table, rot, layout, d);
     if (rc != FL_OK) return rc;
     FL_REQUIRE((int64_t)n_pos >= (int64_t)max_pages * page, FL_E_RANGE,
                "%s: a table of %d positions for sequences of up to %d pages of %d", fn, n_pos, max_pages, page);
   }
+  return FL_OK;
+}
+
+int check_paged(const char* fn, int dtype, const int32_t* cu, const int32_t* lens, int B, int T, int Hkv, int d,
+                const float* table, int n_pos, int rot, int layout, const int32_t* block_table, int max_pages,
+                int num_pages, int page, int format, const void* kc, const void* vc, const float* ks, const float* vs) {
+  FL_REQUIRE(format == FL_KV_I8 || format == FL_KV_E4M3, FL_E_UNSUPPORTED, "%s: unknown cache format %d", fn, format);
+  const int rc = check_ragged(fn, dtype, cu, lens, B, T, Hkv, d, table, n_pos, rot, layout, block_table, max_pages, num_pages, page);
+  if (rc != FL_OK) return rc;
+  FL_REQUIRE(kc && vc && ks && vs, FL_E_NULL, "%s: k_cache, v_cache, k_scale and v_scale are required", fn);
+  FL_REQUIRE(kc != vc && ks != vs, FL_E_SHAPE, "%s: keys and values need a cache and scales each", fn);
+  FL_REQUIRE(((reinterpret_cast<uintptr_t>(kc) | reinterpret_cast<uintptr_t>(vc)) & 15) == 0, FL_E_SHAPE,
+             "%s: the caches must be 16-byte aligned", fn);
   return FL_OK;
 }
 

@@ -1,0 +1,54 @@
+// The paged 4-bit cache: its groups' numbers and codes, as all its kernels read them.
+#pragma once
+
+#include "fl_paged.h"
+
+namespace fl {
+
+constexpr int kGroup = 32;                 // channels of a group
+constexpr uint32_t kNaN4 = 0x7E007E00u;    // numbers of a group that is not there: fp16 NaN, NaN
+constexpr uint32_t kMaxScale4 = 0x6C45u, kMaxZero4 = 0x7800u;      // fp16 bits of 4372 and 2^15
+constexpr int kMinExp4 = -23, kMaxExp4 = 13;
+
+// whether a group's numbers are such as an append writes: int4 scale | zero << 16, e2m1 the exponent's byte
+template <bool INT>
+__device__ __forceinline__ bool group_ok(uint32_t m) {
+  if constexpr (INT) return ((m & 0xFFFFu) <= kMaxScale4) & (((m >> 16) & 0x7FFFu) <= kMaxZero4);
+  else return m - (uint32_t)(kMinExp4 + 127) <= (uint32_t)(kMaxExp4 - kMinExp4);
+}
+
+// Bytes of a group's numbers.
+template <bool INT>
+constexpr int meta_bytes() { return INT ? 4 : 1; }
+
+template <bool INT>
+__device__ __forceinline__ uint32_t load_meta(const uint8_t* at) {
+  if constexpr (INT) return *reinterpret_cast<const uint32_t*>(at);
+  else return *at;
+}
+
+// The eight values of a word of codes in fp32: one rounding of z + s c; c 2^e exactly.  NaN where the group's numbers are none.
+template <bool INT>
+__device__ __forceinline__ void values8(uint32_t w, uint32_t meta, float* x) {
+  const bool ok = group_ok<INT>(meta);
+  if constexpr (INT) {
+    const float s = ok ? f16_bits_to_f32(meta & 0xFFFFu) : NAN, z = f16_bits_to_f32(meta >> 16);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = fmaf(s, (float)((w >> (4 * e)) & 15u), z);
+  } else {
+    const float s = ok ? __uint_as_float(meta << 23) : NAN;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t c = (w >> (4 * e)) & 15u, m = c & 1u, k = (c >> 1) & 3u;
+      const float a = k == 0 ? 0.5f * (float)m : __uint_as_float(((126u + k) << 23) | (m << 22));
+      x[e] = s * (c & 8u ? -a : a);
+    }
+  }
+}
+
+// host: the checks that the calls of the 4-bit cache have in common
+int check_paged4(const char* fn, int dtype, const int32_t* cu, const int32_t* lens, int B, int T, int Hkv, int d,
+                 const float* table, int n_pos, int rot, int layout, const int32_t* block_table, int max_pages,
+                 int num_pages, int page, int format, const void* kc, const void* vc, const void* km, const void* vm);
+
+}  // namespace fl

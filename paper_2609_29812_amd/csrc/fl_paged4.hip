@@ -1,0 +1,339 @@
+// The paged 4-bit cache: appending (rotation of the keys, groups of 32 channels with numbers of their own) and reading back.
+#include "fl_paged4.h"
+
+#include <algorithm>
+
+namespace fl {
+
+int check_paged4(const char* fn, int dtype, const int32_t* cu, const int32_t* lens, int B, int T, int Hkv, int d,
+                 const float* table, int n_pos, int rot, int layout, const int32_t* block_table, int max_pages,
+                 int num_pages, int page, int format, const void* kc, const void* vc, const void* km, const void* vm) {
+  FL_REQUIRE(format == FL_KV4_INT || format == FL_KV4_E2M1, FL_E_UNSUPPORTED, "%s: unknown cache format %d", fn, format);
+  const int rc = check_ragged(fn, dtype, cu, lens, B, T, Hkv, d, table, n_pos, rot, layout, block_table, max_pages, num_pages, page);
+  if (rc != FL_OK) return rc;
+  FL_REQUIRE(kc && vc && km && vm, FL_E_NULL, "%s: k_cache, v_cache, k_meta and v_meta are required", fn);
+  FL_REQUIRE(kc != vc && km != vm, FL_E_SHAPE, "%s: keys and values need a cache and groups' numbers each", fn);
+  FL_REQUIRE(((reinterpret_cast<uintptr_t>(kc) | reinterpret_cast<uintptr_t>(vc) | reinterpret_cast<uintptr_t>(km) |
+               reinterpret_cast<uintptr_t>(vm)) & 15) == 0, FL_E_SHAPE, "%s: the caches and the groups' numbers must be 16-byte aligned",
+             fn);
+  return FL_OK;
+}
+
+struct Rows4Args {
+  const uint16_t *k, *v;           // append: the new rows
+  int64_t ks, vs;
+  Batch bt;
+  Rotary rt;
+  Pages pg;
+  uint8_t *kc, *vc, *km, *vm;
+  uint16_t *kr, *vr;               // the rows that the codes stand for, or nullptr
+  int64_t krs, vrs;
+};
+
+// A wave has a row of the batch; a lane has a chunk of eight channels of a head, so that the four lanes of a quad have a group.
+// The heads of the keys and then those of the values are taken 512 / d at a time.
+struct RowPlace {
+  int pos;                         // position, or -1: the row belongs to no sequence
+  int64_t at;                      // row of [num_pages, Hkv, page] of its head 0; -1: its page is not there
+};
+__device__ __forceinline__ RowPlace place_of_row(const Rows4Args& a, int t) {
+  const Seq s = find_seq(a.bt, t, 0, [](int c) { return c; });
+  if (s.b < 0 || t >= s.r1) return {-1, -1};
+  const int64_t pos = (int64_t)s.len - (s.r1 - t);
+  RowPlace w{(int)max(pos, (int64_t)0), -1};
+  const int64_t pi = pos >> a.pg.log2;
+  if (pos < 0 || pi >= a.bt.max_pages) return w;
+  const int pid = a.bt.table[(int64_t)s.b * a.bt.max_pages + pi];
+  if ((uint32_t)pid < (uint32_t)a.pg.num) w.at = (int64_t)pid * a.pg.heads * a.pg.size + (pos & (a.pg.size - 1));
+  return w;
+}
+
+template <int CTRL>
+__device__ __forceinline__ float quad(float x) {
+  return __uint_as_float(__builtin_amdgcn_mov_dpp((int)__float_as_uint(x), CTRL, 0xF, 0xF, true));
+}
+__device__ __forceinline__ float quad_max(float x) {
+  x = fmaxf(x, quad<0xB1>(x));                     // lanes 1 0 3 2
+  return fmaxf(x, quad<0x4E>(x));                  // lanes 2 3 0 1
+}
+
+// next fp16 away from zero
+__device__ __forceinline__ uint32_t f16_rtz(float x) {
+  return (uint32_t)__builtin_bit_cast(uint16_t, __builtin_amdgcn_cvt_pkrtz(x, 0.0f)[0]);
+}
+
+// The codes of a lane's eight values x (a word), the group's numbers (every lane of the quad has them).
+template <bool INT>
+__device__ __forceinline__ uint32_t encode_group(const float* x, uint32_t& meta) {
+  if constexpr (INT) {
+    float lo = x[0], hi = x[0], bad = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      lo = fminf(lo, x[e]);
+      hi = fmaxf(hi, x[e]);
+      bad = fmaf(x[e], 0.0f, bad);                 // NaN with an infinity or a NaN
+    }
+    lo = -quad_max(-lo);
+    hi = quad_max(hi);
+    bad = quad_max(bad == 0.0f ? 0.0f : 1.0f);
+    lo = fminf(fmaxf(lo, -32768.0f), 32768.0f);
+    hi = fminf(fmaxf(hi, -32768.0f), 32768.0f);
+    if (bad > 0.0f) {
+      meta = kNaN4;
+      return 0;
+    }
+    uint32_t zb = f16_rtz(lo);
+    zb += f16_bits_to_f32(zb) > lo ? 1u : 0u;      // (towards zero is upwards below it)
+    zb = zb == 0x8000u ? 0u : zb;
+    const float z = f16_bits_to_f32(zb);
+    // the smallest s with 15 s >= max - z: at most two steps above what a quotient that is a little too small gives
+    const double range = fabs((double)hi - (double)z);      // (not -0)
+    uint32_t sb = f16_rtz((float)range * (0.99999988f / 15.0f));
+#pragma unroll
+    for (int e = 0; e < 2; ++e) sb += 15.0 * (double)f16_bits_to_f32(sb) < range ? 1u : 0u;
+    meta = sb | zb << 16;
+    if (sb == 0) return 0;
+    const float s = f16_bits_to_f32(sb), inv = __builtin_amdgcn_rcpf(s);
+    // the product with the reciprocal is within 2^-18 of the quotient; next to a half the definition's own steps decide
+    float r[8], off = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float q = fminf(fmaxf((x[e] - z) * inv, 0.0f), 15.0f);
+      r[e] = rintf(q);
+      off = fmaxf(off, fabsf(q - r[e]));
+    }
+    if (off > 0.4999f) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) r[e] = (float)fmin(fmax(rint(((double)x[e] - (double)z) / (double)s), 0.0), 15.0);
+    }
+    const float w0 = fmaf(fmaf(fmaf(r[3], 16.0f, r[2]), 16.0f, r[1]), 16.0f, r[0]);
+    const float w1 = fmaf(fmaf(fmaf(r[7], 16.0f, r[6]), 16.0f, r[5]), 16.0f, r[4]);
+    return (uint32_t)w0 | (uint32_t)w1 << 16;
+  } else {
+    float most = 0.0f, bad = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      most = fmaxf(most, fabsf(x[e]));
+      bad = fmaf(x[e], 0.0f, bad);
+    }
+    most = fminf(quad_max(most), 32768.0f);
+    bad = quad_max(bad == 0.0f ? 0.0f : 1.0f);
+    if (bad > 0.0f) {
+      meta = 255;
+      return 0;
+    }
+    // most = m 2^k with m in [1, 2): within 6 2^e = 1.5 2^(e + 2) from e = k - 2 on, or k - 1 when m > 1.5
+    const uint32_t bits = __float_as_uint(most);
+    const int e = max((int)(bits >> 23) - 127 - 2 + ((bits & 0x7FFFFFu) > 0x400000u ? 1 : 0), kMinExp4);
+    meta = (uint32_t)(e + 127);
+    const float down = __uint_as_float((uint32_t)(127 - e) << 23);
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = fminf(fmaxf(x[i], -32768.0f), 32768.0f) * down;
+    uint32_t w = 0;
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[0], y[1], 1.0f, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[2], y[3], 1.0f, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[4], y[5], 1.0f, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[6], y[7], 1.0f, 3);
+  }
+}
+
+template <int D, bool INT, bool F16>
+__global__ __launch_bounds__(256) void paged4_append_kernel(Rows4Args a) {
+  constexpr int CH = D / 8, HPW = 64 / CH;         // chunks of a head; heads of a wave at a time
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int t = blockIdx.x * 4 + wave;
+  if (t >= a.bt.T) return;
+  const RowPlace w = place_of_row(a, t);
+  if (w.at < 0) return;
+  const int c = lane % CH, sub = lane / CH;
+  const int half = a.rt.table ? a.rt.rot / 16 : 0;                    // chunks of half the rotated part
+  const bool turn = c < 2 * half, apart = a.rt.layout == FL_ROPE_HALF;
+  const int mate = !turn || !apart ? c : c < half ? c + half : c - half;
+  float cs[16];                                                       // cosines and sines of the chunk's pairs
+#pragma unroll
+  for (int e = 0; e < 16; ++e) cs[e] = 0.0f;
+  if (turn) {
+    const float4* row = reinterpret_cast<const float4*>(a.rt.table + (int64_t)w.pos * a.rt.rot + (apart ? 16 * min(c, mate) : 8 * c));
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (e < 2 || apart) {
+        const float4 f = row[e];
+        cs[4 * e] = f.x; cs[4 * e + 1] = f.y; cs[4 * e + 2] = f.z; cs[4 * e + 3] = f.w;
+      }
+  }
+  const int slots = 2 * a.pg.heads;
+  for (int s = sub; s < slots; s += HPW) {
+    const bool is_k = s < a.pg.heads;
+    const int h = is_k ? s : s - a.pg.heads;
+    const uint16_t* src = (is_k ? a.k + (int64_t)t * a.ks : a.v + (int64_t)t * a.vs) + (int64_t)h * D;
+    const uint4 own = reinterpret_cast<const uint4*>(src)[c];
+    float x[8];
+    unpack8<F16>(own, x);
+    if (is_k && turn) {
+      // the products of 8- or 11-bit values with fp32 ones are exact in fp64: one rounding, by the sum, then fp32
+      if (apart) {
+        float y[8];
+        unpack8<F16>(reinterpret_cast<const uint4*>(src)[mate], y);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const double p = x[e], q = y[e], co = cs[2 * e], si = cs[2 * e + 1];
+          x[e] = (float)(c < half ? fma(p, co, -(q * si)) : fma(q, si, p * co));
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const double p = x[2 * e], q = x[2 * e + 1], co = cs[2 * e], si = cs[2 * e + 1];
+          x[2 * e] = (float)fma(p, co, -(q * si));
+          x[2 * e + 1] = (float)fma(p, si, q * co);
+        }
+      }
+    }
+    uint32_t meta;
+    const uint32_t codes = encode_group<INT>(x, meta);
+    const int64_t at = w.at + (int64_t)h * a.pg.size;
+    reinterpret_cast<uint32_t*>((is_k ? a.kc : a.vc) + at * (D / 2))[c] = codes;
+    if ((c & 3) == 0) {
+      uint8_t* m = (is_k ? a.km : a.vm) + (at * (D / kGroup) + c / 4) * meta_bytes<INT>();
+      if constexpr (INT) *reinterpret_cast<uint32_t*>(m) = meta;
+      else *m = (uint8_t)meta;
+    }
+    uint16_t* out = is_k ? a.kr : a.vr;
+    if (out) {
+      values8<INT>(codes, meta, x);
+      reinterpret_cast<uint4*>(out + (int64_t)t * (is_k ? a.krs : a.vrs) + (int64_t)h * D)[c] = pack8<F16>(x);
+    }
+  }
+}
+
+template <int D, bool INT, bool F16>
+__global__ __launch_bounds__(256) void paged4_read_kernel(Rows4Args a) {
+  constexpr int CH = D / 8, HPW = 64 / CH;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int t = blockIdx.x * 4 + wave;
+  if (t >= a.bt.T) return;
+  const RowPlace w = place_of_row(a, t);
+  if (w.pos < 0) return;
+  const int c = lane % CH, sub = lane / CH;
+  for (int s = sub; s < 2 * a.pg.heads; s += HPW) {
+    const bool is_k = s < a.pg.heads;
+    const int h = is_k ? s : s - a.pg.heads;
+    uint16_t* out = is_k ? a.kr : a.vr;
+    if (!out) continue;
+    float x[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    if (w.at >= 0) {
+      const int64_t at = w.at + (int64_t)h * a.pg.size;
+      const uint32_t codes = reinterpret_cast<const uint32_t*>((is_k ? a.kc : a.vc) + at * (D / 2))[c];
+      const uint32_t meta = load_meta<INT>((is_k ? a.km : a.vm) + (at * (D / kGroup) + c / 4) * meta_bytes<INT>());
+      values8<INT>(codes, meta, x);
+    }
+    reinterpret_cast<uint4*>(out + (int64_t)t * (is_k ? a.krs : a.vrs) + (int64_t)h * D)[c] = pack8<F16>(x);
+  }
+}
+
+template <int D>
+static void launch_append4(const Rows4Args& a, unsigned grid, int format, int dtype, hipStream_t st) {
+  if (format == FL_KV4_INT) {
+    if (dtype == FL_F16) paged4_append_kernel<D, true, true><<<grid, 256, 0, st>>>(a);
+    else paged4_append_kernel<D, true, false><<<grid, 256, 0, st>>>(a);
+  } else {
+    if (dtype == FL_F16) paged4_append_kernel<D, false, true><<<grid, 256, 0, st>>>(a);
+    else paged4_append_kernel<D, false, false><<<grid, 256, 0, st>>>(a);
+  }
+}
+template <int D>
+static void launch_read4(const Rows4Args& a, unsigned grid, int format, int dtype, hipStream_t st) {
+  if (format == FL_KV4_INT) {
+    if (dtype == FL_F16) paged4_read_kernel<D, true, true><<<grid, 256, 0, st>>>(a);
+    else paged4_read_kernel<D, true, false><<<grid, 256, 0, st>>>(a);
+  } else {
+    if (dtype == FL_F16) paged4_read_kernel<D, false, true><<<grid, 256, 0, st>>>(a);
+    else paged4_read_kernel<D, false, false><<<grid, 256, 0, st>>>(a);
+  }
+}
+
+}  // namespace fl
+
+using namespace fl;
+
+extern "C" int fl_paged4_append(const void* k, int64_t k_stride, const void* v, int64_t v_stride, int dtype, const int32_t* cu,
+                                const int32_t* lens, int B, int T, int Hkv, int d, const float* table, int n_pos, int rot,
+                                int layout, const int32_t* block_table, int max_pages, int num_pages, int page, int format,
+                                void* k_cache, void* v_cache, void* k_meta, void* v_meta, void* k_rows, int64_t k_rows_stride,
+                                void* v_rows, int64_t v_rows_stride, void* stream) {
+  FL_API_BEGIN
+  const char* fn = "fl_paged4_append";
+  int rc = check_paged4(fn, dtype, cu, lens, B, T, Hkv, d, table, n_pos, rot, layout, block_table, max_pages, num_pages, page,
+                        format, k_cache, v_cache, k_meta, v_meta);
+  if (rc != FL_OK) return rc;
+  if (T == 0) return FL_OK;
+  struct Side {
+    const char* name;
+    const void* x;
+    int64_t stride;
+  };
+  const Side in[2] = {{"k", k, k_stride}, {"v", v, v_stride}}, out[2] = {{"k_rows", k_rows, k_rows_stride}, {"v_rows", v_rows, v_rows_stride}};
+  for (const Side& s : in) {
+    rc = check_rows(fn, s.name, s.x, s.stride, Hkv, d);
+    if (rc != FL_OK) return rc;
+  }
+  for (int o = 0; o < 2; ++o) {
+    if (!out[o].x) continue;
+    rc = check_rows(fn, out[o].name, out[o].x, out[o].stride, Hkv, d);
+    for (int i = 0; i < 2 && rc == FL_OK; ++i)
+      if (i != o || in[i].x != out[o].x || in[i].stride != out[o].stride)
+        rc = check_apart(fn, out[o].name, out[o].x, out[o].stride, in[i].name, in[i].x, in[i].stride, T, Hkv * d);
+    if (rc != FL_OK) return rc;
+  }
+  if (k_rows && v_rows) {
+    rc = check_apart(fn, "k_rows", k_rows, k_rows_stride, "v_rows", v_rows, v_rows_stride, T, Hkv * d);
+    if (rc != FL_OK) return rc;
+  }
+  hipStream_t st = as_stream(stream);
+  Rows4Args a{};
+  a.k = static_cast<const uint16_t*>(k); a.v = static_cast<const uint16_t*>(v); a.ks = k_stride; a.vs = v_stride;
+  a.bt = {cu, lens, block_table, B, T, max_pages};
+  a.rt = {table, rot, layout};
+  a.pg = {num_pages, page, log2_of(page), Hkv};
+  a.kc = static_cast<uint8_t*>(k_cache); a.vc = static_cast<uint8_t*>(v_cache);
+  a.km = static_cast<uint8_t*>(k_meta); a.vm = static_cast<uint8_t*>(v_meta);
+  a.kr = static_cast<uint16_t*>(k_rows); a.vr = static_cast<uint16_t*>(v_rows); a.krs = k_rows_stride; a.vrs = v_rows_stride;
+  rc = check_batch(fn, a.bt, a.pg, true, st);
+  if (rc != FL_OK) return rc;
+  const unsigned grid = ((unsigned)T + 3) / 4;
+  if (d == 128) launch_append4<128>(a, grid, format, dtype, st);
+  else launch_append4<64>(a, grid, format, dtype, st);
+  return check_launch("paged4_append_kernel");
+  FL_API_END
+}
+
+extern "C" int fl_paged4_read(const int32_t* cu, const int32_t* lens, int B, int T, int Hkv, int d, const int32_t* block_table,
+                              int max_pages, int num_pages, int page, int format, const void* k_cache, const void* v_cache,
+                              const void* k_meta, const void* v_meta, int dtype, void* k_out, int64_t k_out_stride, void* v_out,
+                              int64_t v_out_stride, void* stream) {
+  FL_API_BEGIN
+  const char* fn = "fl_paged4_read";
+  int rc = check_paged4(fn, dtype, cu, lens, B, T, Hkv, d, nullptr, 0, 0, 0, block_table, max_pages, num_pages, page, format,
+                        k_cache, v_cache, k_meta, v_meta);
+  if (rc != FL_OK) return rc;
+  if (T == 0) return FL_OK;
+  FL_REQUIRE(k_out || v_out, FL_E_NULL, "%s: k_out and v_out are NULL", fn);
+  if (k_out) rc = check_rows(fn, "k_out", k_out, k_out_stride, Hkv, d);
+  if (rc == FL_OK && v_out) rc = check_rows(fn, "v_out", v_out, v_out_stride, Hkv, d);
+  if (rc == FL_OK && k_out && v_out) rc = check_apart(fn, "k_out", k_out, k_out_stride, "v_out", v_out, v_out_stride, T, Hkv * d);
+  if (rc != FL_OK) return rc;
+  hipStream_t st = as_stream(stream);
+  Rows4Args a{};
+  a.bt = {cu, lens, block_table, B, T, max_pages};
+  a.pg = {num_pages, page, log2_of(page), Hkv};
+  a.kc = static_cast<uint8_t*>(const_cast<void*>(k_cache)); a.vc = static_cast<uint8_t*>(const_cast<void*>(v_cache));
+  a.km = static_cast<uint8_t*>(const_cast<void*>(k_meta)); a.vm = static_cast<uint8_t*>(const_cast<void*>(v_meta));
+  a.kr = static_cast<uint16_t*>(k_out); a.vr = static_cast<uint16_t*>(v_out); a.krs = k_out_stride; a.vrs = v_out_stride;
+  rc = check_batch(fn, a.bt, a.pg, false, st);
+  if (rc != FL_OK) return rc;
+  const unsigned grid = ((unsigned)T + 3) / 4;
+  if (d == 128) launch_read4<128>(a, grid, format, dtype, st);
+  else launch_read4<64>(a, grid, format, dtype, st);
+  return check_launch("paged4_read_kernel");
+  FL_API_END
+}

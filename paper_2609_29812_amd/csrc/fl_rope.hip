@@ -116,16 +116,20 @@ int check_rows(const char* fn, const char* name, const void* x, int64_t stride, 
   return FL_OK;
 }
 
+int check_disjoint(const char* fn, const char* xn, const void* x, int64_t xs, int tx, int wx, const char* yn, const void* y,
+                   int64_t ys, int ty, int wy) {
+  const uintptr_t x0 = reinterpret_cast<uintptr_t>(x), y0 = reinterpret_cast<uintptr_t>(y);
+  const uint64_t bx = 2 * (uint64_t)wx, by = 2 * (uint64_t)wy, step = 2 * (uint64_t)xs;
+  const uint64_t xe = x0 + 2 * (uint64_t)(tx - 1) * xs + bx, ye = y0 + 2 * (uint64_t)(ty - 1) * ys + by;
+  // rows of the one may lie between the rows of the other, as the parts of a fused projection do
+  const uint64_t gap = y0 > x0 ? (y0 - x0) % step : (step - (x0 - y0) % step) % step;
+  FL_REQUIRE(xe <= y0 || ye <= x0 || (xs == ys && gap >= bx && gap + by <= step), FL_E_SHAPE, "%s: %s and %s overlap", fn, xn, yn);
+  return FL_OK;
+}
+
 int check_apart(const char* fn, const char* xn, const void* x, int64_t xs, const char* yn, const void* y, int64_t ys, int T,
                 int width) {
-  const uintptr_t x0 = reinterpret_cast<uintptr_t>(x), y0 = reinterpret_cast<uintptr_t>(y);
-  const uint64_t w = 2 * (uint64_t)width;
-  const uint64_t xe = x0 + 2 * (uint64_t)(T - 1) * xs + w, ye = y0 + 2 * (uint64_t)(T - 1) * ys + w;
-  // rows of the one may lie between the rows of the other, as the parts of a fused projection do
-  const uint64_t gap = (x0 > y0 ? x0 - y0 : y0 - x0) % (2 * (uint64_t)xs);
-  FL_REQUIRE(xe <= y0 || ye <= x0 || (xs == ys && gap >= w && gap <= 2 * (uint64_t)xs - w), FL_E_SHAPE, "%s: %s and %s overlap",
-             fn, xn, yn);
-  return FL_OK;
+  return check_disjoint(fn, xn, x, xs, T, width, yn, y, ys, T, width);
 }
 
 int check_rotary(const char* fn, const float* table, int rot, int layout, int d) {

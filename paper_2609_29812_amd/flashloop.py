@@ -87,6 +87,17 @@ _SIGNATURES = {
     "fl_paged_attn": (_c_i, [_c_p, _c_l, _c_i, _c_p, _c_p, _c_i, _c_i, _c_i, _c_i, _c_i, _c_p, _c_i, _c_i, _c_i, _c_p,
                              _c_i, _c_i, _c_i, _c_i, _c_p, _c_p, _c_p, _c_p, _c_f, _c_i, _c_i, _c_i, _c_i, _c_p, _c_l,
                              _c_p, _c_p, _c_sz, _c_p]),
+    "fl_packed_attn_ws": (_c_sz, [_c_i] * 9),
+    "fl_packed_attn": (_c_i, [_c_p, _c_l, _c_p, _c_l, _c_p, _c_l, _c_i, _c_p, _c_p, _c_i, _c_i, _c_i, _c_i, _c_i, _c_i, _c_p,
+                              _c_i, _c_i, _c_i, _c_f, _c_i, _c_i, _c_i, _c_p, _c_l, _c_p, _c_p, _c_sz, _c_p]),
+    "fl_paged4_append": (_c_i, [_c_p, _c_l, _c_p, _c_l, _c_i, _c_p, _c_p, _c_i, _c_i, _c_i, _c_i, _c_p, _c_i, _c_i, _c_i,
+                                _c_p, _c_i, _c_i, _c_i, _c_i, _c_p, _c_p, _c_p, _c_p, _c_p, _c_l, _c_p, _c_l, _c_p]),
+    "fl_paged4_read": (_c_i, [_c_p, _c_p, _c_i, _c_i, _c_i, _c_i, _c_p, _c_i, _c_i, _c_i, _c_i, _c_p, _c_p, _c_p, _c_p, _c_i,
+                              _c_p, _c_l, _c_p, _c_l, _c_p]),
+    "fl_paged4_attn_ws": (_c_sz, [_c_i] * 11),
+    "fl_paged4_attn": (_c_i, [_c_p, _c_l, _c_i, _c_p, _c_p, _c_i, _c_i, _c_i, _c_i, _c_i, _c_p, _c_i, _c_i, _c_i, _c_p,
+                              _c_i, _c_i, _c_i, _c_i, _c_p, _c_p, _c_p, _c_p, _c_f, _c_i, _c_i, _c_i, _c_i, _c_p, _c_l,
+                              _c_p, _c_p, _c_sz, _c_p]),
 }
 
 EXPORTS = tuple(_SIGNATURES)
@@ -600,6 +611,7 @@ def kv_keep_recent(x_cur, idx, tail, cache=None, rows=None):
 # ---- (9) rotary positions -------------------------------------------------------------------------------
 _DTYPES = {torch.bfloat16: 0, torch.float16: 1}
 _FORMATS = {torch.int8: 0, torch.float8_e4m3fn: 1}
+_FORMATS4 = {torch.float16: 0, torch.uint8: 1}       # by the type of the groups' numbers
 
 
 # (As above, a tensor that passes its checks passes them in one expression: a call's host time is that of its launch.)
@@ -815,4 +827,200 @@ def paged_attn_ws(q, block_table, k_cache, window=0, n_sink=0, max_q=None, max_l
     max_q = -(-T // B) if max_q is None else max_q
     _counts(T=T, B=B, max_pages=max_pages, window=window, n_sink=n_sink, max_q=max_q, max_len=max_len)
     need = load().fl_paged_attn_ws(B, T, Hq, k_cache.shape[1], d, k_cache.shape[2], max_pages, window, n_sink, max_q, max_len)
+    return torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+
+
+# ---- (12) attention of packed prompts ---------------------------------------------------------------------
+def packed_attn(q, k, v, cu_q, cu_k=None, table=None, layout="half", sm_scale=None, window=0, n_sink=0, max_k=0, out=None, lse=None,
+                ws=None):
+    """Causal attention of packed sequences: q bf16 or fp16 [Tq, Hq, d], k and v [Tk, Hkv, d] of its type, any row strides that
+    are multiples of 8; Hq a multiple of Hkv.  Sequence b has the query rows cu_q[b] .. cu_q[b+1]-1 (int32 [B + 1]) and the key rows
+    cu_k[b] .. cu_k[b+1]-1 (default: cu_q, whole prompts); its queries are the last of its positions.  window > 0: a row at position
+    i sees j > i - window and j < n_sink alone.  With a rotary table the queries (not the keys) are turned by their positions, as
+    rope leaves them.  max_k: the largest number of keys of a sequence, as far as known (it chooses how the work is cut, not the
+    result).  lse: optional fp32 [Tq, Hq] to write the log-normalisers to.  ws: optional uint8 workspace (packed_attn_ws).  Returns
+    out [Tq, Hq, d]; rows behind cu_q[B] of a given out are left as they were."""
+    at, dtype = _here(q, "q"), q.dtype
+    qs = _rows(q, at, dtype, "q")
+    Tq, Hq, d = q.shape
+    ks = _rows(k, at, dtype, "k")
+    Tk, Hkv, dk = shape = k.shape
+    vs = _rows(v, at, dtype, "v", shape)
+    if dk != d:
+        raise FlashLoopError(f"k must have heads of {d} channels as q has, got {dk}")
+    if cu_k is None:
+        cu_k = cu_q
+    if cu_q.dim() != 1 or cu_q.shape[0] < 2:
+        raise FlashLoopError(f"cu_q must have shape [B + 1] for at least one sequence, got {tuple(cu_q.shape)}")
+    B = cu_q.shape[0] - 1
+    _on(cu_q, at, torch.int32, "cu_q")
+    _on(cu_k, at, torch.int32, "cu_k", (B + 1,))
+    n_pos, rot = _turns(table, at)
+    if out is None:
+        out, os_ = q.new_empty((Tq, Hq, d)), Hq * d
+    else:
+        os_ = _rows(out, at, dtype, "out", q.shape)
+    _on(lse, at, torch.float32, "lse", (Tq, Hq))
+    if (window | n_sink | max_k | n_pos | Tq | Tk | B) >> 31:
+        _counts(window=window, n_sink=n_sink, max_k=max_k, n_pos=n_pos, Tq=Tq, Tk=Tk, B=B)
+    lib = _lib or load()
+    if ws is None:
+        need = lib.fl_packed_attn_ws(B, Tq, Tk, Hq, Hkv, d, window, n_sink, max_k)
+        ws = cu_q.new_empty(need, dtype=torch.uint8) if need else None
+    else:
+        _on(ws, at, torch.uint8, "ws")
+    rc = lib.fl_packed_attn(q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, _DTYPES[dtype], cu_q.data_ptr(), cu_k.data_ptr(), B,
+                            Tq, Tk, Hq, Hkv, d, _p(table), n_pos, rot, _choice(layout, ROPE_LAYOUT, "layout"),
+                            1.0 / math.sqrt(d) if sm_scale is None else sm_scale, window, n_sink, max_k, out.data_ptr(), os_, _p(lse),
+                            _p(ws), 0 if ws is None else ws.numel(), _stream())
+    if rc:
+        _check(rc, "fl_packed_attn")
+    return out
+
+
+def packed_attn_ws(q, k, B, window=0, n_sink=0, max_k=0):
+    """A workspace for packed_attn over these shapes and hints (None when it needs none)."""
+    (Tq, Hq, d), (Tk, Hkv, _) = q.shape, k.shape
+    _counts(Tq=Tq, Tk=Tk, B=B, window=window, n_sink=n_sink, max_k=max_k)
+    need = load().fl_packed_attn_ws(B, Tq, Tk, Hq, Hkv, d, window, n_sink, max_k)
+    return torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+
+
+# ---- (13) the paged 4-bit cache ---------------------------------------------------------------------------
+KV4_FORMAT = {"int4": torch.float16, "e2m1": torch.uint8}
+
+
+def paged4_cache(num_pages, Hkv, page, d, fmt="int4", device="cuda"):
+    """An empty 4-bit cache: (k_cache, v_cache uint8 [num_pages, Hkv, page, d / 2], k_meta, v_meta).  Groups of 32 channels of a
+    position and head have numbers of their own: "int4" fp16 [num_pages, Hkv, page, d / 32, 2] (scale, zero), "e2m1" uint8
+    [num_pages, Hkv, page, d / 32] exponents + 127.  Pages need no clearing, here or when they are given to another sequence."""
+    kind = _choice(fmt, KV4_FORMAT, "fmt")
+    shape = (num_pages, Hkv, page, d // 32) + ((2,) if fmt == "int4" else ())
+    return (*(torch.empty(num_pages, Hkv, page, d // 2, dtype=torch.uint8, device=device) for _ in range(2)),
+            *(torch.empty(shape, dtype=kind, device=device) for _ in range(2)))
+
+
+def _paged4(at, T, cu, lens, block_table, k_cache, v_cache, k_meta, v_meta, Hkv, d):
+    """(B, max_pages, num_pages, page, format) of a ragged batch over a 4-bit cache."""
+    if block_table.dim() != 2 or k_cache.dim() != 4:
+        raise FlashLoopError("block_table must be [B, max_pages] and the caches [num_pages, Hkv, page, d / 2]")
+    kind = k_meta.dtype
+    if kind not in _FORMATS4:
+        raise FlashLoopError(f"k_meta must be float16 (int4) or uint8 (e2m1), got {kind}")
+    B, max_pages = block_table.shape
+    if B == 0:
+        raise FlashLoopError("a batch has at least one sequence")
+    shape = num_pages, _, page, _ = k_cache.shape
+    if (T | B | max_pages | num_pages) >> 31:
+        _counts(T=T, B=B, max_pages=max_pages, num_pages=num_pages)
+    groups = (num_pages, Hkv, page, d // 32, 2) if kind is torch.float16 else (num_pages, Hkv, page, d // 32)
+    if not (shape[1] == Hkv and shape[3] * 2 == d and k_cache.dtype is v_cache.dtype is torch.uint8 and v_cache.shape == shape
+            and v_meta.dtype is kind and k_meta.shape == v_meta.shape == groups
+            and cu.dtype is lens.dtype is block_table.dtype is torch.int32 and cu.shape == (B + 1,) and lens.shape == (B,)
+            and k_cache.get_device() == v_cache.get_device() == k_meta.get_device() == v_meta.get_device() == cu.get_device()
+            == lens.get_device() == block_table.get_device() == at
+            and k_cache.is_contiguous() and v_cache.is_contiguous() and k_meta.is_contiguous() and v_meta.is_contiguous()
+            and cu.is_contiguous() and lens.is_contiguous() and block_table.is_contiguous()):
+        for name, c in (("k_cache", k_cache), ("v_cache", v_cache)):
+            _on(c, at, torch.uint8, name, (num_pages, Hkv, page, d // 2))
+        for name, c in (("k_meta", k_meta), ("v_meta", v_meta)):
+            _on(c, at, kind, name, groups)
+        _on(cu, at, torch.int32, "cu", (B + 1,))
+        _on(lens, at, torch.int32, "lens", (B,))
+        _on(block_table, at, torch.int32, "block_table")
+        raise FlashLoopError(f"the caches hold heads of {2 * shape[3]} channels, not {d}")
+    return B, max_pages, num_pages, page, _FORMATS4[kind]
+
+
+def paged4_append(k, v, cu, lens, block_table, k_cache, v_cache, k_meta, v_meta, table=None, layout="half", k_rows=None, v_rows=None):
+    """Store the new positions of a ragged batch in 4 bits; the batch, the block table and the rotary table are those of
+    paged_append, the cache is paged4_cache's and updated in place.  k_rows, v_rows: optional [T, Hkv, d] of k's type to write the
+    rows to that the codes stand for (k and v themselves: in place), as paged4_read gives them: the attention of a whole prompt over
+    them (packed_attn) sees what later steps read."""
+    at, dtype = _here(k, "k"), k.dtype
+    ks = _rows(k, at, dtype, "k")
+    T, Hkv, d = shape = k.shape
+    vs = _rows(v, at, dtype, "v", shape)
+    B, max_pages, num_pages, page, fmt = _paged4(at, T, cu, lens, block_table, k_cache, v_cache, k_meta, v_meta, Hkv, d)
+    n_pos, rot = _turns(table, at)
+    if n_pos >> 31:
+        _counts(n_pos=n_pos)
+    krs = 0 if k_rows is None else _rows(k_rows, at, dtype, "k_rows", shape)
+    vrs = 0 if v_rows is None else _rows(v_rows, at, dtype, "v_rows", shape)
+    rc = (_lib or load()).fl_paged4_append(
+        k.data_ptr(), ks, v.data_ptr(), vs, _DTYPES[dtype], cu.data_ptr(), lens.data_ptr(), B, T, Hkv, d, _p(table), n_pos, rot,
+        _choice(layout, ROPE_LAYOUT, "layout"), block_table.data_ptr(), max_pages, num_pages, page, fmt, k_cache.data_ptr(),
+        v_cache.data_ptr(), k_meta.data_ptr(), v_meta.data_ptr(), _p(k_rows), krs, _p(v_rows), vrs, _stream())
+    if rc:
+        _check(rc, "fl_paged4_append")
+
+
+# ---- (14) reading the 4-bit cache back ----------------------------------------------------------------------
+def paged4_read(cu, lens, block_table, k_cache, v_cache, k_meta, v_meta, T, dtype=torch.bfloat16, k_out=None, v_out=None):
+    """Positions of a ragged batch out of a 4-bit cache: rows cu[b] .. cu[b+1]-1 of T are the last positions of sequence b, whose
+    length is lens[b] (cu the cumulative lengths: all of it).  Returns (k, v) [T, Hkv, d] of `dtype` (k_out's or v_out's where one
+    is given; rows of no sequence are left as they were).  A dense [B, N, H, d] state: k_out=state.view(B * N, H, d)."""
+    at = _here(k_cache, "k_cache")
+    if k_cache.dim() != 4:
+        raise FlashLoopError("the caches must be [num_pages, Hkv, page, d / 2]")
+    Hkv, d = k_cache.shape[1], 2 * k_cache.shape[3]
+    if T >> 31:
+        _counts(T=T)
+    for name, given in (("k_out", k_out), ("v_out", v_out)):
+        dtype = dtype if given is None else given.dtype
+    if dtype not in _DTYPES:
+        raise FlashLoopError(f"dtype must be bfloat16 or float16, got {dtype}")
+    B, max_pages, num_pages, page, fmt = _paged4(at, T, cu, lens, block_table, k_cache, v_cache, k_meta, v_meta, Hkv, d)
+    k_out = torch.empty((T, Hkv, d), dtype=dtype, device=k_cache.device) if k_out is None else k_out
+    v_out = torch.empty((T, Hkv, d), dtype=dtype, device=k_cache.device) if v_out is None else v_out
+    ks, vs = _rows(k_out, at, dtype, "k_out", (T, Hkv, d)), _rows(v_out, at, dtype, "v_out", (T, Hkv, d))
+    rc = (_lib or load()).fl_paged4_read(
+        cu.data_ptr(), lens.data_ptr(), B, T, Hkv, d, block_table.data_ptr(), max_pages, num_pages, page, fmt, k_cache.data_ptr(),
+        v_cache.data_ptr(), k_meta.data_ptr(), v_meta.data_ptr(), _DTYPES[dtype], k_out.data_ptr(), ks, v_out.data_ptr(), vs, _stream())
+    if rc:
+        _check(rc, "fl_paged4_read")
+    return k_out, v_out
+
+
+# ---- (15) attention over the 4-bit cache --------------------------------------------------------------------
+def paged4_attn(q, cu, lens, block_table, k_cache, v_cache, k_meta, v_meta, table=None, layout="half", sm_scale=None,
+                window=0, n_sink=0, max_q=None, max_len=0, out=None, lse=None, ws=None):
+    """paged_attn over a 4-bit cache (after paged4_append of the same batch): its arguments, hints and result."""
+    at, dtype = _here(q, "q"), q.dtype
+    qs = _rows(q, at, dtype, "q")
+    T, Hq, d = q.shape
+    Hkv = k_cache.shape[1] if k_cache.dim() == 4 else 0
+    B, max_pages, num_pages, page, fmt = _paged4(at, T, cu, lens, block_table, k_cache, v_cache, k_meta, v_meta, Hkv, d)
+    n_pos, rot = _turns(table, at)
+    if out is None:
+        out, os_ = q.new_empty((T, Hq, d)), Hq * d
+    else:
+        os_ = _rows(out, at, dtype, "out", q.shape)
+    _on(lse, at, torch.float32, "lse", (T, Hq))
+    max_q = -(-T // B) if max_q is None else max_q
+    if (window | n_sink | max_q | max_len | n_pos) >> 31:
+        _counts(window=window, n_sink=n_sink, max_q=max_q, max_len=max_len, n_pos=n_pos)
+    lib = _lib or load()
+    if ws is None:
+        need = lib.fl_paged4_attn_ws(B, T, Hq, Hkv, d, page, max_pages, window, n_sink, max_q, max_len)
+        ws = lens.new_empty(need, dtype=torch.uint8) if need else None
+    else:
+        _on(ws, at, torch.uint8, "ws")
+    rc = lib.fl_paged4_attn(
+        q.data_ptr(), qs, _DTYPES[dtype], cu.data_ptr(), lens.data_ptr(), B, T, Hq, Hkv, d, _p(table), n_pos, rot,
+        _choice(layout, ROPE_LAYOUT, "layout"), block_table.data_ptr(), max_pages, num_pages, page, fmt, k_cache.data_ptr(),
+        v_cache.data_ptr(), k_meta.data_ptr(), v_meta.data_ptr(), 1.0 / math.sqrt(d) if sm_scale is None else sm_scale, window,
+        n_sink, max_q, max_len, out.data_ptr(), os_, _p(lse), _p(ws), 0 if ws is None else ws.numel(), _stream())
+    if rc:
+        _check(rc, "fl_paged4_attn")
+    return out
+
+
+def paged4_attn_ws(q, block_table, k_cache, window=0, n_sink=0, max_q=None, max_len=0):
+    """A workspace for paged4_attn over these shapes and hints (None when it needs none)."""
+    T, Hq, d = q.shape
+    B, max_pages = max(1, block_table.shape[0]), block_table.shape[1]
+    max_q = -(-T // B) if max_q is None else max_q
+    _counts(T=T, B=B, max_pages=max_pages, window=window, n_sink=n_sink, max_q=max_q, max_len=max_len)
+    need = load().fl_paged4_attn_ws(B, T, Hq, k_cache.shape[1], d, k_cache.shape[2], max_pages, window, n_sink, max_q, max_len)
     return torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
