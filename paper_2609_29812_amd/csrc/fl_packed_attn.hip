@@ -1,52 +1,164 @@
-// Dense attention of packed prompts.
-#include "fl_simple_attn.h"
+// Dense attention of packed prompts: keys and values as rows in memory, for the kernel of many rows per sequence.
+#include "fl_prompt.h"
 
-#include <algorithm>
 #include <vector>
 
 namespace fl {
 
-struct PackedArgs {
-  const uint16_t *q, *k, *v;
-  uint16_t* o;
-  float* lse;
-  int64_t qs, ks, vs, os;
-  Batch bt;                        // cu: cu_q, lens: cu_k
-  Rotary rt;
-  int n_pos, Tk, Hq, Hkv, G;
-  float scale;
-  int window, n_sink;
-};
-
-template <int D, bool F16>
-struct PackedRows {
+struct PackedArgs : PagedAttnArgs {          // bt: cu = cu_q, lens = cu_k, one "page" of any length; pg.heads
   const uint16_t *k, *v;
   int64_t ks, vs;
-  __device__ __forceinline__ bool there(int) const { return true; }
-  __device__ __forceinline__ float spoilt(int) const { return 0.0f; }
-  __device__ __forceinline__ float key(int j, int c) const { return to_f32<F16>(k[(int64_t)j * ks + c]); }
-  __device__ __forceinline__ float value(int j, int c) const { return to_f32<F16>(v[(int64_t)j * vs + c]); }
+  int Tk, n_pos;
+};
+__device__ __forceinline__ int key_row(const PackedArgs& a, int b) { return min(max(a.bt.lens[b], 0), a.Tk); }
+// (lens[b] is the first key row: the length is that of the key rows)
+__device__ __forceinline__ Seq seq_of(const PackedArgs& a, int b) {
+  return {b, row_of(a.bt, b), row_of(a.bt, b + 1), max(key_row(a, b + 1) - key_row(a, b), 0)};
+}
+template <int R>
+__device__ __forceinline__ Seq find_row_tile(const PackedArgs& a, int slot) {
+  const int G = a.G;
+  Seq s = find_seq(a.bt, slot, 1, [G](int c) { return (int)((int64_t)c * G / R); });
+  if (s.b >= 0) s.len = max(key_row(a, s.b + 1) - key_row(a, s.b), 0);
+  return s;
+}
+
+// Stages of 64 key and value rows by LDS-DMA; rows behind the sequence's last read zeros.
+template <int D, bool F16>
+struct PackedSource {
+  using Args = PackedArgs;
+  struct Shared {};
+  static constexpr int kD = D;
+  static constexpr bool kF16 = F16, kOut16 = F16, kLow = false;
+  static constexpr int CH = D / 8, RPI = 64 / CH, NI = kStageKeys / RPI / 4;     // chunks of a row; rows of a load; loads of a wave
+
+  const Args& a;
+  const Span& sp;
+  const uint16_t *k, *v;                     // row 0 of the sequence, the head's channels
+  int n_k, t0, wave, lane;
+  uint32_t kofs[NI], vofs[NI];
+
+  __device__ __forceinline__ PackedSource(const Args& args, Shared&, const Seq& sq, const Span& span, int kvh, int tid, int first, int)
+      : a(args), sp(span), n_k(sq.len), t0(first), wave(__builtin_amdgcn_readfirstlane(tid >> 6)), lane(tid & 63) {
+    const int row0 = key_row(a, sq.b);
+    k = a.k + (int64_t)row0 * a.ks + kvh * D;
+    v = a.v + (int64_t)row0 * a.vs + kvh * D;
+#pragma unroll
+    for (int x = 0; x < NI; ++x) {
+      const int c = (wave * NI + x) * RPI + lane / CH;
+      const uint32_t chunk = (uint32_t)((lane % CH) ^ swz32_f<D>(c & 31)) * 16u;
+      kofs[x] = (uint32_t)c * (uint32_t)(2 * a.ks) + chunk;
+      vofs[x] = (uint32_t)c * (uint32_t)(2 * a.vs) + chunk;
+    }
+  }
+  // the rows of a stage: its offsets stay below 64 rows of at most 2^25 bytes
+  __device__ __forceinline__ rsrc_t rows(const uint16_t* x, int64_t stride, int key0) const {
+    const int left = min(n_k - key0, kStageKeys);
+    return make_rsrc(x + key0 * stride, left > 0 ? (uint32_t)(left - 1) * (uint32_t)(2 * stride) + 2u * D : 0u);
+  }
+  __device__ __forceinline__ void load_k(int st, StageTile<D>& t) {
+    const rsrc_t r = rows(k, a.ks, key_of<kStageKeys>(sp, t0 + st));
+#pragma unroll
+    for (int x = 0; x < NI; ++x)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, FL_LDS(t.x + (wave * NI + x) * 512), 16, kofs[x], 0, 0, 0);
+  }
+  __device__ __forceinline__ void load_v(int st, StageTile<D>& t) {
+    const rsrc_t r = rows(v, a.vs, key_of<kStageKeys>(sp, t0 + st));
+#pragma unroll
+    for (int x = 0; x < NI; ++x)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, FL_LDS(t.x + (wave * NI + x) * 512), 16, vofs[x], 0, 0, 0);
+  }
+  __device__ __forceinline__ void land(bool, StageTile<D>&, StageTile<D>&) { FL_WAIT_VM(0); }
+  __device__ __forceinline__ void land_k(StageTile<D>&) { FL_WAIT_VM(0); }
+  // The values that this lane's loads have brought: whether some are not finite (those become 0), and which.
+  __device__ __forceinline__ bool odd(StageTile<D>& t, uint32_t* where) const {
+    constexpr uint32_t kExp = F16 ? 0x7C00u : 0x7F80u;
+    bool any = false;
+#pragma unroll
+    for (int x = 0; x < NI; ++x) {
+      u32x4* at = reinterpret_cast<u32x4*>(t.x + (wave * NI + x) * 512 + lane * 8);
+      u32x4 w = *at;
+      uint32_t bits = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const bool lo = (w[e] & kExp) == kExp, hi = (w[e] & (kExp << 16)) == (kExp << 16);
+        bits |= (lo ? 1u : 0u) << (2 * e) | (hi ? 2u : 0u) << (2 * e);
+        w[e] &= (lo ? 0u : 0xFFFFu) | (hi ? 0u : 0xFFFF0000u);
+      }
+      const int c = (wave * NI + x) * RPI + lane / CH;
+      reinterpret_cast<uint8_t*>(where)[c * CH + ((lane % CH) ^ swz32_f<D>(c & 31))] = (uint8_t)bits;
+      if (bits != 0) *at = w;
+      any |= bits != 0;
+    }
+    return any;
+  }
+  __device__ __forceinline__ bool holes(int) const { return false; }
+  __device__ __forceinline__ bool there(int, int) const { return true; }
+  __device__ __forceinline__ float query(const Args& args, int t, int head, int pos, bool ok, int hw, u32x4* q, u32x4*) const {
+    constexpr int KS = D / 16;
+    const uint16_t* row = args.q + (int64_t)t * args.qs + (int64_t)head * D;
+    if (!args.rt.table) {
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const u32x4 w = reinterpret_cast<const u32x4*>(row)[2 * ks + hw];
+        q[ks] = ok ? w : u32x4{};
+      }
+    } else {
+      const bool in = (uint32_t)pos < (uint32_t)args.n_pos;
+      float x[KS][8];
+      turned_chunks<KS, F16>(args.rt, row, in ? pos : 0, x, [hw](int ks) { return 2 * ks + hw; });
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const bool none = !in && 8 * (2 * ks + hw) < args.rt.rot;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t w = pack2<F16>(none ? NAN : x[ks][2 * e], none ? NAN : x[ks][2 * e + 1]);
+          q[ks][e] = ok ? w : 0u;
+        }
+      }
+    }
+    return args.scale_log2;
+  }
 };
 
-// a wave a row and head
-template <int D, bool F16>
-__global__ __launch_bounds__(256) void packed_row_kernel(PackedArgs a) {
-  const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int t = (int)(w / a.Hq), h = (int)(w % a.Hq);
-  if (t >= a.bt.T) return;
-  const Seq s = find_seq(a.bt, t, 0, [](int c) { return c; });
-  if (s.b < 0 || t >= s.r1) return;
-  const int k0 = min(max(a.bt.lens[s.b], 0), a.Tk), k1 = min(max(a.bt.lens[s.b + 1], 0), a.Tk);
-  const int pos = max(k1 - k0, 0) - (s.r1 - t);
-  const PackedRows<D, F16> src{a.k + (int64_t)k0 * a.ks + (int64_t)(h / a.G) * D, a.v + (int64_t)k0 * a.vs + (int64_t)(h / a.G) * D, a.ks, a.vs};
-  float q[D / 64];
-  const bool ok = !a.rt.table || (uint32_t)pos < (uint32_t)a.n_pos;
-  turned_query<D, F16>(a.q + (int64_t)t * a.qs + (int64_t)h * D, a.rt, ok ? max(pos, 0) : 0, q);
-#pragma unroll
-  for (int x = 0; x < D / 64; ++x)
-    if (a.rt.table) q[x] = ok || (int)(threadIdx.x & 63) + 64 * x >= a.rt.rot ? to_f32<F16>((F16 ? pack_f16x2(q[x], 0.0f) : pack_bf16x2(q[x], 0.0f)) & 0xFFFFu) : NAN;
-  attend_row<D, F16>(src, q, a.scale, pos, a.window > 0 ? max(pos - a.window + 1, 0) : 0, a.n_sink,
-                     a.o + (int64_t)t * a.os + (int64_t)h * D, a.lse ? a.lse + (int64_t)t * a.Hq + h : nullptr);
+// How a call is cut: workgroups of 128 RB rows of a key/value head.
+constexpr int kPackedBlocks = 1;
+template <int RB>
+static bool packed_shared(int64_t slots, int Hkv, int64_t keys) {
+  return slots * Hkv < 2 * 512 / RB && keys >= 1024 && slots * (keys / kStageKeys + 16) < (1ll << 31) - 65536;
+}
+static int packed_shares(int Hkv, int rb) { return std::max(1, 512 / rb / Hkv); }
+
+// (the compiler emits the launching side of one of the two forms alone unless both are named)
+#define FL_FORMS(D, F16)                                                                                               \
+  template __global__ void prompt_kernel<PackedSource<D, F16>, PackedArgs, kPackedBlocks, true>(PackedArgs);           \
+  template __global__ void prompt_kernel<PackedSource<D, F16>, PackedArgs, kPackedBlocks, false>(PackedArgs);
+FL_FORMS(128, true)
+FL_FORMS(128, false)
+FL_FORMS(64, true)
+FL_FORMS(64, false)
+#undef FL_FORMS
+
+template <int D, bool F16, int RB>
+static int launch_packed(PackedArgs& a, bool shared, hipStream_t st) {
+  constexpr int R = 128 * RB;
+  using Source = PackedSource<D, F16>;
+  const unsigned grid = (unsigned)((int64_t)(shared ? a.share : a.slots) * a.pg.heads);
+  if (!shared) {
+    prompt_kernel<Source, PackedArgs, RB, false><<<grid, 256, 0, st>>>(a);
+    return check_launch("prompt_kernel");
+  }
+  const size_t places = (size_t)a.share * a.pg.heads * 2 * R;
+  a.part_ml = a.part + places * D;
+  a.ends = reinterpret_cast<int*>(a.part_ml + places * 2);
+  prompt_plan_kernel<PackedArgs, R><<<1, 1024, 0, st>>>(a);
+  int rc = check_launch("prompt_plan_kernel");
+  if (rc != FL_OK) return rc;
+  prompt_kernel<Source, PackedArgs, RB, true><<<grid, 256, 0, st>>>(a);
+  rc = check_launch("prompt_kernel");
+  if (rc != FL_OK) return rc;
+  prompt_join_kernel<PackedArgs, D, F16, R><<<(unsigned)((int64_t)a.slots * (R / 32) * a.pg.heads), 256, 0, st>>>(a);
+  return check_launch("prompt_join_kernel");
 }
 
 static int check_offsets(const char* fn, const char* name, const int32_t* cu, int B, int T, hipStream_t st) {
@@ -64,7 +176,31 @@ static int check_offsets(const char* fn, const char* name, const int32_t* cu, in
 
 using namespace fl;
 
-extern "C" size_t fl_packed_attn_ws(int, int, int, int, int, int, int, int, int) { return 0; }
+namespace {
+struct PackedPlan {
+  int64_t slots;
+  bool shared;
+  int share;
+  size_t ws;
+};
+PackedPlan packed_plan(int B, int Tq, int Tk, int Hq, int Hkv, int d, int window, int n_sink, int max_k) {
+  constexpr int RB = kPackedBlocks, R = 128 * RB;
+  PackedPlan p{};
+  p.slots = (int64_t)Tq * (Hq / Hkv) / R + B;
+  int64_t keys = max_k > 0 ? std::min(max_k, Tk) : Tk;
+  if (window > 0) keys = std::min<int64_t>(keys, (int64_t)window + n_sink + R);
+  p.shared = packed_shared<RB>(p.slots, Hkv, keys);
+  p.share = packed_shares(Hkv, RB);
+  p.ws = p.shared ? (size_t)p.share * Hkv * 2 * R * (d + 2) * sizeof(float) + (size_t)p.slots * sizeof(int) : 0;
+  return p;
+}
+}  // namespace
+
+extern "C" size_t fl_packed_attn_ws(int B, int Tq, int Tk, int Hq, int Hkv, int d, int window, int n_sink, int max_k) {
+  if (B < 1 || Tq < 1 || Tk < 0 || Hkv < 1 || Hq < Hkv || Hq % Hkv || (d != 64 && d != 128) || window < 0 || n_sink < 0 || max_k < 0)
+    return 0;
+  return packed_plan(B, Tq, Tk, Hq, Hkv, d, window, n_sink, max_k).ws;
+}
 
 extern "C" int fl_packed_attn(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                               int dtype, const int32_t* cu_q, const int32_t* cu_k, int B, int Tq, int Tk, int Hq, int Hkv, int d,
@@ -106,20 +242,20 @@ extern "C" int fl_packed_attn(const void* q, int64_t q_stride, const void* k, in
     if (rc == FL_OK) rc = check_offsets(fn, "cu_k", cu_k, B, Tk, st);
     if (rc != FL_OK) return rc;
   }
+  const PackedPlan p = packed_plan(B, Tq, Tk, Hq, Hkv, d, window, n_sink, max_k);
+  FL_REQUIRE(p.slots * Hkv * 8 < (1ll << 31), FL_E_SHAPE, "%s: too many rows", fn);
+  FL_REQUIRE(p.ws == 0 || (ws && ws_bytes >= p.ws), FL_E_WORKSPACE, "%s: workspace of %zu bytes required", fn, p.ws);
+  FL_REQUIRE((reinterpret_cast<uintptr_t>(ws) & 15) == 0, FL_E_SHAPE, "%s: ws must be 16-byte aligned", fn);
   PackedArgs a{};
   a.q = static_cast<const uint16_t*>(q); a.k = static_cast<const uint16_t*>(k); a.v = static_cast<const uint16_t*>(v);
   a.o = static_cast<uint16_t*>(o); a.lse = lse; a.qs = q_stride; a.ks = k_stride; a.vs = v_stride; a.os = o_stride;
-  a.bt = {cu_q, cu_k, nullptr, B, Tq, 0};
+  a.bt = {cu_q, cu_k, nullptr, B, Tq, INT_MAX - 4096};
   a.rt = {table, rot, layout};
-  a.n_pos = n_pos; a.Tk = Tk; a.Hq = Hq; a.Hkv = Hkv; a.G = Hq / Hkv; a.scale = sm_scale; a.window = window; a.n_sink = n_sink;
-  const unsigned grid = (unsigned)(((int64_t)Tq * Hq + 3) / 4);
-  if (d == 128) {
-    if (dtype == FL_F16) packed_row_kernel<128, true><<<grid, 256, 0, st>>>(a);
-    else packed_row_kernel<128, false><<<grid, 256, 0, st>>>(a);
-  } else {
-    if (dtype == FL_F16) packed_row_kernel<64, true><<<grid, 256, 0, st>>>(a);
-    else packed_row_kernel<64, false><<<grid, 256, 0, st>>>(a);
-  }
-  return check_launch("packed_row_kernel");
+  a.pg = {0, 1, 0, Hkv};
+  a.n_pos = n_pos; a.Tk = Tk; a.Hq = Hq; a.G = Hq / Hkv; a.scale_log2 = sm_scale * 1.4426950408889634f;
+  a.window = window; a.n_sink = n_sink;
+  a.slots = (int)p.slots; a.share = p.share; a.part = static_cast<float*>(ws);
+  if (d == 128) return dtype == FL_F16 ? launch_packed<128, true, kPackedBlocks>(a, p.shared, st) : launch_packed<128, false, kPackedBlocks>(a, p.shared, st);
+  return dtype == FL_F16 ? launch_packed<64, true, kPackedBlocks>(a, p.shared, st) : launch_packed<64, false, kPackedBlocks>(a, p.shared, st);
   FL_API_END
 }

@@ -160,30 +160,20 @@ __device__ __forceinline__ void cut(Span& s, int parts) {
 template <int KT>
 __device__ __forceinline__ int key_of(const Span& s, int tile) { return (tile < s.n_lead ? tile : tile - s.n_lead + s.first) * KT; }
 
-// The chunks of eight channels ch(0) .. ch(N - 1) of a query row as fp16 relative to the row's largest magnitude (2^-e, e its
-// exponent, so that no range is lost), rotated by its position `pos` in fp32 when there is a table (a position outside the block
-// table as if at its border).  `most` takes the largest magnitude of the lane to that of the row.  The row's
-// factor comes back.  Loads stand in front and under no branch that lanes could take apart: a row costs two rounds of them.
-__device__ __forceinline__ float row_down(float m) {
-  const int e = min(max((int)(__float_as_uint(m) >> 23), 1), 253);
-  return __uint_as_float((uint32_t)(254 - e) << 23);
-}
-// fp16 queries get a second part, what the rounding of the rotated values to fp16 left (`low`; bf16 ones do not: their outputs are
-// rounded eight times as coarsely).
-template <int N, bool F16, class Ch, class Most>
-__device__ __forceinline__ float load_query(const PagedAttnArgs& a, const uint16_t* row, bool ok, int pos, int cap, f16x8* q,
-                                            f16x8* low, Ch ch, Most most) {
+// The chunks of eight channels ch(0) .. ch(N - 1) of a row in fp32, turned by row `pos` of the table when there is one.  Loads stand in
+// front and under no branch that lanes could take apart: a row costs two rounds of them.
+template <int N, bool F16, class Ch>
+__device__ __forceinline__ void turned_chunks(const Rotary& rt, const uint16_t* row, int pos, float (*v)[8], Ch ch) {
   uint4 raw[N], par[N];
 #pragma unroll
   for (int k = 0; k < N; ++k) raw[k] = reinterpret_cast<const uint4*>(row)[ch(k)];
-  float v[N][8];
-  if (!a.rt.table) {
+  if (!rt.table) {
 #pragma unroll
     for (int k = 0; k < N; ++k) unpack8<F16>(raw[k], v[k]);
   } else {
-    const float* tr = a.rt.table + (int64_t)min(max(pos, 0), cap - 1) * a.rt.rot;
-    const int half = a.rt.rot / 16;                          // chunks of half the rotated part
-    if (a.rt.layout == FL_ROPE_HALF) {
+    const float* tr = rt.table + (int64_t)pos * rt.rot;
+    const int half = rt.rot / 16;                          // chunks of half the rotated part
+    if (rt.layout == FL_ROPE_HALF) {
 #pragma unroll
       for (int k = 0; k < N; ++k) {
         const int c = ch(k);
@@ -227,6 +217,23 @@ __device__ __forceinline__ float load_query(const PagedAttnArgs& a, const uint16
       }
     }
   }
+}
+
+// The chunks of eight channels ch(0) .. ch(N - 1) of a query row as fp16 relative to the row's largest magnitude (2^-e, e its
+// exponent, so that no range is lost), rotated by its position `pos` in fp32 when there is a table (a position outside the block
+// table as if at its border).  `most` takes the largest magnitude of the lane to that of the row.  The row's
+// factor comes back.
+__device__ __forceinline__ float row_down(float m) {
+  const int e = min(max((int)(__float_as_uint(m) >> 23), 1), 253);
+  return __uint_as_float((uint32_t)(254 - e) << 23);
+}
+// fp16 queries get a second part, what the rounding of the rotated values to fp16 left (`low`; bf16 ones do not: their outputs are
+// rounded eight times as coarsely).
+template <int N, bool F16, class Ch, class Most>
+__device__ __forceinline__ float load_query(const PagedAttnArgs& a, const uint16_t* row, bool ok, int pos, int cap, f16x8* q,
+                                            f16x8* low, Ch ch, Most most) {
+  float v[N][8];
+  turned_chunks<N, F16>(a.rt, row, min(max(pos, 0), cap - 1), v, ch);
   float top = 0.0f;
 #pragma unroll
   for (int k = 0; k < N; ++k)

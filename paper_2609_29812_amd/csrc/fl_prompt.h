@@ -1,0 +1,487 @@
+// Dense causal attention for many rows per sequence, over keys and values from any source that can lay them out in LDS: the kernel,
+// how its work is cut, and the joining of row tiles that a cut splits.
+#pragma once
+
+#include "fl_paged_attn.h"
+
+#include <algorithm>
+
+namespace fl {
+
+constexpr int kStageKeys = 64;
+
+// The keys or the values of a stage in LDS: blocks of 32 rows, 16-byte chunks permuted (swz32_f).  (Each buffer is an object of its
+// own: the compiler orders reads of one behind loads into the same alone.)
+template <int D>
+struct __attribute__((aligned(16))) StageTile {
+  uint16_t x[kStageKeys * D];
+};
+
+// x, as if just computed
+__device__ __forceinline__ void renew(int& x) { asm volatile("" : "+v"(x)); }
+
+template <int R> Seq find_row_tile();      // (a name for the sources' own)
+
+template <bool F16>
+__device__ __forceinline__ f32x16 mma32(const u32x4& a, const u32x4& b, const f32x16& c) {
+  if constexpr (F16) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+template <bool F16>
+__device__ __forceinline__ uint32_t pack2(float a, float b) { return F16 ? pack_f16x2(a, b) : pack_bf16x2(a, b); }
+
+// ends[s]: units of row tiles 0 .. s (SrcArgs: seq_of(a, b) gives a sequence)
+template <class SrcArgs, int R>
+__global__ __launch_bounds__(1024) void prompt_plan_kernel(SrcArgs a) {
+  __shared__ int s_sum[16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int before = 0;
+  for (int s0 = 0; s0 < a.slots; s0 += 1024) {
+    const int slot = s0 + threadIdx.x;
+    int n = 0;
+    if (slot < a.slots) {
+      int lo = 0, hi = a.bt.B;                                // the last sequence whose first slot is at most this one
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if ((int)((int64_t)row_of(a.bt, mid) * a.G / R) + mid <= slot) lo = mid;
+        else hi = mid;
+      }
+      const Seq q = seq_of(a, lo);
+      const Span sp = span_of<R, kStageKeys>(a, q, slot - ((int)((int64_t)q.r0 * a.G / R) + lo));
+      n = sp.rows > 0 ? kTileUnits + max(sp.tiles, 1) : 0;
+    }
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const int x = __shfl_up(n, off, 64);
+      n += lane >= off ? x : 0;
+    }
+    if (lane == 63) s_sum[wave] = n;
+    __syncthreads();
+    int all = 0;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) {
+      if (w < wave) n += s_sum[w];
+      all += s_sum[w];
+    }
+    if (slot < a.slots) a.ends[slot] = before + n;
+    before += all;
+    __syncthreads();
+  }
+}
+
+// first row tile whose end is beyond unit x (the wave looks at 64 places at a time)
+__device__ __forceinline__ int slot_of_unit(const int* ends, int slots, int x) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, n = slots;
+  while (n > 1) {
+    const int step = (n + 63) / 64;
+    const int at = min(lo + (lane + 1) * step, lo + n) - 1;
+    const uint64_t m = __builtin_amdgcn_ballot_w64(ends[at] > x);
+    const int l = m ? __builtin_ctzll(m) : 63;
+    const int next = min(lo + l * step, lo + n - 1);
+    n = min(step, lo + n - next);
+    lo = next;
+  }
+  return lo;
+}
+
+template <class Src, class SrcArgs, int RB, bool SHARED>
+__global__ __launch_bounds__(256, RB == 1 ? 2 : 1) void prompt_kernel(SrcArgs a) {
+  constexpr int D = Src::kD, R = 128 * RB;
+  constexpr int NBK = kStageKeys / 32;     // 32-key blocks of a stage
+  constexpr int KS = D / 16;               // k-steps of QK^T
+  constexpr int DB = D / 32;               // 32-channel output blocks
+  __shared__ StageTile<D> k0, k1, v0, v1;
+  __shared__ typename Src::Shared shared;
+  // Masked stages whose values are not all finite: the values are set to 0, their places are bits of `odd`, a byte for eight channels.
+  __shared__ int s_bad[2];
+  __shared__ uint32_t odd[2][kStageKeys * D / 32];
+
+  const int kvh = blockIdx.x % a.pg.heads, wg = blockIdx.x / a.pg.heads;
+  const int G = a.G;
+  // the workgroup's run of units at .. end - 1 of its head, from row tile `slot` on; or all of one row tile
+  int at = 0, end = 1, slot = gridDim.x / a.pg.heads - 1 - wg;          // (later rows see more keys: first)
+  if constexpr (SHARED) {
+    const Cut cut = cut_of(a);
+    at = cut.begin(wg);
+    end = cut.begin(wg + 1);
+    if (at >= end) return;
+    slot = slot_of_unit(a.ends, a.slots, at);
+  }
+  const int first = at;
+  for (; at < end; ++slot) {
+    int tid = threadIdx.x;
+    if constexpr (SHARED) renew(tid);                        // (what a row tile derives from the lane is formed anew)
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int hw = lane >> 5, r32 = lane & 31;
+    const Seq sq = find_row_tile<R>(a, slot);
+    if (sq.b < 0) return;
+    const Span sp = span_of<R, kStageKeys>(a, sq, slot - ((int)((int64_t)sq.r0 * G / R) + sq.b));
+    if (sp.rows == 0) {
+      if constexpr (SHARED) continue;
+      return;
+    }
+    // its stages t0 .. t0 + n - 1 of the row tile; `whole`: these are all
+    int t0 = 0, n = sp.tiles;
+    bool whole = true;
+    int place = 0;
+    if constexpr (SHARED) {
+      const int tile_end = __builtin_amdgcn_readfirstlane(a.ends[slot]), units = max(sp.tiles, 1), unit0 = tile_end - units;
+      t0 = max(at - unit0, 0);
+      const int t1 = min(end - unit0, units);
+      place = unit0 + t0 == first ? 0 : 1;                   // of the two row tiles that a share may cut
+      at = min(tile_end, end);
+      if (t0 >= t1) continue;                                // (the tile's stages are the next share's)
+      whole = t0 == 0 && t1 == units;
+      n = min(t1, sp.tiles) - t0;
+    } else {
+      at = end;
+    }
+
+    const int cap = a.bt.max_pages * a.pg.size;
+    int row[RB], jmax[RB], jmin[RB];
+    bool row_ok[RB];
+#pragma unroll
+    for (int x = 0; x < RB; ++x) {
+      row[x] = 32 * (RB * wave + x) + r32;
+      row_ok[x] = row[x] < sp.rows;
+      const int pos = sp.start + (sp.rho0 + (row_ok[x] ? row[x] : 0)) / G;
+      jmax[x] = row_ok[x] ? min(pos, cap - 1) : -1;
+      jmin[x] = a.window > 0 && pos >= a.window ? pos - a.window + 1 : 0;
+    }
+    // positions of the wave's first and last row (none: no key is seen)
+    const int row0 = 32 * RB * wave;
+    const int w_min = sp.start + (sp.rho0 + row0) / G;
+    const int w_max = row0 < sp.rows ? min(sp.start + (sp.rho0 + min(row0 + 32 * RB, sp.rows) - 1) / G, cap - 1) : -1;
+    const int w_all = a.window > 0 && w_max >= a.window ? w_max - a.window + 1 : 0;      // the first key (but for the leading) of all
+
+    Src src(a, shared, sq, sp, kvh, tid, t0, n);
+    u32x4 qf[RB][KS], ql[RB][Src::kLow ? KS : 1];
+    float mul[RB];
+#pragma unroll
+    for (int x = 0; x < RB; ++x) {
+      const int rho = sp.rho0 + (row_ok[x] ? row[x] : 0);
+      mul[x] = src.query(a, sp.r0 + rho / G, kvh * G + rho % G, sp.start + rho / G, row_ok[x], hw, qf[x], ql[x]);
+    }
+    // LDS read offsets (elements).  Keys (A operand): row r32, chunk 2 ks + hw.  Values (transposed reads): lane (16 g + 4 t + q)
+    // at V[16 kb + 4 (g >> 1) + t (+ 8)][32 db + 16 (g & 1) + 4 q]
+    int koff[KS], voff[DB], voff8[DB];
+    {
+      const int g16 = lane >> 4, m16 = lane & 15;
+      const int tq = m16 >> 2, q = m16 & 3;
+      const int col0 = 4 * (g16 >> 1) + tq;
+      const int c_lo = 2 * (g16 & 1) + (q >> 1);
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) koff[ks] = r32 * D + ((2 * ks + hw) ^ swz32_f<D>(r32)) * 8;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        voff[db] = col0 * D + ((4 * db + c_lo) ^ swz32_f<D>(col0)) * 8 + 4 * (q & 1);
+        voff8[db] = (col0 + 8) * D + ((4 * db + c_lo) ^ swz32_f<D>(col0 + 8)) * 8 + 4 * (q & 1);
+      }
+    }
+    f32x16 acc[RB][DB];
+    float ref[RB], lsum[RB];
+#pragma unroll
+    for (int x = 0; x < RB; ++x) {
+#pragma unroll
+      for (int db = 0; db < DB; ++db) acc[x][db] = f32x16{};
+      ref[x] = -INFINITY;
+      lsum[x] = 0.0f;
+    }
+    auto key0_of = [&](int st) { return key_of<kStageKeys>(sp, t0 + st); };
+    auto masked = [&](int st) {                              // uniform: some row of the wave does not see some key of it
+      const int key0 = key0_of(st);
+      return key0 + kStageKeys - 1 > w_min || (key0 < w_all && key0 + kStageKeys > a.n_sink) || src.holes(st);
+    };
+    auto tile_masked = [&](int st) {                         // ... some row of the workgroup
+      const int key0 = key0_of(st);
+      const int all = a.window > 0 && sp.i_max >= a.window ? sp.i_max - a.window + 1 : 0;
+      return key0 + kStageKeys - 1 > sp.i_min || (key0 < all && key0 + kStageKeys > a.n_sink);
+    };
+
+    // scores of a stage, S^T = K Q^T: a lane has 16 keys of one row per block
+    auto scores = [&](f32x16 (&s)[RB][NBK], const StageTile<D>& kt) __attribute__((always_inline)) {
+#pragma unroll
+      for (int x = 0; x < RB; ++x)
+#pragma unroll
+        for (int b = 0; b < NBK; ++b) s[x][b] = f32x16{};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int b = 0; b < NBK; ++b) {
+          const u32x4 w = *reinterpret_cast<const u32x4*>(&kt.x[b * 32 * D + koff[ks]]);
+#pragma unroll
+          for (int x = 0; x < RB; ++x) {
+            s[x][b] = mma32<Src::kF16>(w, qf[x][ks], s[x][b]);
+            if constexpr (Src::kLow)
+              if (a.rt.table) s[x][b] = mma32<Src::kF16>(w, ql[x][ks], s[x][b]);
+          }
+        }
+    };
+    auto largest = [&](const f32x16 (&s)[NBK]) __attribute__((always_inline)) {
+      float m[2 * NBK];
+#pragma unroll
+      for (int b = 0; b < NBK; ++b)
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          const f32x16& y = s[b];
+          const float m0 = max3(y[8 * g], y[8 * g + 1], y[8 * g + 2]), m1 = max3(y[8 * g + 3], y[8 * g + 4], y[8 * g + 5]);
+          m[2 * b + g] = max3(max3(m0, y[8 * g + 6], y[8 * g + 7]), m1, m1);
+        }
+      float r = m[0];
+#pragma unroll
+      for (int i = 1; i < 2 * NBK; ++i) r = fmaxf(r, m[i]);
+      return r;
+    };
+    auto mask = [&](f32x16 (&s)[RB][NBK], int st) __attribute__((always_inline)) {
+      const int key0 = key0_of(st);
+#pragma unroll
+      for (int x = 0; x < RB; ++x)
+#pragma unroll
+        for (int b = 0; b < NBK; ++b)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) {
+            const int j = key0 + 32 * b + 8 * (v >> 2) + 4 * hw + (v & 3);
+            const bool see = (j <= jmax[x]) & ((j >= jmin[x]) | (j < a.n_sink)) & src.there(st, 2 * b + (v >> 3));
+            s[x][b][v] = see ? s[x][b][v] : -INFINITY;
+          }
+    };
+    // the running references follow the largest scores of a stage, where those are ahead by more than 8 octaves
+    auto refer = [&](float (&most)[RB]) __attribute__((always_inline)) {
+#pragma unroll
+      for (int x = 0; x < RB; ++x) {
+        const float m = xor32_max(most[x]) * mul[x];
+        const bool raise = m > ref[x] + 8.0f;
+        if (__builtin_amdgcn_ballot_w64(raise) != 0) {
+          const float nm = raise ? m : ref[x];
+          const float alpha = raise ? __builtin_amdgcn_exp2f(ref[x] - nm) : 1.0f;
+          lsum[x] *= alpha;
+#pragma unroll
+          for (int db = 0; db < DB; ++db) acc[x][db] *= alpha;
+          ref[x] = nm;
+        }
+      }
+    };
+    // One pair of a stage's probabilities (16 pairs a row), as half a word of the operands.
+    float ts[RB][2];
+    auto weigh = [&](const f32x16 (&s)[RB][NBK], u32x4 (&pf)[RB][NBK][2], const float (&base)[RB], int i) __attribute__((always_inline)) {
+#pragma unroll
+      for (int x = 0; x < RB; ++x) {
+        const int b = i / 8, v = 2 * (i % 8);
+        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][b][v], mul[x], -base[x]));
+        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][b][v + 1], mul[x], -base[x]));
+        ts[x][0] += p0;
+        ts[x][1] += p1;
+        pf[x][b][v / 8][(v % 8) / 2] = pack2<Src::kF16>(p0, p1);
+      }
+    };
+    auto read_k = [&](const StageTile<D>& kt, int i) __attribute__((always_inline)) {          // k-step i / NBK, block i % NBK
+      return *reinterpret_cast<const u32x4*>(&kt.x[(i % NBK) * 32 * D + koff[i / NBK]]);
+    };
+    auto read_v = [&](const StageTile<D>& vt, int i) __attribute__((always_inline)) {          // keys 16 (i / DB), channels 32 (i % DB)
+      const uint16_t* at_v = vt.x + 16 * (i / DB) * D;
+      const i16x4 va = __builtin_amdgcn_ds_read_tr16_b64_v4i16(FL_LDS4(at_v + voff[i % DB]));
+      const i16x4 vb = __builtin_amdgcn_ds_read_tr16_b64_v4i16(FL_LDS4(at_v + voff8[i % DB]));
+      return __builtin_bit_cast(u32x4, __builtin_shufflevector(va, vb, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    auto score = [&](f32x16 (&s)[RB][NBK], const u32x4& w, int i) __attribute__((always_inline)) {
+#pragma unroll
+      for (int x = 0; x < RB; ++x) {
+        s[x][i % NBK] = mma32<Src::kF16>(w, qf[x][i / NBK], s[x][i % NBK]);
+        if constexpr (Src::kLow)
+          if (a.rt.table) s[x][i % NBK] = mma32<Src::kF16>(w, ql[x][i / NBK], s[x][i % NBK]);
+      }
+    };
+    // NaN for what sees a value that is not finite
+    auto poison = [&](int st) __attribute__((always_inline)) {
+      const int key0 = key0_of(st);
+#pragma unroll
+      for (int x = 0; x < RB; ++x) {
+        uint32_t m[DB];
+#pragma unroll
+        for (int db = 0; db < DB; ++db) m[db] = 0;
+#pragma nounroll
+        for (int i = 0; i < kStageKeys; ++i) {
+          const int j = key0 + i;
+          const bool see = (j <= jmax[x]) & ((j >= jmin[x]) | (j < a.n_sink)) & src.there(st, i / 16);
+#pragma unroll
+          for (int db = 0; db < DB; ++db) m[db] |= see ? odd[st & 1][i * DB + db] : 0u;
+        }
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) acc[x][db][v] = (m[db] >> (8 * (v >> 2) + 4 * hw + (v & 3))) & 1u ? NAN : acc[x][db][v];
+      }
+    };
+    // A stage: the scores of the next one (nxt) beside the probabilities of this one (cur), then O^T += V^T P^T beside what is left of
+    // them and the largest scores of the next.  Each matrix instruction is followed by vector instructions that do not wait for it.
+    constexpr int NQ = KS * NBK, NP = NBK * 2 * DB, EARLY = 12, LA = 2;
+    auto stage = [&](f32x16 (&cur)[RB][NBK], f32x16 (&nxt)[RB][NBK], const StageTile<D>& KN, const StageTile<D>& V, float (&most)[RB])
+        __attribute__((always_inline)) {
+      u32x4 pf[RB][NBK][2], fr[LA + 1];
+      float base[RB];
+#pragma unroll
+      for (int x = 0; x < RB; ++x) {
+        base[x] = ref[x] == -INFINITY ? 0.0f : ref[x];
+        ts[x][0] = ts[x][1] = 0.0f;
+#pragma unroll
+        for (int b = 0; b < NBK; ++b) nxt[x][b] = f32x16{};
+      }
+#pragma unroll
+      for (int i = 0; i < LA; ++i) fr[i] = read_k(KN, i);
+#pragma unroll
+      for (int i = 0; i < NQ; ++i) {
+        fr[(i + LA) % (LA + 1)] = i + LA < NQ ? read_k(KN, i + LA) : read_v(V, i + LA - NQ);
+        score(nxt, fr[i % (LA + 1)], i);
+#pragma unroll
+        for (int y = EARLY * i / NQ; y < EARLY * (i + 1) / NQ; ++y) weigh(cur, pf, base, y);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      constexpr int LATE = NP * 3 / 4;                       // (the last quarter needs the last of them)
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        if (i + LA < NP) fr[(NQ + i + LA) % (LA + 1)] = read_v(V, i + LA);
+#pragma unroll
+        for (int x = 0; x < RB; ++x) acc[x][i % DB] = mma32<Src::kF16>(fr[(NQ + i) % (LA + 1)], pf[x][i / DB / 2][i / DB % 2], acc[x][i % DB]);
+#pragma unroll
+        for (int y = EARLY + (16 - EARLY) * i / LATE; y < EARLY + (16 - EARLY) * (i + 1) / LATE && y < 16; ++y) weigh(cur, pf, base, y);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int x = 0; x < RB; ++x) {
+        lsum[x] += ts[x][0] + ts[x][1];
+        most[x] = largest(nxt[x]);
+      }
+    };
+    if (n > 0) {
+      if constexpr (SHARED) __syncthreads();                 // (the last row tile's stages are read)
+      if (tid < 2) s_bad[tid] = -1;
+      __syncthreads();
+      // stages go K(t), then V(t), one behind: the scores of stage t + 1 are formed beside the probabilities of stage t
+      src.load_k(0, k0);
+      src.load_v(0, v0);
+      src.land(0, k0, v0);
+      if (n > 1) src.load_k(1, k1);
+      if (tile_masked(0) && src.odd(v0, odd[0])) s_bad[0] = 0;
+      if (n > 1) src.land_k(k1);
+      __syncthreads();
+      f32x16 sa[RB][NBK], sb[RB][NBK];
+      float most[RB];
+      auto enter = [&](f32x16 (&s)[RB][NBK], int st) __attribute__((always_inline)) {
+        if (masked(st)) {                                    // uniform
+          mask(s, st);
+#pragma unroll
+          for (int x = 0; x < RB; ++x) most[x] = largest(s[x]);
+        }
+        refer(most);
+      };
+      scores(sa, k0);
+#pragma unroll
+      for (int x = 0; x < RB; ++x) most[x] = largest(sa[x]);
+      enter(sa, 0);
+      __syncthreads();                                       // (the first keys are read)
+      // K: where stage st's keys were and st + 2's come; KN: st + 1's; V: st's values; VN: where st + 1's come
+      auto step = [&](f32x16 (&cur)[RB][NBK], f32x16 (&nxt)[RB][NBK], int st, StageTile<D>& K, StageTile<D>& KN, StageTile<D>& V,
+                      StageTile<D>& VN) __attribute__((always_inline)) {
+        const bool more = st + 1 < n;                        // uniform
+        if (st + 2 < n) src.load_k(st + 2, K);
+        if (more) src.load_v(st + 1, VN);
+        if (__builtin_expect(tile_masked(st) && s_bad[st & 1] == st, 0)) poison(st);
+        // (behind the last stage the next one's scores are of no use, and without harm)
+        stage(cur, nxt, KN, V, most);
+        if (more) enter(nxt, st + 1);
+        if (more) {
+          src.land(st + 2 < n, K, VN);
+          if (tile_masked(st + 1) && src.odd(VN, odd[(st + 1) & 1])) s_bad[(st + 1) & 1] = st + 1;
+        }
+        __syncthreads();
+      };
+      for (int st = 0; st < n; st += 2) {
+        step(sa, sb, st, k0, k1, v0, v1);
+        if (st + 1 < n) step(sb, sa, st + 1, k1, k0, v1, v0);
+      }
+    }
+#pragma unroll
+    for (int x = 0; x < RB; ++x) {
+      lsum[x] = xor32_add(lsum[x]);
+      if (!row_ok[x]) continue;
+      const int rho = sp.rho0 + row[x], tok = rho / G, head = kvh * G + rho % G;
+      const bool none = ref[x] == -INFINITY && lsum[x] == 0.0f;
+      if (SHARED && !whole) {
+        // a share cuts at most two row tiles: the one it begins with and the one it ends with
+        const int64_t pr = ((int64_t)(kvh * a.share + wg) * 2 + place) * R + row[x];
+        float* out = a.part + pr * D + 4 * hw;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            *reinterpret_cast<float4*>(out + db * 32 + 8 * j) =
+                make_float4(acc[x][db][4 * j], acc[x][db][4 * j + 1], acc[x][db][4 * j + 2], acc[x][db][4 * j + 3]);
+        if (hw == 0) *reinterpret_cast<float2*>(a.part_ml + pr * 2) = make_float2(ref[x], lsum[x]);
+      } else {
+        const float inv = none ? 0.0f : 1.0f / lsum[x];
+        uint16_t* out = a.o + (int64_t)(sp.r0 + tok) * a.os + (int64_t)head * D + 4 * hw;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const f32x16& o = acc[x][db];
+            *reinterpret_cast<u32x2*>(out + db * 32 + 8 * j) = u32x2{pack2<Src::kOut16>(o[4 * j] * inv, o[4 * j + 1] * inv),
+                                                                     pack2<Src::kOut16>(o[4 * j + 2] * inv, o[4 * j + 3] * inv)};
+          }
+        if (hw == 0 && a.lse)
+          a.lse[(int64_t)(sp.r0 + tok) * a.Hq + head] = none ? -INFINITY : (ref[x] + __builtin_amdgcn_logf(lsum[x])) * 0.6931471805599453f;
+      }
+    }
+  }
+}
+
+// Row tiles that shares cut: a workgroup has 32 rows of one, d / 4 threads a row.
+template <class Args, int D, bool OUT16, int R>
+__global__ __launch_bounds__(256) void prompt_join_kernel(Args a) {
+  constexpr int LN = D / 4, PER = R / 32;
+  const int kvh = blockIdx.x % a.pg.heads, rest = blockIdx.x / a.pg.heads;
+  const int slot = rest / PER, r0 = (rest % PER) * 32;
+  const Cut cut = cut_of(a);
+  const int before = slot > 0 ? a.ends[slot - 1] : 0, end = a.ends[slot];
+  if (before >= end) return;
+  const int begin = before + kTileUnits;                     // its first stage
+  const int p0 = cut.owner(begin), p1 = cut.owner(end - 1);
+  if (p0 == p1) return;
+  const int G = a.G;
+  const Seq sq = find_row_tile<R>(a, slot);
+  if (sq.b < 0) return;
+  const Span sp = span_of<R, kStageKeys>(a, sq, slot - ((int)((int64_t)sq.r0 * G / R) + sq.b));
+  const int c = threadIdx.x % LN;
+  for (int rr = r0 + threadIdx.x / LN; rr < min(r0 + 32, sp.rows); rr += 256 / LN) {
+    auto place = [&](int p) { return ((int64_t)(kvh * a.share + p) * 2 + (max(begin, cut.begin(p)) == cut.begin(p) ? 0 : 1)) * R + rr; };
+    const float2* ml = reinterpret_cast<const float2*>(a.part_ml);
+    float m = -INFINITY;
+#pragma unroll 4
+    for (int p = p0; p <= p1; ++p) m = fmaxf(m, ml[place(p)].x);
+    float sum = 0.0f;
+    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+    for (int p = p0; p <= p1; ++p) {
+      const int64_t at = place(p);
+      const float2 w = ml[at];
+      const float4 x = *reinterpret_cast<const float4*>(a.part + at * D + 4 * c);
+      // (a part with NaN scores alone has no reference, but counts)
+      const float f = w.x == -INFINITY ? (w.y == 0.0f ? 0.0f : 1.0f) : __builtin_amdgcn_exp2f(w.x - m);
+      sum = fmaf(f, w.y, sum);
+      o.x = fmaf(f, x.x, o.x);
+      o.y = fmaf(f, x.y, o.y);
+      o.z = fmaf(f, x.z, o.z);
+      o.w = fmaf(f, x.w, o.w);
+    }
+    const bool none = m == -INFINITY && sum == 0.0f;
+    const float inv = none ? 0.0f : 1.0f / sum;
+    const int rho = sp.rho0 + rr, tok = rho / G, head = kvh * G + rho % G;
+    *reinterpret_cast<u32x2*>(a.o + (int64_t)(sp.r0 + tok) * a.os + (int64_t)head * D + 4 * c) =
+        u32x2{pack2<OUT16>(o.x * inv, o.y * inv), pack2<OUT16>(o.z * inv, o.w * inv)};
+    if (a.lse && c == 0)
+      a.lse[(int64_t)(sp.r0 + tok) * a.Hq + head] = none ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+  }
+}
+
+}  // namespace fl
