@@ -24,50 +24,49 @@ __device__ __forceinline__ Seq find_row_tile(const PackedArgs& a, int slot) {
 }
 
 // Stages of 64 key and value rows by LDS-DMA; rows behind the sequence's last read zeros.
-template <int D, bool F16>
+template <int D, bool F16, int NW>
 struct PackedSource {
   using Args = PackedArgs;
   struct Shared {};
-  static constexpr int kD = D;
+  static constexpr int kD = D, kWaves = NW;
   static constexpr bool kF16 = F16, kOut16 = F16, kLow = false;
-  static constexpr int CH = D / 8, RPI = 64 / CH, NI = kStageKeys / RPI / 4;     // chunks of a row; rows of a load; loads of a wave
+  // Chunks of a row, rows of a load, loads of a wave, rows from one of these to the next: a lane's chunk is permuted alike in all.
+  static constexpr int CH = D / 8, RPI = 64 / CH, NI = kStageKeys / RPI / NW, ROWS = NW * RPI;
 
   const Args& a;
   const Span& sp;
   const uint16_t *k, *v;                     // row 0 of the sequence, the head's channels
   int n_k, t0, wave, lane;
-  uint32_t kofs[NI], vofs[NI];
+  uint32_t kofs, vofs;                       // of the lane's chunk in a wave's first load (the others: ROWS rows on)
 
   __device__ __forceinline__ PackedSource(const Args& args, Shared&, const Seq& sq, const Span& span, int kvh, int tid, int first, int)
       : a(args), sp(span), n_k(sq.len), t0(first), wave(__builtin_amdgcn_readfirstlane(tid >> 6)), lane(tid & 63) {
     const int row0 = key_row(a, sq.b);
     k = a.k + (int64_t)row0 * a.ks + kvh * D;
     v = a.v + (int64_t)row0 * a.vs + kvh * D;
+    const int c = wave * RPI + lane / CH;
+    const uint32_t chunk = (uint32_t)((lane % CH) ^ swz32_f<D>(c)) * 16u;
+    kofs = (uint32_t)c * (uint32_t)(2 * a.ks) + chunk;
+    vofs = (uint32_t)c * (uint32_t)(2 * a.vs) + chunk;
+  }
+  // (offsets stay below 64 rows of at most 2^25 bytes)
+  __device__ __forceinline__ void load(const uint16_t* rows, int64_t stride, uint32_t ofs, int key0, StageTile<D>& t) const {
+    const int left = n_k - key0;
+    const uint32_t step = ROWS * (uint32_t)(2 * stride);
+    if (left >= kStageKeys) {                // uniform
+      const rsrc_t r = make_rsrc(rows + key0 * stride, 0x7FFFFFFFu);
 #pragma unroll
-    for (int x = 0; x < NI; ++x) {
-      const int c = (wave * NI + x) * RPI + lane / CH;
-      const uint32_t chunk = (uint32_t)((lane % CH) ^ swz32_f<D>(c & 31)) * 16u;
-      kofs[x] = (uint32_t)c * (uint32_t)(2 * a.ks) + chunk;
-      vofs[x] = (uint32_t)c * (uint32_t)(2 * a.vs) + chunk;
+      for (int x = 0; x < NI; ++x)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, FL_LDS(t.x + (x * ROWS + wave * RPI) * D), 16, ofs, x * step, 0, 0);
+    } else {
+      const rsrc_t r = make_rsrc(rows + key0 * stride, left > 0 ? (uint32_t)(left - 1) * (uint32_t)(2 * stride) + 2u * D : 0u);
+#pragma unroll
+      for (int x = 0; x < NI; ++x)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, FL_LDS(t.x + (x * ROWS + wave * RPI) * D), 16, ofs + x * step, 0, 0, 0);
     }
   }
-  // the rows of a stage: its offsets stay below 64 rows of at most 2^25 bytes
-  __device__ __forceinline__ rsrc_t rows(const uint16_t* x, int64_t stride, int key0) const {
-    const int left = min(n_k - key0, kStageKeys);
-    return make_rsrc(x + key0 * stride, left > 0 ? (uint32_t)(left - 1) * (uint32_t)(2 * stride) + 2u * D : 0u);
-  }
-  __device__ __forceinline__ void load_k(int st, StageTile<D>& t) {
-    const rsrc_t r = rows(k, a.ks, key_of<kStageKeys>(sp, t0 + st));
-#pragma unroll
-    for (int x = 0; x < NI; ++x)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, FL_LDS(t.x + (wave * NI + x) * 512), 16, kofs[x], 0, 0, 0);
-  }
-  __device__ __forceinline__ void load_v(int st, StageTile<D>& t) {
-    const rsrc_t r = rows(v, a.vs, key_of<kStageKeys>(sp, t0 + st));
-#pragma unroll
-    for (int x = 0; x < NI; ++x)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, FL_LDS(t.x + (wave * NI + x) * 512), 16, vofs[x], 0, 0, 0);
-  }
+  __device__ __forceinline__ void load_k(int st, StageTile<D>& t) { load(k, a.ks, kofs, key_of<kStageKeys>(sp, t0 + st), t); }
+  __device__ __forceinline__ void load_v(int st, StageTile<D>& t) { load(v, a.vs, vofs, key_of<kStageKeys>(sp, t0 + st), t); }
   __device__ __forceinline__ void land(bool, StageTile<D>&, StageTile<D>&) { FL_WAIT_VM(0); }
   __device__ __forceinline__ void land_k(StageTile<D>&) { FL_WAIT_VM(0); }
   // The values that this lane's loads have brought: whether some are not finite (those become 0), and which.
@@ -76,7 +75,7 @@ struct PackedSource {
     bool any = false;
 #pragma unroll
     for (int x = 0; x < NI; ++x) {
-      u32x4* at = reinterpret_cast<u32x4*>(t.x + (wave * NI + x) * 512 + lane * 8);
+      u32x4* at = reinterpret_cast<u32x4*>(t.x + (x * ROWS + wave * RPI) * D + lane * 8);
       u32x4 w = *at;
       uint32_t bits = 0;
 #pragma unroll
@@ -85,7 +84,7 @@ struct PackedSource {
         bits |= (lo ? 1u : 0u) << (2 * e) | (hi ? 2u : 0u) << (2 * e);
         w[e] &= (lo ? 0u : 0xFFFFu) | (hi ? 0u : 0xFFFF0000u);
       }
-      const int c = (wave * NI + x) * RPI + lane / CH;
+      const int c = x * ROWS + wave * RPI + lane / CH;
       reinterpret_cast<uint8_t*>(where)[c * CH + ((lane % CH) ^ swz32_f<D>(c & 31))] = (uint8_t)bits;
       if (bits != 0) *at = w;
       any |= bits != 0;
@@ -122,30 +121,30 @@ struct PackedSource {
 };
 
 // How a call is cut: workgroups of 128 RB rows of a key/value head.
-constexpr int kPackedBlocks = 1;
-template <int RB>
+constexpr int kPackedWaves = 4;
+template <int NW>
 static bool packed_shared(int64_t slots, int Hkv, int64_t keys) {
-  return slots * Hkv < 2 * 512 / RB && keys >= 1024 && slots * (keys / kStageKeys + 16) < (1ll << 31) - 65536;
+  return slots * Hkv < 4096 / NW && keys >= 1024 && slots * (keys / kStageKeys + 16) < (1ll << 31) - 65536;
 }
-static int packed_shares(int Hkv, int rb) { return std::max(1, 512 / rb / Hkv); }
+static int packed_shares(int Hkv, int nw) { return std::max(1, 2048 / nw / Hkv); }
 
 // (the compiler emits the launching side of one of the two forms alone unless both are named)
 #define FL_FORMS(D, F16)                                                                                               \
-  template __global__ void prompt_kernel<PackedSource<D, F16>, PackedArgs, kPackedBlocks, true>(PackedArgs);           \
-  template __global__ void prompt_kernel<PackedSource<D, F16>, PackedArgs, kPackedBlocks, false>(PackedArgs);
+  template __global__ void prompt_kernel<PackedSource<D, F16, kPackedWaves>, PackedArgs, true>(PackedArgs);            \
+  template __global__ void prompt_kernel<PackedSource<D, F16, kPackedWaves>, PackedArgs, false>(PackedArgs);
 FL_FORMS(128, true)
 FL_FORMS(128, false)
 FL_FORMS(64, true)
 FL_FORMS(64, false)
 #undef FL_FORMS
 
-template <int D, bool F16, int RB>
+template <int D, bool F16, int NW>
 static int launch_packed(PackedArgs& a, bool shared, hipStream_t st) {
-  constexpr int R = 128 * RB;
-  using Source = PackedSource<D, F16>;
+  constexpr int R = 32 * NW;
+  using Source = PackedSource<D, F16, NW>;
   const unsigned grid = (unsigned)((int64_t)(shared ? a.share : a.slots) * a.pg.heads);
   if (!shared) {
-    prompt_kernel<Source, PackedArgs, RB, false><<<grid, 256, 0, st>>>(a);
+    prompt_kernel<Source, PackedArgs, false><<<grid, 64 * NW, 0, st>>>(a);
     return check_launch("prompt_kernel");
   }
   const size_t places = (size_t)a.share * a.pg.heads * 2 * R;
@@ -154,7 +153,7 @@ static int launch_packed(PackedArgs& a, bool shared, hipStream_t st) {
   prompt_plan_kernel<PackedArgs, R><<<1, 1024, 0, st>>>(a);
   int rc = check_launch("prompt_plan_kernel");
   if (rc != FL_OK) return rc;
-  prompt_kernel<Source, PackedArgs, RB, true><<<grid, 256, 0, st>>>(a);
+  prompt_kernel<Source, PackedArgs, true><<<grid, 64 * NW, 0, st>>>(a);
   rc = check_launch("prompt_kernel");
   if (rc != FL_OK) return rc;
   prompt_join_kernel<PackedArgs, D, F16, R><<<(unsigned)((int64_t)a.slots * (R / 32) * a.pg.heads), 256, 0, st>>>(a);
@@ -184,13 +183,13 @@ struct PackedPlan {
   size_t ws;
 };
 PackedPlan packed_plan(int B, int Tq, int Tk, int Hq, int Hkv, int d, int window, int n_sink, int max_k) {
-  constexpr int RB = kPackedBlocks, R = 128 * RB;
+  constexpr int NW = kPackedWaves, R = 32 * NW;
   PackedPlan p{};
   p.slots = (int64_t)Tq * (Hq / Hkv) / R + B;
   int64_t keys = max_k > 0 ? std::min(max_k, Tk) : Tk;
   if (window > 0) keys = std::min<int64_t>(keys, (int64_t)window + n_sink + R);
-  p.shared = packed_shared<RB>(p.slots, Hkv, keys);
-  p.share = packed_shares(Hkv, RB);
+  p.shared = packed_shared<NW>(p.slots, Hkv, keys);
+  p.share = packed_shares(Hkv, NW);
   p.ws = p.shared ? (size_t)p.share * Hkv * 2 * R * (d + 2) * sizeof(float) + (size_t)p.slots * sizeof(int) : 0;
   return p;
 }
@@ -255,7 +254,7 @@ extern "C" int fl_packed_attn(const void* q, int64_t q_stride, const void* k, in
   a.n_pos = n_pos; a.Tk = Tk; a.Hq = Hq; a.G = Hq / Hkv; a.scale_log2 = sm_scale * 1.4426950408889634f;
   a.window = window; a.n_sink = n_sink;
   a.slots = (int)p.slots; a.share = p.share; a.part = static_cast<float*>(ws);
-  if (d == 128) return dtype == FL_F16 ? launch_packed<128, true, kPackedBlocks>(a, p.shared, st) : launch_packed<128, false, kPackedBlocks>(a, p.shared, st);
-  return dtype == FL_F16 ? launch_packed<64, true, kPackedBlocks>(a, p.shared, st) : launch_packed<64, false, kPackedBlocks>(a, p.shared, st);
+  if (d == 128) return dtype == FL_F16 ? launch_packed<128, true, kPackedWaves>(a, p.shared, st) : launch_packed<128, false, kPackedWaves>(a, p.shared, st);
+  return dtype == FL_F16 ? launch_packed<64, true, kPackedWaves>(a, p.shared, st) : launch_packed<64, false, kPackedWaves>(a, p.shared, st);
   FL_API_END
 }

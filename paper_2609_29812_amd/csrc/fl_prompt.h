@@ -19,6 +19,7 @@ struct __attribute__((aligned(16))) StageTile {
 
 // x, as if just computed
 __device__ __forceinline__ void renew(int& x) { asm volatile("" : "+v"(x)); }
+__device__ __forceinline__ void renew(float& x) { asm volatile("" : "+v"(x)); }
 
 template <int R> Seq find_row_tile();      // (a name for the sources' own)
 
@@ -85,9 +86,9 @@ __device__ __forceinline__ int slot_of_unit(const int* ends, int slots, int x) {
   return lo;
 }
 
-template <class Src, class SrcArgs, int RB, bool SHARED>
-__global__ __launch_bounds__(256, RB == 1 ? 2 : 1) void prompt_kernel(SrcArgs a) {
-  constexpr int D = Src::kD, R = 128 * RB;
+template <class Src, class SrcArgs, bool SHARED>
+__global__ __launch_bounds__(64 * Src::kWaves, 2) void prompt_kernel(SrcArgs a) {
+  constexpr int D = Src::kD, R = 32 * Src::kWaves, RB = 1;
   constexpr int NBK = kStageKeys / 32;     // 32-key blocks of a stage
   constexpr int KS = D / 16;               // k-steps of QK^T
   constexpr int DB = D / 32;               // 32-channel output blocks
@@ -189,15 +190,21 @@ __global__ __launch_bounds__(256, RB == 1 ? 2 : 1) void prompt_kernel(SrcArgs a)
       lsum[x] = 0.0f;
     }
     auto key0_of = [&](int st) { return key_of<kStageKeys>(sp, t0 + st); };
-    auto masked = [&](int st) {                              // uniform: some row of the wave does not see some key of it
-      const int key0 = key0_of(st);
-      return key0 + kStageKeys - 1 > w_min || (key0 < w_all && key0 + kStageKeys > a.n_sink) || src.holes(st);
+    // stages from .. from + len - 1, uniform: every row sees every key (the tiles of leading positions count as masked)
+    struct Clear {
+      int from;
+      uint32_t len;
+      __device__ __forceinline__ bool operator()(int st) const { return (uint32_t)(st - from) < len; }
     };
-    auto tile_masked = [&](int st) {                         // ... some row of the workgroup
-      const int key0 = key0_of(st);
-      const int all = a.window > 0 && sp.i_max >= a.window ? sp.i_max - a.window + 1 : 0;
-      return key0 + kStageKeys - 1 > sp.i_min || (key0 < all && key0 + kStageKeys > a.n_sink);
+    auto clear_of = [&](int least, int low) {                // least: the first row's position; low: first key that all see
+      const int c0 = sp.n_lead + max((low + kStageKeys - 1) / kStageKeys - sp.first, 0) - t0;
+      const int c1 = sp.n_lead + ((least + 1) >> 6) - sp.first - t0;         // (kStageKeys is 64; -1 >> 6 is -1)
+      return Clear{max(c0, 0), (uint32_t)max(c1 - max(c0, 0), 0)};
     };
+    const Clear wave_clear = clear_of(w_min, w_all);
+    const Clear tile_clear = clear_of(sp.i_min, a.window > 0 && sp.i_max >= a.window ? sp.i_max - a.window + 1 : 0);
+    auto masked = [&](int st) { return !wave_clear(st) || src.holes(st); };
+    auto tile_masked = [&](int st) { return !tile_clear(st); };
 
     // scores of a stage, S^T = K Q^T: a lane has 16 keys of one row per block
     auto scores = [&](f32x16 (&s)[RB][NBK], const StageTile<D>& kt) __attribute__((always_inline)) {
@@ -218,20 +225,17 @@ __global__ __launch_bounds__(256, RB == 1 ? 2 : 1) void prompt_kernel(SrcArgs a)
           }
         }
     };
-    auto largest = [&](const f32x16 (&s)[NBK]) __attribute__((always_inline)) {
-      float m[2 * NBK];
+    auto largest = [&](const f32x16 (&s)[NBK], int g) __attribute__((always_inline)) {        // of half a block
+      const f32x16& y = s[g / 2];
+      const int v = 8 * (g & 1);
+      const float m0 = max3(y[v], y[v + 1], y[v + 2]), m1 = max3(y[v + 3], y[v + 4], y[v + 5]);
+      return max3(max3(m0, y[v + 6], y[v + 7]), m1, m1);
+    };
+    auto largest_of = [&](const f32x16 (&s)[NBK]) __attribute__((always_inline)) {
+      float m = largest(s, 0);
 #pragma unroll
-      for (int b = 0; b < NBK; ++b)
-#pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          const f32x16& y = s[b];
-          const float m0 = max3(y[8 * g], y[8 * g + 1], y[8 * g + 2]), m1 = max3(y[8 * g + 3], y[8 * g + 4], y[8 * g + 5]);
-          m[2 * b + g] = max3(max3(m0, y[8 * g + 6], y[8 * g + 7]), m1, m1);
-        }
-      float r = m[0];
-#pragma unroll
-      for (int i = 1; i < 2 * NBK; ++i) r = fmaxf(r, m[i]);
-      return r;
+      for (int g = 1; g < 2 * NBK; ++g) m = fmaxf(m, largest(s, g));
+      return m;
     };
     auto mask = [&](f32x16 (&s)[RB][NBK], int st) __attribute__((always_inline)) {
       const int key0 = key0_of(st);
@@ -315,7 +319,7 @@ __global__ __launch_bounds__(256, RB == 1 ? 2 : 1) void prompt_kernel(SrcArgs a)
     };
     // A stage: the scores of the next one (nxt) beside the probabilities of this one (cur), then O^T += V^T P^T beside what is left of
     // them and the largest scores of the next.  Each matrix instruction is followed by vector instructions that do not wait for it.
-    constexpr int NQ = KS * NBK, NP = NBK * 2 * DB, EARLY = 12, LA = 2;
+    constexpr int NQ = KS * NBK, NP = NBK * 2 * DB, EARLY = 12, LA = 2, MG = 2 * NBK;
     auto stage = [&](f32x16 (&cur)[RB][NBK], f32x16 (&nxt)[RB][NBK], const StageTile<D>& KN, const StageTile<D>& V, float (&most)[RB])
         __attribute__((always_inline)) {
       u32x4 pf[RB][NBK][2], fr[LA + 1];
@@ -345,13 +349,18 @@ __global__ __launch_bounds__(256, RB == 1 ? 2 : 1) void prompt_kernel(SrcArgs a)
         for (int x = 0; x < RB; ++x) acc[x][i % DB] = mma32<Src::kF16>(fr[(NQ + i) % (LA + 1)], pf[x][i / DB / 2][i / DB % 2], acc[x][i % DB]);
 #pragma unroll
         for (int y = EARLY + (16 - EARLY) * i / LATE; y < EARLY + (16 - EARLY) * (i + 1) / LATE && y < 16; ++y) weigh(cur, pf, base, y);
+#pragma unroll
+        for (int g = MG * i / NP; g < MG * (i + 1) / NP; ++g)
+#pragma unroll
+          for (int x = 0; x < RB; ++x) {
+            const float m = largest(nxt[x], g);
+            most[x] = g == 0 ? m : fmaxf(most[x], m);
+            if (g == MG - 1) renew(most[x]);                 // (here, beside the products)
+          }
         __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll
-      for (int x = 0; x < RB; ++x) {
-        lsum[x] += ts[x][0] + ts[x][1];
-        most[x] = largest(nxt[x]);
-      }
+      for (int x = 0; x < RB; ++x) lsum[x] += ts[x][0] + ts[x][1];
     };
     if (n > 0) {
       if constexpr (SHARED) __syncthreads();                 // (the last row tile's stages are read)
@@ -371,13 +380,13 @@ __global__ __launch_bounds__(256, RB == 1 ? 2 : 1) void prompt_kernel(SrcArgs a)
         if (masked(st)) {                                    // uniform
           mask(s, st);
 #pragma unroll
-          for (int x = 0; x < RB; ++x) most[x] = largest(s[x]);
+          for (int x = 0; x < RB; ++x) most[x] = largest_of(s[x]);
         }
         refer(most);
       };
       scores(sa, k0);
 #pragma unroll
-      for (int x = 0; x < RB; ++x) most[x] = largest(sa[x]);
+      for (int x = 0; x < RB; ++x) most[x] = largest_of(sa[x]);
       enter(sa, 0);
       __syncthreads();                                       // (the first keys are read)
       // K: where stage st's keys were and st + 2's come; KN: st + 1's; V: st's values; VN: where st + 1's come
