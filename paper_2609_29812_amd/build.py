@@ -24,7 +24,8 @@ LIB = os.path.join(PKG, "libflashloop.so")
 
 SOURCES = ["fl_common.hip", "fl_select.hip", "fl_codec.hip", "fl_attn.hip", "fl_dense_attn.hip",
            "fl_seg_attn.hip", "fl_colscore.hip", "fl_decode.hip", "fl_rope.hip", "fl_paged.hip", "fl_paged_attn.hip",
-           "fl_paged_prompt.hip", "fl_packed_attn.hip", "fl_paged4.hip", "fl_paged4_attn.hip"]
+           "fl_paged_prompt.hip", "fl_packed_attn.hip", "fl_paged4.hip", "fl_paged4_attn.hip",
+           "fl_paged4_prompt.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 

@@ -24,14 +24,13 @@ __device__ __forceinline__ Seq find_row_tile(const PackedArgs& a, int slot) {
 }
 
 // Stages of 64 key and value rows by LDS-DMA; rows behind the sequence's last read zeros.
-template <int D, bool F16, int NW>
+template <int D, bool F16>
 struct PackedSource {
   using Args = PackedArgs;
-  struct Shared {};
-  static constexpr int kD = D, kWaves = NW;
-  static constexpr bool kF16 = F16, kOut16 = F16, kLow = false;
+  static constexpr int kD = D;
+  static constexpr bool kF16 = F16, kOut16 = F16, kLow = false, kMixed = false, kOdd = true;
   // Chunks of a row, rows of a load, loads of a wave, rows from one of these to the next: a lane's chunk is permuted alike in all.
-  static constexpr int CH = D / 8, RPI = 64 / CH, NI = kStageKeys / RPI / NW, ROWS = NW * RPI;
+  static constexpr int CH = D / 8, RPI = 64 / CH, NI = kStageKeys / RPI / 4, ROWS = 4 * RPI;
 
   const Args& a;
   const Span& sp;
@@ -39,7 +38,7 @@ struct PackedSource {
   int n_k, t0, wave, lane;
   uint32_t kofs, vofs;                       // of the lane's chunk in a wave's first load (the others: ROWS rows on)
 
-  __device__ __forceinline__ PackedSource(const Args& args, Shared&, const Seq& sq, const Span& span, int kvh, int tid, int first, int)
+  __device__ __forceinline__ PackedSource(const Args& args, const Seq& sq, const Span& span, int kvh, int tid, int first, int)
       : a(args), sp(span), n_k(sq.len), t0(first), wave(__builtin_amdgcn_readfirstlane(tid >> 6)), lane(tid & 63) {
     const int row0 = key_row(a, sq.b);
     k = a.k + (int64_t)row0 * a.ks + kvh * D;
@@ -91,6 +90,7 @@ struct PackedSource {
     }
     return any;
   }
+  __device__ __forceinline__ void ahead(int) const {}
   __device__ __forceinline__ bool holes(int) const { return false; }
   __device__ __forceinline__ bool there(int, int) const { return true; }
   __device__ __forceinline__ float query(const Args& args, int t, int head, int pos, bool ok, int hw, u32x4* q, u32x4*) const {
@@ -120,44 +120,20 @@ struct PackedSource {
   }
 };
 
-// How a call is cut: workgroups of 128 RB rows of a key/value head.
-constexpr int kPackedWaves = 4;
-template <int NW>
-static bool packed_shared(int64_t slots, int Hkv, int64_t keys) {
-  return slots * Hkv < 4096 / NW && keys >= 1024 && slots * (keys / kStageKeys + 16) < (1ll << 31) - 65536;
-}
-static int packed_shares(int Hkv, int nw) { return std::max(1, 2048 / nw / Hkv); }
-
 // (the compiler emits the launching side of one of the two forms alone unless both are named)
-#define FL_FORMS(D, F16)                                                                                               \
-  template __global__ void prompt_kernel<PackedSource<D, F16, kPackedWaves>, PackedArgs, true>(PackedArgs);            \
-  template __global__ void prompt_kernel<PackedSource<D, F16, kPackedWaves>, PackedArgs, false>(PackedArgs);
+#define FL_FORMS(D, F16)                                                                      \
+  template __global__ void prompt_kernel<PackedSource<D, F16>, PackedArgs, true>(PackedArgs); \
+  template __global__ void prompt_kernel<PackedSource<D, F16>, PackedArgs, false>(PackedArgs);
 FL_FORMS(128, true)
 FL_FORMS(128, false)
 FL_FORMS(64, true)
 FL_FORMS(64, false)
 #undef FL_FORMS
 
-template <int D, bool F16, int NW>
-static int launch_packed(PackedArgs& a, bool shared, hipStream_t st) {
-  constexpr int R = 32 * NW;
-  using Source = PackedSource<D, F16, NW>;
-  const unsigned grid = (unsigned)((int64_t)(shared ? a.share : a.slots) * a.pg.heads);
-  if (!shared) {
-    prompt_kernel<Source, PackedArgs, false><<<grid, 64 * NW, 0, st>>>(a);
-    return check_launch("prompt_kernel");
-  }
-  const size_t places = (size_t)a.share * a.pg.heads * 2 * R;
-  a.part_ml = a.part + places * D;
-  a.ends = reinterpret_cast<int*>(a.part_ml + places * 2);
-  prompt_plan_kernel<PackedArgs, R><<<1, 1024, 0, st>>>(a);
-  int rc = check_launch("prompt_plan_kernel");
-  if (rc != FL_OK) return rc;
-  prompt_kernel<Source, PackedArgs, true><<<grid, 64 * NW, 0, st>>>(a);
-  rc = check_launch("prompt_kernel");
-  if (rc != FL_OK) return rc;
-  prompt_join_kernel<PackedArgs, D, F16, R><<<(unsigned)((int64_t)a.slots * (R / 32) * a.pg.heads), 256, 0, st>>>(a);
-  return check_launch("prompt_join_kernel");
+// keys of a sequence at most, as far as the caller knows
+static int64_t packed_keys(int Tk, int window, int n_sink, int max_k) {
+  const int64_t keys = max_k > 0 ? std::min(max_k, Tk) : Tk;
+  return window > 0 ? std::min<int64_t>(keys, (int64_t)window + n_sink + kRowsOfTile) : keys;
 }
 
 static int check_offsets(const char* fn, const char* name, const int32_t* cu, int B, int T, hipStream_t st) {
@@ -175,30 +151,10 @@ static int check_offsets(const char* fn, const char* name, const int32_t* cu, in
 
 using namespace fl;
 
-namespace {
-struct PackedPlan {
-  int64_t slots;
-  bool shared;
-  int share;
-  size_t ws;
-};
-PackedPlan packed_plan(int B, int Tq, int Tk, int Hq, int Hkv, int d, int window, int n_sink, int max_k) {
-  constexpr int NW = kPackedWaves, R = 32 * NW;
-  PackedPlan p{};
-  p.slots = (int64_t)Tq * (Hq / Hkv) / R + B;
-  int64_t keys = max_k > 0 ? std::min(max_k, Tk) : Tk;
-  if (window > 0) keys = std::min<int64_t>(keys, (int64_t)window + n_sink + R);
-  p.shared = packed_shared<NW>(p.slots, Hkv, keys);
-  p.share = packed_shares(Hkv, NW);
-  p.ws = p.shared ? (size_t)p.share * Hkv * 2 * R * (d + 2) * sizeof(float) + (size_t)p.slots * sizeof(int) : 0;
-  return p;
-}
-}  // namespace
-
 extern "C" size_t fl_packed_attn_ws(int B, int Tq, int Tk, int Hq, int Hkv, int d, int window, int n_sink, int max_k) {
   if (B < 1 || Tq < 1 || Tk < 0 || Hkv < 1 || Hq < Hkv || Hq % Hkv || (d != 64 && d != 128) || window < 0 || n_sink < 0 || max_k < 0)
     return 0;
-  return packed_plan(B, Tq, Tk, Hq, Hkv, d, window, n_sink, max_k).ws;
+  return prompt_ws((int64_t)Tq * (Hq / Hkv) / kRowsOfTile + B, Hkv, d, Tk, packed_keys(Tk, window, n_sink, max_k));
 }
 
 extern "C" int fl_packed_attn(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
@@ -241,9 +197,8 @@ extern "C" int fl_packed_attn(const void* q, int64_t q_stride, const void* k, in
     if (rc == FL_OK) rc = check_offsets(fn, "cu_k", cu_k, B, Tk, st);
     if (rc != FL_OK) return rc;
   }
-  const PackedPlan p = packed_plan(B, Tq, Tk, Hq, Hkv, d, window, n_sink, max_k);
-  FL_REQUIRE(p.slots * Hkv * 8 < (1ll << 31), FL_E_SHAPE, "%s: too many rows", fn);
-  FL_REQUIRE(p.ws == 0 || (ws && ws_bytes >= p.ws), FL_E_WORKSPACE, "%s: workspace of %zu bytes required", fn, p.ws);
+  const size_t need = fl_packed_attn_ws(B, Tq, Tk, Hq, Hkv, d, window, n_sink, max_k);
+  FL_REQUIRE(need == 0 || (ws && ws_bytes >= need), FL_E_WORKSPACE, "%s: workspace of %zu bytes required", fn, need);
   FL_REQUIRE((reinterpret_cast<uintptr_t>(ws) & 15) == 0, FL_E_SHAPE, "%s: ws must be 16-byte aligned", fn);
   PackedArgs a{};
   a.q = static_cast<const uint16_t*>(q); a.k = static_cast<const uint16_t*>(k); a.v = static_cast<const uint16_t*>(v);
@@ -253,8 +208,12 @@ extern "C" int fl_packed_attn(const void* q, int64_t q_stride, const void* k, in
   a.pg = {0, 1, 0, Hkv};
   a.n_pos = n_pos; a.Tk = Tk; a.Hq = Hq; a.G = Hq / Hkv; a.scale_log2 = sm_scale * 1.4426950408889634f;
   a.window = window; a.n_sink = n_sink;
-  a.slots = (int)p.slots; a.share = p.share; a.part = static_cast<float*>(ws);
-  if (d == 128) return dtype == FL_F16 ? launch_packed<128, true, kPackedWaves>(a, p.shared, st) : launch_packed<128, false, kPackedWaves>(a, p.shared, st);
-  return dtype == FL_F16 ? launch_packed<64, true, kPackedWaves>(a, p.shared, st) : launch_packed<64, false, kPackedWaves>(a, p.shared, st);
+  a.part = static_cast<float*>(ws);
+  const int64_t keys = packed_keys(Tk, window, n_sink, max_k);
+  if (d == 128)
+    return dtype == FL_F16 ? launch_prompt<PackedSource<128, true>, 128, true>(a, fn, Tk, keys, st)
+                           : launch_prompt<PackedSource<128, false>, 128, false>(a, fn, Tk, keys, st);
+  return dtype == FL_F16 ? launch_prompt<PackedSource<64, true>, 64, true>(a, fn, Tk, keys, st)
+                         : launch_prompt<PackedSource<64, false>, 64, false>(a, fn, Tk, keys, st);
   FL_API_END
 }

@@ -1,0 +1,55 @@
+// The 4-bit cache's attention: its arguments and the widening of codes that its kernels share.
+#pragma once
+
+#include "fl_paged4.h"
+#include "fl_paged_attn.h"
+
+namespace fl {
+
+struct Paged4Args : PagedAttnArgs {
+  const uint8_t *km, *vm;
+};
+
+// Two codes of 4 bits as fp16, from a word whose halves hold one each at the same place: at the low four bits of a byte they stand
+// under the exponent of 1024 as they are, at the high four sixteenfold.  Exact.
+__device__ __forceinline__ f16x2 low_pair(uint32_t w) {
+  const f16x2 off = {(_Float16)-1024.0f, (_Float16)-1024.0f};
+  return __builtin_bit_cast(f16x2, (w & 0x000F000Fu) | 0x64006400u) + off;
+}
+__device__ __forceinline__ f16x2 high_pair(uint32_t w) {
+  const f16x2 f = {(_Float16)0.0625f, (_Float16)0.0625f}, off = {(_Float16)-64.0f, (_Float16)-64.0f};
+  return __builtin_elementwise_fma(__builtin_bit_cast(f16x2, (w & 0x00F000F0u) | 0x64006400u), f, off);
+}
+__device__ __forceinline__ uint32_t apply(f16x2 c, f16x2 s, f16x2 z) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(c, s, z));
+}
+__device__ __forceinline__ f16x2 both_low(uint32_t a, uint32_t b) { return __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(b, a, 0x05040100u)); }
+__device__ __forceinline__ f16x2 both_high(uint32_t a, uint32_t b) { return __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(b, a, 0x07060302u)); }
+
+// Eight codes of one group in fp16: int4 one rounding of z + s c, in the order 0 4 1 5 2 6 3 7; e2m1 exactly, in their order.
+template <bool INT>
+__device__ __forceinline__ u32x4 widen8(uint32_t w, uint32_t meta) {
+  if constexpr (INT) {
+    const f16x2 s = both_low(meta, meta), z = both_high(meta, meta);
+    const uint32_t v = w >> 8;
+    return u32x4{apply(low_pair(w), s, z), apply(high_pair(w), s, z), apply(low_pair(v), s, z), apply(high_pair(v), s, z)};
+  } else {
+    const float s = __uint_as_float(meta << 23);
+    return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 0)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 1)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 2)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 3))};
+  }
+}
+// eight channels of a query in widen8's order
+template <bool INT>
+__device__ __forceinline__ f16x8 in_order(const f16x8& q) {
+  if constexpr (INT) return __builtin_shufflevector(q, q, 0, 4, 1, 5, 2, 6, 3, 7);
+  else return q;
+}
+
+// many rows
+size_t paged4_prompt_ws(int64_t slots, int Hkv, int d, int64_t cap, int64_t keys);
+int launch_paged4_prompt(const Paged4Args& a, int d, int format, bool f16, int64_t keys, hipStream_t st);
+
+}  // namespace fl

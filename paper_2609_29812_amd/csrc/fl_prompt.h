@@ -87,13 +87,12 @@ __device__ __forceinline__ int slot_of_unit(const int* ends, int slots, int x) {
 }
 
 template <class Src, class SrcArgs, bool SHARED>
-__global__ __launch_bounds__(64 * Src::kWaves, 2) void prompt_kernel(SrcArgs a) {
-  constexpr int D = Src::kD, R = 32 * Src::kWaves, RB = 1;
+__global__ __launch_bounds__(256, 2) void prompt_kernel(SrcArgs a) {
+  constexpr int D = Src::kD, R = 128, RB = 1;
   constexpr int NBK = kStageKeys / 32;     // 32-key blocks of a stage
   constexpr int KS = D / 16;               // k-steps of QK^T
   constexpr int DB = D / 32;               // 32-channel output blocks
   __shared__ StageTile<D> k0, k1, v0, v1;
-  __shared__ typename Src::Shared shared;
   // Masked stages whose values are not all finite: the values are set to 0, their places are bits of `odd`, a byte for eight channels.
   __shared__ int s_bad[2];
   __shared__ uint32_t odd[2][kStageKeys * D / 32];
@@ -156,7 +155,7 @@ __global__ __launch_bounds__(64 * Src::kWaves, 2) void prompt_kernel(SrcArgs a) 
     const int w_max = row0 < sp.rows ? min(sp.start + (sp.rho0 + min(row0 + 32 * RB, sp.rows) - 1) / G, cap - 1) : -1;
     const int w_all = a.window > 0 && w_max >= a.window ? w_max - a.window + 1 : 0;      // the first key (but for the leading) of all
 
-    Src src(a, shared, sq, sp, kvh, tid, t0, n);
+    Src src(a, sq, sp, kvh, tid, t0, n);
     u32x4 qf[RB][KS], ql[RB][Src::kLow ? KS : 1];
     float mul[RB];
 #pragma unroll
@@ -369,9 +368,9 @@ __global__ __launch_bounds__(64 * Src::kWaves, 2) void prompt_kernel(SrcArgs a) 
       // stages go K(t), then V(t), one behind: the scores of stage t + 1 are formed beside the probabilities of stage t
       src.load_k(0, k0);
       src.load_v(0, v0);
-      src.land(0, k0, v0);
+      src.land(true, k0, v0);
       if (n > 1) src.load_k(1, k1);
-      if (tile_masked(0) && src.odd(v0, odd[0])) s_bad[0] = 0;
+      if (Src::kOdd && tile_masked(0) && src.odd(v0, odd[0])) s_bad[0] = 0;
       if (n > 1) src.land_k(k1);
       __syncthreads();
       f32x16 sa[RB][NBK], sb[RB][NBK];
@@ -393,15 +392,16 @@ __global__ __launch_bounds__(64 * Src::kWaves, 2) void prompt_kernel(SrcArgs a) 
       auto step = [&](f32x16 (&cur)[RB][NBK], f32x16 (&nxt)[RB][NBK], int st, StageTile<D>& K, StageTile<D>& KN, StageTile<D>& V,
                       StageTile<D>& VN) __attribute__((always_inline)) {
         const bool more = st + 1 < n;                        // uniform
+        src.ahead(st);
         if (st + 2 < n) src.load_k(st + 2, K);
         if (more) src.load_v(st + 1, VN);
-        if (__builtin_expect(tile_masked(st) && s_bad[st & 1] == st, 0)) poison(st);
+        if (Src::kOdd && __builtin_expect(tile_masked(st) && s_bad[st & 1] == st, 0)) poison(st);
         // (behind the last stage the next one's scores are of no use, and without harm)
         stage(cur, nxt, KN, V, most);
         if (more) enter(nxt, st + 1);
         if (more) {
           src.land(st + 2 < n, K, VN);
-          if (tile_masked(st + 1) && src.odd(VN, odd[(st + 1) & 1])) s_bad[(st + 1) & 1] = st + 1;
+          if (Src::kOdd && tile_masked(st + 1) && src.odd(VN, odd[(st + 1) & 1])) s_bad[(st + 1) & 1] = st + 1;
         }
         __syncthreads();
       };
@@ -409,6 +409,23 @@ __global__ __launch_bounds__(64 * Src::kWaves, 2) void prompt_kernel(SrcArgs a) 
         step(sa, sb, st, k0, k1, v0, v1);
         if (st + 1 < n) step(sb, sa, st + 1, k1, k0, v1, v0);
       }
+    }
+    if constexpr (Src::kMixed) {
+      // values lie in the order 0 4 1 5 2 6 3 7: a half-wave's four become channels 0 .. 3 or 4 .. 7 of eight
+#pragma unroll
+      for (int x = 0; x < RB; ++x)
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            f32x16& o = acc[x][db];
+            const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(o[4 * j]), __float_as_uint(o[4 * j + 1]), false, false);
+            const auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(o[4 * j + 2]), __float_as_uint(o[4 * j + 3]), false, false);
+            o[4 * j] = __uint_as_float(p[0]);
+            o[4 * j + 1] = __uint_as_float(q[0]);
+            o[4 * j + 2] = __uint_as_float(p[1]);
+            o[4 * j + 3] = __uint_as_float(q[1]);
+          }
     }
 #pragma unroll
     for (int x = 0; x < RB; ++x) {
@@ -491,6 +508,42 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(Args a) {
     if (a.lse && c == 0)
       a.lse[(int64_t)(sp.r0 + tok) * a.Hq + head] = none ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
   }
+}
+
+// How a call is cut: equal shares of the work where fewer workgroups of 128 rows than two rounds would run, for rows that see 1024
+// keys or more (below, the two kernels more cost more than idle CUs); else a workgroup each.  cap: keys of a sequence at most (all units
+// of a head count below 2^31).
+constexpr int kRowsOfTile = 128;
+inline int prompt_shares(int Hkv) { return std::max(1, 512 / Hkv); }
+inline bool prompt_shared(int64_t slots, int Hkv, int64_t cap, int64_t keys) {
+  return slots * Hkv < 1024 && keys >= 1024 && slots * (cap / kStageKeys + 16) < (1ll << 31) - 65536;
+}
+inline size_t prompt_ws(int64_t slots, int Hkv, int d, int64_t cap, int64_t keys) {
+  if (!prompt_shared(slots, Hkv, cap, keys)) return 0;
+  return (size_t)prompt_shares(Hkv) * Hkv * 2 * kRowsOfTile * (d + 2) * sizeof(float) + (size_t)slots * sizeof(int);
+}
+template <class Src, int D, bool OUT16, class SrcArgs>
+int launch_prompt(SrcArgs& a, const char* fn, int64_t cap, int64_t keys, hipStream_t st) {
+  constexpr int R = kRowsOfTile;
+  const int64_t slots = (int64_t)a.bt.T * a.G / R + a.bt.B;
+  FL_REQUIRE(slots * a.pg.heads * 4 < (1ll << 31), FL_E_SHAPE, "%s: too many rows", fn);
+  a.slots = (int)slots;
+  if (!prompt_shared(slots, a.pg.heads, cap, keys)) {
+    prompt_kernel<Src, SrcArgs, false><<<(unsigned)(slots * a.pg.heads), 256, 0, st>>>(a);
+    return check_launch("prompt_kernel");
+  }
+  a.share = prompt_shares(a.pg.heads);
+  const size_t places = (size_t)a.share * a.pg.heads * 2 * R;
+  a.part_ml = a.part + places * D;
+  a.ends = reinterpret_cast<int*>(a.part_ml + places * 2);
+  prompt_plan_kernel<SrcArgs, R><<<1, 1024, 0, st>>>(a);
+  int rc = check_launch("prompt_plan_kernel");
+  if (rc != FL_OK) return rc;
+  prompt_kernel<Src, SrcArgs, true><<<(unsigned)(a.share * a.pg.heads), 256, 0, st>>>(a);
+  rc = check_launch("prompt_kernel");
+  if (rc != FL_OK) return rc;
+  prompt_join_kernel<SrcArgs, D, OUT16, R><<<(unsigned)(slots * (R / 32) * a.pg.heads), 256, 0, st>>>(a);
+  return check_launch("prompt_join_kernel");
 }
 
 }  // namespace fl

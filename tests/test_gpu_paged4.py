@@ -283,7 +283,8 @@ def check_attn(F, rng, new, past, page, Hq, Hkv, d, dtype, fmt, layout=None, rot
         assert np.all(got[n:] == 7) and torch.all(out[:, :Hq * d] == 7) and torch.all(out[:, 2 * Hq * d:] == 7)
         fin = np.isfinite(want[:n])
         what = f"new={list(new)[:5]} past={list(past)[:5]} page={page} {Hq}/{Hkv}x{d} {dtype} {fmt} w={window}+{n_sink} hint={max_q},{max_len}"
-        assert np.array_equal(np.isnan(got[:n]), ~fin), f"NaN where none belongs, {what}"
+        at = np.argwhere(np.isnan(got[:n]) != ~fin)
+        assert len(at) == 0, f"{len(at)} NaN where none belongs or the other way round, first at {at[0]}, {what}"
         keys = int(max(lens))
         wide = 2.0 ** -11 if fmt == "int4" else 0.0
         e = (2.0 ** -11 + wide + (d + 8) * 2.0 ** -23) * aq[:n]
