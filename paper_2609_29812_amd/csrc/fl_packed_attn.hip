@@ -92,7 +92,7 @@ struct PackedSource {
   }
   __device__ __forceinline__ void ahead(int) const {}
   __device__ __forceinline__ bool holes(int) const { return false; }
-  __device__ __forceinline__ bool there(int, int) const { return true; }
+  __device__ __forceinline__ uint32_t there(int) const { return 15; }
   __device__ __forceinline__ float query(const Args& args, int t, int head, int pos, bool ok, int hw, u32x4* q, u32x4*) const {
     constexpr int KS = D / 16;
     const uint16_t* row = args.q + (int64_t)t * args.qs + (int64_t)head * D;

@@ -14,10 +14,11 @@ __device__ __forceinline__ Seq find_row_tile(const Paged4Args& a, int slot) {
 }
 
 // A thread has a quarter of a key (and of a value) of each stage, which is of one group; a wave has 16 keys, which are of one page.
-template <int D, bool INT, bool F16>
+// LOW: fp16 queries that are rotated, in two parts.
+template <int D, bool INT, bool F16, bool LOW>
 struct Paged4Source {
   static constexpr int kD = D;
-  static constexpr bool kF16 = true, kOut16 = F16, kLow = F16, kMixed = INT;
+  static constexpr bool kF16 = true, kOut16 = F16, kLow = LOW, kMixed = INT;
   static constexpr int NW = D / 32, NG = D / kGroup, MB = meta_bytes<INT>();      // words of a thread, groups of a head
 
   const Paged4Args& a;
@@ -25,58 +26,59 @@ struct Paged4Source {
   int b, kvh, t0, n, wave, lane;
   int pid[2];                                // the wave's page of stage 64 i + lane, by the parity of i
   uint64_t hole[2];                          // stages with a page that is not there
-  int next[4];
   uint32_t kw[NW], vw[NW], km, kmv, vm;
 
   __device__ __forceinline__ Paged4Source(const Paged4Args& args, const Seq& sq, const Span& span, int head, int tid, int first, int stages)
       : a(args), sp(span), b(sq.b), kvh(head), t0(first), n(stages), wave(__builtin_amdgcn_readfirstlane(tid >> 6)), lane(tid & 63) {
+    pid[0] = pid[1] = -1;
+    hole[0] = hole[1] = 0;
     pages(0);
-    use_pages(0);
-    pid[1] = -1;
-    hole[1] = 0;
   }
   __device__ __forceinline__ void pages(int block) {
     const int st = 64 * block + lane;
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      next[g] = 0;
-      if (st < n) {
-        const int page = (key_of<kStageKeys>(sp, t0 + st) + 16 * g) >> a.pg.log2;
-        next[g] = page < a.bt.max_pages ? a.bt.table[(int64_t)b * a.bt.max_pages + page] : -1;
-      }
-    }
-  }
-  __device__ __forceinline__ void use_pages(int block) {
     bool gone = false;
     int own = -1;
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-      const bool none = (uint32_t)next[g] >= (uint32_t)a.pg.num;
+      int p = 0;
+      if (st < n) {
+        const int page = (key_of<kStageKeys>(sp, t0 + st) + 16 * g) >> a.pg.log2;
+        p = page < a.bt.max_pages ? a.bt.table[(int64_t)b * a.bt.max_pages + page] : -1;
+      }
+      const bool none = (uint32_t)p >= (uint32_t)a.pg.num;
       gone |= none;
-      own = g == wave ? (none ? -1 : next[g]) : own;
+      own = g == wave ? (none ? -1 : p) : own;
     }
     const uint64_t m = __builtin_amdgcn_ballot_w64(gone);
-    if (block & 1) {
-      pid[1] = own;
-      hole[1] = m;
-    } else {
-      pid[0] = own;
-      hole[0] = m;
-    }
+    pid[0] = block & 1 ? pid[0] : own;
+    pid[1] = block & 1 ? own : pid[1];
+    hole[0] = block & 1 ? hole[0] : m;
+    hole[1] = block & 1 ? m : hole[1];
   }
+  // (half way through a block the next one's, of 64 stages; waited for at once)
   __device__ __forceinline__ void ahead(int st) {
-    if ((st & 63) == 0) pages((st >> 6) + 1);
-    if ((st & 63) == 32) use_pages((st >> 6) + 1);
+    if ((st & 63) == 32) pages((st >> 6) + 1);
   }
-  __device__ __forceinline__ bool holes(int st) const { return ((st & 64 ? hole[1] : hole[0]) >> (st & 63)) & 1; }
-  __device__ __forceinline__ bool there(int st, int g) const {
-    if (!holes(st)) return true;
-    const int page = (key_of<kStageKeys>(sp, t0 + st) + 16 * g) >> a.pg.log2;
-    return page < a.bt.max_pages && (uint32_t)a.bt.table[(int64_t)b * a.bt.max_pages + page] < (uint32_t)a.pg.num;
+  __device__ __forceinline__ bool holes(int st) const {
+    const uint64_t even = hole[0], odd = hole[1];
+    return ((st & 64 ? odd : even) >> (st & 63)) & 1;
+  }
+  __device__ __forceinline__ uint32_t there(int st) const {  // a bit for 16 keys
+    uint32_t bits = 15;
+    if (holes(st)) {                         // uniform
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int page = (key_of<kStageKeys>(sp, t0 + st) + 16 * g) >> a.pg.log2;
+        const bool here = page < a.bt.max_pages && (uint32_t)a.bt.table[(int64_t)b * a.bt.max_pages + page] < (uint32_t)a.pg.num;
+        bits &= ~((here ? 0u : 1u) << g);
+      }
+    }
+    return bits;
   }
   // row of the wave's 16 keys of a stage (a page that is not there: any other's, masked)
   __device__ __forceinline__ int64_t row_of_stage(int st) const {
-    const int p = max(__builtin_amdgcn_readlane(st & 64 ? pid[1] : pid[0], st & 63), 0);
+    const int even = pid[0], odd = pid[1];
+    const int p = max(__builtin_amdgcn_readlane(st & 64 ? odd : even, st & 63), 0);
     return ((int64_t)p * a.pg.heads + kvh) * a.pg.size + ((key_of<kStageKeys>(sp, t0 + st) + 16 * wave) & (a.pg.size - 1));
   }
   __device__ __forceinline__ void codes(const uint8_t* at, uint32_t* w) const {
@@ -105,12 +107,14 @@ struct Paged4Source {
     vm = number(a.vm, row);
   }
   __device__ __forceinline__ void put(StageTile<D>& t, const uint32_t* w, uint32_t meta, uint32_t bad) const {
-    const int key = 16 * wave + (lane >> 2), g = swz32_f<D>(key & 31);
+    int l = lane;
+    renew(l);                                // (places in LDS are formed anew: kept over the stages, they spilled)
+    const int key = 16 * wave + (l >> 2), g = swz32_f<D>(key & 31);
 #pragma unroll
     for (int e = 0; e < NW; ++e) {
       u32x4 x = widen8<INT>(w[e], meta);
       if (e == 0) x[0] |= bad;
-      *reinterpret_cast<u32x4*>(t.x + key * D + (((lane & 3) * NW + e) ^ g) * 8) = x;
+      *reinterpret_cast<u32x4*>(t.x + key * D + (((l & 3) * NW + e) ^ g) * 8) = x;
     }
   }
   // a group that reads as NaN, of the key or the value, makes the key's scores NaN; the value's counts as 0
@@ -138,41 +142,43 @@ struct Paged4Source {
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
       q[k] = __builtin_bit_cast(u32x4, in_order<INT>(x[k]));
-      if constexpr (F16) low[k] = __builtin_bit_cast(u32x4, in_order<INT>(y[k]));
+      if constexpr (LOW) low[k] = __builtin_bit_cast(u32x4, in_order<INT>(y[k]));
       if (none) q[k] = u32x4{0x7E007E00u, 0x7E007E00u, 0x7E007E00u, 0x7E007E00u};
     }
     return m;
   }
 };
 
-#define FL_FORMS(D, I, F16)                                                                           \
-  template __global__ void prompt_kernel<Paged4Source<D, I, F16>, Paged4Args, true>(Paged4Args);      \
-  template __global__ void prompt_kernel<Paged4Source<D, I, F16>, Paged4Args, false>(Paged4Args);
-FL_FORMS(128, true, true)
-FL_FORMS(128, true, false)
-FL_FORMS(128, false, true)
-FL_FORMS(128, false, false)
-FL_FORMS(64, true, true)
-FL_FORMS(64, true, false)
-FL_FORMS(64, false, true)
-FL_FORMS(64, false, false)
+// (the compiler emits the launching side of one of the two forms alone unless both are named)
+#define FL_FORMS(D, I, F16, LOW)                                                                           \
+  template __global__ void prompt_kernel<Paged4Source<D, I, F16, LOW>, Paged4Args, true>(Paged4Args);      \
+  template __global__ void prompt_kernel<Paged4Source<D, I, F16, LOW>, Paged4Args, false>(Paged4Args);
+#define FL_FORMS_OF(D)            \
+  FL_FORMS(D, true, false, false)  \
+  FL_FORMS(D, true, true, false)   \
+  FL_FORMS(D, true, true, true)    \
+  FL_FORMS(D, false, false, false) \
+  FL_FORMS(D, false, true, false)  \
+  FL_FORMS(D, false, true, true)
+FL_FORMS_OF(128)
+FL_FORMS_OF(64)
+#undef FL_FORMS_OF
 #undef FL_FORMS
 
 size_t paged4_prompt_ws(int64_t slots, int Hkv, int d, int64_t cap, int64_t keys) { return prompt_ws(slots, Hkv, d, cap, keys); }
 
-template <int D, bool INT, bool F16>
-static int launch_prompt4(Paged4Args& a, int64_t keys, hipStream_t st) {
-  return launch_prompt<Paged4Source<D, INT, F16>, D, F16>(a, "fl_paged4_attn", (int64_t)a.bt.max_pages * a.pg.size, keys, st);
+template <int D, bool INT>
+static int launch_prompt4(Paged4Args& a, bool f16, int64_t keys, hipStream_t st) {
+  const char* fn = "fl_paged4_attn";
+  const int64_t cap = (int64_t)a.bt.max_pages * a.pg.size;
+  if (!f16) return launch_prompt<Paged4Source<D, INT, false, false>, D, false>(a, fn, cap, keys, st);
+  if (a.rt.table) return launch_prompt<Paged4Source<D, INT, true, true>, D, true>(a, fn, cap, keys, st);
+  return launch_prompt<Paged4Source<D, INT, true, false>, D, true>(a, fn, cap, keys, st);
 }
 int launch_paged4_prompt(const Paged4Args& args, int d, int format, bool f16, int64_t keys, hipStream_t st) {
   Paged4Args a = args;
-  const bool i = format == FL_KV4_INT;
-  if (d == 128) {
-    if (i) return f16 ? launch_prompt4<128, true, true>(a, keys, st) : launch_prompt4<128, true, false>(a, keys, st);
-    return f16 ? launch_prompt4<128, false, true>(a, keys, st) : launch_prompt4<128, false, false>(a, keys, st);
-  }
-  if (i) return f16 ? launch_prompt4<64, true, true>(a, keys, st) : launch_prompt4<64, true, false>(a, keys, st);
-  return f16 ? launch_prompt4<64, false, true>(a, keys, st) : launch_prompt4<64, false, false>(a, keys, st);
+  if (d == 128) return format == FL_KV4_INT ? launch_prompt4<128, true>(a, f16, keys, st) : launch_prompt4<128, false>(a, f16, keys, st);
+  return format == FL_KV4_INT ? launch_prompt4<64, true>(a, f16, keys, st) : launch_prompt4<64, false>(a, f16, keys, st);
 }
 
 }  // namespace fl

@@ -219,8 +219,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(SrcArgs a) {
 #pragma unroll
           for (int x = 0; x < RB; ++x) {
             s[x][b] = mma32<Src::kF16>(w, qf[x][ks], s[x][b]);
-            if constexpr (Src::kLow)
-              if (a.rt.table) s[x][b] = mma32<Src::kF16>(w, ql[x][ks], s[x][b]);
+            if constexpr (Src::kLow) s[x][b] = mma32<Src::kF16>(w, ql[x][ks], s[x][b]);
           }
         }
     };
@@ -237,17 +236,20 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(SrcArgs a) {
       return m;
     };
     auto mask = [&](f32x16 (&s)[RB][NBK], int st) __attribute__((always_inline)) {
-      const int key0 = key0_of(st);
+      const uint32_t here = src.there(st);                   // uniform: a bit for 16 keys
 #pragma unroll
-      for (int x = 0; x < RB; ++x)
+      for (int x = 0; x < RB; ++x) {
+        // the lane's keys count from here, so that what is compared with are constants
+        const int origin = key0_of(st) + 4 * hw, most = jmax[x] - origin, least = jmin[x] - origin, sinks = a.n_sink - origin;
 #pragma unroll
         for (int b = 0; b < NBK; ++b)
 #pragma unroll
           for (int v = 0; v < 16; ++v) {
-            const int j = key0 + 32 * b + 8 * (v >> 2) + 4 * hw + (v & 3);
-            const bool see = (j <= jmax[x]) & ((j >= jmin[x]) | (j < a.n_sink)) & src.there(st, 2 * b + (v >> 3));
+            const int j = 32 * b + 8 * (v >> 2) + (v & 3);
+            const bool see = (j <= most) & ((j >= least) | (j < sinks)) & ((here >> (2 * b + (v >> 3))) & 1u);
             s[x][b][v] = see ? s[x][b][v] : -INFINITY;
           }
+      }
     };
     // the running references follow the largest scores of a stage, where those are ahead by more than 8 octaves
     auto refer = [&](float (&most)[RB]) __attribute__((always_inline)) {
@@ -291,8 +293,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(SrcArgs a) {
 #pragma unroll
       for (int x = 0; x < RB; ++x) {
         s[x][i % NBK] = mma32<Src::kF16>(w, qf[x][i / NBK], s[x][i % NBK]);
-        if constexpr (Src::kLow)
-          if (a.rt.table) s[x][i % NBK] = mma32<Src::kF16>(w, ql[x][i / NBK], s[x][i % NBK]);
+        if constexpr (Src::kLow) s[x][i % NBK] = mma32<Src::kF16>(w, ql[x][i / NBK], s[x][i % NBK]);
       }
     };
     // NaN for what sees a value that is not finite
@@ -306,7 +307,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(SrcArgs a) {
 #pragma nounroll
         for (int i = 0; i < kStageKeys; ++i) {
           const int j = key0 + i;
-          const bool see = (j <= jmax[x]) & ((j >= jmin[x]) | (j < a.n_sink)) & src.there(st, i / 16);
+          const bool see = (j <= jmax[x]) & ((j >= jmin[x]) | (j < a.n_sink));
 #pragma unroll
           for (int db = 0; db < DB; ++db) m[db] |= see ? odd[st & 1][i * DB + db] : 0u;
         }
@@ -318,7 +319,9 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(SrcArgs a) {
     };
     // A stage: the scores of the next one (nxt) beside the probabilities of this one (cur), then O^T += V^T P^T beside what is left of
     // them and the largest scores of the next.  Each matrix instruction is followed by vector instructions that do not wait for it.
-    constexpr int NQ = KS * NBK, NP = NBK * 2 * DB, EARLY = 12, LA = 2, MG = 2 * NBK;
+    // (With a second part of 128-channel queries the registers hold one stage's scores alone: there they are formed behind the products.)
+    constexpr bool kBeside = !(Src::kLow && D == 128);
+    constexpr int NQ = KS * NBK, NP = NBK * 2 * DB, EARLY = 12, LATE = NP * 3 / 4, LA = 2, MG = 2 * NBK;
     auto stage = [&](f32x16 (&cur)[RB][NBK], f32x16 (&nxt)[RB][NBK], const StageTile<D>& KN, const StageTile<D>& V, float (&most)[RB])
         __attribute__((always_inline)) {
       u32x4 pf[RB][NBK][2], fr[LA + 1];
@@ -327,36 +330,68 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(SrcArgs a) {
       for (int x = 0; x < RB; ++x) {
         base[x] = ref[x] == -INFINITY ? 0.0f : ref[x];
         ts[x][0] = ts[x][1] = 0.0f;
+        if constexpr (kBeside) {
 #pragma unroll
-        for (int b = 0; b < NBK; ++b) nxt[x][b] = f32x16{};
+          for (int b = 0; b < NBK; ++b) nxt[x][b] = f32x16{};
+        }
       }
+      // the probabilities' pairs up to which each scores' and each products' instruction goes
+      auto early = [](int i) { return EARLY * i / NQ; };
+      auto late = [](int i) { return min(EARLY + (16 - EARLY) * i / LATE, 16); };
+      auto score_all = [&](bool beside) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < LA; ++i) fr[i] = read_k(KN, i);
+        for (int i = 0; i < LA; ++i) fr[i] = read_k(KN, i);
 #pragma unroll
-      for (int i = 0; i < NQ; ++i) {
-        fr[(i + LA) % (LA + 1)] = i + LA < NQ ? read_k(KN, i + LA) : read_v(V, i + LA - NQ);
-        score(nxt, fr[i % (LA + 1)], i);
+        for (int i = 0; i < NQ; ++i) {
+          if (i + LA < NQ) fr[(i + LA) % (LA + 1)] = read_k(KN, i + LA);
+          else if (beside) fr[(i + LA) % (LA + 1)] = read_v(V, i + LA - NQ);
+          score(nxt, fr[i % (LA + 1)], i);
+          if (beside) {
 #pragma unroll
-        for (int y = EARLY * i / NQ; y < EARLY * (i + 1) / NQ; ++y) weigh(cur, pf, base, y);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      constexpr int LATE = NP * 3 / 4;                       // (the last quarter needs the last of them)
-#pragma unroll
-      for (int i = 0; i < NP; ++i) {
-        if (i + LA < NP) fr[(NQ + i + LA) % (LA + 1)] = read_v(V, i + LA);
-#pragma unroll
-        for (int x = 0; x < RB; ++x) acc[x][i % DB] = mma32<Src::kF16>(fr[(NQ + i) % (LA + 1)], pf[x][i / DB / 2][i / DB % 2], acc[x][i % DB]);
-#pragma unroll
-        for (int y = EARLY + (16 - EARLY) * i / LATE; y < EARLY + (16 - EARLY) * (i + 1) / LATE && y < 16; ++y) weigh(cur, pf, base, y);
-#pragma unroll
-        for (int g = MG * i / NP; g < MG * (i + 1) / NP; ++g)
-#pragma unroll
-          for (int x = 0; x < RB; ++x) {
-            const float m = largest(nxt[x], g);
-            most[x] = g == 0 ? m : fmaxf(most[x], m);
-            if (g == MG - 1) renew(most[x]);                 // (here, beside the products)
+            for (int y = early(i); y < early(i + 1); ++y) weigh(cur, pf, base, y);
           }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      };
+      auto multiply = [&](int first) __attribute__((always_inline)) {       // (first: of the fragments' registers)
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+          if (i + LA < NP) fr[(first + i + LA) % (LA + 1)] = read_v(V, i + LA);
+#pragma unroll
+          for (int x = 0; x < RB; ++x)
+            acc[x][i % DB] = mma32<Src::kF16>(fr[(first + i) % (LA + 1)], pf[x][i / DB / 2][i / DB % 2], acc[x][i % DB]);
+#pragma unroll
+          for (int y = late(i); y < late(i + 1); ++y) weigh(cur, pf, base, y);
+          if constexpr (kBeside) {
+#pragma unroll
+            for (int g = MG * i / NP; g < MG * (i + 1) / NP; ++g)
+#pragma unroll
+              for (int x = 0; x < RB; ++x) {
+                const float m = largest(nxt[x], g);
+                most[x] = g == 0 ? m : fmaxf(most[x], m);
+                if (g == MG - 1) renew(most[x]);             // (here, beside the products)
+              }
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      };
+      if constexpr (kBeside) {
+        score_all(true);
+        multiply(NQ);
+      } else {
+#pragma unroll
+        for (int y = 0; y < EARLY; ++y) weigh(cur, pf, base, y);
+#pragma unroll
+        for (int i = 0; i < LA; ++i) fr[i] = read_v(V, i);
         __builtin_amdgcn_sched_barrier(0);
+        multiply(0);
+#pragma unroll
+        for (int x = 0; x < RB; ++x)
+#pragma unroll
+          for (int b = 0; b < NBK; ++b) nxt[x][b] = f32x16{};
+        score_all(false);
+#pragma unroll
+        for (int x = 0; x < RB; ++x) most[x] = largest_of(nxt[x]);
       }
 #pragma unroll
       for (int x = 0; x < RB; ++x) lsum[x] += ts[x][0] + ts[x][1];
@@ -392,7 +427,6 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(SrcArgs a) {
       auto step = [&](f32x16 (&cur)[RB][NBK], f32x16 (&nxt)[RB][NBK], int st, StageTile<D>& K, StageTile<D>& KN, StageTile<D>& V,
                       StageTile<D>& VN) __attribute__((always_inline)) {
         const bool more = st + 1 < n;                        // uniform
-        src.ahead(st);
         if (st + 2 < n) src.load_k(st + 2, K);
         if (more) src.load_v(st + 1, VN);
         if (Src::kOdd && __builtin_expect(tile_masked(st) && s_bad[st & 1] == st, 0)) poison(st);
@@ -403,6 +437,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(SrcArgs a) {
           src.land(st + 2 < n, K, VN);
           if (Src::kOdd && tile_masked(st + 1) && src.odd(VN, odd[(st + 1) & 1])) s_bad[(st + 1) & 1] = st + 1;
         }
+        src.ahead(st);
         __syncthreads();
       };
       for (int st = 0; st < n; st += 2) {
