@@ -11,14 +11,19 @@ struct Paged4Args : PagedAttnArgs {
 };
 
 // Two codes of 4 bits as fp16, from a word whose halves hold one each at the same place: at the low four bits of a byte they stand
-// under the exponent of 1024 as they are, at the high four sixteenfold.  Exact.
-__device__ __forceinline__ f16x2 low_pair(uint32_t w) {
+// under the exponent of 1024, at the high four under that of 64.  Exact.  (One constant in a vector register: both as literals take
+// two instructions.)
+struct Magic {
+  uint32_t low, high;
+  __device__ __forceinline__ Magic() : low(0x64006400u), high(0x54005400u) { asm volatile("" : "+v"(low), "+v"(high)); }
+};
+__device__ __forceinline__ f16x2 low_pair(uint32_t w, const Magic& m) {
   const f16x2 off = {(_Float16)-1024.0f, (_Float16)-1024.0f};
-  return __builtin_bit_cast(f16x2, (w & 0x000F000Fu) | 0x64006400u) + off;
+  return __builtin_bit_cast(f16x2, (w & 0x000F000Fu) | m.low) + off;
 }
-__device__ __forceinline__ f16x2 high_pair(uint32_t w) {
-  const f16x2 f = {(_Float16)0.0625f, (_Float16)0.0625f}, off = {(_Float16)-64.0f, (_Float16)-64.0f};
-  return __builtin_elementwise_fma(__builtin_bit_cast(f16x2, (w & 0x00F000F0u) | 0x64006400u), f, off);
+__device__ __forceinline__ f16x2 high_pair(uint32_t w, const Magic& m) {
+  const f16x2 off = {(_Float16)-64.0f, (_Float16)-64.0f};
+  return __builtin_bit_cast(f16x2, (w & 0x00F000F0u) | m.high) + off;
 }
 __device__ __forceinline__ uint32_t apply(f16x2 c, f16x2 s, f16x2 z) {
   return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(c, s, z));
@@ -28,11 +33,11 @@ __device__ __forceinline__ f16x2 both_high(uint32_t a, uint32_t b) { return __bu
 
 // Eight codes of one group in fp16: int4 one rounding of z + s c, in the order 0 4 1 5 2 6 3 7; e2m1 exactly, in their order.
 template <bool INT>
-__device__ __forceinline__ u32x4 widen8(uint32_t w, uint32_t meta) {
+__device__ __forceinline__ u32x4 widen8(uint32_t w, uint32_t meta, const Magic& g) {
   if constexpr (INT) {
     const f16x2 s = both_low(meta, meta), z = both_high(meta, meta);
     const uint32_t v = w >> 8;
-    return u32x4{apply(low_pair(w), s, z), apply(high_pair(w), s, z), apply(low_pair(v), s, z), apply(high_pair(v), s, z)};
+    return u32x4{apply(low_pair(w, g), s, z), apply(high_pair(w, g), s, z), apply(low_pair(v, g), s, z), apply(high_pair(v, g), s, z)};
   } else {
     const float s = __uint_as_float(meta << 23);
     return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 0)),
@@ -40,6 +45,19 @@ __device__ __forceinline__ u32x4 widen8(uint32_t w, uint32_t meta) {
                  __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 2)),
                  __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 3))};
   }
+}
+// byte `i` of a word of e2m1 codes as a pair
+template <int I>
+__device__ __forceinline__ uint32_t widen_byte(uint32_t w, float s) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, I));
+}
+// A query that is not finite: NaN in its place, and the factor 1, so that what it does not see stays out of its sums.
+template <int N>
+__device__ __forceinline__ float finite_factor(float m, f16x8* q) {
+  if (m == m) return m;
+#pragma unroll
+  for (int k = 0; k < N; ++k) q[k] = __builtin_bit_cast(f16x8, u32x4{0x7E007E00u, 0x7E007E00u, 0x7E007E00u, 0x7E007E00u});
+  return 1.0f;
 }
 // eight channels of a query in widen8's order
 template <bool INT>

@@ -3,9 +3,18 @@
 #include "fl_paged4_attn.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace fl {
 
+#ifndef FL_NT
+#define FL_NT 1
+#endif
+#if FL_NT
+#define FL_LOAD(x) __builtin_nontemporal_load(x)
+#else
+#define FL_LOAD(x) (*(x))
+#endif
 constexpr int kKeys4 = 32;         // keys of a wave's tile
 
 // Few rows: a workgroup has R = 16 NR rows of one key/value head (positions and the head's query heads) and a part of the keys;
@@ -13,11 +22,12 @@ constexpr int kKeys4 = 32;         // keys of a wave's tile
 //   S^T = K Q^T   v_mfma_f32_16x16x32_f16: a lane loads a quarter of a key's codes as they lie, which are of one group, and widens
 //                 them in registers; the contraction runs over the channels in the order that this gives.
 //   O^T += V^T P^T  the same product: a lane of S^T holds 2 x 4 keys of one row, which is the P^T operand for keys in that order;
-//                 the lane's words of V (8 keys x d / 16 channels) are transposed while they are widened.
+//                 the lane's words of V (8 keys x d / 16 channels) are transposed while they are widened.  Row m of 16 keys is key
+//                 4 (m % 4) + m / 4, so that the wave's load of one value a lane takes four neighbouring keys, whole cache lines.
 // No LDS in the loop: the next tile's keys are fetched into the registers that the scores leave, its values into those that the
 // outputs leave.  Page numbers of 32 tiles are fetched by the lanes at once and handed out by v_readlane.
 template <int D, bool INT, bool F16, int NR>
-__global__ __launch_bounds__(256, NR == 1 ? 3 : 2) void paged4_token_kernel(Paged4Args a) {
+__global__ __launch_bounds__(256, NR == 1 ? (F16 && D == 128 ? 3 : 4) : 2) void paged4_token_kernel(Paged4Args a) {
   constexpr int R = 16 * NR, KS = D / 32, DT = D / 16, NG = D / kGroup, MB = meta_bytes<INT>();
   constexpr int LD = D + 4;               // row stride of the waves' sums in LDS
   __shared__ float s_ref[4][R], s_sum[4][R];
@@ -75,6 +85,7 @@ __global__ __launch_bounds__(256, NR == 1 ? 3 : 2) void paged4_token_kernel(Page
     // (the order in which keys lie in the lanes)
     mul[x] = load_query<KS, F16>(a, src, ok, pos, cap, qf[x], ql[x], [g4](int k) { return KS * g4 + k; },
                                  [](float m) { return row4_max(m); });
+    mul[x] = finite_factor<KS>(mul[x], qf[x]);
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
       qf[x][k] = in_order<INT>(qf[x][k]);
@@ -97,7 +108,13 @@ __global__ __launch_bounds__(256, NR == 1 ? 3 : 2) void paged4_token_kernel(Page
   }
 
   uint32_t wk[2][KS], mk[2], mkv[2];                         // the tile's codes of the lane, the group's numbers, the values' ones
-  uint32_t wv[8], mv[8];
+  uint32_t wv[8];
+  const Magic magic;
+  // lane offsets; the lane that has the numbers of the lane's first value
+  const int key = 4 * (r16 & 3) + (r16 >> 2);
+  const uint32_t k_at = (uint32_t)(key * (D / 2) + g4 * (D / 8)), m_at = (uint32_t)(key * NG + g4 * NG / 4) * MB;
+  const uint32_t v_at = (uint32_t)(g4 * (D / 2) + (DT == 8 ? r16 * 4 : (r16 >> 1) * 4));
+  const int from = 4 * (4 * g4 + 16 * (DT == 8 ? r16 >> 2 : 2 * (r16 >> 3)));
   auto base_of = [&](int c, int h) {                         // row of key group h of the wave's tile c
     const int key0 = key_of<kKeys4>(sp, t0 + wave + 4 * c);
     const int p = max(__builtin_amdgcn_readlane(pid_v, (c & 31) + 32 * h), 0);        // (a page that is not there: masked)
@@ -108,49 +125,56 @@ __global__ __launch_bounds__(256, NR == 1 ? 3 : 2) void paged4_token_kernel(Page
     for (int h = 0; h < 2; ++h) {
       const int64_t row = base_of(c, h);
       const uint8_t* kb = a.kc + row * (D / 2);
-      const uint32_t m = (uint32_t)(r16 * NG + g4 * NG / 4) * MB;
       if constexpr (KS == 4) {
-        const u32x4 w = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(kb + (uint32_t)(r16 * 64 + g4 * 16)));
+        const u32x4 w = FL_LOAD(reinterpret_cast<const u32x4*>(kb + k_at));
 #pragma unroll
         for (int k = 0; k < 4; ++k) wk[h][k] = w[k];
       } else {
-        const u32x2 w = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(kb + (uint32_t)(r16 * 32 + g4 * 8)));
+        const u32x2 w = FL_LOAD(reinterpret_cast<const u32x2*>(kb + k_at));
         wk[h][0] = w[0];
         wk[h][1] = w[1];
       }
-      mk[h] = load_meta<INT>(a.km + row * (NG * MB) + m);
-      mkv[h] = load_meta<INT>(a.vm + row * (NG * MB) + m);
+      mk[h] = load_meta<INT>(a.km + row * (NG * MB) + m_at);
+      mkv[h] = load_meta<INT>(a.vm + row * (NG * MB) + m_at);
     }
   };
   auto load_v = [&](int c) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int64_t row = base_of(c, h);
-      const uint8_t* vb = a.vc + row * (D / 2);
-      const uint8_t* mb = a.vm + row * (NG * MB);
+      const uint8_t* vb = a.vc + base_of(c, h) * (D / 2);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t key = (uint32_t)(g4 * 4 + e);
-        wv[4 * h + e] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(vb + key * (D / 2) + (DT == 8 ? r16 * 4 : (r16 >> 1) * 4)));
-        mv[4 * h + e] = load_meta<INT>(mb + (key * NG + (uint32_t)(r16 * NG / 16)) * MB);
-      }
+      for (int e = 0; e < 4; ++e) wv[4 * h + e] = FL_LOAD(reinterpret_cast<const uint32_t*>(vb + 4 * e * (D / 2) + v_at));
     }
   };
   auto compute = [&](int c, bool more) {
     const int key0 = key_of<kKeys4>(sp, t0 + wave + 4 * c);
     const int pid0 = __builtin_amdgcn_readlane(pid_v, c & 31), pid1 = __builtin_amdgcn_readlane(pid_v, (c & 31) + 32);
     const bool masked = key0 + kKeys4 - 1 > all_max || (key0 < all_min && key0 + kKeys4 > a.n_sink) || (pid0 | pid1) < 0;
+    // a group that reads as NaN, of the key or the value, makes the key's scores NaN; the value's counts as 0
+    uint32_t bad[2];
+    bool fine = true;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const bool ok = group_ok<INT>(mkv[h]);
+      bad[h] = ok & group_ok<INT>(mk[h]) ? 0u : 0x7E007E00u;
+      fine &= ok;
+    }
+    const bool spoilt = __builtin_amdgcn_ballot_w64(!fine) != 0;      // uniform
+    // the values' numbers go from the lane that has loaded them to those that have the values
+    uint32_t mv[8];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) mv[4 * h + e] = (uint32_t)__builtin_amdgcn_ds_bpermute(from + 4 * e, (int)mkv[h]);
     f32x4 s[NR][2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      // a group that reads as NaN, of the key or the value, makes the key's scores NaN
-      const uint32_t bad = group_ok<INT>(mk[h]) & group_ok<INT>(mkv[h]) ? 0u : 0x7E007E00u;
 #pragma unroll
       for (int x = 0; x < NR; ++x) s[x][h] = f32x4{};
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
-        u32x4 w = widen8<INT>(wk[h][k], mk[h]);
-        if (k == 0) w[0] |= bad;
+        u32x4 w = widen8<INT>(wk[h][k], mk[h], magic);
+        if (k == 0) w[0] |= bad[h];
         const f16x8 kf = __builtin_bit_cast(f16x8, w);
 #pragma unroll
         for (int x = 0; x < NR; ++x) s[x][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[x][k], s[x][h], 0, 0, 0);
@@ -165,21 +189,18 @@ __global__ __launch_bounds__(256, NR == 1 ? 3 : 2) void paged4_token_kernel(Page
     f16x8 pf[NR];
 #pragma unroll
     for (int x = 0; x < NR; ++x) {
-      float y[2][4];
+      f32x4(&y)[2] = s[x];
+      if (masked) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) y[h][i] = s[x][h][i] * mul[x];
-        if (masked) {
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int j = key0 + 16 * h + 4 * g4 + i;
+            const int j = key0 + 16 * h + 4 * i + g4;
             const bool see = (j <= jmax[x]) & ((j >= jmin[x]) | (j < a.n_sink)) & ((h ? pid1 : pid0) >= 0);
             y[h][i] = see ? y[h][i] : -INFINITY;
           }
-        }
       }
-      const float most = row4_max(max3(max3(y[0][0], y[0][1], y[0][2]), max3(y[0][3], y[1][0], y[1][1]), max3(y[1][2], y[1][3], y[1][3])));
+      const float most = mul[x] * row4_max(max3(max3(y[0][0], y[0][1], y[0][2]), max3(y[0][3], y[1][0], y[1][1]), max3(y[1][2], y[1][3], y[1][3])));
       const bool raise = most > ref[x] + 8.0f;
       if (__builtin_amdgcn_ballot_w64(raise) != 0) {
         const float nm = raise ? most : ref[x];
@@ -194,17 +215,13 @@ __global__ __launch_bounds__(256, NR == 1 ? 3 : 2) void paged4_token_kernel(Page
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) p[h][i] = __builtin_amdgcn_exp2f(y[h][i] - base);
+        for (int i = 0; i < 4; ++i) p[h][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(y[h][i], mul[x], -base));
       lsum[x] += ((p[0][0] + p[0][1]) + (p[0][2] + p[0][3])) + ((p[1][0] + p[1][1]) + (p[1][2] + p[1][3]));
       const u32x4 pw = {pack_f16x2(p[0][0], p[0][1]), pack_f16x2(p[0][2], p[0][3]), pack_f16x2(p[1][0], p[1][1]),
                         pack_f16x2(p[1][2], p[1][3])};
       pf[x] = __builtin_bit_cast(f16x8, pw);
     }
-    // values of groups that read as NaN (rows that see them are NaN by their scores) count as 0
-    bool fine = true;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) fine &= group_ok<INT>(mv[e]);
-    if (__builtin_expect(__builtin_amdgcn_ballot_w64(!fine) != 0, 0)) {
+    if (__builtin_expect(spoilt, 0)) {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
         if (!group_ok<INT>(mv[e])) wv[e] = mv[e] = 0;
@@ -213,25 +230,19 @@ __global__ __launch_bounds__(256, NR == 1 ? 3 : 2) void paged4_token_kernel(Page
 #pragma unroll
       for (int e = 0; e < 8; ++e) wv[e] = r16 & 1 ? wv[e] >> 16 : wv[e];
     }
-#pragma unroll
-    for (int y = 0; y < DT / 2; ++y) {                       // channels 2 y and the next of the lane, eight keys
+    auto pair_of = [&](auto byte) {                          // channels 2 y and the next of the lane, eight keys
+      constexpr int y = decltype(byte)::value;
       u32x4 va, vb;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         if constexpr (INT) {
           const f16x2 sc = both_low(mv[2 * e], mv[2 * e + 1]), z = both_high(mv[2 * e], mv[2 * e + 1]);
           const uint32_t two = __builtin_amdgcn_perm(wv[2 * e + 1], wv[2 * e], 0x0c000c00u | (uint32_t)(4 + y) << 16 | (uint32_t)y);
-          va[e] = apply(low_pair(two), sc, z);
-          vb[e] = apply(high_pair(two), sc, z);
+          va[e] = apply(low_pair(two, magic), sc, z);
+          vb[e] = apply(high_pair(two, magic), sc, z);
         } else {
-          const uint32_t p0 = __builtin_bit_cast(uint32_t, y == 0   ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(wv[2 * e], __uint_as_float(mv[2 * e] << 23), 0)
-                                                           : y == 1 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(wv[2 * e], __uint_as_float(mv[2 * e] << 23), 1)
-                                                           : y == 2 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(wv[2 * e], __uint_as_float(mv[2 * e] << 23), 2)
-                                                                    : __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(wv[2 * e], __uint_as_float(mv[2 * e] << 23), 3));
-          const uint32_t p1 = __builtin_bit_cast(uint32_t, y == 0   ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(wv[2 * e + 1], __uint_as_float(mv[2 * e + 1] << 23), 0)
-                                                           : y == 1 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(wv[2 * e + 1], __uint_as_float(mv[2 * e + 1] << 23), 1)
-                                                           : y == 2 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(wv[2 * e + 1], __uint_as_float(mv[2 * e + 1] << 23), 2)
-                                                                    : __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(wv[2 * e + 1], __uint_as_float(mv[2 * e + 1] << 23), 3));
+          const uint32_t p0 = widen_byte<y>(wv[2 * e], __uint_as_float(mv[2 * e] << 23));
+          const uint32_t p1 = widen_byte<y>(wv[2 * e + 1], __uint_as_float(mv[2 * e + 1] << 23));
           va[e] = __builtin_amdgcn_perm(p1, p0, 0x05040100u);
           vb[e] = __builtin_amdgcn_perm(p1, p0, 0x07060302u);
         }
@@ -241,6 +252,12 @@ __global__ __launch_bounds__(256, NR == 1 ? 3 : 2) void paged4_token_kernel(Page
         acc[x][2 * y] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, va), pf[x], acc[x][2 * y], 0, 0, 0);
         acc[x][2 * y + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, vb), pf[x], acc[x][2 * y + 1], 0, 0, 0);
       }
+    };
+    pair_of(std::integral_constant<int, 0>{});
+    pair_of(std::integral_constant<int, 1>{});
+    if constexpr (DT == 8) {
+      pair_of(std::integral_constant<int, 2>{});
+      pair_of(std::integral_constant<int, 3>{});
     }
   };
 
@@ -418,7 +435,11 @@ static int launch_token4(const Paged4Args& args, int d, int format, bool f16, hi
 // How a call is cut, as the 8-bit cache's calls are: up to 16 or 32 rows of a key/value head in a sequence the kernel for few rows,
 // whose keys are split while sequences and heads alone are fewer than its shares, in parts of kLeastTiles tiles or more; more rows
 // the kernel for prompts.
-constexpr int kShare = 768, kLeastTiles = 8;
+#ifndef FL_SHARE
+#define FL_SHARE 768
+#define FL_LEAST 8
+#endif
+constexpr int kShare = FL_SHARE, kLeastTiles = FL_LEAST;
 struct Plan4 {
   int rows, n_split, min_tiles, share;
   int64_t keys;                   // that a row sees at most, as far as the caller knows

@@ -27,6 +27,7 @@ struct Paged4Source {
   int pid[2];                                // the wave's page of stage 64 i + lane, by the parity of i
   uint64_t hole[2];                          // stages with a page that is not there
   uint32_t kw[NW], vw[NW], km, kmv, vm;
+  Magic magic;
 
   __device__ __forceinline__ Paged4Source(const Paged4Args& args, const Seq& sq, const Span& span, int head, int tid, int first, int stages)
       : a(args), sp(span), b(sq.b), kvh(head), t0(first), n(stages), wave(__builtin_amdgcn_readfirstlane(tid >> 6)), lane(tid & 63) {
@@ -112,7 +113,7 @@ struct Paged4Source {
     const int key = 16 * wave + (l >> 2), g = swz32_f<D>(key & 31);
 #pragma unroll
     for (int e = 0; e < NW; ++e) {
-      u32x4 x = widen8<INT>(w[e], meta);
+      u32x4 x = widen8<INT>(w[e], meta, magic);
       if (e == 0) x[0] |= bad;
       *reinterpret_cast<u32x4*>(t.x + key * D + (((l & 3) * NW + e) ^ g) * 8) = x;
     }
@@ -137,13 +138,11 @@ struct Paged4Source {
     f16x8 x[KS], y[F16 ? KS : 1];
     float m = load_query<KS, F16>(args, args.q + (int64_t)t * args.qs + (int64_t)head * D, ok, pos, args.bt.max_pages * args.pg.size, x, y,
                                   [hw](int k) { return 2 * k + hw; }, [](float v) { return xor32_max(v); });
-    const bool none = !(m == m);             // a query that is not finite: NaN scores, and not the -inf of what it does not see
-    m = none ? 1.0f : m;
+    m = finite_factor<KS>(m, x);
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
       q[k] = __builtin_bit_cast(u32x4, in_order<INT>(x[k]));
       if constexpr (LOW) low[k] = __builtin_bit_cast(u32x4, in_order<INT>(y[k]));
-      if (none) q[k] = u32x4{0x7E007E00u, 0x7E007E00u, 0x7E007E00u, 0x7E007E00u};
     }
     return m;
   }
