@@ -33,16 +33,16 @@ __device__ __forceinline__ void values8(uint32_t w, uint32_t meta, float* x) {
   const bool ok = group_ok<INT>(meta);
   if constexpr (INT) {
     const float s = ok ? f16_bits_to_f32(meta & 0xFFFFu) : NAN, z = f16_bits_to_f32(meta >> 16);
+    const uint32_t even = w & 0x0F0F0F0Fu, odd = (w >> 4) & 0x0F0F0F0Fu;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = fmaf(s, (float)((w >> (4 * e)) & 15u), z);
+    for (int e = 0; e < 8; ++e) x[e] = fmaf(s, (float)(((e & 1 ? odd : even) >> (8 * (e / 2))) & 0xFFu), z);
   } else {
     const float s = ok ? __uint_as_float(meta << 23) : NAN;
+    typedef float pair __attribute__((ext_vector_type(2)));
+    const pair y[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 1),
+                       __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 3)};
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t c = (w >> (4 * e)) & 15u, m = c & 1u, k = (c >> 1) & 3u;
-      const float a = k == 0 ? 0.5f * (float)m : __uint_as_float(((126u + k) << 23) | (m << 22));
-      x[e] = s * (c & 8u ? -a : a);
-    }
+    for (int e = 0; e < 8; ++e) x[e] = s * y[e / 2][e & 1];
   }
 }
 

@@ -62,26 +62,33 @@ __device__ __forceinline__ uint32_t f16_rtz(float x) {
   return (uint32_t)__builtin_bit_cast(uint16_t, __builtin_amdgcn_cvt_pkrtz(x, 0.0f)[0]);
 }
 
-// The codes of a lane's eight values x (a word), the group's numbers (every lane of the quad has them).
+// The codes of a lane's eight values x (a word) and the group's numbers (every lane of the quad has them); x becomes what the codes
+// stand for.
 template <bool INT>
-__device__ __forceinline__ uint32_t encode_group(const float* x, uint32_t& meta) {
-  if constexpr (INT) {
-    float lo = x[0], hi = x[0], bad = 0.0f;
+__device__ __forceinline__ uint32_t encode_group(float* x, uint32_t& meta) {
+  float lo = x[0], hi = x[0], bad = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      lo = fminf(lo, x[e]);
-      hi = fmaxf(hi, x[e]);
-      bad = fmaf(x[e], 0.0f, bad);                 // NaN with an infinity or a NaN
-    }
-    lo = -quad_max(-lo);
-    hi = quad_max(hi);
-    bad = quad_max(bad == 0.0f ? 0.0f : 1.0f);
+  for (int e = 0; e < 8; ++e) {
+    if constexpr (INT) lo = fminf(lo, x[e]);
+    hi = INT ? fmaxf(hi, x[e]) : fmaxf(fabsf(hi), fabsf(x[e]));
+    bad = fmaf(x[e], 0.0f, bad);                   // NaN with an infinity or a NaN
+  }
+  if constexpr (INT) lo = -quad_max(-lo);
+  hi = quad_max(hi);
+  bad = quad_max(bad == 0.0f ? 0.0f : 1.0f);
+  if (bad > 0.0f) {
+    meta = INT ? kNaN4 : 255u;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = NAN;
+    return 0;
+  }
+  if (hi > 32768.0f || (INT && lo < -32768.0f)) {
     lo = fminf(fmaxf(lo, -32768.0f), 32768.0f);
     hi = fminf(fmaxf(hi, -32768.0f), 32768.0f);
-    if (bad > 0.0f) {
-      meta = kNaN4;
-      return 0;
-    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = fminf(fmaxf(x[e], -32768.0f), 32768.0f);
+  }
+  if constexpr (INT) {
     uint32_t zb = f16_rtz(lo);
     zb += f16_bits_to_f32(zb) > lo ? 1u : 0u;      // (towards zero is upwards below it)
     zb = zb == 0x8000u ? 0u : zb;
@@ -92,13 +99,18 @@ __device__ __forceinline__ uint32_t encode_group(const float* x, uint32_t& meta)
 #pragma unroll
     for (int e = 0; e < 2; ++e) sb += 15.0 * (double)f16_bits_to_f32(sb) < range ? 1u : 0u;
     meta = sb | zb << 16;
-    if (sb == 0) return 0;
+    if (sb == 0) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = z;
+      return 0;
+    }
     const float s = f16_bits_to_f32(sb), inv = __builtin_amdgcn_rcpf(s);
-    // the product with the reciprocal is within 2^-18 of the quotient; next to a half the definition's own steps decide
+    // The product with the reciprocal is within 2^-18 of the quotient, and that in [0, 15]; next to a half the definition's own
+    // steps decide.
     float r[8], off = 0.0f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float q = fminf(fmaxf((x[e] - z) * inv, 0.0f), 15.0f);
+      const float q = (x[e] - z) * inv;
       r[e] = rintf(q);
       off = fmaxf(off, fabsf(q - r[e]));
     }
@@ -106,39 +118,42 @@ __device__ __forceinline__ uint32_t encode_group(const float* x, uint32_t& meta)
 #pragma unroll
       for (int e = 0; e < 8; ++e) r[e] = (float)fmin(fmax(rint(((double)x[e] - (double)z) / (double)s), 0.0), 15.0);
     }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = fmaf(s, r[e], z);
     const float w0 = fmaf(fmaf(fmaf(r[3], 16.0f, r[2]), 16.0f, r[1]), 16.0f, r[0]);
     const float w1 = fmaf(fmaf(fmaf(r[7], 16.0f, r[6]), 16.0f, r[5]), 16.0f, r[4]);
     return (uint32_t)w0 | (uint32_t)w1 << 16;
   } else {
-    float most = 0.0f, bad = 0.0f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      most = fmaxf(most, fabsf(x[e]));
-      bad = fmaf(x[e], 0.0f, bad);
-    }
-    most = fminf(quad_max(most), 32768.0f);
-    bad = quad_max(bad == 0.0f ? 0.0f : 1.0f);
-    if (bad > 0.0f) {
-      meta = 255;
-      return 0;
-    }
-    // most = m 2^k with m in [1, 2): within 6 2^e = 1.5 2^(e + 2) from e = k - 2 on, or k - 1 when m > 1.5
-    const uint32_t bits = __float_as_uint(most);
+    // hi = m 2^k with m in [1, 2): within 6 2^e = 1.5 2^(e + 2) from e = k - 2 on, or k - 1 when m > 1.5
+    const uint32_t bits = __float_as_uint(hi);
     const int e = max((int)(bits >> 23) - 127 - 2 + ((bits & 0x7FFFFFu) > 0x400000u ? 1 : 0), kMinExp4);
     meta = (uint32_t)(e + 127);
     const float down = __uint_as_float((uint32_t)(127 - e) << 23);
-    float y[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = fminf(fmaxf(x[i], -32768.0f), 32768.0f) * down;
     uint32_t w = 0;
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[0], y[1], 1.0f, 0);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[2], y[3], 1.0f, 1);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[4], y[5], 1.0f, 2);
-    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[6], y[7], 1.0f, 3);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0] * down, x[1] * down, 1.0f, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2] * down, x[3] * down, 1.0f, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4] * down, x[5] * down, 1.0f, 2);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6] * down, x[7] * down, 1.0f, 3);
+    values8<false>(w, meta, x);
+    return w;
   }
 }
 
-template <int D, bool INT, bool F16>
+// What a wave's lanes do at step s0 of a row's 2 Hkv heads: the lane's head, and where its row and its cached position begin.  EVEN: the
+// wave's heads are all keys' or all values' (a whole number of steps each), so that all but the lane's offset is uniform.
+template <int D, bool EVEN>
+struct HeadOf {
+  bool is_k, there;
+  int h;
+  __device__ __forceinline__ HeadOf(int s0, int sub, int heads) {
+    const int s = EVEN ? s0 : s0 + sub;
+    is_k = s < heads;
+    h = (is_k ? s : s - heads) + (EVEN ? sub : 0);
+    there = EVEN || s < 2 * heads;
+  }
+};
+
+template <int D, bool INT, bool F16, bool EVEN>
 __global__ __launch_bounds__(256) void paged4_append_kernel(Rows4Args a) {
   constexpr int CH = D / 8, HPW = 64 / CH;         // chunks of a head; heads of a wave at a time
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -162,24 +177,21 @@ __global__ __launch_bounds__(256) void paged4_append_kernel(Rows4Args a) {
         cs[4 * e] = f.x; cs[4 * e + 1] = f.y; cs[4 * e + 2] = f.z; cs[4 * e + 3] = f.w;
       }
   }
-  const int slots = 2 * a.pg.heads;
-  for (int s = sub; s < slots; s += HPW) {
-    const bool is_k = s < a.pg.heads;
-    const int h = is_k ? s : s - a.pg.heads;
-    const uint16_t* src = (is_k ? a.k + (int64_t)t * a.ks : a.v + (int64_t)t * a.vs) + (int64_t)h * D;
-    const uint4 own = reinterpret_cast<const uint4*>(src)[c];
+  for (int s0 = 0; s0 < 2 * a.pg.heads; s0 += HPW) {
+    const HeadOf<D, EVEN> o(s0, sub, a.pg.heads);
+    if (!o.there) break;
+    const uint16_t* src = o.is_k ? a.k + (int64_t)t * a.ks : a.v + (int64_t)t * a.vs;
+    const uint32_t in_row = (uint32_t)(o.h * D + c * 8);
     float x[8];
-    unpack8<F16>(own, x);
-    if (is_k && turn) {
+    unpack8<F16>(*reinterpret_cast<const uint4*>(src + in_row), x);
+    if (o.is_k && turn) {
       // the products of 8- or 11-bit values with fp32 ones are exact in fp64: one rounding, by the sum, then fp32
       if (apart) {
         float y[8];
-        unpack8<F16>(reinterpret_cast<const uint4*>(src)[mate], y);
+        unpack8<F16>(*reinterpret_cast<const uint4*>(src + (uint32_t)(o.h * D + mate * 8)), y);
+        const double sign = c < half ? -1.0 : 1.0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const double p = x[e], q = y[e], co = cs[2 * e], si = cs[2 * e + 1];
-          x[e] = (float)(c < half ? fma(p, co, -(q * si)) : fma(q, si, p * co));
-        }
+        for (int e = 0; e < 8; ++e) x[e] = (float)fma((double)x[e], (double)cs[2 * e], sign * (double)y[e] * (double)cs[2 * e + 1]);
       } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -191,64 +203,64 @@ __global__ __launch_bounds__(256) void paged4_append_kernel(Rows4Args a) {
     }
     uint32_t meta;
     const uint32_t codes = encode_group<INT>(x, meta);
-    const int64_t at = w.at + (int64_t)h * a.pg.size;
-    reinterpret_cast<uint32_t*>((is_k ? a.kc : a.vc) + at * (D / 2))[c] = codes;
+    const int64_t row0 = (w.at + (int64_t)(EVEN ? o.h - sub : 0) * a.pg.size) * (D / 2);      // bytes
+    const uint32_t at = (uint32_t)(EVEN ? sub : o.h) * (uint32_t)a.pg.size;
+    *reinterpret_cast<uint32_t*>((o.is_k ? a.kc : a.vc) + row0 + at * (D / 2) + c * 4) = codes;
     if ((c & 3) == 0) {
-      uint8_t* m = (is_k ? a.km : a.vm) + (at * (D / kGroup) + c / 4) * meta_bytes<INT>();
+      constexpr int MB = meta_bytes<INT>(), NG = D / kGroup;
+      uint8_t* m = (o.is_k ? a.km : a.vm) + row0 / (D / 2) * (NG * MB) + (at * NG + (uint32_t)(c / 4)) * MB;
       if constexpr (INT) *reinterpret_cast<uint32_t*>(m) = meta;
       else *m = (uint8_t)meta;
     }
-    uint16_t* out = is_k ? a.kr : a.vr;
-    if (out) {
-      values8<INT>(codes, meta, x);
-      reinterpret_cast<uint4*>(out + (int64_t)t * (is_k ? a.krs : a.vrs) + (int64_t)h * D)[c] = pack8<F16>(x);
-    }
+    uint16_t* out = o.is_k ? a.kr : a.vr;
+    if (out) *reinterpret_cast<uint4*>(out + (int64_t)t * (o.is_k ? a.krs : a.vrs) + in_row) = pack8<F16>(x);
   }
 }
 
-template <int D, bool INT, bool F16>
+template <int D, bool INT, bool F16, bool EVEN>
 __global__ __launch_bounds__(256) void paged4_read_kernel(Rows4Args a) {
-  constexpr int CH = D / 8, HPW = 64 / CH;
+  constexpr int CH = D / 8, HPW = 64 / CH, MB = meta_bytes<INT>(), NG = D / kGroup;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int t = blockIdx.x * 4 + wave;
   if (t >= a.bt.T) return;
   const RowPlace w = place_of_row(a, t);
   if (w.pos < 0) return;
   const int c = lane % CH, sub = lane / CH;
-  for (int s = sub; s < 2 * a.pg.heads; s += HPW) {
-    const bool is_k = s < a.pg.heads;
-    const int h = is_k ? s : s - a.pg.heads;
-    uint16_t* out = is_k ? a.kr : a.vr;
+  for (int s0 = 0; s0 < 2 * a.pg.heads; s0 += HPW) {
+    const HeadOf<D, EVEN> o(s0, sub, a.pg.heads);
+    if (!o.there) break;
+    uint16_t* out = o.is_k ? a.kr : a.vr;
     if (!out) continue;
     float x[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
     if (w.at >= 0) {
-      const int64_t at = w.at + (int64_t)h * a.pg.size;
-      const uint32_t codes = reinterpret_cast<const uint32_t*>((is_k ? a.kc : a.vc) + at * (D / 2))[c];
-      const uint32_t meta = load_meta<INT>((is_k ? a.km : a.vm) + (at * (D / kGroup) + c / 4) * meta_bytes<INT>());
+      const int64_t row0 = (w.at + (int64_t)(EVEN ? o.h - sub : 0) * a.pg.size) * (D / 2);
+      const uint32_t at = (uint32_t)(EVEN ? sub : o.h) * (uint32_t)a.pg.size;
+      const uint32_t codes = *reinterpret_cast<const uint32_t*>((o.is_k ? a.kc : a.vc) + row0 + at * (D / 2) + c * 4);
+      const uint32_t meta = load_meta<INT>((o.is_k ? a.km : a.vm) + row0 / (D / 2) * (NG * MB) + (at * NG + (uint32_t)(c / 4)) * MB);
       values8<INT>(codes, meta, x);
     }
-    reinterpret_cast<uint4*>(out + (int64_t)t * (is_k ? a.krs : a.vrs) + (int64_t)h * D)[c] = pack8<F16>(x);
+    *reinterpret_cast<uint4*>(out + (int64_t)t * (o.is_k ? a.krs : a.vrs) + (uint32_t)(o.h * D + c * 8)) = pack8<F16>(x);
   }
 }
 
-template <int D>
+template <int D, bool EVEN>
 static void launch_append4(const Rows4Args& a, unsigned grid, int format, int dtype, hipStream_t st) {
   if (format == FL_KV4_INT) {
-    if (dtype == FL_F16) paged4_append_kernel<D, true, true><<<grid, 256, 0, st>>>(a);
-    else paged4_append_kernel<D, true, false><<<grid, 256, 0, st>>>(a);
+    if (dtype == FL_F16) paged4_append_kernel<D, true, true, EVEN><<<grid, 256, 0, st>>>(a);
+    else paged4_append_kernel<D, true, false, EVEN><<<grid, 256, 0, st>>>(a);
   } else {
-    if (dtype == FL_F16) paged4_append_kernel<D, false, true><<<grid, 256, 0, st>>>(a);
-    else paged4_append_kernel<D, false, false><<<grid, 256, 0, st>>>(a);
+    if (dtype == FL_F16) paged4_append_kernel<D, false, true, EVEN><<<grid, 256, 0, st>>>(a);
+    else paged4_append_kernel<D, false, false, EVEN><<<grid, 256, 0, st>>>(a);
   }
 }
-template <int D>
+template <int D, bool EVEN>
 static void launch_read4(const Rows4Args& a, unsigned grid, int format, int dtype, hipStream_t st) {
   if (format == FL_KV4_INT) {
-    if (dtype == FL_F16) paged4_read_kernel<D, true, true><<<grid, 256, 0, st>>>(a);
-    else paged4_read_kernel<D, true, false><<<grid, 256, 0, st>>>(a);
+    if (dtype == FL_F16) paged4_read_kernel<D, true, true, EVEN><<<grid, 256, 0, st>>>(a);
+    else paged4_read_kernel<D, true, false, EVEN><<<grid, 256, 0, st>>>(a);
   } else {
-    if (dtype == FL_F16) paged4_read_kernel<D, false, true><<<grid, 256, 0, st>>>(a);
-    else paged4_read_kernel<D, false, false><<<grid, 256, 0, st>>>(a);
+    if (dtype == FL_F16) paged4_read_kernel<D, false, true, EVEN><<<grid, 256, 0, st>>>(a);
+    else paged4_read_kernel<D, false, false, EVEN><<<grid, 256, 0, st>>>(a);
   }
 }
 
@@ -301,8 +313,9 @@ extern "C" int fl_paged4_append(const void* k, int64_t k_stride, const void* v, 
   rc = check_batch(fn, a.bt, a.pg, true, st);
   if (rc != FL_OK) return rc;
   const unsigned grid = ((unsigned)T + 3) / 4;
-  if (d == 128) launch_append4<128>(a, grid, format, dtype, st);
-  else launch_append4<64>(a, grid, format, dtype, st);
+  const bool even = Hkv * d % 512 == 0;      // (a wave takes 512 channels at a time)
+  if (d == 128) even ? launch_append4<128, true>(a, grid, format, dtype, st) : launch_append4<128, false>(a, grid, format, dtype, st);
+  else even ? launch_append4<64, true>(a, grid, format, dtype, st) : launch_append4<64, false>(a, grid, format, dtype, st);
   return check_launch("paged4_append_kernel");
   FL_API_END
 }
@@ -332,8 +345,9 @@ extern "C" int fl_paged4_read(const int32_t* cu, const int32_t* lens, int B, int
   rc = check_batch(fn, a.bt, a.pg, false, st);
   if (rc != FL_OK) return rc;
   const unsigned grid = ((unsigned)T + 3) / 4;
-  if (d == 128) launch_read4<128>(a, grid, format, dtype, st);
-  else launch_read4<64>(a, grid, format, dtype, st);
+  const bool even = Hkv * d % 512 == 0;      // (a wave takes 512 channels at a time)
+  if (d == 128) even ? launch_read4<128, true>(a, grid, format, dtype, st) : launch_read4<128, false>(a, grid, format, dtype, st);
+  else even ? launch_read4<64, true>(a, grid, format, dtype, st) : launch_read4<64, false>(a, grid, format, dtype, st);
   return check_launch("paged4_read_kernel");
   FL_API_END
 }
