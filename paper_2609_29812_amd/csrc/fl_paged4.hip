@@ -159,12 +159,22 @@ __global__ __launch_bounds__(256) void paged4_append_kernel(Rows4Args a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int t = blockIdx.x * 4 + wave;
   if (t >= a.bt.T) return;
-  const RowPlace w = place_of_row(a, t);
-  if (w.at < 0) return;
   const int c = lane % CH, sub = lane / CH;
   const int half = a.rt.table ? a.rt.rot / 16 : 0;                    // chunks of half the rotated part
   const bool turn = c < 2 * half, apart = a.rt.layout == FL_ROPE_HALF;
   const int mate = !turn || !apart ? c : c < half ? c + half : c - half;
+  // a step's values are asked for one step ahead, the first before the row's place is known
+  uint4 own = make_uint4(0, 0, 0, 0), other = own;
+  auto load = [&](int s0) {
+    const HeadOf<D, EVEN> o(s0, sub, a.pg.heads);
+    if (s0 >= 2 * a.pg.heads || !o.there) return;
+    const uint16_t* src = o.is_k ? a.k + (int64_t)t * a.ks : a.v + (int64_t)t * a.vs;
+    own = *reinterpret_cast<const uint4*>(src + (uint32_t)(o.h * D + c * 8));
+    if (o.is_k && apart && half > 0) other = *reinterpret_cast<const uint4*>(src + (uint32_t)(o.h * D + mate * 8));
+  };
+  load(0);
+  const RowPlace w = place_of_row(a, t);
+  if (w.at < 0) return;
   float cs[16];                                                       // cosines and sines of the chunk's pairs
 #pragma unroll
   for (int e = 0; e < 16; ++e) cs[e] = 0.0f;
@@ -180,15 +190,16 @@ __global__ __launch_bounds__(256) void paged4_append_kernel(Rows4Args a) {
   for (int s0 = 0; s0 < 2 * a.pg.heads; s0 += HPW) {
     const HeadOf<D, EVEN> o(s0, sub, a.pg.heads);
     if (!o.there) break;
-    const uint16_t* src = o.is_k ? a.k + (int64_t)t * a.ks : a.v + (int64_t)t * a.vs;
     const uint32_t in_row = (uint32_t)(o.h * D + c * 8);
+    const uint4 raw = own, raw2 = other;
+    load(s0 + HPW);
     float x[8];
-    unpack8<F16>(*reinterpret_cast<const uint4*>(src + in_row), x);
+    unpack8<F16>(raw, x);
     if (o.is_k && turn) {
       // the products of 8- or 11-bit values with fp32 ones are exact in fp64: one rounding, by the sum, then fp32
       if (apart) {
         float y[8];
-        unpack8<F16>(*reinterpret_cast<const uint4*>(src + (uint32_t)(o.h * D + mate * 8)), y);
+        unpack8<F16>(raw2, y);
         const double sign = c < half ? -1.0 : 1.0;
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = (float)fma((double)x[e], (double)cs[2 * e], sign * (double)y[e] * (double)cs[2 * e + 1]);
