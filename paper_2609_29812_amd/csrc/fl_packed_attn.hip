@@ -66,15 +66,22 @@ struct PackedSource {
   }
   __device__ __forceinline__ void load_k(int st, StageTile<D>& t) { load(k, a.ks, kofs, key_of<kStageKeys>(sp, t0 + st), t); }
   __device__ __forceinline__ void load_v(int st, StageTile<D>& t) { load(v, a.vs, vofs, key_of<kStageKeys>(sp, t0 + st), t); }
-  __device__ __forceinline__ void land(bool, StageTile<D>&, StageTile<D>&) { FL_WAIT_VM(0); }
-  __device__ __forceinline__ void land_k(StageTile<D>&) { FL_WAIT_VM(0); }
+  static constexpr int kItems = 0;
+  __device__ __forceinline__ void item(int, StageTile<D>&, StageTile<D>&) const {}
+  __device__ __forceinline__ void land() const { FL_WAIT_VM(0); }
+  __device__ __forceinline__ void land_k(StageTile<D>&) const { land(); }
+  __device__ __forceinline__ void land_v(StageTile<D>&) const { land(); }
   // The values that this lane's loads have brought: whether some are not finite (those become 0), and which.
   __device__ __forceinline__ bool odd(StageTile<D>& t, uint32_t* where) const {
     constexpr uint32_t kExp = F16 ? 0x7C00u : 0x7F80u;
+    int l = lane;
+    renew(l);                                // (places in LDS are formed anew: kept over the stages, they spilled)
+    const int c = wave * RPI + l / CH;
+    u32x4* at = reinterpret_cast<u32x4*>(t.x + wave * RPI * D + l * 8);
+    uint8_t* mark = reinterpret_cast<uint8_t*>(where) + c * CH + ((l % CH) ^ swz32_f<D>(c));
     bool any = false;
-#pragma unroll
+#pragma nounroll
     for (int x = 0; x < NI; ++x) {
-      u32x4* at = reinterpret_cast<u32x4*>(t.x + (x * ROWS + wave * RPI) * D + lane * 8);
       u32x4 w = *at;
       uint32_t bits = 0;
 #pragma unroll
@@ -83,10 +90,11 @@ struct PackedSource {
         bits |= (lo ? 1u : 0u) << (2 * e) | (hi ? 2u : 0u) << (2 * e);
         w[e] &= (lo ? 0u : 0xFFFFu) | (hi ? 0u : 0xFFFF0000u);
       }
-      const int c = x * ROWS + wave * RPI + lane / CH;
-      reinterpret_cast<uint8_t*>(where)[c * CH + ((lane % CH) ^ swz32_f<D>(c & 31))] = (uint8_t)bits;
+      *mark = (uint8_t)bits;
       if (bits != 0) *at = w;
       any |= bits != 0;
+      at += ROWS * D / 8;
+      mark += ROWS * CH;
     }
     return any;
   }

@@ -26,11 +26,15 @@ struct Paged4Source {
   int b, kvh, t0, n, wave, lane;
   int pid[2];                                // the wave's page of stage 64 i + lane, by the parity of i
   uint64_t hole[2];                          // stages with a page that is not there
-  uint32_t kw[NW], vw[NW], km, kmv, vm;
+  uint32_t kw[NW], vw[NW], km, kmv, vm, place;
   Magic magic;
 
   __device__ __forceinline__ Paged4Source(const Paged4Args& args, const Seq& sq, const Span& span, int head, int tid, int first, int stages)
       : a(args), sp(span), b(sq.b), kvh(head), t0(first), n(stages), wave(__builtin_amdgcn_readfirstlane(tid >> 6)), lane(tid & 63) {
+    place = place_of();
+    km = kmv = vm = 0;
+#pragma unroll
+    for (int e = 0; e < NW; ++e) kw[e] = vw[e] = 0;
     pid[0] = pid[1] = -1;
     hole[0] = hole[1] = 0;
     pages(0);
@@ -82,19 +86,24 @@ struct Paged4Source {
     const int p = max(__builtin_amdgcn_readlane(st & 64 ? odd : even, st & 63), 0);
     return ((int64_t)p * a.pg.heads + kvh) * a.pg.size + ((key_of<kStageKeys>(sp, t0 + st) + 16 * wave) & (a.pg.size - 1));
   }
+  // (the lane's offset is formed anew beside a uniform address: added to it ahead of the stages, the sums spilled)
   __device__ __forceinline__ void codes(const uint8_t* at, uint32_t* w) const {
+    int l = lane;
+    renew(l);
     if constexpr (NW == 4) {
-      const u32x4 x = reinterpret_cast<const u32x4*>(at)[lane];
+      const u32x4 x = *reinterpret_cast<const u32x4*>(at + (uint32_t)(16 * l));
 #pragma unroll
       for (int e = 0; e < 4; ++e) w[e] = x[e];
     } else {
-      const u32x2 x = reinterpret_cast<const u32x2*>(at)[lane];
+      const u32x2 x = *reinterpret_cast<const u32x2*>(at + (uint32_t)(8 * l));
       w[0] = x[0];
       w[1] = x[1];
     }
   }
   __device__ __forceinline__ uint32_t number(const uint8_t* m, int64_t row) const {
-    return load_meta<INT>(m + row * (NG * MB) + (uint32_t)(D == 128 ? lane : lane >> 1) * MB);
+    int l = lane;
+    renew(l);
+    return load_meta<INT>(m + row * (NG * MB) + (uint32_t)((D == 128 ? l : l >> 1) * MB));
   }
   __device__ __forceinline__ void load_k(int st, StageTile<D>&) {
     const int64_t row = row_of_stage(st);
@@ -107,30 +116,53 @@ struct Paged4Source {
     codes(a.vc + row * (D / 2), vw);
     vm = number(a.vm, row);
   }
-  __device__ __forceinline__ void put(StageTile<D>& t, const uint32_t* w, uint32_t meta, uint32_t bad) const {
-    int l = lane;
-    renew(l);                                // (places in LDS are formed anew: kept over the stages, they spilled)
-    const int key = 16 * wave + (l >> 2), g = swz32_f<D>(key & 31);
+  // Word e of the thread's keys or values widened into its place.  Neighbouring threads write their words in different orders (e ^ turn),
+  // so that 16 of them meet 16 different 16-byte groups of banks.
+  __device__ __forceinline__ void place_words(uint32_t* w) const {
+    const int turn = D == 128 ? lane >> 2 & 3 : lane >> 3 & 1;         // (of the thread's key)
 #pragma unroll
-    for (int e = 0; e < NW; ++e) {
-      u32x4 x = widen8<INT>(w[e], meta, magic);
-      if (e == 0) x[0] |= bad;
-      *reinterpret_cast<u32x4*>(t.x + key * D + (((l & 3) * NW + e) ^ g) * 8) = x;
+    for (int bit = 1; bit < NW; bit *= 2)
+#pragma unroll
+      for (int e = 0; e < NW; ++e)
+        if (!(e & bit)) {
+          const uint32_t x = w[e], y = w[e | bit];
+          w[e] = turn & bit ? y : x;
+          w[e | bit] = turn & bit ? x : y;
+        }
+  }
+  __device__ __forceinline__ uint32_t place_of() const {
+    const int key = 16 * wave + (lane >> 2), turn = D == 128 ? lane >> 2 & 3 : lane >> 3 & 1;
+    return (uint32_t)(key * D + ((((lane & 3) * NW) ^ turn ^ swz32_f<D>(key & 31)) * 8));
+  }
+  __device__ __forceinline__ void put(StageTile<D>& t, uint32_t w, uint32_t meta, uint32_t bad, int e) const {
+    u32x4 x = widen8<INT>(w, meta, magic);
+    x[0] |= bad;
+    *reinterpret_cast<u32x4*>(t.x + (place ^ (uint32_t)(8 * e))) = x;
+  }
+  // The work of a stage beside its products: its loads, widened into their buffers, a word a time.  A group that reads as NaN, of the
+  // key or the value, makes the key's scores NaN; the value's counts as 0.
+  static constexpr int kItems = 2 * NW;
+  __device__ __forceinline__ void item(int i, StageTile<D>& k, StageTile<D>& v) {
+    if (i < NW) {
+      if (i == 0) place_words(kw);
+      put(k, kw[i], km, i == 0 && !(group_ok<INT>(km) & group_ok<INT>(kmv)) ? 0x7E007E00u : 0u, i);
+    } else {
+      if (i == NW) {
+        place_words(vw);
+        vm = group_ok<INT>(vm) ? vm : 0u;
+      }
+      put(v, vw[i - NW], vm, 0, i - NW);
     }
   }
-  // a group that reads as NaN, of the key or the value, makes the key's scores NaN; the value's counts as 0
-  __device__ __forceinline__ void land_k(StageTile<D>& t) const {
-    put(t, kw, km, group_ok<INT>(km) & group_ok<INT>(kmv) ? 0u : 0x7E007E00u);
-  }
-  __device__ __forceinline__ void land(bool with_k, StageTile<D>& k, StageTile<D>& v) {
-    if (with_k) land_k(k);
-    if (!group_ok<INT>(vm)) {
-      vm = 0;
+  __device__ __forceinline__ void land_k(StageTile<D>& k) {
 #pragma unroll
-      for (int e = 0; e < NW; ++e) vw[e] = 0;
-    }
-    put(v, vw, vm, 0);
+    for (int i = 0; i < NW; ++i) item(i, k, k);
   }
+  __device__ __forceinline__ void land_v(StageTile<D>& v) {
+#pragma unroll
+    for (int i = NW; i < 2 * NW; ++i) item(i, v, v);
+  }
+  __device__ __forceinline__ void land() const {}
   static constexpr bool kOdd = false;        // (values are finite)
   __device__ __forceinline__ bool odd(StageTile<D>&, uint32_t*) const { return false; }
   __device__ __forceinline__ float query(const Paged4Args& args, int t, int head, int pos, bool ok, int hw, u32x4* q, u32x4* low) const {

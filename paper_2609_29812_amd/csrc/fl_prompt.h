@@ -19,6 +19,7 @@ struct __attribute__((aligned(16))) StageTile {
 
 // x, as if just computed
 __device__ __forceinline__ void renew(int& x) { asm volatile("" : "+v"(x)); }
+__device__ __forceinline__ void renew(uint32_t& x) { asm volatile("" : "+v"(x)); }
 __device__ __forceinline__ void renew(float& x) { asm volatile("" : "+v"(x)); }
 
 template <int R> Seq find_row_tile();      // (a name for the sources' own)
@@ -277,7 +278,11 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(SrcArgs a) {
         const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][b][v + 1], mul[x], -base[x]));
         ts[x][0] += p0;
         ts[x][1] += p1;
-        pf[x][b][v / 8][(v % 8) / 2] = pack2<Src::kF16>(p0, p1);
+        uint32_t two = pack2<Src::kF16>(p0, p1);
+        renew(ts[x][0]);                                     // (here: summed and packed later, the probabilities would stay in registers)
+        renew(ts[x][1]);
+        renew(two);
+        pf[x][b][v / 8][(v % 8) / 2] = two;
       }
     };
     auto read_k = [&](const StageTile<D>& kt, int i) __attribute__((always_inline)) {          // k-step i / NBK, block i % NBK
@@ -312,9 +317,11 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(SrcArgs a) {
           for (int db = 0; db < DB; ++db) m[db] |= see ? odd[st & 1][i * DB + db] : 0u;
         }
 #pragma unroll
-        for (int db = 0; db < DB; ++db)
+        for (int db = 0; db < DB; ++db) {
+          m[db] >>= 4 * hw;
 #pragma unroll
-          for (int v = 0; v < 16; ++v) acc[x][db][v] = (m[db] >> (8 * (v >> 2) + 4 * hw + (v & 3))) & 1u ? NAN : acc[x][db][v];
+          for (int v = 0; v < 16; ++v) acc[x][db][v] = (m[db] >> (8 * (v >> 2) + (v & 3))) & 1u ? NAN : acc[x][db][v];
+        }
       }
     };
     // A stage: the scores of the next one (nxt) beside the probabilities of this one (cur), then O^T += V^T P^T beside what is left of
@@ -322,7 +329,8 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(SrcArgs a) {
     // (With a second part of 128-channel queries the registers hold one stage's scores alone: there they are formed behind the products.)
     constexpr bool kBeside = !(Src::kLow && D == 128);
     constexpr int NQ = KS * NBK, NP = NBK * 2 * DB, EARLY = 12, LATE = NP * 3 / 4, LA = 2, MG = 2 * NBK;
-    auto stage = [&](f32x16 (&cur)[RB][NBK], f32x16 (&nxt)[RB][NBK], const StageTile<D>& KN, const StageTile<D>& V, float (&most)[RB])
+    auto stage = [&](f32x16 (&cur)[RB][NBK], f32x16 (&nxt)[RB][NBK], StageTile<D>& K, const StageTile<D>& KN, const StageTile<D>& V,
+                     StageTile<D>& VN, float (&most)[RB])
         __attribute__((always_inline)) {
       u32x4 pf[RB][NBK][2], fr[LA + 1];
       float base[RB];
@@ -362,6 +370,9 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(SrcArgs a) {
             acc[x][i % DB] = mma32<Src::kF16>(fr[(first + i) % (LA + 1)], pf[x][i / DB / 2][i / DB % 2], acc[x][i % DB]);
 #pragma unroll
           for (int y = late(i); y < late(i + 1); ++y) weigh(cur, pf, base, y);
+          // (the source's own work; behind the last stages into buffers that are not read again)
+#pragma unroll
+          for (int y = Src::kItems * i / NP; y < Src::kItems * (i + 1) / NP; ++y) src.item(y, K, VN);
           if constexpr (kBeside) {
 #pragma unroll
             for (int g = MG * i / NP; g < MG * (i + 1) / NP; ++g)
@@ -403,7 +414,8 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(SrcArgs a) {
       // stages go K(t), then V(t), one behind: the scores of stage t + 1 are formed beside the probabilities of stage t
       src.load_k(0, k0);
       src.load_v(0, v0);
-      src.land(true, k0, v0);
+      src.land_k(k0);
+      src.land_v(v0);
       if (n > 1) src.load_k(1, k1);
       if (Src::kOdd && tile_masked(0) && src.odd(v0, odd[0])) s_bad[0] = 0;
       if (n > 1) src.land_k(k1);
@@ -431,10 +443,10 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(SrcArgs a) {
         if (more) src.load_v(st + 1, VN);
         if (Src::kOdd && __builtin_expect(tile_masked(st) && s_bad[st & 1] == st, 0)) poison(st);
         // (behind the last stage the next one's scores are of no use, and without harm)
-        stage(cur, nxt, KN, V, most);
+        stage(cur, nxt, K, KN, V, VN, most);
         if (more) enter(nxt, st + 1);
+        src.land();
         if (more) {
-          src.land(st + 2 < n, K, VN);
           if (Src::kOdd && tile_masked(st + 1) && src.odd(VN, odd[(st + 1) & 1])) s_bad[(st + 1) & 1] = st + 1;
         }
         src.ahead(st);
