@@ -17,7 +17,7 @@ __device__ __forceinline__ Seq find_row_tile(const Paged4Args& a, int slot) {
 // LOW: fp16 queries that are rotated, in two parts.
 template <int D, bool INT, bool F16, bool LOW>
 struct Paged4Source {
-  static constexpr int kD = D;
+  static constexpr int kD = D, kWavesPerSimd = 2;
   static constexpr bool kF16 = true, kOut16 = F16, kLow = LOW, kMixed = INT;
   static constexpr int NW = D / 32, NG = D / kGroup, MB = meta_bytes<INT>();      // words of a thread, groups of a head
 
@@ -158,9 +158,16 @@ struct Paged4Source {
 #pragma unroll
     for (int i = 0; i < NW; ++i) item(i, k, k);
   }
-  __device__ __forceinline__ void land_v(StageTile<D>& v) {
+  __device__ __forceinline__ void begin(StageTile<D>& k0, StageTile<D>&, StageTile<D>& v0) {
+    load_k(0, k0);
+    load_v(0, v0);
+  }
+  __device__ __forceinline__ void finish(StageTile<D>& k0, StageTile<D>& k1, StageTile<D>& v0) {
+    land_k(k0);
+    if (n > 1) load_k(1, k1);
 #pragma unroll
-    for (int i = NW; i < 2 * NW; ++i) item(i, v, v);
+    for (int i = NW; i < 2 * NW; ++i) item(i, k0, v0);
+    if (n > 1) land_k(k1);
   }
   __device__ __forceinline__ void land() const {}
   static constexpr bool kOdd = false;        // (values are finite)

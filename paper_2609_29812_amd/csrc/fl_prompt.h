@@ -88,14 +88,14 @@ __device__ __forceinline__ int slot_of_unit(const int* ends, int slots, int x) {
 }
 
 template <class Src, class SrcArgs, bool SHARED>
-__global__ __launch_bounds__(256, 2) void prompt_kernel(SrcArgs a) {
+__global__ __launch_bounds__(256, Src::kWavesPerSimd) void prompt_kernel(SrcArgs a) {
   constexpr int D = Src::kD, R = 128, RB = 1;
   constexpr int NBK = kStageKeys / 32;     // 32-key blocks of a stage
   constexpr int KS = D / 16;               // k-steps of QK^T
   constexpr int DB = D / 32;               // 32-channel output blocks
   __shared__ StageTile<D> k0, k1, v0, v1;
   // Masked stages whose values are not all finite: the values are set to 0, their places are bits of `odd`, a byte for eight channels.
-  __shared__ int s_bad[2];
+  __shared__ int s_bad[2][4];              // by wave
   __shared__ uint32_t odd[2][kStageKeys * D / 32];
 
   const int kvh = blockIdx.x % a.pg.heads, wg = blockIdx.x / a.pg.heads;
@@ -157,6 +157,10 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(SrcArgs a) {
     const int w_all = a.window > 0 && w_max >= a.window ? w_max - a.window + 1 : 0;      // the first key (but for the leading) of all
 
     Src src(a, sq, sp, kvh, tid, t0, n);
+    if (n > 0) {
+      if constexpr (SHARED) __syncthreads();                 // (the last row tile's stages are read)
+      src.begin(k0, k1, v0);                                 // (the first loads, before those of the queries)
+    }
     u32x4 qf[RB][KS], ql[RB][Src::kLow ? KS : 1];
     float mul[RB];
 #pragma unroll
@@ -407,18 +411,18 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(SrcArgs a) {
 #pragma unroll
       for (int x = 0; x < RB; ++x) lsum[x] += ts[x][0] + ts[x][1];
     };
+    // masked stages: the values that the wave's loads have brought
+    auto look = [&](int st, StageTile<D>& v) __attribute__((always_inline)) {
+      if constexpr (Src::kOdd)
+        if (tile_masked(st)) {                               // uniform
+          const bool any = __builtin_amdgcn_ballot_w64(src.odd(v, odd[st & 1])) != 0;
+          if (lane == 0) s_bad[st & 1][wave] = any ? st : -1;
+        }
+    };
     if (n > 0) {
-      if constexpr (SHARED) __syncthreads();                 // (the last row tile's stages are read)
-      if (tid < 2) s_bad[tid] = -1;
-      __syncthreads();
       // stages go K(t), then V(t), one behind: the scores of stage t + 1 are formed beside the probabilities of stage t
-      src.load_k(0, k0);
-      src.load_v(0, v0);
-      src.land_k(k0);
-      src.land_v(v0);
-      if (n > 1) src.load_k(1, k1);
-      if (Src::kOdd && tile_masked(0) && src.odd(v0, odd[0])) s_bad[0] = 0;
-      if (n > 1) src.land_k(k1);
+      src.finish(k0, k1, v0);
+      look(0, v0);
       __syncthreads();
       f32x16 sa[RB][NBK], sb[RB][NBK];
       float most[RB];
@@ -441,14 +445,16 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(SrcArgs a) {
         const bool more = st + 1 < n;                        // uniform
         if (st + 2 < n) src.load_k(st + 2, K);
         if (more) src.load_v(st + 1, VN);
-        if (Src::kOdd && __builtin_expect(tile_masked(st) && s_bad[st & 1] == st, 0)) poison(st);
+        if constexpr (Src::kOdd)
+          if (tile_masked(st)) {                             // uniform
+            const int* bad = s_bad[st & 1];
+            if (__builtin_expect(bad[0] == st || bad[1] == st || bad[2] == st || bad[3] == st, 0)) poison(st);
+          }
         // (behind the last stage the next one's scores are of no use, and without harm)
         stage(cur, nxt, K, KN, V, VN, most);
         if (more) enter(nxt, st + 1);
         src.land();
-        if (more) {
-          if (Src::kOdd && tile_masked(st + 1) && src.odd(VN, odd[(st + 1) & 1])) s_bad[(st + 1) & 1] = st + 1;
-        }
+        if (more) look(st + 1, VN);
         src.ahead(st);
         __syncthreads();
       };
