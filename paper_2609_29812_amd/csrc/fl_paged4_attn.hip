@@ -7,14 +7,6 @@
 
 namespace fl {
 
-#ifndef FL_NT
-#define FL_NT 1
-#endif
-#if FL_NT
-#define FL_LOAD(x) __builtin_nontemporal_load(x)
-#else
-#define FL_LOAD(x) (*(x))
-#endif
 constexpr int kKeys4 = 32;         // keys of a wave's tile
 
 // Few rows: a workgroup has R = 16 NR rows of one key/value head (positions and the head's query heads) and a part of the keys;
@@ -126,11 +118,11 @@ __global__ __launch_bounds__(256, NR == 1 ? (F16 && D == 128 ? 3 : 4) : 2) void 
       const int64_t row = base_of(c, h);
       const uint8_t* kb = a.kc + row * (D / 2);
       if constexpr (KS == 4) {
-        const u32x4 w = FL_LOAD(reinterpret_cast<const u32x4*>(kb + k_at));
+        const u32x4 w = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(kb + k_at));
 #pragma unroll
         for (int k = 0; k < 4; ++k) wk[h][k] = w[k];
       } else {
-        const u32x2 w = FL_LOAD(reinterpret_cast<const u32x2*>(kb + k_at));
+        const u32x2 w = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(kb + k_at));
         wk[h][0] = w[0];
         wk[h][1] = w[1];
       }
@@ -143,7 +135,7 @@ __global__ __launch_bounds__(256, NR == 1 ? (F16 && D == 128 ? 3 : 4) : 2) void 
     for (int h = 0; h < 2; ++h) {
       const uint8_t* vb = a.vc + base_of(c, h) * (D / 2);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) wv[4 * h + e] = FL_LOAD(reinterpret_cast<const uint32_t*>(vb + 4 * e * (D / 2) + v_at));
+      for (int e = 0; e < 4; ++e) wv[4 * h + e] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(vb + 4 * e * (D / 2) + v_at));
     }
   };
   auto compute = [&](int c, bool more) {
@@ -435,11 +427,7 @@ static int launch_token4(const Paged4Args& args, int d, int format, bool f16, hi
 // How a call is cut, as the 8-bit cache's calls are: up to 16 or 32 rows of a key/value head in a sequence the kernel for few rows,
 // whose keys are split while sequences and heads alone are fewer than its shares, in parts of kLeastTiles tiles or more; more rows
 // the kernel for prompts.
-#ifndef FL_SHARE
-#define FL_SHARE 768
-#define FL_LEAST 8
-#endif
-constexpr int kShare = FL_SHARE, kLeastTiles = FL_LEAST;
+constexpr int kShare = 768, kLeastTiles = 8;
 struct Plan4 {
   int rows, n_split, min_tiles, share;
   int64_t keys;                   // that a row sees at most, as far as the caller knows

@@ -22,8 +22,6 @@ __device__ __forceinline__ void renew(int& x) { asm volatile("" : "+v"(x)); }
 __device__ __forceinline__ void renew(uint32_t& x) { asm volatile("" : "+v"(x)); }
 __device__ __forceinline__ void renew(float& x) { asm volatile("" : "+v"(x)); }
 
-template <int R> Seq find_row_tile();      // (a name for the sources' own)
-
 template <bool F16>
 __device__ __forceinline__ f32x16 mma32(const u32x4& a, const u32x4& b, const f32x16& c) {
   if constexpr (F16) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
@@ -89,7 +87,7 @@ __device__ __forceinline__ int slot_of_unit(const int* ends, int slots, int x) {
 
 template <class Src, class SrcArgs, bool SHARED>
 __global__ __launch_bounds__(256, Src::kWavesPerSimd) void prompt_kernel(SrcArgs a) {
-  constexpr int D = Src::kD, R = 128, RB = 1;
+  constexpr int D = Src::kD, R = 128;
   constexpr int NBK = kStageKeys / 32;     // 32-key blocks of a stage
   constexpr int KS = D / 16;               // k-steps of QK^T
   constexpr int DB = D / 32;               // 32-channel output blocks
@@ -140,20 +138,15 @@ __global__ __launch_bounds__(256, Src::kWavesPerSimd) void prompt_kernel(SrcArgs
     }
 
     const int cap = a.bt.max_pages * a.pg.size;
-    int row[RB], jmax[RB], jmin[RB];
-    bool row_ok[RB];
-#pragma unroll
-    for (int x = 0; x < RB; ++x) {
-      row[x] = 32 * (RB * wave + x) + r32;
-      row_ok[x] = row[x] < sp.rows;
-      const int pos = sp.start + (sp.rho0 + (row_ok[x] ? row[x] : 0)) / G;
-      jmax[x] = row_ok[x] ? min(pos, cap - 1) : -1;
-      jmin[x] = a.window > 0 && pos >= a.window ? pos - a.window + 1 : 0;
-    }
+    const int row = 32 * wave + r32;
+    const bool row_ok = row < sp.rows;
+    const int rho_q = sp.rho0 + (row_ok ? row : 0), pos = sp.start + rho_q / G;
+    const int jmax = row_ok ? min(pos, cap - 1) : -1;
+    const int jmin = a.window > 0 && pos >= a.window ? pos - a.window + 1 : 0;
     // positions of the wave's first and last row (none: no key is seen)
-    const int row0 = 32 * RB * wave;
+    const int row0 = 32 * wave;
     const int w_min = sp.start + (sp.rho0 + row0) / G;
-    const int w_max = row0 < sp.rows ? min(sp.start + (sp.rho0 + min(row0 + 32 * RB, sp.rows) - 1) / G, cap - 1) : -1;
+    const int w_max = row0 < sp.rows ? min(sp.start + (sp.rho0 + min(row0 + 32, sp.rows) - 1) / G, cap - 1) : -1;
     const int w_all = a.window > 0 && w_max >= a.window ? w_max - a.window + 1 : 0;      // the first key (but for the leading) of all
 
     Src src(a, sq, sp, kvh, tid, t0, n);
@@ -161,13 +154,8 @@ __global__ __launch_bounds__(256, Src::kWavesPerSimd) void prompt_kernel(SrcArgs
       if constexpr (SHARED) __syncthreads();                 // (the last row tile's stages are read)
       src.begin(k0, k1, v0);                                 // (the first loads, before those of the queries)
     }
-    u32x4 qf[RB][KS], ql[RB][Src::kLow ? KS : 1];
-    float mul[RB];
-#pragma unroll
-    for (int x = 0; x < RB; ++x) {
-      const int rho = sp.rho0 + (row_ok[x] ? row[x] : 0);
-      mul[x] = src.query(a, sp.r0 + rho / G, kvh * G + rho % G, sp.start + rho / G, row_ok[x], hw, qf[x], ql[x]);
-    }
+    u32x4 qf[KS], ql[Src::kLow ? KS : 1];
+    const float mul = src.query(a, sp.r0 + rho_q / G, kvh * G + rho_q % G, pos, row_ok, hw, qf, ql);
     // LDS read offsets (elements).  Keys (A operand): row r32, chunk 2 ks + hw.  Values (transposed reads): lane (16 g + 4 t + q)
     // at V[16 kb + 4 (g >> 1) + t (+ 8)][32 db + 16 (g & 1) + 4 q]
     int koff[KS], voff[DB], voff8[DB];
@@ -184,15 +172,10 @@ __global__ __launch_bounds__(256, Src::kWavesPerSimd) void prompt_kernel(SrcArgs
         voff8[db] = (col0 + 8) * D + ((4 * db + c_lo) ^ swz32_f<D>(col0 + 8)) * 8 + 4 * (q & 1);
       }
     }
-    f32x16 acc[RB][DB];
-    float ref[RB], lsum[RB];
+    f32x16 acc[DB];
+    float ref = -INFINITY, lsum = 0.0f;
 #pragma unroll
-    for (int x = 0; x < RB; ++x) {
-#pragma unroll
-      for (int db = 0; db < DB; ++db) acc[x][db] = f32x16{};
-      ref[x] = -INFINITY;
-      lsum[x] = 0.0f;
-    }
+    for (int db = 0; db < DB; ++db) acc[db] = f32x16{};
     auto key0_of = [&](int st) { return key_of<kStageKeys>(sp, t0 + st); };
     // stages from .. from + len - 1, uniform: every row sees every key (the tiles of leading positions count as masked)
     struct Clear {
@@ -211,21 +194,16 @@ __global__ __launch_bounds__(256, Src::kWavesPerSimd) void prompt_kernel(SrcArgs
     auto tile_masked = [&](int st) { return !tile_clear(st); };
 
     // scores of a stage, S^T = K Q^T: a lane has 16 keys of one row per block
-    auto scores = [&](f32x16 (&s)[RB][NBK], const StageTile<D>& kt) __attribute__((always_inline)) {
+    auto scores = [&](f32x16 (&s)[NBK], const StageTile<D>& kt) __attribute__((always_inline)) {
 #pragma unroll
-      for (int x = 0; x < RB; ++x)
-#pragma unroll
-        for (int b = 0; b < NBK; ++b) s[x][b] = f32x16{};
+      for (int b = 0; b < NBK; ++b) s[b] = f32x16{};
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
         for (int b = 0; b < NBK; ++b) {
           const u32x4 w = *reinterpret_cast<const u32x4*>(&kt.x[b * 32 * D + koff[ks]]);
-#pragma unroll
-          for (int x = 0; x < RB; ++x) {
-            s[x][b] = mma32<Src::kF16>(w, qf[x][ks], s[x][b]);
-            if constexpr (Src::kLow) s[x][b] = mma32<Src::kF16>(w, ql[x][ks], s[x][b]);
-          }
+          s[b] = mma32<Src::kF16>(w, qf[ks], s[b]);
+          if constexpr (Src::kLow) s[b] = mma32<Src::kF16>(w, ql[ks], s[b]);
         }
     };
     auto largest = [&](const f32x16 (&s)[NBK], int g) __attribute__((always_inline)) {        // of half a block
@@ -240,54 +218,45 @@ __global__ __launch_bounds__(256, Src::kWavesPerSimd) void prompt_kernel(SrcArgs
       for (int g = 1; g < 2 * NBK; ++g) m = fmaxf(m, largest(s, g));
       return m;
     };
-    auto mask = [&](f32x16 (&s)[RB][NBK], int st) __attribute__((always_inline)) {
+    auto mask = [&](f32x16 (&s)[NBK], int st) __attribute__((always_inline)) {
       const uint32_t here = src.there(st);                   // uniform: a bit for 16 keys
+      // the lane's keys count from here, so that what is compared with are constants
+      const int origin = key0_of(st) + 4 * hw, most = jmax - origin, least = jmin - origin, sinks = a.n_sink - origin;
 #pragma unroll
-      for (int x = 0; x < RB; ++x) {
-        // the lane's keys count from here, so that what is compared with are constants
-        const int origin = key0_of(st) + 4 * hw, most = jmax[x] - origin, least = jmin[x] - origin, sinks = a.n_sink - origin;
+      for (int b = 0; b < NBK; ++b)
 #pragma unroll
-        for (int b = 0; b < NBK; ++b)
-#pragma unroll
-          for (int v = 0; v < 16; ++v) {
-            const int j = 32 * b + 8 * (v >> 2) + (v & 3);
-            const bool see = (j <= most) & ((j >= least) | (j < sinks)) & ((here >> (2 * b + (v >> 3))) & 1u);
-            s[x][b][v] = see ? s[x][b][v] : -INFINITY;
-          }
-      }
+        for (int v = 0; v < 16; ++v) {
+          const int j = 32 * b + 8 * (v >> 2) + (v & 3);
+          const bool see = (j <= most) & ((j >= least) | (j < sinks)) & ((here >> (2 * b + (v >> 3))) & 1u);
+          s[b][v] = see ? s[b][v] : -INFINITY;
+        }
     };
     // the running references follow the largest scores of a stage, where those are ahead by more than 8 octaves
-    auto refer = [&](float (&most)[RB]) __attribute__((always_inline)) {
+    auto refer = [&](float& most) __attribute__((always_inline)) {
+      const float m = xor32_max(most) * mul;
+      const bool raise = m > ref + 8.0f;
+      if (__builtin_amdgcn_ballot_w64(raise) != 0) {
+        const float nm = raise ? m : ref;
+        const float alpha = raise ? __builtin_amdgcn_exp2f(ref - nm) : 1.0f;
+        lsum *= alpha;
 #pragma unroll
-      for (int x = 0; x < RB; ++x) {
-        const float m = xor32_max(most[x]) * mul[x];
-        const bool raise = m > ref[x] + 8.0f;
-        if (__builtin_amdgcn_ballot_w64(raise) != 0) {
-          const float nm = raise ? m : ref[x];
-          const float alpha = raise ? __builtin_amdgcn_exp2f(ref[x] - nm) : 1.0f;
-          lsum[x] *= alpha;
-#pragma unroll
-          for (int db = 0; db < DB; ++db) acc[x][db] *= alpha;
-          ref[x] = nm;
-        }
+        for (int db = 0; db < DB; ++db) acc[db] *= alpha;
+        ref = nm;
       }
     };
     // One pair of a stage's probabilities (16 pairs a row), as half a word of the operands.
-    float ts[RB][2];
-    auto weigh = [&](const f32x16 (&s)[RB][NBK], u32x4 (&pf)[RB][NBK][2], const float (&base)[RB], int i) __attribute__((always_inline)) {
-#pragma unroll
-      for (int x = 0; x < RB; ++x) {
-        const int b = i / 8, v = 2 * (i % 8);
-        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][b][v], mul[x], -base[x]));
-        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][b][v + 1], mul[x], -base[x]));
-        ts[x][0] += p0;
-        ts[x][1] += p1;
-        uint32_t two = pack2<Src::kF16>(p0, p1);
-        renew(ts[x][0]);                                     // (here: summed and packed later, the probabilities would stay in registers)
-        renew(ts[x][1]);
-        renew(two);
-        pf[x][b][v / 8][(v % 8) / 2] = two;
-      }
+    float ts[2];
+    auto weigh = [&](const f32x16 (&s)[NBK], u32x4 (&pf)[NBK][2], float base, int i) __attribute__((always_inline)) {
+      const int b = i / 8, v = 2 * (i % 8);
+      const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][v], mul, -base));
+      const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][v + 1], mul, -base));
+      ts[0] += p0;
+      ts[1] += p1;
+      uint32_t two = pack2<Src::kF16>(p0, p1);
+      renew(ts[0]);                                          // (here: summed and packed later, the probabilities would stay in registers)
+      renew(ts[1]);
+      renew(two);
+      pf[b][v / 8][(v % 8) / 2] = two;
     };
     auto read_k = [&](const StageTile<D>& kt, int i) __attribute__((always_inline)) {          // k-step i / NBK, block i % NBK
       return *reinterpret_cast<const u32x4*>(&kt.x[(i % NBK) * 32 * D + koff[i / NBK]]);
@@ -298,34 +267,28 @@ __global__ __launch_bounds__(256, Src::kWavesPerSimd) void prompt_kernel(SrcArgs
       const i16x4 vb = __builtin_amdgcn_ds_read_tr16_b64_v4i16(FL_LDS4(at_v + voff8[i % DB]));
       return __builtin_bit_cast(u32x4, __builtin_shufflevector(va, vb, 0, 1, 2, 3, 4, 5, 6, 7));
     };
-    auto score = [&](f32x16 (&s)[RB][NBK], const u32x4& w, int i) __attribute__((always_inline)) {
-#pragma unroll
-      for (int x = 0; x < RB; ++x) {
-        s[x][i % NBK] = mma32<Src::kF16>(w, qf[x][i / NBK], s[x][i % NBK]);
-        if constexpr (Src::kLow) s[x][i % NBK] = mma32<Src::kF16>(w, ql[x][i / NBK], s[x][i % NBK]);
-      }
+    auto score = [&](f32x16 (&s)[NBK], const u32x4& w, int i) __attribute__((always_inline)) {
+      s[i % NBK] = mma32<Src::kF16>(w, qf[i / NBK], s[i % NBK]);
+      if constexpr (Src::kLow) s[i % NBK] = mma32<Src::kF16>(w, ql[i / NBK], s[i % NBK]);
     };
     // NaN for what sees a value that is not finite
     auto poison = [&](int st) __attribute__((always_inline)) {
       const int key0 = key0_of(st);
+      uint32_t m[DB];
 #pragma unroll
-      for (int x = 0; x < RB; ++x) {
-        uint32_t m[DB];
-#pragma unroll
-        for (int db = 0; db < DB; ++db) m[db] = 0;
+      for (int db = 0; db < DB; ++db) m[db] = 0;
 #pragma nounroll
-        for (int i = 0; i < kStageKeys; ++i) {
-          const int j = key0 + i;
-          const bool see = (j <= jmax[x]) & ((j >= jmin[x]) | (j < a.n_sink));
+      for (int i = 0; i < kStageKeys; ++i) {
+        const int j = key0 + i;
+        const bool see = (j <= jmax) & ((j >= jmin) | (j < a.n_sink));
 #pragma unroll
-          for (int db = 0; db < DB; ++db) m[db] |= see ? odd[st & 1][i * DB + db] : 0u;
-        }
+        for (int db = 0; db < DB; ++db) m[db] |= see ? odd[st & 1][i * DB + db] : 0u;
+      }
 #pragma unroll
-        for (int db = 0; db < DB; ++db) {
-          m[db] >>= 4 * hw;
+      for (int db = 0; db < DB; ++db) {
+        m[db] >>= 4 * hw;
 #pragma unroll
-          for (int v = 0; v < 16; ++v) acc[x][db][v] = (m[db] >> (8 * (v >> 2) + (v & 3))) & 1u ? NAN : acc[x][db][v];
-        }
+        for (int v = 0; v < 16; ++v) acc[db][v] = (m[db] >> (8 * (v >> 2) + (v & 3))) & 1u ? NAN : acc[db][v];
       }
     };
     // A stage: the scores of the next one (nxt) beside the probabilities of this one (cur), then O^T += V^T P^T beside what is left of
@@ -333,19 +296,15 @@ __global__ __launch_bounds__(256, Src::kWavesPerSimd) void prompt_kernel(SrcArgs
     // (With a second part of 128-channel queries the registers hold one stage's scores alone: there they are formed behind the products.)
     constexpr bool kBeside = !(Src::kLow && D == 128);
     constexpr int NQ = KS * NBK, NP = NBK * 2 * DB, EARLY = 12, LATE = NP * 3 / 4, LA = 2, MG = 2 * NBK;
-    auto stage = [&](f32x16 (&cur)[RB][NBK], f32x16 (&nxt)[RB][NBK], StageTile<D>& K, const StageTile<D>& KN, const StageTile<D>& V,
-                     StageTile<D>& VN, float (&most)[RB])
+    auto stage = [&](f32x16 (&cur)[NBK], f32x16 (&nxt)[NBK], StageTile<D>& K, const StageTile<D>& KN, const StageTile<D>& V,
+                     StageTile<D>& VN, float& most)
         __attribute__((always_inline)) {
-      u32x4 pf[RB][NBK][2], fr[LA + 1];
-      float base[RB];
+      u32x4 pf[NBK][2], fr[LA + 1];
+      const float base = ref == -INFINITY ? 0.0f : ref;
+      ts[0] = ts[1] = 0.0f;
+      if constexpr (kBeside) {
 #pragma unroll
-      for (int x = 0; x < RB; ++x) {
-        base[x] = ref[x] == -INFINITY ? 0.0f : ref[x];
-        ts[x][0] = ts[x][1] = 0.0f;
-        if constexpr (kBeside) {
-#pragma unroll
-          for (int b = 0; b < NBK; ++b) nxt[x][b] = f32x16{};
-        }
+        for (int b = 0; b < NBK; ++b) nxt[b] = f32x16{};
       }
       // the probabilities' pairs up to which each scores' and each products' instruction goes
       auto early = [](int i) { return EARLY * i / NQ; };
@@ -369,9 +328,7 @@ __global__ __launch_bounds__(256, Src::kWavesPerSimd) void prompt_kernel(SrcArgs
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
           if (i + LA < NP) fr[(first + i + LA) % (LA + 1)] = read_v(V, i + LA);
-#pragma unroll
-          for (int x = 0; x < RB; ++x)
-            acc[x][i % DB] = mma32<Src::kF16>(fr[(first + i) % (LA + 1)], pf[x][i / DB / 2][i / DB % 2], acc[x][i % DB]);
+          acc[i % DB] = mma32<Src::kF16>(fr[(first + i) % (LA + 1)], pf[i / DB / 2][i / DB % 2], acc[i % DB]);
 #pragma unroll
           for (int y = late(i); y < late(i + 1); ++y) weigh(cur, pf, base, y);
           // (the source's own work; behind the last stages into buffers that are not read again)
@@ -379,13 +336,11 @@ __global__ __launch_bounds__(256, Src::kWavesPerSimd) void prompt_kernel(SrcArgs
           for (int y = Src::kItems * i / NP; y < Src::kItems * (i + 1) / NP; ++y) src.item(y, K, VN);
           if constexpr (kBeside) {
 #pragma unroll
-            for (int g = MG * i / NP; g < MG * (i + 1) / NP; ++g)
-#pragma unroll
-              for (int x = 0; x < RB; ++x) {
-                const float m = largest(nxt[x], g);
-                most[x] = g == 0 ? m : fmaxf(most[x], m);
-                if (g == MG - 1) renew(most[x]);             // (here, beside the products)
-              }
+            for (int g = MG * i / NP; g < MG * (i + 1) / NP; ++g) {
+              const float m = largest(nxt, g);
+              most = g == 0 ? m : fmaxf(most, m);
+              if (g == MG - 1) renew(most);                  // (here, beside the products)
+            }
           }
           __builtin_amdgcn_sched_barrier(0);
         }
@@ -401,15 +356,11 @@ __global__ __launch_bounds__(256, Src::kWavesPerSimd) void prompt_kernel(SrcArgs
         __builtin_amdgcn_sched_barrier(0);
         multiply(0);
 #pragma unroll
-        for (int x = 0; x < RB; ++x)
-#pragma unroll
-          for (int b = 0; b < NBK; ++b) nxt[x][b] = f32x16{};
+        for (int b = 0; b < NBK; ++b) nxt[b] = f32x16{};
         score_all(false);
-#pragma unroll
-        for (int x = 0; x < RB; ++x) most[x] = largest_of(nxt[x]);
+        most = largest_of(nxt);
       }
-#pragma unroll
-      for (int x = 0; x < RB; ++x) lsum[x] += ts[x][0] + ts[x][1];
+      lsum += ts[0] + ts[1];
     };
     // masked stages: the values that the wave's loads have brought
     auto look = [&](int st, StageTile<D>& v) __attribute__((always_inline)) {
@@ -424,23 +375,21 @@ __global__ __launch_bounds__(256, Src::kWavesPerSimd) void prompt_kernel(SrcArgs
       src.finish(k0, k1, v0);
       look(0, v0);
       __syncthreads();
-      f32x16 sa[RB][NBK], sb[RB][NBK];
-      float most[RB];
-      auto enter = [&](f32x16 (&s)[RB][NBK], int st) __attribute__((always_inline)) {
+      f32x16 sa[NBK], sb[NBK];
+      float most;
+      auto enter = [&](f32x16 (&s)[NBK], int st) __attribute__((always_inline)) {
         if (masked(st)) {                                    // uniform
           mask(s, st);
-#pragma unroll
-          for (int x = 0; x < RB; ++x) most[x] = largest_of(s[x]);
+          most = largest_of(s);
         }
         refer(most);
       };
       scores(sa, k0);
-#pragma unroll
-      for (int x = 0; x < RB; ++x) most[x] = largest_of(sa[x]);
+      most = largest_of(sa);
       enter(sa, 0);
       __syncthreads();                                       // (the first keys are read)
       // K: where stage st's keys were and st + 2's come; KN: st + 1's; V: st's values; VN: where st + 1's come
-      auto step = [&](f32x16 (&cur)[RB][NBK], f32x16 (&nxt)[RB][NBK], int st, StageTile<D>& K, StageTile<D>& KN, StageTile<D>& V,
+      auto step = [&](f32x16 (&cur)[NBK], f32x16 (&nxt)[NBK], int st, StageTile<D>& K, StageTile<D>& KN, StageTile<D>& V,
                       StageTile<D>& VN) __attribute__((always_inline)) {
         const bool more = st + 1 < n;                        // uniform
         if (st + 2 < n) src.load_k(st + 2, K);
@@ -466,50 +415,46 @@ __global__ __launch_bounds__(256, Src::kWavesPerSimd) void prompt_kernel(SrcArgs
     if constexpr (Src::kMixed) {
       // values lie in the order 0 4 1 5 2 6 3 7: a half-wave's four become channels 0 .. 3 or 4 .. 7 of eight
 #pragma unroll
-      for (int x = 0; x < RB; ++x)
+      for (int db = 0; db < DB; ++db)
 #pragma unroll
-        for (int db = 0; db < DB; ++db)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            f32x16& o = acc[x][db];
-            const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(o[4 * j]), __float_as_uint(o[4 * j + 1]), false, false);
-            const auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(o[4 * j + 2]), __float_as_uint(o[4 * j + 3]), false, false);
-            o[4 * j] = __uint_as_float(p[0]);
-            o[4 * j + 1] = __uint_as_float(q[0]);
-            o[4 * j + 2] = __uint_as_float(p[1]);
-            o[4 * j + 3] = __uint_as_float(q[1]);
-          }
+        for (int j = 0; j < 4; ++j) {
+          f32x16& o = acc[db];
+          const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(o[4 * j]), __float_as_uint(o[4 * j + 1]), false, false);
+          const auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(o[4 * j + 2]), __float_as_uint(o[4 * j + 3]), false, false);
+          o[4 * j] = __uint_as_float(p[0]);
+          o[4 * j + 1] = __uint_as_float(q[0]);
+          o[4 * j + 2] = __uint_as_float(p[1]);
+          o[4 * j + 3] = __uint_as_float(q[1]);
+        }
     }
-#pragma unroll
-    for (int x = 0; x < RB; ++x) {
-      lsum[x] = xor32_add(lsum[x]);
-      if (!row_ok[x]) continue;
-      const int rho = sp.rho0 + row[x], tok = rho / G, head = kvh * G + rho % G;
-      const bool none = ref[x] == -INFINITY && lsum[x] == 0.0f;
+    lsum = xor32_add(lsum);
+    if (row_ok) {
+      const int rho = sp.rho0 + row, tok = rho / G, head = kvh * G + rho % G;
+      const bool none = ref == -INFINITY && lsum == 0.0f;
       if (SHARED && !whole) {
         // a share cuts at most two row tiles: the one it begins with and the one it ends with
-        const int64_t pr = ((int64_t)(kvh * a.share + wg) * 2 + place) * R + row[x];
+        const int64_t pr = ((int64_t)(kvh * a.share + wg) * 2 + place) * R + row;
         float* out = a.part + pr * D + 4 * hw;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
           for (int j = 0; j < 4; ++j)
             *reinterpret_cast<float4*>(out + db * 32 + 8 * j) =
-                make_float4(acc[x][db][4 * j], acc[x][db][4 * j + 1], acc[x][db][4 * j + 2], acc[x][db][4 * j + 3]);
-        if (hw == 0) *reinterpret_cast<float2*>(a.part_ml + pr * 2) = make_float2(ref[x], lsum[x]);
+                make_float4(acc[db][4 * j], acc[db][4 * j + 1], acc[db][4 * j + 2], acc[db][4 * j + 3]);
+        if (hw == 0) *reinterpret_cast<float2*>(a.part_ml + pr * 2) = make_float2(ref, lsum);
       } else {
-        const float inv = none ? 0.0f : 1.0f / lsum[x];
+        const float inv = none ? 0.0f : 1.0f / lsum;
         uint16_t* out = a.o + (int64_t)(sp.r0 + tok) * a.os + (int64_t)head * D + 4 * hw;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const f32x16& o = acc[x][db];
+            const f32x16& o = acc[db];
             *reinterpret_cast<u32x2*>(out + db * 32 + 8 * j) = u32x2{pack2<Src::kOut16>(o[4 * j] * inv, o[4 * j + 1] * inv),
                                                                      pack2<Src::kOut16>(o[4 * j + 2] * inv, o[4 * j + 3] * inv)};
           }
         if (hw == 0 && a.lse)
-          a.lse[(int64_t)(sp.r0 + tok) * a.Hq + head] = none ? -INFINITY : (ref[x] + __builtin_amdgcn_logf(lsum[x])) * 0.6931471805599453f;
+          a.lse[(int64_t)(sp.r0 + tok) * a.Hq + head] = none ? -INFINITY : (ref + __builtin_amdgcn_logf(lsum)) * 0.6931471805599453f;
       }
     }
   }
