@@ -634,7 +634,8 @@ int fl_packed_attn(const void* q, int64_t q_stride, const void* k, int64_t k_str
  *   FL_KV4_INT  : fp16 [num_pages, Hkv, page, d / 32, 2], (scale s, zero z); a code c in 0 .. 15 stands for z + s c
  *   FL_KV4_E2M1 : uint8 [num_pages, Hkv, page, d / 32], e + 127; a code is an OCP e2m1 number c (0, 0.5, 1, 1.5, 2, 3, 4, 6 and
  *                 their negatives) and stands for c 2^e
- * A group with numbers that an append does not write (|z| > 2^15, s < 0, s > 4372 or NaN; e outside [-23, 13]) reads as NaN.
+ * A group with numbers that an append does not write (|z| > 2^15, s < 0, s > 4372, z + 15 s >= 65520 or NaN; e outside [-23, 13])
+ * reads as NaN.
  * Every position stands by itself: nothing that a page holds changes when another position is written.
  *
  * fl_paged4_append stores the new positions; x: the values, or the keys rotated by their positions when `table` is given (the

@@ -16,6 +16,7 @@ from oracle.paged import seen_by
 GROUP, MOST = 32, 32768.0
 E2M1 = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
 S_MOST, E_LEAST, E_MOST = 4372.0, -23, 13
+TOP = 65520.0                              # what rounds to an infinity in fp16
 
 
 def half_down(x):
@@ -58,7 +59,7 @@ def decode_group(c, meta, fmt):
     c = c.astype(int)
     if fmt == "int4":
         s, z = float(meta[0]), float(meta[1])
-        ok = 0 <= s <= S_MOST and abs(z) <= MOST and not (s == 0 and math.copysign(1, s) < 0)
+        ok = 0 <= s <= S_MOST and abs(z) <= MOST and z + 15 * s < TOP and not (s == 0 and math.copysign(1, s) < 0)
         return z + s * c if ok else np.full(len(c), np.nan)
     e = int(meta) - 127
     if not E_LEAST <= e <= E_MOST:
@@ -99,7 +100,7 @@ def rows_of(codes, meta, fmt):
     c = unpack(codes).reshape(*codes.shape[:-1], 2 * codes.shape[-1] // GROUP, GROUP).astype(int)
     if fmt == "int4":
         s, z = meta[..., 0].astype(np.float64), meta[..., 1].astype(np.float64)
-        ok = (s >= 0) & (s <= S_MOST) & (np.abs(z) <= MOST) & ~((s == 0) & np.signbit(s))
+        ok = (s >= 0) & (s <= S_MOST) & (np.abs(z) <= MOST) & (z + 15 * s < TOP) & ~((s == 0) & np.signbit(s))
         x = z[..., None] + s[..., None] * c
     else:
         e = meta.astype(int) - 127

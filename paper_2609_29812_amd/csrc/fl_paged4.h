@@ -13,8 +13,12 @@ constexpr int kMinExp4 = -23, kMaxExp4 = 13;
 // whether a group's numbers are such as an append writes: int4 scale | zero << 16, e2m1 the exponent's byte
 template <bool INT>
 __device__ __forceinline__ bool group_ok(uint32_t m) {
-  if constexpr (INT) return ((m & 0xFFFFu) <= kMaxScale4) & (((m >> 16) & 0x7FFFu) <= kMaxZero4);
-  else return m - (uint32_t)(kMinExp4 + 127) <= (uint32_t)(kMaxExp4 - kMinExp4);
+  if constexpr (INT) {
+    // (pages are never cleared: two numbers within their bounds may still stand for values beyond fp16's)
+    const _Float16 s = __builtin_bit_cast(_Float16, (uint16_t)m), z = __builtin_bit_cast(_Float16, (uint16_t)(m >> 16));
+    return ((m & 0xFFFFu) <= kMaxScale4) & (((m >> 16) & 0x7FFFu) <= kMaxZero4) & (__builtin_elementwise_fma(s, (_Float16)15.0f, z) <= (_Float16)65504.0f);
+  }
+  return m - (uint32_t)(kMinExp4 + 127) <= (uint32_t)(kMaxExp4 - kMinExp4);
 }
 
 // Bytes of a group's numbers.

@@ -409,6 +409,36 @@ def test_groups_that_read_as_nan(F, fmt, d):
 
 
 @pytest.mark.parametrize("fmt", ["int4", "e2m1"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_pages_of_any_bytes(F, fmt, d):
+    """Pages that were never cleared: every byte that no sequence holds is random, single numbers of it within their bounds and
+    groups beyond them among it; and such groups where rows do see them."""
+    rng = np.random.default_rng(20)
+
+    def edit(sides, tab):
+        for c, m in sides:
+            c[:] = np.frombuffer(rng.bytes(c.size), np.uint8).reshape(c.shape)
+            raw, keep = m.view(np.uint8), m.copy()
+            raw[:] = np.frombuffer(rng.bytes(raw.size), np.uint8).reshape(raw.shape)
+            if fmt == "int4":
+                m[rng.random(m.shape[:-1]) < 0.3] = (4372, 32768)
+            for b, L in enumerate(lens):                       # what the sequences hold
+                for p in range(-(-L // page)):
+                    m[tab[b, p], :, :L - p * page] = keep[tab[b, p], :, :L - p * page]
+    page = 64
+    for new, past in (([1, 2, 1], [700, 30, 0]), ([90, 1, 64], [301, 5, 64]), ([500, 3], [37, 2])):
+        lens = [a + b for a, b in zip(new, past)]
+        for window, n_sink in ((0, 0), (40, 3)):
+            check_attn(F, rng, new, past, page, 4, 2, d, "bf16", fmt, window=window, n_sink=n_sink, edit=edit,
+                       hints=((None, 0), (1, 0), (200, 0)))
+    if fmt == "int4":
+        def edge(sides, tab):                                  # just within, just beyond
+            for i, (_, m) in enumerate(sides):
+                m[tab[0, 4], 0, 3, 0] = [(2182, 32768), (2184, 32768)][i]
+        check_attn(F, rng, [3, 300], [600, 1], page, 4, 2, d, "bf16", fmt, edit=edge, hints=((None, 0), (1, 0), (200, 0)))
+
+
+@pytest.mark.parametrize("fmt", ["int4", "e2m1"])
 def test_values_of_any_size(F, fmt):
     """Groups whose values differ by far side by side, and as large and as small as the format has them."""
     rng = np.random.default_rng(17)
