@@ -19,6 +19,7 @@ and the attention's segment kernels load value tiles from it instead of converti
 (bitwise the same results).
 paged_step()  a dense loop (a prompt, a chunk of one, the newest positions) of a ragged batch whose contexts lie in a
               paged 8-bit cache: new keys rotated and stored with the values, then attention over the cache.
+paged4_step() the same over the paged 4-bit cache; whole prompts attend to the rows that their codes stand for.
 prune_list()  a smaller column budget for the next loop (Section 4.2): keep the sinks and the entries the
               last loop's updated rows gave the most probability mass.  The next loop then runs both passes
               (its subtract pass recomputes the kept columns' share with the same lse_ref).
@@ -145,6 +146,22 @@ def paged_step(cache, q, k, v, cu, lens, block_table, table=None, layout="half",
     fl.paged_append(k, v, cu, lens, block_table, *cache, table=table, layout=layout)
     return fl.paged_attn(q, cu, lens, block_table, *cache, table=table, layout=layout, window=window, n_sink=n_sink,
                          max_q=max_q, max_len=max_len, out=out, lse=lse, ws=ws)
+
+
+def paged4_step(cache, q, k, v, cu, lens, block_table, table=None, layout="half", window=0, n_sink=0, max_q=None, max_len=0,
+                whole=False, rows=None, out=None, lse=None, ws=None):
+    """paged_step over a 4-bit cache (fl.paged4_cache).  whole: the batch is whole prompts (lens[b] rows each, every page there); its
+    attention then runs over the rows that the stored codes stand for, rounded to q's type (fl.packed_attn), and not over the codes:
+    the same numbers but for that rounding, in less time.  rows: optional (k_rows, v_rows) to hold them, (k, v) themselves if those
+    are of no further use; ws is then fl.packed_attn_ws's (max_k = max_len), else fl.paged4_attn_ws's."""
+    if not whole:
+        fl.paged4_append(k, v, cu, lens, block_table, *cache, table=table, layout=layout)
+        return fl.paged4_attn(q, cu, lens, block_table, *cache, table=table, layout=layout, window=window, n_sink=n_sink,
+                              max_q=max_q, max_len=max_len, out=out, lse=lse, ws=ws)
+    k_rows, v_rows = (k.new_empty(k.shape), v.new_empty(v.shape)) if rows is None else rows
+    fl.paged4_append(k, v, cu, lens, block_table, *cache, table=table, layout=layout, k_rows=k_rows, v_rows=v_rows)
+    return fl.packed_attn(q, k_rows, v_rows, cu, table=table, layout=layout, window=window, n_sink=n_sink, max_k=max_len, out=out,
+                          lse=lse, ws=ws)
 
 
 def prune_list(st: LayerState, qr, t_next, n_sink):
