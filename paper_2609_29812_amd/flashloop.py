@@ -971,8 +971,8 @@ def paged4_read(cu, lens, block_table, k_cache, v_cache, k_meta, v_meta, T, dtyp
     if dtype not in _DTYPES:
         raise FlashLoopError(f"dtype must be bfloat16 or float16, got {dtype}")
     B, max_pages, num_pages, page, fmt = _paged4(at, T, cu, lens, block_table, k_cache, v_cache, k_meta, v_meta, Hkv, d)
-    k_out = torch.empty((T, Hkv, d), dtype=dtype, device=k_cache.device) if k_out is None else k_out
-    v_out = torch.empty((T, Hkv, d), dtype=dtype, device=k_cache.device) if v_out is None else v_out
+    k_out = k_cache.new_empty((T, Hkv, d), dtype=dtype) if k_out is None else k_out
+    v_out = k_cache.new_empty((T, Hkv, d), dtype=dtype) if v_out is None else v_out
     ks, vs = _rows(k_out, at, dtype, "k_out", (T, Hkv, d)), _rows(v_out, at, dtype, "v_out", (T, Hkv, d))
     rc = (_lib or load()).fl_paged4_read(
         cu.data_ptr(), lens.data_ptr(), B, T, Hkv, d, block_table.data_ptr(), max_pages, num_pages, page, fmt, k_cache.data_ptr(),

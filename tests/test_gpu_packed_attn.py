@@ -261,3 +261,11 @@ def test_graphs_that_share_a_workspace_and_streams(F):
     torch.cuda.synchronize()
     for w, many in zip(want, got):
         assert all(torch.equal(x[:2400], w[:2400]) for x in many)
+
+
+def test_far_positions(F):
+    """Few rows after hundreds of thousands of keys, and a chunk after many."""
+    rng = np.random.default_rng(30)
+    for window, n_sink in ((0, 0), (5000, 70)):
+        check(F, rng, [1, 3], [5, 300000], 2, 1, 64, "bf16", window=window, n_sink=n_sink, hints=(0, 100))
+        check(F, rng, [130, 1], [100000, 77], 1, 1, 128, "f16", window=window, n_sink=n_sink, layout="half", rot=64)

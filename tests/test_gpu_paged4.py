@@ -468,3 +468,41 @@ def test_queries_of_any_size(F):
     for max_q in (1, 100):
         got = F.paged4_attn(q, i32([0, 2]), i32([40]), i32([[0, 1, 2, 3]]), *cache, max_q=max_q)
         assert torch.isnan(got[0, 0]).all() and torch.isnan(got[1, 1]).all() and torch.isfinite(got[0, 1]).all() and torch.isfinite(got[1, 0]).all()
+
+
+@pytest.mark.parametrize("fmt", ["int4", "e2m1"])
+def test_far_positions(F, fmt):
+    """A position and a chunk after hundreds of thousands, with and without a window, however the call is hinted."""
+    rng = np.random.default_rng(21)
+    for window, n_sink in ((0, 0), (5000, 70)):
+        check_attn(F, rng, [1, 2], [300000, 17], 64, 4, 1, 64, "bf16", fmt, window=window, n_sink=n_sink, hints=((None, 0), (1, 300001), (200, 0)))
+        check_attn(F, rng, [130, 1], [100000, 77], 128, 1, 1, 128, "f16", fmt, window=window, n_sink=n_sink, hints=((None, 0), (1, 0)))
+
+
+@pytest.mark.parametrize("fmt", ["int4", "e2m1"])
+def test_empty_calls_and_one_side_alone(F, fmt):
+    """Calls without rows write nothing; one side's rows can be had without the other's."""
+    rng = np.random.default_rng(22)
+    H, d, page, T = 3, 64, 16, 21
+    cache = F.paged4_cache(4, H, page, d, fmt)
+    for c in cache:
+        c.view(torch.uint8).fill_(5)
+    before = [c.clone() for c in cache]
+    tab, none = i32([[2, 0]]), torch.empty(0, H, d, dtype=torch.bfloat16, device="cuda")
+    F.paged4_append(none, none, i32([0, 0]), i32([9]), tab, *cache, k_rows=none, v_rows=none)
+    F.paged4_read(i32([0, 0]), i32([9]), tab, *cache, 0)
+    assert F.paged4_attn(none, i32([0, 0]), i32([9]), tab, *cache).shape == none.shape
+    assert F.packed_attn(none, none, none, i32([0, 0])).shape == none.shape
+    torch.cuda.synchronize()
+    assert all(torch.equal(bits_t(a), bits_t(b)) for a, b in zip(cache, before))
+    k, v = (torch.from_numpy(rng.normal(size=(T, H, d))).to(torch.bfloat16).cuda() for _ in range(2))
+    batch_of = (i32([0, T]), i32([T]), tab)
+    kr, vr, k1, v1 = (torch.full_like(k, 7.0) for _ in range(4))
+    F.paged4_append(k, v, *batch_of, *cache, k_rows=kr, v_rows=vr)
+    F.paged4_append(k, v, *batch_of, *cache, k_rows=k1)
+    F.paged4_append(k, v, *batch_of, *cache, v_rows=v1)
+    assert torch.equal(k1, kr) and torch.equal(v1, vr)
+    # rows that see no key at all: the sequence has none
+    q = torch.ones(2, H, d, dtype=torch.bfloat16, device="cuda")
+    lse = torch.zeros(2, H, device="cuda")
+    assert torch.all(F.packed_attn(q, none, none, i32([0, 2]), i32([0, 0]), lse=lse) == 0) and torch.all(lse == -float("inf"))
