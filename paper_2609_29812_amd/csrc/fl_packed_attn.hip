@@ -75,13 +75,24 @@ struct PackedSource {
     if (n > 1) load_k(1, k1);
   }
   __device__ __forceinline__ void finish(StageTile<D>&, StageTile<D>&, StageTile<D>&) const { land(); }
-  // The values that this lane's loads have brought: whether some are not finite (those become 0), and which.
+  // The values that the wave's loads have brought: whether some of this lane's are not finite (those become 0), and which (`where` is
+  // written if the wave has some).
+  static __device__ __forceinline__ int wave_of(int key) { return key / RPI & 3; }
   __device__ __forceinline__ bool odd(StageTile<D>& t, uint32_t* where) const {
     constexpr uint32_t kExp = F16 ? 0x7C00u : 0x7F80u;
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
     int l = lane;
     renew(l);                                // (places in LDS are formed anew: kept over the stages, they spilled)
-    const int c = wave * RPI + l / CH;
     u32x4* at = reinterpret_cast<u32x4*>(t.x + wave * RPI * D + l * 8);
+    u16x2 most = {0, 0};
+#pragma unroll
+    for (int x = 0; x < NI; ++x) {
+      const u32x4 w = at[x * (ROWS * D / 8)];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, w[e] & (kExp | kExp << 16)));
+    }
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(most[0] == kExp || most[1] == kExp) == 0, 1)) return false;      // uniform
+    const int c = wave * RPI + l / CH;
     uint8_t* mark = reinterpret_cast<uint8_t*>(where) + c * CH + ((l % CH) ^ swz32_f<D>(c));
     bool any = false;
 #pragma nounroll

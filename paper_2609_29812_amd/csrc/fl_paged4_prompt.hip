@@ -171,6 +171,7 @@ struct Paged4Source {
   }
   __device__ __forceinline__ void land() const {}
   static constexpr bool kOdd = false;        // (values are finite)
+  static __device__ __forceinline__ int wave_of(int) { return 0; }
   __device__ __forceinline__ bool odd(StageTile<D>&, uint32_t*) const { return false; }
   __device__ __forceinline__ float query(const Paged4Args& args, int t, int head, int pos, bool ok, int hw, u32x4* q, u32x4* low) const {
     constexpr int KS = D / 16;

@@ -93,7 +93,7 @@ __global__ __launch_bounds__(256, Src::kWavesPerSimd) void prompt_kernel(SrcArgs
   constexpr int DB = D / 32;               // 32-channel output blocks
   __shared__ StageTile<D> k0, k1, v0, v1;
   // Masked stages whose values are not all finite: the values are set to 0, their places are bits of `odd`, a byte for eight channels.
-  __shared__ int s_bad[2][4];              // by wave
+  __shared__ int s_bad[2][4];              // by the wave that looked: the stage where there are some
   __shared__ uint32_t odd[2][kStageKeys * D / 32];
 
   const int kvh = blockIdx.x % a.pg.heads, wg = blockIdx.x / a.pg.heads;
@@ -218,17 +218,21 @@ __global__ __launch_bounds__(256, Src::kWavesPerSimd) void prompt_kernel(SrcArgs
       for (int g = 1; g < 2 * NBK; ++g) m = fmaxf(m, largest(s, g));
       return m;
     };
+    // What a row does not see is -inf: a word of bits for the lane's keys, taken by two instructions a score.
     auto mask = [&](f32x16 (&s)[NBK], int st) __attribute__((always_inline)) {
-      const uint32_t here = src.there(st);                   // uniform: a bit for 16 keys
-      // the lane's keys count from here, so that what is compared with are constants
-      const int origin = key0_of(st) + 4 * hw, most = jmax - origin, least = jmin - origin, sinks = a.n_sink - origin;
+      const int origin = key0_of(st) + 4 * hw;               // the lane's keys count from here: 0 .. 3, 8 .. 11, .. 56 .. 59
+      auto until = [&](int j) {                              // keys 0 .. j
+        const uint32_t n = min(4u * (uint32_t)(j >> 3) + min((uint32_t)(j & 7), 3u), 31u);
+        return j < 0 ? 0u : ~0u >> (31u - n);
+      };
+      const uint32_t here = ((src.there(st) * 0x00204081u) & 0x01010101u) * 0xFFu;         // uniform: a byte of bits for 16 keys
+      const uint32_t see = until(jmax - origin) & (~until(jmin - origin - 1) | until(a.n_sink - origin - 1)) & here;
 #pragma unroll
       for (int b = 0; b < NBK; ++b)
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
-          const int j = 32 * b + 8 * (v >> 2) + (v & 3);
-          const bool see = (j <= most) & ((j >= least) | (j < sinks)) & ((here >> (2 * b + (v >> 3))) & 1u);
-          s[b][v] = see ? s[b][v] : -INFINITY;
+          const uint32_t all = (uint32_t)__builtin_amdgcn_sbfe((int)see, 16 * b + v, 1);
+          s[b][v] = __uint_as_float((__float_as_uint(s[b][v]) & all) | (0xFF800000u & ~all));
         }
     };
     // the running references follow the largest scores of a stage, where those are ahead by more than 8 octaves
@@ -280,7 +284,7 @@ __global__ __launch_bounds__(256, Src::kWavesPerSimd) void prompt_kernel(SrcArgs
 #pragma nounroll
       for (int i = 0; i < kStageKeys; ++i) {
         const int j = key0 + i;
-        const bool see = (j <= jmax) & ((j >= jmin) | (j < a.n_sink));
+        const bool see = (j <= jmax) & ((j >= jmin) | (j < a.n_sink)) & (s_bad[st & 1][Src::wave_of(i)] == st);
 #pragma unroll
         for (int db = 0; db < DB; ++db) m[db] |= see ? odd[st & 1][i * DB + db] : 0u;
       }
