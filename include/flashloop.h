@@ -608,7 +608,7 @@ int fl_paged_attn(const void* q, int64_t q_stride, int dtype, const int32_t* cu,
  *   table      : fp32 [n_pos, rot / 2, 2] as in (9), or NULL.  With it the queries are turned by their positions and rounded to
  *                `dtype`, as fl_rope leaves them (a position outside [0, n_pos): NaN).  Keys are taken as they are.
  *   lse        : fp32 [Tq, Hq], or NULL.
- *   max_k      : the largest n_k as far as the caller knows it (0: Tk).  It chooses how the work is cut; any value gives the
+ *   max_k      : the largest n_k as far as the caller knows it (0: Tk / B).  It chooses how the work is cut; any value gives the
  *                result, up to rounding.
  *   ws         : 16-byte aligned, at least fl_packed_attn_ws(...) bytes, for the same arguments; nothing is kept in it between calls.
  *                Calls that overlap need one each.

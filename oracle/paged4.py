@@ -101,7 +101,7 @@ def rows_of(codes, meta, fmt):
     if fmt == "int4":
         s, z = meta[..., 0].astype(np.float64), meta[..., 1].astype(np.float64)
         ok = (s >= 0) & (s <= S_MOST) & (np.abs(z) <= MOST) & (z + 15 * s < TOP) & ~((s == 0) & np.signbit(s))
-        x = z[..., None] + s[..., None] * c
+        x = np.where(ok, z, 0.0)[..., None] + np.where(ok, s, 0.0)[..., None] * c
     else:
         e = meta.astype(int) - 127
         ok = (e >= E_LEAST) & (e <= E_MOST)

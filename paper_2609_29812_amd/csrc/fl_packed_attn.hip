@@ -153,10 +153,10 @@ FL_FORMS(64, true)
 FL_FORMS(64, false)
 #undef FL_FORMS
 
-// keys of a sequence at most, as far as the caller knows
-static int64_t packed_keys(int Tk, int window, int n_sink, int max_k) {
-  const int64_t keys = max_k > 0 ? std::min(max_k, Tk) : Tk;
-  return window > 0 ? std::min<int64_t>(keys, (int64_t)window + n_sink + kRowsOfTile) : keys;
+static PromptShape packed_shape(int B, int Tq, int Tk, int Hq, int Hkv, int window, int n_sink, int max_k) {
+  int64_t keys = max_k > 0 ? std::min(max_k, Tk) : ((int64_t)Tk + B - 1) / B;
+  if (window > 0) keys = std::min<int64_t>(keys, (int64_t)window + n_sink + kRowsOfTile);
+  return {B, Tq, Hq / Hkv, Hkv, std::max(0, Tk - Tq) / B, keys, Tk};
 }
 
 static int check_offsets(const char* fn, const char* name, const int32_t* cu, int B, int T, hipStream_t st) {
@@ -177,7 +177,7 @@ using namespace fl;
 extern "C" size_t fl_packed_attn_ws(int B, int Tq, int Tk, int Hq, int Hkv, int d, int window, int n_sink, int max_k) {
   if (B < 1 || Tq < 1 || Tk < 0 || Hkv < 1 || Hq < Hkv || Hq % Hkv || (d != 64 && d != 128) || window < 0 || n_sink < 0 || max_k < 0)
     return 0;
-  return prompt_ws((int64_t)Tq * (Hq / Hkv) / kRowsOfTile + B, Hkv, d, Tk, packed_keys(Tk, window, n_sink, max_k));
+  return prompt_ws(packed_shape(B, Tq, Tk, Hq, Hkv, window, n_sink, max_k), d);
 }
 
 extern "C" int fl_packed_attn(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
@@ -220,7 +220,8 @@ extern "C" int fl_packed_attn(const void* q, int64_t q_stride, const void* k, in
     if (rc == FL_OK) rc = check_offsets(fn, "cu_k", cu_k, B, Tk, st);
     if (rc != FL_OK) return rc;
   }
-  const size_t need = fl_packed_attn_ws(B, Tq, Tk, Hq, Hkv, d, window, n_sink, max_k);
+  const PromptShape shape = packed_shape(B, Tq, Tk, Hq, Hkv, window, n_sink, max_k);
+  const size_t need = prompt_ws(shape, d);
   FL_REQUIRE(need == 0 || (ws && ws_bytes >= need), FL_E_WORKSPACE, "%s: workspace of %zu bytes required", fn, need);
   FL_REQUIRE((reinterpret_cast<uintptr_t>(ws) & 15) == 0, FL_E_SHAPE, "%s: ws must be 16-byte aligned", fn);
   PackedArgs a{};
@@ -232,11 +233,10 @@ extern "C" int fl_packed_attn(const void* q, int64_t q_stride, const void* k, in
   a.n_pos = n_pos; a.Tk = Tk; a.Hq = Hq; a.G = Hq / Hkv; a.scale_log2 = sm_scale * 1.4426950408889634f;
   a.window = window; a.n_sink = n_sink;
   a.part = static_cast<float*>(ws);
-  const int64_t keys = packed_keys(Tk, window, n_sink, max_k);
   if (d == 128)
-    return dtype == FL_F16 ? launch_prompt<PackedSource<128, true>, 128, true>(a, fn, Tk, keys, st)
-                           : launch_prompt<PackedSource<128, false>, 128, false>(a, fn, Tk, keys, st);
-  return dtype == FL_F16 ? launch_prompt<PackedSource<64, true>, 64, true>(a, fn, Tk, keys, st)
-                         : launch_prompt<PackedSource<64, false>, 64, false>(a, fn, Tk, keys, st);
+    return dtype == FL_F16 ? launch_prompt<PackedSource<128, true>, 128, true>(a, fn, shape, st)
+                           : launch_prompt<PackedSource<128, false>, 128, false>(a, fn, shape, st);
+  return dtype == FL_F16 ? launch_prompt<PackedSource<64, true>, 64, true>(a, fn, shape, st)
+                         : launch_prompt<PackedSource<64, false>, 64, false>(a, fn, shape, st);
   FL_API_END
 }

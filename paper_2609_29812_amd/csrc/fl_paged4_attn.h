@@ -67,7 +67,8 @@ __device__ __forceinline__ f16x8 in_order(const f16x8& q) {
 }
 
 // many rows
-size_t paged4_prompt_ws(int64_t slots, int Hkv, int d, int64_t cap, int64_t keys);
-int launch_paged4_prompt(const Paged4Args& a, int d, int format, bool f16, int64_t keys, hipStream_t st);
+struct PromptShape;
+size_t paged4_prompt_ws(const PromptShape& s, int d);
+int launch_paged4_prompt(const Paged4Args& a, int d, int format, bool f16, const PromptShape& shape, hipStream_t st);
 
 }  // namespace fl

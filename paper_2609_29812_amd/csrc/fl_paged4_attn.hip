@@ -1,6 +1,7 @@
 // Dense attention of a ragged batch over the paged 4-bit cache: few rows per sequence (single positions), the joining of split keys,
 // and the entry points.
 #include "fl_paged4_attn.h"
+#include "fl_prompt.h"
 
 #include <algorithm>
 #include <type_traits>
@@ -430,7 +431,7 @@ static int launch_token4(const Paged4Args& args, int d, int format, bool f16, hi
 constexpr int kShare = 768, kLeastTiles = 8;
 struct Plan4 {
   int rows, n_split, min_tiles, share;
-  int64_t keys;                   // that a row sees at most, as far as the caller knows
+  PromptShape shape;              // (the kernel for prompts)
   size_t ws;
 };
 static Plan4 plan4_of(int B, int T, int Hq, int Hkv, int d, int page, int max_pages, int window, int n_sink, int max_q, int max_len) {
@@ -440,11 +441,12 @@ static Plan4 plan4_of(int B, int T, int Hq, int Hkv, int d, int page, int max_pa
   p.rows = per_seq <= 16 ? 16 : per_seq <= 32 ? 32 : 128;
   const int64_t cap = (int64_t)max_pages * page;
   int64_t len = max_len > 0 ? std::min<int64_t>(max_len, cap) : cap;
+  const int64_t past = std::max<int64_t>(0, len - T / B);
   if (window > 0) len = std::min<int64_t>(len, (int64_t)window + n_sink + std::max(max_q, 1));
   p.n_split = p.min_tiles = 1;
-  p.keys = len;
   if (p.rows == 128) {
-    p.ws = paged4_prompt_ws((int64_t)T * G / kPromptRows + B, Hkv, d, cap, len);
+    p.shape = {B, T, (int)G, Hkv, past, len, cap};
+    p.ws = paged4_prompt_ws(p.shape, d);
     return p;
   }
   const int64_t tiles = std::max<int64_t>(1, (len + kKeys4 - 1) / kKeys4);
@@ -512,6 +514,6 @@ extern "C" int fl_paged4_attn(const void* q, int64_t q_stride, int dtype, const 
   if (rc != FL_OK) return rc;
   if (p.rows == 16) return launch_token4<1>(a, d, format, dtype == FL_F16, st);
   if (p.rows == 32) return launch_token4<2>(a, d, format, dtype == FL_F16, st);
-  return launch_paged4_prompt(a, d, format, dtype == FL_F16, p.keys, st);
+  return launch_paged4_prompt(a, d, format, dtype == FL_F16, p.shape, st);
   FL_API_END
 }

@@ -204,20 +204,19 @@ FL_FORMS_OF(64)
 #undef FL_FORMS_OF
 #undef FL_FORMS
 
-size_t paged4_prompt_ws(int64_t slots, int Hkv, int d, int64_t cap, int64_t keys) { return prompt_ws(slots, Hkv, d, cap, keys); }
+size_t paged4_prompt_ws(const PromptShape& s, int d) { return prompt_ws(s, d); }
 
 template <int D, bool INT>
-static int launch_prompt4(Paged4Args& a, bool f16, int64_t keys, hipStream_t st) {
+static int launch_prompt4(Paged4Args& a, bool f16, const PromptShape& shape, hipStream_t st) {
   const char* fn = "fl_paged4_attn";
-  const int64_t cap = (int64_t)a.bt.max_pages * a.pg.size;
-  if (!f16) return launch_prompt<Paged4Source<D, INT, false, false>, D, false>(a, fn, cap, keys, st);
-  if (a.rt.table) return launch_prompt<Paged4Source<D, INT, true, true>, D, true>(a, fn, cap, keys, st);
-  return launch_prompt<Paged4Source<D, INT, true, false>, D, true>(a, fn, cap, keys, st);
+  if (!f16) return launch_prompt<Paged4Source<D, INT, false, false>, D, false>(a, fn, shape, st);
+  if (a.rt.table) return launch_prompt<Paged4Source<D, INT, true, true>, D, true>(a, fn, shape, st);
+  return launch_prompt<Paged4Source<D, INT, true, false>, D, true>(a, fn, shape, st);
 }
-int launch_paged4_prompt(const Paged4Args& args, int d, int format, bool f16, int64_t keys, hipStream_t st) {
+int launch_paged4_prompt(const Paged4Args& args, int d, int format, bool f16, const PromptShape& shape, hipStream_t st) {
   Paged4Args a = args;
-  if (d == 128) return format == FL_KV4_INT ? launch_prompt4<128, true>(a, f16, keys, st) : launch_prompt4<128, false>(a, f16, keys, st);
-  return format == FL_KV4_INT ? launch_prompt4<64, true>(a, f16, keys, st) : launch_prompt4<64, false>(a, f16, keys, st);
+  if (d == 128) return format == FL_KV4_INT ? launch_prompt4<128, true>(a, f16, shape, st) : launch_prompt4<128, false>(a, f16, shape, st);
+  return format == FL_KV4_INT ? launch_prompt4<64, true>(a, f16, shape, st) : launch_prompt4<64, false>(a, f16, shape, st);
 }
 
 }  // namespace fl

@@ -5,6 +5,7 @@
 #include "fl_paged_attn.h"
 
 #include <algorithm>
+#include <cmath>
 
 namespace fl {
 
@@ -21,6 +22,12 @@ struct __attribute__((aligned(16))) StageTile {
 __device__ __forceinline__ void renew(int& x) { asm volatile("" : "+v"(x)); }
 __device__ __forceinline__ void renew(uint32_t& x) { asm volatile("" : "+v"(x)); }
 __device__ __forceinline__ void renew(float& x) { asm volatile("" : "+v"(x)); }
+
+// What the host knows of a call, as far as it decides how the work is cut.
+struct PromptShape {
+  int B, T, G, Hkv;                          // sequences, query positions, query heads of a key/value head, these
+  int64_t past, keys, cap;                   // positions before the first query, on average; keys that a row sees at most; of a sequence at most
+};
 
 template <bool F16>
 __device__ __forceinline__ f32x16 mma32(const u32x4& a, const u32x4& b, const f32x16& c) {
@@ -512,25 +519,41 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(Args a) {
   }
 }
 
-// How a call is cut: equal shares of the work where fewer workgroups of 128 rows than two rounds would run, for rows that see 1024
-// keys or more (below, the two kernels more cost more than idle CUs); else a workgroup each.  cap: keys of a sequence at most (all units
-// of a head count below 2^31).
 constexpr int kRowsOfTile = 128;
 inline int prompt_shares(int Hkv) { return std::max(1, 512 / Hkv); }
-inline bool prompt_shared(int64_t slots, int Hkv, int64_t cap, int64_t keys) {
-  return slots * Hkv < 1024 && keys >= 1024 && slots * (cap / kStageKeys + 16) < (1ll << 31) - 65536;
+// How a call is cut: a workgroup for each row tile, or equal shares of all tiles' stages for 512 workgroups (two a CU), which the plan,
+// the join and the parts' way through memory make 35 to 45 us dearer.  Cut where tiles one by one would leave CUs idle for longer, as far
+// as the host can tell: the longest tile beyond an even share of the stages, at 1.0 us a stage then and at 1.75 where its keys are read
+// by few tiles (a chunk after a long context); or the last round's free places, where all tiles are about as long, at 2.
+// Tiles one by one against shares: prompts of 16 heads x 128, 1500 positions 33 and 42 us, 4096 90 and 103, 8192 272 and 307; of 4
+// heads, 4096 positions 74 and 48 us, 16384 326 and 285; 512 rows of 16 heads after 3584 keys 109 and 83 us; from the 4-bit cache, 100
+// rows of 8 heads after 5000 positions 122 and 37 us, 512 after each of 4 x 4000 (32 / 8 heads) 177 and 202, chunks of 1009, 512 and
+// 2000 after 15000, 0 and 6001 (912 tiles: 1.8 rounds) 728 and 602.
+inline bool prompt_shared(const PromptShape& s) {
+  const int64_t slots = (int64_t)s.T * s.G / kRowsOfTile + s.B;
+  if (slots * (s.cap / kStageKeys + 16) >= (1ll << 31) - 65536) return false;      // (units of a head fit an int)
+  const double rows = (double)s.T / s.B, keys = (double)s.keys;
+  const double least = std::min((double)s.past, keys), most = std::min((double)s.past + rows, keys), grow = most - least;
+  const double seen = rows > 0 ? (grow * (least + most) / 2 + (rows - grow) * keys) / rows : 0;      // of a row, on average
+  const double rounds = s.B * std::ceil(rows * s.G / kRowsOfTile) * s.Hkv / 512;
+  // (a long sequence among short ones has many of the rows)
+  const double longest = std::min((double)s.T, keys - least) * s.G / kRowsOfTile * s.Hkv / 512 * (least + keys) / 2;
+  const double alone = (keys - std::max(rounds * seen, longest)) * (keys > 0 ? 1 + 0.75 * least / keys : 1.0);
+  const double idle = std::max(alone, rounds > 1 ? 2 * least * (std::ceil(rounds) - rounds) : 0.0);
+  return idle >= 36 * kStageKeys;
 }
-inline size_t prompt_ws(int64_t slots, int Hkv, int d, int64_t cap, int64_t keys) {
-  if (!prompt_shared(slots, Hkv, cap, keys)) return 0;
-  return (size_t)prompt_shares(Hkv) * Hkv * 2 * kRowsOfTile * (d + 2) * sizeof(float) + (size_t)slots * sizeof(int);
+inline size_t prompt_ws(const PromptShape& s, int d) {
+  if (!prompt_shared(s)) return 0;
+  const int64_t slots = (int64_t)s.T * s.G / kRowsOfTile + s.B;
+  return (size_t)prompt_shares(s.Hkv) * s.Hkv * 2 * kRowsOfTile * (d + 2) * sizeof(float) + (size_t)slots * sizeof(int);
 }
 template <class Src, int D, bool OUT16, class SrcArgs>
-int launch_prompt(SrcArgs& a, const char* fn, int64_t cap, int64_t keys, hipStream_t st) {
+int launch_prompt(SrcArgs& a, const char* fn, const PromptShape& shape, hipStream_t st) {
   constexpr int R = kRowsOfTile;
   const int64_t slots = (int64_t)a.bt.T * a.G / R + a.bt.B;
   FL_REQUIRE(slots * a.pg.heads * 4 < (1ll << 31), FL_E_SHAPE, "%s: too many rows", fn);
   a.slots = (int)slots;
-  if (!prompt_shared(slots, a.pg.heads, cap, keys)) {
+  if (!prompt_shared(shape)) {
     prompt_kernel<Src, SrcArgs, false><<<(unsigned)(slots * a.pg.heads), 256, 0, st>>>(a);
     return check_launch("prompt_kernel");
   }

@@ -136,6 +136,13 @@ def test_long_chunks(F, dtype, d, window, n_sink):
     check(F, np.random.default_rng(13), [33, 0, 64, 1], [2533, 0, 1164, 4], 2, 1, d, dtype, window, n_sink, hints=(0,))
 
 
+@pytest.mark.parametrize("dtype,d,window,n_sink", [("bf16", 128, 0, 0), ("f16", 64, 2600, 40), ("bf16", 64, 0, 0), ("f16", 128, 3000, 130)])
+def test_chunks_after_long_contexts(F, dtype, d, window, n_sink):
+    """Few row tiles over thousands of keys, cut into shares, which begin and end inside row tiles and between sequences."""
+    check(F, np.random.default_rng(15), [300, 0, 1, 170], [4500, 50, 5001, 173], 4, 2, d, dtype, window, n_sink, hints=(0, 500, 5001))
+    check(F, np.random.default_rng(16), [33, 0, 64, 1], [3033, 0, 2564, 4], 2, 1, d, dtype, window, n_sink, hints=(3033,), layout="half", rot=64)
+
+
 def test_long_prompt(F):
     check(F, np.random.default_rng(14), [2100, 5], None, 2, 1, 128, "bf16", hints=(0, 100))
 

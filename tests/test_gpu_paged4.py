@@ -348,6 +348,17 @@ def test_attention_of_long_chunks(F, dtype, fmt, d, page, window, n_sink):
                hints=((64, 2533),), spoil=True)
 
 
+@pytest.mark.parametrize("dtype,fmt,d,page,window,n_sink", [("bf16", "int4", 128, 64, 0, 0), ("f16", "e2m1", 64, 32, 2600, 40),
+                                                            ("bf16", "e2m1", 128, 16, 3000, 130), ("f16", "int4", 64, 128, 0, 0)])
+def test_attention_of_chunks_after_long_contexts(F, dtype, fmt, d, page, window, n_sink):
+    """Few row tiles over thousands of keys: shares as above, with and without a window."""
+    rng = np.random.default_rng(23)
+    check_attn(F, rng, [300, 0, 1, 170], [4200, 50, 5000, 3], page, 4, 2, d, dtype, fmt, "half", d, window, n_sink,
+               hints=((300, 5001), (300, 0)), spoil=True, holes=((0, 40), (2, 3)))
+    check_attn(F, rng, [33, 0, 64, 1], [3000, 0, 2500, 3], page, 2, 1, d, dtype, fmt, "half", d, window, n_sink,
+               hints=((64, 3033),), spoil=True)
+
+
 def test_thousands_of_sequences(F):
     """More sequences than a search looks at in one or two rounds, many of them without a row."""
     rng = np.random.default_rng(14)

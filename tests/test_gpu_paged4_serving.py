@@ -153,19 +153,19 @@ def test_graph_replays_match_eager_steps(F, fmt):
 
 @pytest.mark.parametrize("fmt", ["int4", "e2m1"])
 def test_graphs_that_share_a_workspace(F, fmt):
-    """Captured calls with one workspace - two of many rows, two of few, whole prompts - replayed in turn with eager work between."""
-    page, max_pages = 64, 40
-    cache, tab = _filled(F, fmt, page, max_pages, [2200, 1800])
+    """Captured calls with one workspace - two of many rows, two of few, packed chunks - replayed in turn with eager work between."""
+    page, max_pages = 64, 60
+    cache, tab = _filled(F, fmt, page, max_pages, [3600, 3200])
     calls = []
-    for new, lens in (([700, 300], [2200, 1800]), ([1, 1], [2200, 1800]), ([300, 290], [1500, 1700]), ([2, 0], [1999, 7])):
+    for new, lens in (([700, 300], [3600, 3200]), ([1, 1], [3600, 3200]), ([300, 290], [2900, 3100]), ([2, 0], [1999, 7])):
         q = _batch(len(calls), sum(new))[0]
         args = (q, i32([0, new[0], sum(new)]), i32(lens), tab, *cache)
-        calls.append((F.paged4_attn, args, dict(max_q=max(new), max_len=2200), torch.empty_like(q)))
-    q, k, v = _batch(9, 2000)
-    calls.append((F.packed_attn, (q, k, v, i32([0, 1500, 2000])), {}, torch.empty_like(q)))
-    wss = [F.paged4_attn_ws(a[0], tab, cache[0], **kw) for f, a, kw, _ in calls[:-1]] + [F.packed_attn_ws(q, k, 2)]
-    assert all(w is not None for w in wss)
-    ws = max(wss, key=lambda t: t.numel())
+        calls.append((F.paged4_attn, args, dict(max_q=max(new), max_len=3600), torch.empty_like(q)))
+    q, k, v = _batch(9, 6000)
+    calls.append((F.packed_attn, (q[:500], k, v, i32([0, 300, 500]), i32([0, 3100, 6000])), {}, torch.empty_like(q[:500])))
+    wss = [F.paged4_attn_ws(a[0], tab, cache[0], **kw) for f, a, kw, _ in calls[:-1]] + [F.packed_attn_ws(q[:500], k, 2)]
+    ws = max((w for w in wss if w is not None), key=lambda t: t.numel())
+    assert sum(w is not None for w in wss) >= 3
     eager = [f(*a, **kw) for f, a, kw, _ in calls]
     graphs = []
     for f, a, kw, out in calls:
