@@ -23,12 +23,15 @@ __device__ __forceinline__ Seq find_row_tile(const PackedArgs& a, int slot) {
   return s;
 }
 
-// Stages of 64 key and value rows by LDS-DMA; rows behind the sequence's last read zeros.
+// Stages of 64 key and value rows by LDS-DMA, 16 bytes a lane, with the permutation of a row's chunks on the way (no bank conflicts);
+// rows behind the sequence's last read zeros.  A key that a row does not see cannot reach it: its score is replaced.  A value can, as 0
+// times an infinity: in stages that some row does not see in full, values that are not finite are set to 0 and noted, and what does see
+// them gets NaN.
 template <int D, bool F16>
 struct PackedSource {
   using Args = PackedArgs;
-  static constexpr int kD = D, kWavesPerSimd = D == 64 ? 3 : 2;      // (64 channels, 8192 positions of 16 heads: 186 us with 2, 173 with 3)
-  static constexpr bool kF16 = F16, kOut16 = F16, kLow = false, kMixed = false, kOdd = true;
+  static constexpr int kD = D, kWavesPerSimd = D == 64 ? 3 : 2;      // (64 channels, 8192 positions of 16 heads: 186 us with 2, 173 with 3; 128 channels need 250 registers)
+  static constexpr bool kF16 = F16, kOut16 = F16, kLow = false, kMixed = false, kOdd = true, kTwo = false;
   // Chunks of a row, rows of a load, loads of a wave, rows from one of these to the next: a lane's chunk is permuted alike in all.
   static constexpr int CH = D / 8, RPI = 64 / CH, NI = kStageKeys / RPI / 4, ROWS = 4 * RPI;
 

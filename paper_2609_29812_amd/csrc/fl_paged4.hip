@@ -31,7 +31,11 @@ struct Rows4Args {
 };
 
 // A wave has a row of the batch; a lane has a chunk of eight channels of a head, so that the four lanes of a quad have a group.
-// The heads of the keys and then those of the values are taken 512 / d at a time.
+// The heads of the keys and then those of the values are taken 512 / d at a time.  Each position stands by itself, so nothing is read
+// but the new rows, and rows need no order.
+// What bounds it: appending int4, the vector units (32768 rows of 8 heads x 128 with rotation and rows out: busy for 99 % of the
+// cycles, 71 us at 4.5 TB/s; a copy has 4.9); reading back, memory (32768 rows 35 us, 5.0 TB/s); one row a sequence, the launch (5.5 and
+// 3.3 us).
 struct RowPlace {
   int pos;                         // position, or -1: the row belongs to no sequence
   int64_t at;                      // row of [num_pages, Hkv, page] of its head 0; -1: its page is not there
@@ -140,7 +144,8 @@ __device__ __forceinline__ uint32_t encode_group(float* x, uint32_t& meta) {
 }
 
 // What a wave's lanes do at step s0 of a row's 2 Hkv heads: the lane's head, and where its row and its cached position begin.  EVEN: the
-// wave's heads are all keys' or all values' (a whole number of steps each), so that all but the lane's offset is uniform.
+// wave's heads are all keys' or all values' (a whole number of steps each), so that all but the lane's offset is uniform (32768 rows of 8
+// heads x 128: appending without rotation 54 us so, 61 in the general form, reading back 35 and 36.6).
 template <int D, bool EVEN>
 struct HeadOf {
   bool is_k, there;

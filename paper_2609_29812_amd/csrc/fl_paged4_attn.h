@@ -31,6 +31,12 @@ __device__ __forceinline__ uint32_t apply(f16x2 c, f16x2 s, f16x2 z) {
 __device__ __forceinline__ f16x2 both_low(uint32_t a, uint32_t b) { return __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(b, a, 0x05040100u)); }
 __device__ __forceinline__ f16x2 both_high(uint32_t a, uint32_t b) { return __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(b, a, 0x07060302u)); }
 
+// What a pair's rounding to fp16 leaves, in fp16.
+__device__ __forceinline__ uint32_t pack_rest(float x, float y, uint32_t rounded) {
+  const f16x2 r = __builtin_bit_cast(f16x2, rounded);
+  return pack_f16x2(fmaf((float)r[0], -1.0f, x), fmaf((float)r[1], -1.0f, y));
+}
+
 // Eight codes of one group in fp16: int4 one rounding of z + s c, in the order 0 4 1 5 2 6 3 7; e2m1 exactly, in their order.
 template <bool INT>
 __device__ __forceinline__ u32x4 widen8(uint32_t w, uint32_t meta, const Magic& g) {
@@ -44,6 +50,19 @@ __device__ __forceinline__ u32x4 widen8(uint32_t w, uint32_t meta, const Magic& 
                  __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 1)),
                  __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 2)),
                  __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 3))};
+  }
+}
+// Eight int4 codes as two parts each whose sum is z + s c to 22 bits: the value's rounding, and that of what it leaves.
+__device__ __forceinline__ void widen8_two(uint32_t w, uint32_t meta, const Magic& g, u32x4& hi, u32x4& lo) {
+  const f16x2 sz = __builtin_bit_cast(f16x2, meta);
+  const float s = (float)sz[0], z = (float)sz[1];
+  const uint32_t v = w >> 8;
+  const f16x2 c[4] = {low_pair(w, g), high_pair(w, g), low_pair(v, g), high_pair(v, g)};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float x = fmaf((float)c[e][0], s, z), y = fmaf((float)c[e][1], s, z);
+    hi[e] = pack_f16x2(x, y);
+    lo[e] = pack_rest(x, y, hi[e]);
   }
 }
 // byte `i` of a word of e2m1 codes as a pair

@@ -19,8 +19,17 @@ constexpr int kKeys4 = 32;         // keys of a wave's tile
 //                 4 (m % 4) + m / 4, so that the wave's load of one value a lane takes four neighbouring keys, whole cache lines.
 // No LDS in the loop: the next tile's keys are fetched into the registers that the scores leave, its values into those that the
 // outputs leave.  Page numbers of 32 tiles are fetched by the lanes at once and handed out by v_readlane.
+// What bounds it: memory, and the 300 to 400 vector instructions of a tile close behind (32 sequences of up to 8191 positions, 32 / 8
+// heads x 128, int4: 147 MB in 43 us, 3.4 TB/s, vector units busy for 69 % of the cycles; 131072 positions, e2m1: 142 MB in 33 us, 4.3
+// TB/s, 55 %), at both ends the chain from the lengths over the block table to the first product, about 9 us (a single sequence of 300).
+// Taken against: codes through the caches' default policy (48 and 47 us, 39.8 and 38; windows of 4096 26 and 28.5), the first tile's
+// loads ahead of the queries (40.5 and 38).
+// fp16 outputs of int4 codes: keys and probabilities are each rounded to fp16 in two parts (widen8_two, pack_rest).  An output has one
+// rounding to fp16 of its own; with those of keys, values and probabilities in one part each it would be off by 1.9 times that, with the
+// values' alone it is by 1.35 times.
 template <int D, bool INT, bool F16, int NR>
 __global__ __launch_bounds__(256, NR == 1 ? (F16 && D == 128 ? 3 : 4) : 2) void paged4_token_kernel(Paged4Args a) {
+  constexpr bool TWO = INT && F16;
   constexpr int R = 16 * NR, KS = D / 32, DT = D / 16, NG = D / kGroup, MB = meta_bytes<INT>();
   constexpr int LD = D + 4;               // row stride of the waves' sums in LDS
   __shared__ float s_ref[4][R], s_sum[4][R];
@@ -166,9 +175,15 @@ __global__ __launch_bounds__(256, NR == 1 ? (F16 && D == 128 ? 3 : 4) : 2) void 
       for (int x = 0; x < NR; ++x) s[x][h] = f32x4{};
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
-        u32x4 w = widen8<INT>(wk[h][k], mk[h], magic);
+        u32x4 w, rest;
+        if constexpr (TWO) widen8_two(wk[h][k], mk[h], magic, w, rest);
+        else w = widen8<INT>(wk[h][k], mk[h], magic);
         if (k == 0) w[0] |= bad[h];
         const f16x8 kf = __builtin_bit_cast(f16x8, w);
+        if constexpr (TWO) {
+#pragma unroll
+          for (int x = 0; x < NR; ++x) s[x][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, rest), qf[x][k], s[x][h], 0, 0, 0);
+        }
 #pragma unroll
         for (int x = 0; x < NR; ++x) s[x][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[x][k], s[x][h], 0, 0, 0);
         if constexpr (F16)
@@ -179,7 +194,7 @@ __global__ __launch_bounds__(256, NR == 1 ? (F16 && D == 128 ? 3 : 4) : 2) void 
       }
     }
     if (more) load_k(c + 1);
-    f16x8 pf[NR];
+    f16x8 pf[NR], pl[TWO ? NR : 1];
 #pragma unroll
     for (int x = 0; x < NR; ++x) {
       f32x4(&y)[2] = s[x];
@@ -213,6 +228,9 @@ __global__ __launch_bounds__(256, NR == 1 ? (F16 && D == 128 ? 3 : 4) : 2) void 
       const u32x4 pw = {pack_f16x2(p[0][0], p[0][1]), pack_f16x2(p[0][2], p[0][3]), pack_f16x2(p[1][0], p[1][1]),
                         pack_f16x2(p[1][2], p[1][3])};
       pf[x] = __builtin_bit_cast(f16x8, pw);
+      if constexpr (TWO)
+        pl[x] = __builtin_bit_cast(f16x8, u32x4{pack_rest(p[0][0], p[0][1], pw[0]), pack_rest(p[0][2], p[0][3], pw[1]),
+                                                pack_rest(p[1][0], p[1][1], pw[2]), pack_rest(p[1][2], p[1][3], pw[3])});
     }
     if (__builtin_expect(spoilt, 0)) {
 #pragma unroll
@@ -244,6 +262,10 @@ __global__ __launch_bounds__(256, NR == 1 ? (F16 && D == 128 ? 3 : 4) : 2) void 
       for (int x = 0; x < NR; ++x) {
         acc[x][2 * y] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, va), pf[x], acc[x][2 * y], 0, 0, 0);
         acc[x][2 * y + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, vb), pf[x], acc[x][2 * y + 1], 0, 0, 0);
+        if constexpr (TWO) {
+          acc[x][2 * y] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, va), pl[x], acc[x][2 * y], 0, 0, 0);
+          acc[x][2 * y + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, vb), pl[x], acc[x][2 * y + 1], 0, 0, 0);
+        }
       }
     };
     pair_of(std::integral_constant<int, 0>{});
@@ -325,6 +347,7 @@ __global__ __launch_bounds__(256, NR == 1 ? (F16 && D == 128 ? 3 : 4) : 2) void 
 
 // The parts of a row's keys joined: a workgroup a row, d / 4 threads across its channels and 1024 / d groups that take the
 // parts in turn, so that the loads of one part are never waited for before those of the next.
+// (1024 rows of about 4 parts 5.3 us, 32 rows of 96 4.7: a launch and two rounds of loads)
 constexpr int kMaxSplit = 256;
 template <int D, int R, bool F16>
 __global__ __launch_bounds__(256) void paged4_merge_kernel(Paged4Args a) {
@@ -427,7 +450,11 @@ static int launch_token4(const Paged4Args& args, int d, int format, bool f16, hi
 
 // How a call is cut, as the 8-bit cache's calls are: up to 16 or 32 rows of a key/value head in a sequence the kernel for few rows,
 // whose keys are split while sequences and heads alone are fewer than its shares, in parts of kLeastTiles tiles or more; more rows
-// the kernel for prompts.
+// the kernel for prompts.  (32 / 8 heads x 128, eight sequences after 4000 positions: 16 rows 23 us, and 32 in the form for 32 rows; 32
+// rows 36, and 50 in the kernel for prompts; 64 rows 47 and 49 in the forms for few, 52 in that, which gains from there on: 100 rows
+// of 8 heads after 5000 positions 37 us.  Shares: 512 and 1024 take 49 and 52 us for 32 sequences where 768 take 47, 39 and 44 for
+// 131072 positions where 768 take 37.  Least tiles: 4 and 16 take 73 and 71 us for eight sequences of 32000 where 8 take 70, and are
+// within 5 % elsewhere.)
 constexpr int kShare = 768, kLeastTiles = 8;
 struct Plan4 {
   int rows, n_split, min_tiles, share;

@@ -1,6 +1,9 @@
 // Dense attention over the paged 4-bit cache for many rows per sequence (prompts and their chunks): a source of the prompt kernel.
-// The codes of a stage are loaded while earlier ones are multiplied, widened to fp16 in registers and written to LDS once for the
-// workgroup's 128 rows.
+// The codes of a stage are loaded while earlier ones are multiplied, widened to fp16 in registers beside the products and written to LDS
+// once for the workgroup's 128 rows: 13 instructions for eight int4 codes, 4 for eight e2m1 ones, about a third of a stage's vector
+// instructions for int4.  What bounds it: the vector units and the matrix cores in turn (chunks of 1009, 512 and 2000 of 32 / 8 heads x
+// 128 with a window of 8192: busy for 60 and 38 % of the cycles; 490 us with plan and join; 8192 positions of 16 heads int4 367 us, e2m1
+// 317, and 285 over bf16 rows).
 #include "fl_paged4_attn.h"
 #include "fl_prompt.h"
 
@@ -17,7 +20,11 @@ __device__ __forceinline__ Seq find_row_tile(const Paged4Args& a, int slot) {
 // LOW: fp16 queries that are rotated, in two parts.
 template <int D, bool INT, bool F16, bool LOW>
 struct Paged4Source {
-  static constexpr int kD = D, kWavesPerSimd = 2;
+  // fp16 outputs of int4 codes: keys and probabilities in two parts, as for few rows; the keys' second parts double their stages in LDS
+  static constexpr bool kTwo = INT && F16;
+  static constexpr int kD = D, kWavesPerSimd = kTwo && D == 128 ? 1 : 2;    // (64 channels, 8192 positions of 16 heads: 231 us with 2, 236 with 3)
+  using KTile = StageTile<D, kTwo ? 2 : 1>;
+  static __device__ __forceinline__ uint32_t rest(float p0, float p1, uint32_t rounded) { return pack_rest(p0, p1, rounded); }
   static constexpr bool kF16 = true, kOut16 = F16, kLow = LOW, kMixed = INT;
   static constexpr int NW = D / 32, NG = D / kGroup, MB = meta_bytes<INT>();      // words of a thread, groups of a head
 
@@ -105,7 +112,7 @@ struct Paged4Source {
     renew(l);
     return load_meta<INT>(m + row * (NG * MB) + (uint32_t)((D == 128 ? l : l >> 1) * MB));
   }
-  __device__ __forceinline__ void load_k(int st, StageTile<D>&) {
+  __device__ __forceinline__ void load_k(int st, KTile&) {
     const int64_t row = row_of_stage(st);
     codes(a.kc + row * (D / 2), kw);
     km = number(a.km, row);
@@ -134,39 +141,49 @@ struct Paged4Source {
     const int key = 16 * wave + (lane >> 2), turn = D == 128 ? lane >> 2 & 3 : lane >> 3 & 1;
     return (uint32_t)(key * D + ((((lane & 3) * NW) ^ turn ^ swz32_f<D>(key & 31)) * 8));
   }
-  __device__ __forceinline__ void put(StageTile<D>& t, uint32_t w, uint32_t meta, uint32_t bad, int e) const {
-    u32x4 x = widen8<INT>(w, meta, magic);
+  __device__ __forceinline__ void put_k(KTile& t, uint32_t w, uint32_t bad, int e) const {
+    uint16_t* at = t.x + (place ^ (uint32_t)(8 * e));
+    u32x4 x, low;
+    if constexpr (kTwo) {
+      widen8_two(w, km, magic, x, low);
+      *reinterpret_cast<u32x4*>(at + kStageKeys * D) = low;
+    } else {
+      x = widen8<INT>(w, km, magic);
+    }
     x[0] |= bad;
-    *reinterpret_cast<u32x4*>(t.x + (place ^ (uint32_t)(8 * e))) = x;
+    *reinterpret_cast<u32x4*>(at) = x;
   }
   // The work of a stage beside its products: its loads, widened into their buffers, a word a time.  A group that reads as NaN, of the
   // key or the value, makes the key's scores NaN; the value's counts as 0.
   static constexpr int kItems = 2 * NW;
-  __device__ __forceinline__ void item(int i, StageTile<D>& k, StageTile<D>& v) {
-    if (i < NW) {
-      if (i == 0) place_words(kw);
-      put(k, kw[i], km, i == 0 && !(group_ok<INT>(km) & group_ok<INT>(kmv)) ? 0x7E007E00u : 0u, i);
-    } else {
-      if (i == NW) {
-        place_words(vw);
-        vm = group_ok<INT>(vm) ? vm : 0u;
-      }
-      put(v, vw[i - NW], vm, 0, i - NW);
+  __device__ __forceinline__ void item_k(int i, KTile& k) {
+    if (i == 0) place_words(kw);
+    put_k(k, kw[i], i == 0 && !(group_ok<INT>(km) & group_ok<INT>(kmv)) ? 0x7E007E00u : 0u, i);
+  }
+  __device__ __forceinline__ void item_v(int i, StageTile<D>& v) {
+    if (i == 0) {
+      place_words(vw);
+      vm = group_ok<INT>(vm) ? vm : 0u;
     }
+    *reinterpret_cast<u32x4*>(v.x + (place ^ (uint32_t)(8 * i))) = widen8<INT>(vw[i], vm, magic);
   }
-  __device__ __forceinline__ void land_k(StageTile<D>& k) {
+  __device__ __forceinline__ void item(int i, KTile& k, StageTile<D>& v) {
+    if (i < NW) item_k(i, k);
+    else item_v(i - NW, v);
+  }
+  __device__ __forceinline__ void land_k(KTile& k) {
 #pragma unroll
-    for (int i = 0; i < NW; ++i) item(i, k, k);
+    for (int i = 0; i < NW; ++i) item_k(i, k);
   }
-  __device__ __forceinline__ void begin(StageTile<D>& k0, StageTile<D>&, StageTile<D>& v0) {
+  __device__ __forceinline__ void begin(KTile& k0, KTile&, StageTile<D>& v0) {
     load_k(0, k0);
     load_v(0, v0);
   }
-  __device__ __forceinline__ void finish(StageTile<D>& k0, StageTile<D>& k1, StageTile<D>& v0) {
+  __device__ __forceinline__ void finish(KTile& k0, KTile& k1, StageTile<D>& v0) {
     land_k(k0);
     if (n > 1) load_k(1, k1);
 #pragma unroll
-    for (int i = NW; i < 2 * NW; ++i) item(i, k0, v0);
+    for (int i = 0; i < NW; ++i) item_v(i, v0);
     if (n > 1) land_k(k1);
   }
   __device__ __forceinline__ void land() const {}

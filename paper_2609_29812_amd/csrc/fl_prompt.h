@@ -13,9 +13,9 @@ constexpr int kStageKeys = 64;
 
 // The keys or the values of a stage in LDS: blocks of 32 rows, 16-byte chunks permuted (swz32_f).  (Each buffer is an object of its
 // own: the compiler orders reads of one behind loads into the same alone.)
-template <int D>
+template <int D, int PARTS = 1>
 struct __attribute__((aligned(16))) StageTile {
-  uint16_t x[kStageKeys * D];
+  uint16_t x[PARTS * kStageKeys * D];        // (the second part of each behind all first ones)
 };
 
 // x, as if just computed
@@ -37,7 +37,8 @@ __device__ __forceinline__ f32x16 mma32(const u32x4& a, const u32x4& b, const f3
 template <bool F16>
 __device__ __forceinline__ uint32_t pack2(float a, float b) { return F16 ? pack_f16x2(a, b) : pack_bf16x2(a, b); }
 
-// ends[s]: units of row tiles 0 .. s (SrcArgs: seq_of(a, b) gives a sequence)
+// ends[s]: units of row tiles 0 .. s, for shares of equal work (SrcArgs: seq_of(a, b) gives a sequence).  One workgroup: 5 us, its chain
+// of loads and sums.
 template <class SrcArgs, int R>
 __global__ __launch_bounds__(1024) void prompt_plan_kernel(SrcArgs a) {
   __shared__ int s_sum[16];
@@ -92,13 +93,31 @@ __device__ __forceinline__ int slot_of_unit(const int* ends, int slots, int x) {
   return lo;
 }
 
+// A workgroup has 128 rows of a sequence and key/value head (positions and the head's query heads), its four waves 32 each, and goes
+// through the keys that they see in stages of 64, which the source lays out in LDS (two buffers for keys, two for values).
+//   S^T = K Q^T     v_mfma_f32_32x32x16: a lane has one row (lane % 32) and half of the stage's keys, so that a row's largest score and
+//                   sum stay in the lane but for one exchange with the other half.
+//   O^T += V^T P^T  the same product: what a lane holds of P is the operand as it lies; V comes through transposing LDS reads.
+// One pass: o and the sum are relative to a running reference, which is raised (and they rescaled) when a score is ahead of it by more
+// than 8 octaves: probabilities reach 2^8 and are rounded to the products' type, scores, sums and outputs stay in fp32.
+// Stages are a step apart: the scores of stage t + 1 are multiplied while the exponentials of stage t are taken, O of stage t while what
+// is left of them and the largest scores of t + 1 are; a barrier a stage, loads waited for where the stage ends.
+// What bounds it: the matrix cores (16384 positions of 16 heads x 128, bf16: busy for 63 % of the cycles, the vector units for 53 %; 990
+// to 1080 us from card to card, 1020 to 1110 TFLOP/s, where a large product has 1224), with 64 channels the vector units (67 and 37 %; 32
+// exponentials of 8 cycles and 100 instructions of 4 a wave and stage either way, beside half of the products; 8192 positions 172 us,
+// 800 TFLOP/s), below a thousand positions the chain of a stage's loads, products and exponentials (300 positions 12 us).
+// Taken against: 64 rows a wave, which halve the reads of LDS (512 registers, spilled: 3350 us for 1070); eight waves a workgroup (16384
+// positions 1026 and 1033 us, windows of 1024 97 and 80); fragments read three or four ahead in place of two (0.5 %); wave priorities
+// around the products (1 %).
 template <class Src, class SrcArgs, bool SHARED>
 __global__ __launch_bounds__(256, Src::kWavesPerSimd) void prompt_kernel(SrcArgs a) {
   constexpr int D = Src::kD, R = 128;
   constexpr int NBK = kStageKeys / 32;     // 32-key blocks of a stage
   constexpr int KS = D / 16;               // k-steps of QK^T
   constexpr int DB = D / 32;               // 32-channel output blocks
-  __shared__ StageTile<D> k0, k1, v0, v1;
+  using KTile = StageTile<D, Src::kTwo ? 2 : 1>;
+  __shared__ KTile k0, k1;
+  __shared__ StageTile<D> v0, v1;
   // Masked stages whose values are not all finite: the values are set to 0, their places are bits of `odd`, a byte for eight channels.
   __shared__ int s_bad[2][4];              // by the wave that looked: the stage where there are some
   __shared__ uint32_t odd[2][kStageKeys * D / 32];
@@ -201,7 +220,7 @@ __global__ __launch_bounds__(256, Src::kWavesPerSimd) void prompt_kernel(SrcArgs
     auto tile_masked = [&](int st) { return !tile_clear(st); };
 
     // scores of a stage, S^T = K Q^T: a lane has 16 keys of one row per block
-    auto scores = [&](f32x16 (&s)[NBK], const StageTile<D>& kt) __attribute__((always_inline)) {
+    auto scores = [&](f32x16 (&s)[NBK], const KTile& kt) __attribute__((always_inline)) {
 #pragma unroll
       for (int b = 0; b < NBK; ++b) s[b] = f32x16{};
 #pragma unroll
@@ -211,6 +230,8 @@ __global__ __launch_bounds__(256, Src::kWavesPerSimd) void prompt_kernel(SrcArgs
           const u32x4 w = *reinterpret_cast<const u32x4*>(&kt.x[b * 32 * D + koff[ks]]);
           s[b] = mma32<Src::kF16>(w, qf[ks], s[b]);
           if constexpr (Src::kLow) s[b] = mma32<Src::kF16>(w, ql[ks], s[b]);
+          if constexpr (Src::kTwo)
+            s[b] = mma32<Src::kF16>(*reinterpret_cast<const u32x4*>(&kt.x[kStageKeys * D + b * 32 * D + koff[ks]]), qf[ks], s[b]);
         }
     };
     auto largest = [&](const f32x16 (&s)[NBK], int g) __attribute__((always_inline)) {        // of half a block
@@ -257,7 +278,7 @@ __global__ __launch_bounds__(256, Src::kWavesPerSimd) void prompt_kernel(SrcArgs
     };
     // One pair of a stage's probabilities (16 pairs a row), as half a word of the operands.
     float ts[2];
-    auto weigh = [&](const f32x16 (&s)[NBK], u32x4 (&pf)[NBK][2], float base, int i) __attribute__((always_inline)) {
+    auto weigh = [&](const f32x16 (&s)[NBK], u32x4 (&pf)[NBK][2], u32x4 (&pl)[NBK][2], float base, int i) __attribute__((always_inline)) {
       const int b = i / 8, v = 2 * (i % 8);
       const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][v], mul, -base));
       const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][v + 1], mul, -base));
@@ -268,9 +289,14 @@ __global__ __launch_bounds__(256, Src::kWavesPerSimd) void prompt_kernel(SrcArgs
       renew(ts[1]);
       renew(two);
       pf[b][v / 8][(v % 8) / 2] = two;
+      if constexpr (Src::kTwo) {
+        uint32_t rest = Src::rest(p0, p1, two);
+        renew(rest);
+        pl[b][v / 8][(v % 8) / 2] = rest;
+      }
     };
-    auto read_k = [&](const StageTile<D>& kt, int i) __attribute__((always_inline)) {          // k-step i / NBK, block i % NBK
-      return *reinterpret_cast<const u32x4*>(&kt.x[(i % NBK) * 32 * D + koff[i / NBK]]);
+    auto read_k = [&](const KTile& kt, int i, int part) __attribute__((always_inline)) {       // k-step i / NBK, block i % NBK
+      return *reinterpret_cast<const u32x4*>(&kt.x[part * kStageKeys * D + (i % NBK) * 32 * D + koff[i / NBK]]);
     };
     auto read_v = [&](const StageTile<D>& vt, int i) __attribute__((always_inline)) {          // keys 16 (i / DB), channels 32 (i % DB)
       const uint16_t* at_v = vt.x + 16 * (i / DB) * D;
@@ -304,13 +330,14 @@ __global__ __launch_bounds__(256, Src::kWavesPerSimd) void prompt_kernel(SrcArgs
     };
     // A stage: the scores of the next one (nxt) beside the probabilities of this one (cur), then O^T += V^T P^T beside what is left of
     // them and the largest scores of the next.  Each matrix instruction is followed by vector instructions that do not wait for it.
-    // (With a second part of 128-channel queries the registers hold one stage's scores alone: there they are formed behind the products.)
+    // (With a second part of 128-channel queries the registers hold one stage's scores alone: there they are formed behind the products;
+    // beside them, 6000 rows of 16 heads after 2000 positions take 543 us and not 461.)
     constexpr bool kBeside = !(Src::kLow && D == 128);
     constexpr int NQ = KS * NBK, NP = NBK * 2 * DB, EARLY = 12, LATE = NP * 3 / 4, LA = 2, MG = 2 * NBK;
-    auto stage = [&](f32x16 (&cur)[NBK], f32x16 (&nxt)[NBK], StageTile<D>& K, const StageTile<D>& KN, const StageTile<D>& V,
+    auto stage = [&](f32x16 (&cur)[NBK], f32x16 (&nxt)[NBK], KTile& K, const KTile& KN, const StageTile<D>& V,
                      StageTile<D>& VN, float& most)
         __attribute__((always_inline)) {
-      u32x4 pf[NBK][2], fr[LA + 1];
+      u32x4 pf[NBK][2], pl[NBK][2], fr[LA + 1], fl[LA + 1];  // (second parts: kTwo)
       const float base = ref == -INFINITY ? 0.0f : ref;
       ts[0] = ts[1] = 0.0f;
       if constexpr (kBeside) {
@@ -322,15 +349,22 @@ __global__ __launch_bounds__(256, Src::kWavesPerSimd) void prompt_kernel(SrcArgs
       auto late = [](int i) { return min(EARLY + (16 - EARLY) * i / LATE, 16); };
       auto score_all = [&](bool beside) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < LA; ++i) fr[i] = read_k(KN, i);
+        for (int i = 0; i < LA; ++i) {
+          fr[i] = read_k(KN, i, 0);
+          if constexpr (Src::kTwo) fl[i] = read_k(KN, i, 1);
+        }
 #pragma unroll
         for (int i = 0; i < NQ; ++i) {
-          if (i + LA < NQ) fr[(i + LA) % (LA + 1)] = read_k(KN, i + LA);
+          if (i + LA < NQ) fr[(i + LA) % (LA + 1)] = read_k(KN, i + LA, 0);
           else if (beside) fr[(i + LA) % (LA + 1)] = read_v(V, i + LA - NQ);
           score(nxt, fr[i % (LA + 1)], i);
+          if constexpr (Src::kTwo) {
+            if (i + LA < NQ) fl[(i + LA) % (LA + 1)] = read_k(KN, i + LA, 1);
+            nxt[i % NBK] = mma32<Src::kF16>(fl[i % (LA + 1)], qf[i / NBK], nxt[i % NBK]);
+          }
           if (beside) {
 #pragma unroll
-            for (int y = early(i); y < early(i + 1); ++y) weigh(cur, pf, base, y);
+            for (int y = early(i); y < early(i + 1); ++y) weigh(cur, pf, pl, base, y);
           }
           __builtin_amdgcn_sched_barrier(0);
         }
@@ -340,8 +374,9 @@ __global__ __launch_bounds__(256, Src::kWavesPerSimd) void prompt_kernel(SrcArgs
         for (int i = 0; i < NP; ++i) {
           if (i + LA < NP) fr[(first + i + LA) % (LA + 1)] = read_v(V, i + LA);
           acc[i % DB] = mma32<Src::kF16>(fr[(first + i) % (LA + 1)], pf[i / DB / 2][i / DB % 2], acc[i % DB]);
+          if constexpr (Src::kTwo) acc[i % DB] = mma32<Src::kF16>(fr[(first + i) % (LA + 1)], pl[i / DB / 2][i / DB % 2], acc[i % DB]);
 #pragma unroll
-          for (int y = late(i); y < late(i + 1); ++y) weigh(cur, pf, base, y);
+          for (int y = late(i); y < late(i + 1); ++y) weigh(cur, pf, pl, base, y);
           // (the source's own work; behind the last stages into buffers that are not read again)
 #pragma unroll
           for (int y = Src::kItems * i / NP; y < Src::kItems * (i + 1) / NP; ++y) src.item(y, K, VN);
@@ -361,7 +396,7 @@ __global__ __launch_bounds__(256, Src::kWavesPerSimd) void prompt_kernel(SrcArgs
         multiply(NQ);
       } else {
 #pragma unroll
-        for (int y = 0; y < EARLY; ++y) weigh(cur, pf, base, y);
+        for (int y = 0; y < EARLY; ++y) weigh(cur, pf, pl, base, y);
 #pragma unroll
         for (int i = 0; i < LA; ++i) fr[i] = read_v(V, i);
         __builtin_amdgcn_sched_barrier(0);
@@ -400,7 +435,7 @@ __global__ __launch_bounds__(256, Src::kWavesPerSimd) void prompt_kernel(SrcArgs
       enter(sa, 0);
       __syncthreads();                                       // (the first keys are read)
       // K: where stage st's keys were and st + 2's come; KN: st + 1's; V: st's values; VN: where st + 1's come
-      auto step = [&](f32x16 (&cur)[NBK], f32x16 (&nxt)[NBK], int st, StageTile<D>& K, StageTile<D>& KN, StageTile<D>& V,
+      auto step = [&](f32x16 (&cur)[NBK], f32x16 (&nxt)[NBK], int st, KTile& K, KTile& KN, StageTile<D>& V,
                       StageTile<D>& VN) __attribute__((always_inline)) {
         const bool more = st + 1 < n;                        // uniform
         if (st + 2 < n) src.load_k(st + 2, K);
@@ -471,7 +506,8 @@ __global__ __launch_bounds__(256, Src::kWavesPerSimd) void prompt_kernel(SrcArgs
   }
 }
 
-// Row tiles that shares cut: a workgroup has 32 rows of one, d / 4 threads a row.
+// Row tiles that shares cut: a workgroup has 32 rows of one, d / 4 threads a row.  The parts are read once, in fp32 as they were summed
+// (912 tiles of 130 stages in 512 shares: 70 MB of parts, 19 us).
 template <class Args, int D, bool OUT16, int R>
 __global__ __launch_bounds__(256) void prompt_join_kernel(Args a) {
   constexpr int LN = D / 4, PER = R / 32;

@@ -517,3 +517,28 @@ def test_empty_calls_and_one_side_alone(F, fmt):
     q = torch.ones(2, H, d, dtype=torch.bfloat16, device="cuda")
     lse = torch.zeros(2, H, device="cuda")
     assert torch.all(F.packed_attn(q, none, none, i32([0, 2]), i32([0, 0]), lse=lse) == 0) and torch.all(lse == -float("inf"))
+
+
+@pytest.mark.parametrize("fmt", ["int4", "e2m1"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_fp16_outputs_are_half_as_far_off_again(F, fmt, d):
+    """Ordinary numbers, keys and values as appended: besides an output's own rounding to fp16 only one more rounding of the same relative
+    size is in it (the probabilities', or the values'), so the norm of its error is at most sqrt(2) times, with 6 % for the rest 1.5
+    times, that of rounding the exact output."""
+    rng = np.random.default_rng(24)
+    page, Hkv, Hq = 64, 2, 8
+    for new, past in (([1, 1, 1], [900, 30, 5]), ([4, 2], [300, 60]), ([8], [500]), ([150, 40], [0, 400])):
+        cu, lens, tab, n_pages = batch(rng, new, past, page)
+        sides = [paged4.empty(n_pages, Hkv, page, d, fmt) for _ in range(2)]
+        at = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+        for c, m in sides:
+            paged4.append(rng.normal(size=(int(at[-1]), Hkv, d)), at, lens, tab, c, m, fmt)
+        q = torch.from_numpy(rng.normal(size=(int(cu[-1]), Hq, d))).half()
+        want = paged4.attend(f64(q), paged4.paged_seqs(cu, lens, tab, sides, fmt), Hkv, d ** -0.5)[0]
+        least = np.linalg.norm(want.astype(np.float16).astype(np.float64) - want)
+        for max_q in (None, 8, 100):
+            got = F.paged4_attn(q.cuda(), i32(cu), i32(lens), i32(tab), up(sides[0][0]), up(sides[1][0]), up(sides[0][1]), up(sides[1][1]),
+                                max_q=max_q)
+            err = np.linalg.norm(f64(got) - want)
+            say(f"  {new} after {past} d={d} {fmt} max_q={max_q}: {err / least:.2f} times the rounding's")
+            assert err <= 1.5 * least
