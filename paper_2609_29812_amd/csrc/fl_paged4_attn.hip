@@ -448,13 +448,13 @@ static int launch_token4(const Paged4Args& args, int d, int format, bool f16, hi
   return check_launch("paged4_merge_kernel");
 }
 
-// How a call is cut, as the 8-bit cache's calls are: up to 16 or 32 rows of a key/value head in a sequence the kernel for few rows,
-// whose keys are split while sequences and heads alone are fewer than its shares, in parts of kLeastTiles tiles or more; more rows
-// the kernel for prompts.  (32 / 8 heads x 128, eight sequences after 4000 positions: 16 rows 23 us, and 32 in the form for 32 rows; 32
-// rows 36, and 50 in the kernel for prompts; 64 rows 47 and 49 in the forms for few, 52 in that, which gains from there on: 100 rows
-// of 8 heads after 5000 positions 37 us.  Shares: 512 and 1024 take 49 and 52 us for 32 sequences where 768 take 47, 39 and 44 for
-// 131072 positions where 768 take 37.  Least tiles: 4 and 16 take 73 and 71 us for eight sequences of 32000 where 8 take 70, and are
-// within 5 % elsewhere.)
+// How a call is cut: up to 32 rows of a key/value head in a sequence (up to 64 where sequences and heads are few) the kernel for few
+// rows, whose keys are split while sequences and heads alone are fewer than its shares, in parts of kLeastTiles tiles or more; more rows
+// the kernel for prompts.  (32 / 8 heads x 128, int4.  16 rows after each of eight times 4000 positions: 23 us, and 32 in the form for 32
+// rows.  32 rows after eight times 32000: 101 us, in the form for 16 rows 123, in the kernel for prompts 167.  64 rows after one, four
+// and eight contexts of 4000, 2000 and 32000: 18, 24 and 178 us, in the kernel for prompts 36, 35 and 175; after 32 of 4000 123 and
+// 102.  Shares: 512 and 1024 take 49 and 52 us for 32 sequences where 768 take 47, 39 and 44 for 131072 positions where 768 take 37.
+// Least tiles: 4 and 16 take 73 and 71 us for eight sequences of 32000 where 8 take 70, and are within 5 % elsewhere.)
 constexpr int kShare = 768, kLeastTiles = 8;
 struct Plan4 {
   int rows, n_split, min_tiles, share;
@@ -465,7 +465,7 @@ static Plan4 plan4_of(int B, int T, int Hq, int Hkv, int d, int page, int max_pa
   Plan4 p{};
   const int64_t G = Hq / Hkv;
   const int64_t per_seq = std::max<int64_t>(1, std::min<int64_t>(max_q > 0 ? max_q : 1, T)) * G;
-  p.rows = per_seq <= 16 ? 16 : per_seq <= 32 ? 32 : 128;
+  p.rows = per_seq <= 16 ? 16 : per_seq <= ((int64_t)B * Hkv <= 128 ? 64 : 32) ? 32 : 128;
   const int64_t cap = (int64_t)max_pages * page;
   int64_t len = max_len > 0 ? std::min<int64_t>(max_len, cap) : cap;
   const int64_t past = std::max<int64_t>(0, len - T / B);
