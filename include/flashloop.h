@@ -676,7 +676,8 @@ int fl_paged4_read(const int32_t* cu, const int32_t* lens, int B, int T, int Hkv
  * A row that sees a position of which a key's or a value's group reads as NaN is NaN.
  * Precision: codes are widened to fp16 (one rounding of z + s c; e2m1 exactly); q (rotated in fp32) is multiplied as fp16 relative
  * to the row's largest magnitude, for FL_F16 with what that rounding leaves as a second part where it is rotated; probabilities
- * are fp16 relative to a running reference of the row.  Scores, sums and outputs are held in fp32.
+ * are fp16 relative to a running reference of the row.  For FL_F16 over FL_KV4_INT keys and probabilities have a second fp16 part each
+ * (of the roundings that are left the values' is the largest).  Scores, sums and outputs are held in fp32.
  * ---------------------------------------------------------------------------------------------- */
 size_t fl_paged4_attn_ws(int B, int T, int Hq, int Hkv, int d, int page, int max_pages, int window, int n_sink, int max_q,
                          int max_len);
