@@ -143,6 +143,31 @@ def test_attn_refusals(lib):
     assert b"fl_paged4_attn" in lib.fl_last_error()
 
 
+def test_workspaces(lib):
+    """None where the work is not cut; else what 512 workgroups leave in two row tiles each, or a place for every part of a row, however
+    long the contexts are.  Calls with less, or with an address that is no multiple of 16, are refused."""
+    most = 65536 * 2 * 130 * 4
+    for n in (1, 300, 4096, 16384):                                                       # whole prompts of 16 heads
+        assert lib.fl_packed_attn_ws(1, n, n, 16, 16, 128, 0, 0, 0) == 0
+    for n in (8192, 1 << 20, 1 << 30):
+        assert 0 < lib.fl_packed_attn_ws(1, 512, n, 16, 16, 128, 0, 0, 0) <= most + 4 * 1024
+        assert 0 < lib.fl_paged4_attn_ws(1, 512, 16, 16, 128, 64, n // 64, 0, 0, 512, n) <= most + 4 * 1024
+        assert 0 < lib.fl_paged4_attn_ws(8, 8, 16, 16, 128, 64, n // 64, 0, 0, 1, n) <= 2 * 768 * 16 * 130 * 4
+    assert lib.fl_paged4_attn_ws(1, 512, 16, 16, 128, 64, 128, 300, 4, 512, 8192) == 0    # a short window
+    assert lib.fl_paged4_attn_ws(1, 1, 16, 16, 128, 64, 128, 0, 0, 1, 64) == 0
+    call = dict(B=1, Tq=512, Tk=8192, Hq=16, Hkv=16, q=at(1 << 30), k=at(2 << 30), v=at(3 << 30), o=at(4 << 30), qs=2048, ks=2048, vs=2048,
+                os=2048, max_k=8192)
+    need = lib.fl_packed_attn_ws(1, 512, 8192, 16, 16, 128, 0, 0, 8192)
+    assert _packed(lib, **call, ws=None) == FL_E_WORKSPACE and _packed(lib, **call, ws_bytes=need - 1) == FL_E_WORKSPACE
+    assert _packed(lib, **call, ws=at(0x1000008)) == FL_E_SHAPE
+    for T, max_q in ((512, 512), (1, 1)):
+        call = dict(B=1, T=T, Hq=16, Hkv=16, q=at(1 << 30), o=at(4 << 30), qs=2048, os=2048, table=None, max_pages=128, max_q=max_q)
+        need = lib.fl_paged4_attn_ws(1, T, 16, 16, 128, 64, 128, 0, 0, max_q, 0)
+        assert need > 0
+        assert _attn(lib, **call, ws=None) == FL_E_WORKSPACE and _attn(lib, **call, ws_bytes=need - 1) == FL_E_WORKSPACE
+        assert _attn(lib, **call, ws=at(0x1000008)) == FL_E_SHAPE
+
+
 def test_binding_refuses_tensors_of_another_place():
     x = torch.zeros(4, 2, 64, dtype=torch.bfloat16)
     for call in (lambda: fl.packed_attn(x, x, x, None), lambda: fl.paged4_append(x, x, None, None, None, None, None, None, None),
