@@ -30,7 +30,8 @@ __device__ __forceinline__ Seq find_row_tile(const PackedArgs& a, int slot) {
 template <int D, bool F16>
 struct PackedSource {
   using Args = PackedArgs;
-  static constexpr int kD = D, kWavesPerSimd = D == 64 ? 3 : 2;      // (64 channels, 8192 positions of 16 heads: 186 us with 2, 173 with 3; 128 channels need 250 registers)
+  // (64 channels, 8192 positions of 16 heads: 186 us with two waves a SIMD, 173 with three; 128 channels need 250 registers)
+  static constexpr int kD = D, kWavesPerSimd = D == 64 ? 3 : 2;
   static constexpr bool kF16 = F16, kOut16 = F16, kLow = false, kMixed = false, kOdd = true, kTwo = false;
   // Chunks of a row, rows of a load, loads of a wave, rows from one of these to the next: a lane's chunk is permuted alike in all.
   static constexpr int CH = D / 8, RPI = 64 / CH, NI = kStageKeys / RPI / 4, ROWS = 4 * RPI;

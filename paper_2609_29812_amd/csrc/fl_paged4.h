@@ -16,7 +16,8 @@ __device__ __forceinline__ bool group_ok(uint32_t m) {
   if constexpr (INT) {
     // (pages are never cleared: two numbers within their bounds may still stand for values beyond fp16's)
     const _Float16 s = __builtin_bit_cast(_Float16, (uint16_t)m), z = __builtin_bit_cast(_Float16, (uint16_t)(m >> 16));
-    return ((m & 0xFFFFu) <= kMaxScale4) & (((m >> 16) & 0x7FFFu) <= kMaxZero4) & (__builtin_elementwise_fma(s, (_Float16)15.0f, z) <= (_Float16)65504.0f);
+    const bool finite = __builtin_elementwise_fma(s, (_Float16)15.0f, z) <= (_Float16)65504.0f;
+    return ((m & 0xFFFFu) <= kMaxScale4) & (((m >> 16) & 0x7FFFu) <= kMaxZero4) & finite;
   }
   return m - (uint32_t)(kMinExp4 + 127) <= (uint32_t)(kMaxExp4 - kMinExp4);
 }

@@ -27,8 +27,10 @@ constexpr int kKeys4 = 32;         // keys of a wave's tile
 // fp16 outputs of int4 codes: keys and probabilities are each rounded to fp16 in two parts (widen8_two, pack_rest).  An output has one
 // rounding to fp16 of its own; with those of keys, values and probabilities in one part each it would be off by 1.9 times that, with the
 // values' alone it is by 1.35 times.
+// (Workgroups of a CU: 16 rows three, as there are shares; with four, fp16 queries of 128 channels spill, 58 us for 131072 positions and
+// not 37, and bf16 ones gain nothing.  32 rows two; with three 54.5 us for eight sequences of 8000 and not 53.)
 template <int D, bool INT, bool F16, int NR>
-__global__ __launch_bounds__(256, NR == 1 ? (F16 && D == 128 ? 3 : 4) : 2) void paged4_token_kernel(Paged4Args a) {
+__global__ __launch_bounds__(256, NR == 1 ? 3 : 2) void paged4_token_kernel(Paged4Args a) {
   constexpr bool TWO = INT && F16;
   constexpr int R = 16 * NR, KS = D / 32, DT = D / 16, NG = D / kGroup, MB = meta_bytes<INT>();
   constexpr int LD = D + 4;               // row stride of the waves' sums in LDS

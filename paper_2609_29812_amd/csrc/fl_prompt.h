@@ -23,6 +23,9 @@ __device__ __forceinline__ void renew(int& x) { asm volatile("" : "+v"(x)); }
 __device__ __forceinline__ void renew(uint32_t& x) { asm volatile("" : "+v"(x)); }
 __device__ __forceinline__ void renew(float& x) { asm volatile("" : "+v"(x)); }
 
+// The sources' own are found by their arguments; a template of the name has to be known for that.
+template <int R> Seq find_row_tile();
+
 // What the host knows of a call, as far as it decides how the work is cut.
 struct PromptShape {
   int B, T, G, Hkv;                          // sequences, query positions, query heads of a key/value head, these

@@ -838,8 +838,8 @@ def packed_attn(q, k, v, cu_q, cu_k=None, table=None, layout="half", sm_scale=No
     cu_k[b] .. cu_k[b+1]-1 (default: cu_q, whole prompts); its queries are the last of its positions.  window > 0: a row at position
     i sees j > i - window and j < n_sink alone.  With a rotary table the queries (not the keys) are turned by their positions, as
     rope leaves them.  max_k: the largest number of keys of a sequence, as far as known (it chooses how the work is cut, not the
-    result; default: an even batch).  lse: optional fp32 [Tq, Hq] to write the log-normalisers to.  ws: optional uint8 workspace (packed_attn_ws).  Returns
-    out [Tq, Hq, d]; rows behind cu_q[B] of a given out are left as they were."""
+    result; default: an even batch).  lse: optional fp32 [Tq, Hq] to write the log-normalisers to.  ws: optional uint8 workspace
+    (packed_attn_ws).  Returns out [Tq, Hq, d]; rows behind cu_q[B] of a given out are left as they were."""
     at, dtype = _here(q, "q"), q.dtype
     qs = _rows(q, at, dtype, "q")
     Tq, Hq, d = q.shape
