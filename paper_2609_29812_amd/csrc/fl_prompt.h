@@ -172,11 +172,13 @@ __global__ __launch_bounds__(256, Src::kWavesPerSimd) void prompt_kernel(SrcArgs
     const int rho_q = sp.rho0 + (row_ok ? row : 0), pos = sp.start + rho_q / G;
     const int jmax = row_ok ? min(pos, cap - 1) : -1;
     const int jmin = a.window > 0 && pos >= a.window ? pos - a.window + 1 : 0;
-    // positions of the wave's first and last row (none: no key is seen)
+    // positions of the wave's first and last row, also behind the last key (a wave without rows: -1)
     const int row0 = 32 * wave;
     const int w_min = sp.start + (sp.rho0 + row0) / G;
-    const int w_max = row0 < sp.rows ? min(sp.start + (sp.rho0 + min(row0 + 32, sp.rows) - 1) / G, cap - 1) : -1;
-    const int w_all = a.window > 0 && w_max >= a.window ? w_max - a.window + 1 : 0;      // the first key (but for the leading) of all
+    const int w_max = row0 < sp.rows ? sp.start + (sp.rho0 + min(row0 + 32, sp.rows) - 1) / G : -1;
+    // the first key (but for the leading) that all rows up to position `last` see
+    auto first_of_all = [&](int last) { return a.window > 0 && last >= a.window ? min(last - a.window + 1, cap) : 0; };
+    const int w_all = first_of_all(w_max);
 
     Src src(a, sq, sp, kvh, tid, t0, n);
     if (n > 0) {
@@ -218,7 +220,7 @@ __global__ __launch_bounds__(256, Src::kWavesPerSimd) void prompt_kernel(SrcArgs
       return Clear{max(c0, 0), (uint32_t)max(c1 - max(c0, 0), 0)};
     };
     const Clear wave_clear = clear_of(w_min, w_all);
-    const Clear tile_clear = clear_of(sp.i_min, a.window > 0 && sp.i_max >= a.window ? sp.i_max - a.window + 1 : 0);
+    const Clear tile_clear = clear_of(sp.i_min, first_of_all(sp.i_max));
     auto masked = [&](int st) { return !wave_clear(st) || src.holes(st); };
     auto tile_masked = [&](int st) { return !tile_clear(st); };
 
