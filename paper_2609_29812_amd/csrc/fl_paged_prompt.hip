@@ -146,11 +146,11 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttnArgs a) {
   const bool row_ok = rr < sp.rows;
   const int rho = sp.rho0 + (row_ok ? rr : 0);
   const int tok = rho / G, head = kvh * G + rho % G, pos = sp.start + tok;
-  // positions of the wave's first and last row (none: no key is seen)
+  // positions of the wave's first and last row, also behind the last key (a wave without rows: -1, no key is seen)
   const int last_row = min(32 * wave + 31, sp.rows - 1);
   const bool wave_ok = 32 * wave < sp.rows;
   const int w_min = sp.start + (sp.rho0 + 32 * wave) / G;
-  const int w_max = wave_ok ? min(sp.start + (sp.rho0 + last_row) / G, cap - 1) : -1;
+  const int w_max = wave_ok ? sp.start + (sp.rho0 + last_row) / G : -1;
   const int w_lo = a.window > 0 && w_min >= a.window ? w_min - a.window + 1 : 0;         // the first key (but for the leading) of any
   const int w_all = a.window > 0 && w_max >= a.window ? w_max - a.window + 1 : 0;        // ... of every row
   const int jmax = row_ok ? min(pos, cap - 1) : -1;
