@@ -137,7 +137,8 @@ __global__ __launch_bounds__(256, Src::kWavesPerSimd) void prompt_kernel(SrcArgs
     slot = slot_of_unit(a.ends, a.slots, at);
   }
   const int first = at;
-  for (; at < end; ++slot) {
+  // (offsets that do not ascend: the plan may give units to row tiles that have no rows here, so units alone do not end the walk)
+  for (; at < end && (!SHARED || slot < a.slots); ++slot) {
     int tid = threadIdx.x;
     if constexpr (SHARED) renew(tid);                        // (what a row tile derives from the lane is formed anew)
     const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
