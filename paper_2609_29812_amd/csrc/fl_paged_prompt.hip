@@ -109,7 +109,8 @@ __global__ __launch_bounds__(256, 2) void paged_prompt_kernel(PagedAttnArgs a) {
     slot = tile_of_unit(a.ends, a.slots, at);
   }
   const int first = at;
-  for (; at < end; ++slot) {
+  // (offsets that do not ascend: the plan may give units to row tiles that have no rows here, so units alone do not end the walk)
+  for (; at < end && (!SHARED || slot < a.slots); ++slot) {
   int tid = threadIdx.x;
   // what a row tile derives from the lane is formed anew: kept over the stages, it spilled (128 channels with fp16 queries still
   // hold 3 to 9 registers of a lane in scratch, all but one of them read outside the stages)

@@ -52,3 +52,19 @@ def test_4_bit_offsets_that_do_not_ascend(F, case, fmt):
     assert ws is not None
     say(f"  4 bits {cu}")
     check(lambda q, c, out: F.paged4_attn(q, c, lens, tab, *cache, max_q=T, out=out, ws=ws), q, cu, B)
+
+
+@pytest.mark.parametrize("fmt", [torch.int8, torch.float8_e4m3fn])
+@pytest.mark.parametrize("case", range(len(OTHERS)))
+def test_8_bit_offsets_that_do_not_ascend(F, case, fmt):
+    cu, T, G = OTHERS[case]
+    B, page, n_pages, L = len(cu) - 1, 64, 128, 6000
+    cache = F.paged_cache(n_pages, 1, page, 64, fmt)
+    k = torch.randn(L, 1, 64, device="cuda").to(torch.bfloat16)
+    tab = i32(np.stack([np.random.default_rng(b).permutation(n_pages) for b in range(B)]))
+    F.paged_append(k, k, i32([0, L]), i32([L]), tab[:1].contiguous(), *cache)
+    q = torch.randn(T, G, 64, device="cuda").to(torch.bfloat16)
+    lens, ws = i32([L] * B), F.paged_attn_ws(q, tab, cache[0], max_q=T)
+    assert ws is not None
+    say(f"  8 bits {cu}")
+    check(lambda q, c, out: F.paged_attn(q, c, lens, tab, *cache, max_q=T, out=out, ws=ws), q, cu, B)
