@@ -70,10 +70,12 @@ template <int I>
 __device__ __forceinline__ uint32_t widen_byte(uint32_t w, float s) {
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, I));
 }
-// A query that is not finite: NaN in its place, and the factor 1, so that what it does not see stays out of its sums.
+// A query that is not finite: NaN in its place, and the factor 1, so that what it does not see stays out of its sums.  A factor below
+// 2^-126 (a query near 0 and a small sm_scale) counts as that: masked scores, -inf, are multiplied by it, and -inf times 0 would be NaN.
+// (The products with it are below 2^24, so their exponents are 0 to 2^-102 either way.)
 template <int N>
 __device__ __forceinline__ float finite_factor(float m, f16x8* q) {
-  if (m == m) return m;
+  if (m == m) return fmaxf(m, 0x1p-126f);
 #pragma unroll
   for (int k = 0; k < N; ++k) q[k] = __builtin_bit_cast(f16x8, u32x4{0x7E007E00u, 0x7E007E00u, 0x7E007E00u, 0x7E007E00u});
   return 1.0f;
