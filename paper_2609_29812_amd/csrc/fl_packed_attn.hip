@@ -132,7 +132,7 @@ struct PackedSource {
     } else {
       const bool in = (uint32_t)pos < (uint32_t)args.n_pos;
       float x[KS][8];
-      turned_chunks<KS, F16>(args.rt, row, in ? pos : 0, x, [hw](int ks) { return 2 * ks + hw; });
+      turned_chunks<KS, F16, true>(args.rt, row, in ? pos : 0, x, [hw](int ks) { return 2 * ks + hw; });
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
         const bool none = !in && 8 * (2 * ks + hw) < args.rt.rot;

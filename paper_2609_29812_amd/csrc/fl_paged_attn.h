@@ -161,8 +161,9 @@ template <int KT>
 __device__ __forceinline__ int key_of(const Span& s, int tile) { return (tile < s.n_lead ? tile : tile - s.n_lead + s.first) * KT; }
 
 // The chunks of eight channels ch(0) .. ch(N - 1) of a row in fp32, turned by row `pos` of the table when there is one.  Loads stand in
-// front and under no branch that lanes could take apart: a row costs two rounds of them.
-template <int N, bool F16, class Ch>
+// front and under no branch that lanes could take apart: a row costs two rounds of them.  AS_ROPE: the bits of rope_kernel (interleaved
+// pairs' products are otherwise joined as the compiler likes; those of halves are its bits in any case).
+template <int N, bool F16, bool AS_ROPE = false, class Ch>
 __device__ __forceinline__ void turned_chunks(const Rotary& rt, const uint16_t* row, int pos, float (*v)[8], Ch ch) {
   uint4 raw[N], par[N];
 #pragma unroll
@@ -207,8 +208,12 @@ __device__ __forceinline__ void turned_chunks(const Rotary& rt, const uint16_t* 
         for (int e = 0; e < 2; ++e) {
           const float4 w = p[e];
           float* x = v[k] + 4 * e;
-          const float r0 = x[0] * w.x - x[1] * w.y, r1 = x[0] * w.y + x[1] * w.x;
-          const float r2 = x[2] * w.z - x[3] * w.w, r3 = x[2] * w.w + x[3] * w.z;
+          float r0 = x[0] * w.x - x[1] * w.y, r1 = x[0] * w.y + x[1] * w.x;
+          float r2 = x[2] * w.z - x[3] * w.w, r3 = x[2] * w.w + x[3] * w.z;
+          if constexpr (AS_ROPE) {
+            r0 = fmaf(x[0], w.x, -(x[1] * w.y)), r1 = fmaf(x[0], w.y, x[1] * w.x);
+            r2 = fmaf(x[2], w.z, -(x[3] * w.w)), r3 = fmaf(x[2], w.w, x[3] * w.z);
+          }
           x[0] = turn ? r0 : x[0];
           x[1] = turn ? r1 : x[1];
           x[2] = turn ? r2 : x[2];

@@ -96,10 +96,10 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
     unpack8<F16>(w0, v);
     unpack8<F16>(w1, v + 8);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {           // pair e: (v[e], v[e + 8]) or (v[2e], v[2e + 1])
+    for (int e = 0; e < 8; ++e) {           // pair e: (v[e], v[e + 8]) or (v[2e], v[2e + 1]); the products joined as turned_chunks does
       const int i0 = HALF ? e : 2 * e, i1 = HALF ? e + 8 : 2 * e + 1;
-      r[i0] = v[i0] * cs[2 * e] - v[i1] * cs[2 * e + 1];
-      r[i1] = v[i0] * cs[2 * e + 1] + v[i1] * cs[2 * e];
+      r[i0] = fmaf(v[i0], cs[2 * e], -(v[i1] * cs[2 * e + 1]));
+      r[i1] = HALF ? fmaf(v[i1], cs[2 * e], v[i0] * cs[2 * e + 1]) : fmaf(v[i0], cs[2 * e + 1], v[i1] * cs[2 * e]);
     }
     w0 = pack8<F16>(r);
     w1 = pack8<F16>(r + 8);
