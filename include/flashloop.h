@@ -69,8 +69,9 @@ int fl_abi_version(void);
  * outside its range (rows and columns in [0, N), or [0, T) for decode).  The same switch has
  * fl_loop_sparse_attn check that every V value it reads (v_cache, and v_new when given) has magnitude
  * <= 65504, since its products with V run in fp16 (a small reduction launch, then FL_E_RANGE).  Off by
- * default; not usable under stream capture.  Process-wide. */
+ * default; not usable under stream capture.  Process-wide.  fl_index_checks tells whether they are on. */
 void fl_set_index_checks(int on);
+int fl_index_checks(void);
 
 /* ------------------------------------------------------------------------------------------------
  * (1) Token selection -- Section 4.1; Appendix D.1, Eq. 5.

@@ -117,3 +117,4 @@ extern "C" const char* fl_last_error(void) { return fl::g_last_error; }
 extern "C" int fl_abi_version(void) { return FL_ABI_VERSION; }
 
 extern "C" void fl_set_index_checks(int on) { fl::g_checks.store(on ? 1 : 0, std::memory_order_relaxed); }
+extern "C" int fl_index_checks(void) { return fl::index_checks_on() ? 1 : 0; }

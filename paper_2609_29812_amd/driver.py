@@ -150,14 +150,17 @@ def paged_step(cache, q, k, v, cu, lens, block_table, table=None, layout="half",
 
 def paged4_step(cache, q, k, v, cu, lens, block_table, table=None, layout="half", window=0, n_sink=0, max_q=None, max_len=0,
                 whole=False, rows=None, out=None, lse=None, ws=None):
-    """paged_step over a 4-bit cache (fl.paged4_cache).  whole: the batch is whole prompts (lens[b] rows each, every page there); its
-    attention then runs over the rows that the stored codes stand for, rounded to q's type (fl.packed_attn), and not over the codes:
-    the same numbers but for that rounding, in less time.  rows: optional (k_rows, v_rows) to hold them, (k, v) themselves if those
+    """paged_step over a 4-bit cache (fl.paged4_cache).  whole: the batch is whole prompts (lens[b] rows each, every page there; both
+    are checked with the index checks on); its attention then runs over the rows that the stored codes stand for, rounded to q's type
+    (fl.packed_attn), and not over the codes, so positions that the cache held before would not be seen: the same numbers but for that
+    rounding, in less time.  rows: optional (k_rows, v_rows) to hold them, (k, v) themselves if those
     are of no further use; ws is then fl.packed_attn_ws's (max_k = max_len), else fl.paged4_attn_ws's."""
     if not whole:
         fl.paged4_append(k, v, cu, lens, block_table, *cache, table=table, layout=layout)
         return fl.paged4_attn(q, cu, lens, block_table, *cache, table=table, layout=layout, window=window, n_sink=n_sink,
                               max_q=max_q, max_len=max_len, out=out, lse=lse, ws=ws)
+    if fl.index_checks() and not torch.equal(cu[1:] - cu[:-1], lens):
+        raise fl.FlashLoopError("paged4_step: FL_E_RANGE: whole prompts have lens[b] rows each")
     k_rows, v_rows = (k.new_empty(k.shape), v.new_empty(v.shape)) if rows is None else rows
     fl.paged4_append(k, v, cu, lens, block_table, *cache, table=table, layout=layout, k_rows=k_rows, v_rows=v_rows)
     return fl.packed_attn(q, k_rows, v_rows, cu, table=table, layout=layout, window=window, n_sink=n_sink, max_k=max_len, out=out,

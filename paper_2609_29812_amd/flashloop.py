@@ -37,6 +37,7 @@ _SIGNATURES = {
     "fl_last_error": (ctypes.c_char_p, []),
     "fl_abi_version": (_c_i, []),
     "fl_set_index_checks": (None, [_c_i]),
+    "fl_index_checks": (_c_i, []),
     "fl_select_tokens": (_c_i, [_c_p, _c_p, _c_p, _c_p, _c_i, _c_i, _c_i, _c_p, _c_i, _c_i, _c_i, _c_d,
                                 _c_p, _c_p, _c_p, _c_p]),
     "fl_kv_residual_quant": (_c_i, [_c_p, _c_p, _c_p, _c_i, _c_i, _c_i, _c_i, _c_i, _c_i, _c_i, _c_i,
@@ -128,6 +129,11 @@ def load(path: str = LIB_PATH):
 def set_index_checks(on: bool):
     """Turn the library's index-list checks on or off (every call then validates its lists on the host)."""
     load().fl_set_index_checks(1 if on else 0)
+
+
+def index_checks() -> bool:
+    """Whether the library's index-list checks are on."""
+    return load().fl_index_checks() != 0
 
 
 def _check(rc: int, fn: str):
