@@ -61,7 +61,7 @@ __device__ __forceinline__ float quad_max(float x) {
   return fmaxf(x, quad<0x4E>(x));                  // lanes 2 3 0 1
 }
 
-// next fp16 away from zero
+// x rounded to fp16 towards zero
 __device__ __forceinline__ uint32_t f16_rtz(float x) {
   return (uint32_t)__builtin_bit_cast(uint16_t, __builtin_amdgcn_cvt_pkrtz(x, 0.0f)[0]);
 }
