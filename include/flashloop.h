@@ -661,7 +661,8 @@ int fl_paged4_append(const void* k, int64_t k_stride, const void* v, int64_t v_s
 
 /* ------------------------------------------------------------------------------------------------
  * (14) Positions of a ragged batch back out of the cache of (13), as rows: row cu[b] + t of k_out and v_out is position
- * lens[b] - n + t of sequence b (n = cu[b+1] - cu[b]; with n = lens[b] all of it), z + s c or c 2^e rounded to `dtype`.
+ * lens[b] - n + t of sequence b (n = cu[b+1] - cu[b]; with n = lens[b] all of it): z + s c, rounded to fp32, or c 2^e (exact), rounded to
+ * `dtype`.
  *   k_out, v_out : [T, Hkv, d] of `dtype`, strides as in (13); either may be NULL, not both.  They do not overlap.
  * Rows of positions that are negative, or whose page is not there, become 0; rows behind cu[B] are not touched.
  * Limits and index checks: as in (10), a page that is not there being no error.
